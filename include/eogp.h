@@ -434,6 +434,115 @@ eogp_status eogp_srht_project(const float* Z, int64_t ldz, int64_t N, int64_t m,
                               int64_t ldx, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The ends of a language model: what makes activations and output-gradients
+ * of the attributed linear modules out of tokens and logits. Element types
+ * are fp32, bf16 and fp16; sums, statistics and weight gradients are fp32.
+ * Rows are tokens (n = examples * tokens of each), `ld_*` their strides in
+ * elements, at any element's address. token_mask ([n] uint8 or NULL = all
+ * valid) works as in the first stage: masked rows are never read, their
+ * outputs are zero, and they count for no sum. Results do not depend on the
+ * order in which the GPU runs blocks: repeated calls agree bit for bit.
+ * Every call is enqueued on `stream` and launches kernels only.
+ * ------------------------------------------------------------------------ */
+
+/* Token embedding: out[i] = scale * table[tokens[i]], added to out[i] if
+ * accumulate != 0 (position rows, a second table). One rounding to out's type.
+ *   table   [V, ld_table >= d];  tokens [n];  out [n, ld_out >= d] of the
+ *           table's type or fp32. A valid row whose token lies outside [0, V)
+ *           gets NaN.
+ * Errors: EOGP_ERR_INVALID for bad sizes or NULL pointers;
+ * EOGP_ERR_UNSUPPORTED for another output type. */
+eogp_status eogp_embed_tokens(const void* table, eogp_dtype table_dtype, int64_t ld_table, int64_t V,
+                              int64_t d, const int64_t* tokens, const uint8_t* token_mask, int64_t n,
+                              float scale, int32_t accumulate, void* out, eogp_dtype out_dtype,
+                              int64_t ld_out, void* stream);
+
+/* Its gradient: d_table[v] = scale * sum of d_out[i] over the valid rows with
+ * tokens[i] = v, zero for a token without rows (accumulate != 0: added to
+ * d_table). The rows are sorted by token (stable) and summed in that order.
+ * A token outside [0, V) counts for none.
+ *   d_out    [n, ld_d_out >= d] of `dtype`;  d_table [V, ld_d_table >= d] fp32.
+ *   ws       eogp_embed_backward_workspace_size bytes (none for n = 0). */
+size_t eogp_embed_backward_workspace_size(int64_t n, int64_t d);
+eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_d_out,
+                                const int64_t* tokens, const uint8_t* token_mask, int64_t n, int64_t V,
+                                int64_t d, float scale, int32_t accumulate, float* d_table,
+                                int64_t ld_d_table, void* ws, size_t ws_bytes, void* stream);
+
+/* Layer norm: y = (x - mean) * rstd * gamma + beta over each row's d elements,
+ * rstd = (mean of (x - mean)^2 + eps)^-1/2. With ones_column != 0, element d of
+ * each valid row of y is 1: the constant column of an attributed bias
+ * (Appendix C.1), so y is a linear module's input as the first stage takes it.
+ *   gamma, beta  [d] of x's type or fp32 (w_dtype), or NULL (1 and 0).
+ *   y            [n, ld_y] of x's type or fp32; must not overlap x.
+ *   mean, rstd   [n] fp32 for the backward pass, or NULL.
+ * Errors: EOGP_ERR_INVALID for bad sizes, NULL pointers or eps < 0;
+ * EOGP_ERR_UNSUPPORTED for d > 16,384 or another mix of types. */
+eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, const void* gamma,
+                            const void* beta, eogp_dtype w_dtype, float eps, const uint8_t* token_mask,
+                            int64_t n, int64_t d, void* y, eogp_dtype y_dtype, int64_t ld_y,
+                            int32_t ones_column, float* mean, float* rstd, void* stream);
+
+/* Its backward pass. With xh = (x - mean) rstd and t = dy gamma,
+ *   dx = rstd (t - mean(t) - xh mean(t xh)) + residual,
+ * where residual (or NULL) is the gradient that reaches x beside the norm: dx is
+ * then the gradient of the residual stream, the output-gradient of the module
+ * that wrote x. Weight gradients are sums over each of `groups` groups of `rows`
+ * consecutive rows: one group for a batch's gradient, one per example for
+ * per-example gradients.
+ *   dy, x, residual, dx   [groups * rows, ld] of `dtype`; dx may be residual
+ *                         itself, and overlaps nothing else.
+ *   mean, rstd            [groups * rows] fp32 of the forward pass.
+ *   d_gamma, d_beta       [groups, d] fp32, or NULL.
+ *   ws                    eogp_layer_norm_backward_workspace_size bytes.
+ * Errors as for eogp_layer_norm; EOGP_ERR_WORKSPACE if ws is too small. */
+size_t eogp_layer_norm_backward_workspace_size(int64_t groups, int64_t rows, int64_t d,
+                                               eogp_dtype dtype);
+eogp_status eogp_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                                     eogp_dtype dtype, const void* gamma, eogp_dtype w_dtype,
+                                     const float* mean, const float* rstd, const uint8_t* token_mask,
+                                     const void* residual, int64_t ld_residual, int64_t groups,
+                                     int64_t rows, int64_t d, void* dx, int64_t ld_dx, float* d_gamma,
+                                     float* d_beta, void* ws, size_t ws_bytes, void* stream);
+
+/* Cross-entropy of one label per row and its gradient at the logits:
+ *   loss[i] = ln sum_v exp(l[i, v]) - l[i, label],
+ *   d_logits[i, v] = grad_scale * (softmax(l[i])[v] - [v = label]),
+ * the paper's token-summed loss when summed over an example's valid tokens
+ * (Appendix C.1). A label outside [0, V) masks its row (loss and gradient 0).
+ * Logits of -inf have probability 0.
+ *   logits    [n, ld_logits >= V];  labels [n].
+ *   loss      [n] fp32, or NULL;  d_logits [n, ld_d_logits >= V] of the
+ *             logits' type, or NULL; may be the logits themselves. */
+eogp_status eogp_softmax_xent(const void* logits, eogp_dtype dtype, int64_t ld_logits,
+                              const int64_t* labels, const uint8_t* token_mask, int64_t n, int64_t V,
+                              float grad_scale, float* loss, void* d_logits, int64_t ld_d_logits,
+                              void* stream);
+
+/* Sampling: one token per row from softmax(l / temperature), drawn with the
+ * row's uniform number u in [0, 1). The EK-FAC pass takes its labels so
+ * (Appendix C.2: labels sampled from the model). Probabilities are integers,
+ * so that the token does not depend on the order of a sum:
+ *   t_v = (l_v - max l) * fp32(log2 e / temperature)      in fp32
+ *   w_v = floor(2^30 * 2^t_v), 2^t = 2^rint(t) * p(t - rint(t)) with the
+ *         degree-5 polynomial p in Horner's form, fp32, each operation rounded.
+ * In the order (logit descending, index ascending), kept are the first top_k
+ * (0: all); of those the shortest prefix whose mass reaches
+ * floor(mass * rint(top_p 2^24) / 2^24), at least one; of those w_v >= min_p 2^30
+ * (the largest weight is 2^30). The token is the lowest index whose running
+ * kept mass exceeds floor(floor(u 2^24) * kept mass / 2^24).
+ *   uniforms      [n] fp32 (clamped to [0, 1)); may be NULL at temperature 0.
+ *   temperature   >= 0; at 0 the token is the lowest index of the largest logit.
+ *   tokens        [n] int64; -1 for a masked row and for one without a logit
+ *                 above -inf. NaN logits count as -inf.
+ * Errors: EOGP_ERR_INVALID for bad sizes, options out of range or NULL
+ * pointers; EOGP_ERR_UNSUPPORTED for V > 2^20. */
+eogp_status eogp_sample_tokens(const void* logits, eogp_dtype dtype, int64_t ld_logits, int64_t n,
+                               int64_t V, const float* uniforms, const uint8_t* token_mask,
+                               double temperature, int64_t top_k, double top_p, double min_p,
+                               int64_t* tokens, void* stream);
+
+/* ------------------------------------------------------------------------
  * Kernel timing, for measurement harnesses. While enabled, each launch of a
  * kernel class below is bracketed by two HIP events recorded on the stream it
  * is launched on. eogp_timing_read waits for the recorded events of one class,
@@ -452,7 +561,11 @@ typedef enum {
   EOGP_KT_SRHT = 8,           /* random second stage (EOGP-R)                    */
   EOGP_KT_EKFAC = 9,          /* EK-FAC squared rotated gradients                */
   EOGP_KT_PCA_FIT = 10,       /* PCA fit: Gram and projection contractions       */
-  EOGP_KT_COUNT = 11
+  EOGP_KT_EMBED = 11,         /* token embedding and its gradient                */
+  EOGP_KT_LAYER_NORM = 12,    /* layer norm, forward and backward                */
+  EOGP_KT_XENT = 13,          /* cross-entropy and its gradient                  */
+  EOGP_KT_SAMPLE = 14,        /* sampling                                        */
+  EOGP_KT_COUNT = 15
 } eogp_kernel_class;
 eogp_status eogp_timing_enable(int32_t enable);
 eogp_status eogp_timing_read(int32_t kernel_class, double* total_ms, int64_t* launches);

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <mutex>
 #include <set>
@@ -59,6 +60,30 @@ eogp_status score_topk_tiled(const uint8_t* codes, const uint16_t* scales, int64
                              const int64_t* kmod, const float* Y, int64_t ldy, int64_t Q,
                              int32_t topk, int64_t* out_idx, float* out_score, float* full,
                              void* ws, size_t ws_bytes, hipStream_t s);
+int64_t norm_max_width();
+eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* gamma, const void* beta,
+                       eogp_dtype wt, float eps, const uint8_t* mask, int64_t n, int64_t d, void* y,
+                       eogp_dtype yt, int64_t ldy, int ones, float* mean, float* rstd, hipStream_t s);
+size_t layer_norm_back_ws(int64_t groups, int64_t rows, int64_t d, eogp_dtype t);
+eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t ldx, eogp_dtype t,
+                            const void* gamma, eogp_dtype wt, const float* mean, const float* rstd,
+                            const uint8_t* mask, const void* res, int64_t ldres, int64_t groups,
+                            int64_t rows, int64_t d, void* dx, int64_t lddx, float* dgamma,
+                            float* dbeta, void* ws, hipStream_t s);
+eogp_status embed_tokens(const void* table, eogp_dtype tt, int64_t ldt, int64_t V, int64_t d,
+                         const int64_t* tokens, const uint8_t* mask, int64_t n, float scale, int accumulate,
+                         void* out, eogp_dtype ot, int64_t ldo, hipStream_t s);
+size_t embed_back_ws(int64_t n, int64_t d);
+eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_t* tokens, const uint8_t* mask,
+                       int64_t n, int64_t V, int64_t d, float scale, int accumulate, float* dtable, int64_t ldt,
+                       void* ws, hipStream_t s);
+eogp_status softmax_xent(const void* logits, eogp_dtype t, int64_t ldl, const int64_t* labels,
+                         const uint8_t* mask, int64_t n, int64_t V, float gscale, float* loss, void* dlogits,
+                         int64_t ldd, hipStream_t s);
+int64_t sample_max_vocab();
+eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t n, int64_t V,
+                          const float* uniforms, const uint8_t* mask, double temperature, int64_t top_k,
+                          double top_p, double min_p, int64_t* out, hipStream_t s);
 
 namespace {
 thread_local std::string g_last_error;
@@ -521,6 +546,197 @@ eogp_status eogp_score_topk_noalloc(const uint8_t* codes, int64_t code_row_strid
   if (st != EOGP_OK) return st;
   return score_topk(codes, code_row_stride, scales, N, U, k_per_module, Y, ldy, Q, topk, out_idx,
                     out_score, full_scores, scratch, score_scratch_bytes(), S(stream));
+}
+
+namespace {
+// Element types of the operators on a model's rows; a row of `width` elements `ld` apart.
+bool model_type(eogp_dtype t) { return t == EOGP_F32 || t == EOGP_BF16 || t == EOGP_F16; }
+
+eogp_status check_rows(const char* op, int64_t n, int64_t width) {
+  if (n < 0 || width < 1) return fail(EOGP_ERR_INVALID, std::string(op) + ": bad sizes");
+  if (n >= kMaxFlat || width >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": rows and widths must be < 2^31");
+  return EOGP_OK;
+}
+
+eogp_status check_ld(const char* op, const char* what, int64_t ld, int64_t width) {
+  if (ld < width || ld >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": row stride of " + what + " outside [width, 2^31)");
+  return EOGP_OK;
+}
+
+eogp_status check_aligned(const char* op, const char* what, const void* p, eogp_dtype t) {
+  if ((uintptr_t)p % (t == EOGP_F32 ? 4 : 2))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": " + what + " must be aligned to its elements");
+  return EOGP_OK;
+}
+}  // namespace
+
+#define EOGP_CHECK(call)                 \
+  do {                                   \
+    const eogp_status st_ = (call);      \
+    if (st_ != EOGP_OK) return st_;      \
+  } while (0)
+
+eogp_status eogp_embed_tokens(const void* table, eogp_dtype table_dtype, int64_t ld_table, int64_t V,
+                              int64_t d, const int64_t* tokens, const uint8_t* token_mask, int64_t n,
+                              float scale, int32_t accumulate, void* out, eogp_dtype out_dtype,
+                              int64_t ld_out, void* stream) {
+  const char* op = "embed_tokens";
+  EOGP_CHECK(check_rows(op, n, d));
+  if (V < 1 || V >= kMaxFlat) return fail(EOGP_ERR_INVALID, "embed_tokens: need 1 <= V < 2^31");
+  if (!model_type(table_dtype) || !model_type(out_dtype))
+    return fail(EOGP_ERR_INVALID, "embed_tokens: unknown element type");
+  if (out_dtype != table_dtype && out_dtype != EOGP_F32)
+    return fail(EOGP_ERR_UNSUPPORTED, "embed_tokens: out must have the table's type or be fp32");
+  EOGP_CHECK(check_ld(op, "table", ld_table, d));
+  EOGP_CHECK(check_ld(op, "out", ld_out, d));
+  if (n == 0) return EOGP_OK;
+  if (!table || !tokens || !out) return fail(EOGP_ERR_INVALID, "embed_tokens: NULL pointer");
+  EOGP_CHECK(check_aligned(op, "table", table, table_dtype));
+  EOGP_CHECK(check_aligned(op, "out", out, out_dtype));
+  return embed_tokens(table, table_dtype, ld_table, V, d, tokens, token_mask, n, scale, accumulate, out,
+                      out_dtype, ld_out, S(stream));
+}
+
+size_t eogp_embed_backward_workspace_size(int64_t n, int64_t d) {
+  if (n < 1 || n >= kMaxFlat || d < 1 || d >= kMaxFlat) return 0;
+  return embed_back_ws(n, d);
+}
+
+eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_d_out,
+                                const int64_t* tokens, const uint8_t* token_mask, int64_t n, int64_t V,
+                                int64_t d, float scale, int32_t accumulate, float* d_table,
+                                int64_t ld_d_table, void* ws, size_t ws_bytes, void* stream) {
+  const char* op = "embed_backward";
+  EOGP_CHECK(check_rows(op, n, d));
+  if (V < 1 || V >= kMaxFlat) return fail(EOGP_ERR_INVALID, "embed_backward: need 1 <= V < 2^31");
+  if (!model_type(dtype)) return fail(EOGP_ERR_INVALID, "embed_backward: unknown element type");
+  EOGP_CHECK(check_ld(op, "d_out", ld_d_out, d));
+  EOGP_CHECK(check_ld(op, "d_table", ld_d_table, d));
+  if (!d_table || (n > 0 && (!d_out || !tokens)))
+    return fail(EOGP_ERR_INVALID, "embed_backward: NULL pointer");
+  if (n > 0) EOGP_CHECK(check_aligned(op, "d_out", d_out, dtype));
+  EOGP_CHECK(check_aligned(op, "d_table", d_table, EOGP_F32));
+  if (n > 0 && (!ws || ws_bytes < embed_back_ws(n, d)))
+    return fail(EOGP_ERR_WORKSPACE, "embed_backward: workspace too small");
+  return embed_back(d_out, dtype, ld_d_out, tokens, token_mask, n, V, d, scale, accumulate, d_table,
+                    ld_d_table, ws, S(stream));
+}
+
+namespace {
+eogp_status check_norm(const char* op, int64_t n, int64_t d, eogp_dtype x_dtype, eogp_dtype w_dtype) {
+  EOGP_CHECK(check_rows(op, n, d));
+  if (!model_type(x_dtype) || !model_type(w_dtype))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": unknown element type");
+  if (w_dtype != x_dtype && w_dtype != EOGP_F32)
+    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": weights must have the rows' type or be fp32");
+  if (d > norm_max_width())
+    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": d > 16384 is not supported");
+  return EOGP_OK;
+}
+}  // namespace
+
+eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, const void* gamma,
+                            const void* beta, eogp_dtype w_dtype, float eps, const uint8_t* token_mask,
+                            int64_t n, int64_t d, void* y, eogp_dtype y_dtype, int64_t ld_y,
+                            int32_t ones_column, float* mean, float* rstd, void* stream) {
+  const char* op = "layer_norm";
+  EOGP_CHECK(check_norm(op, n, d, x_dtype, w_dtype));
+  if (!model_type(y_dtype)) return fail(EOGP_ERR_INVALID, "layer_norm: unknown element type");
+  if (y_dtype != x_dtype && y_dtype != EOGP_F32)
+    return fail(EOGP_ERR_UNSUPPORTED, "layer_norm: y must have the type of x or be fp32");
+  if (!(eps >= 0.f) || std::isinf(eps)) return fail(EOGP_ERR_INVALID, "layer_norm: eps must be >= 0");
+  EOGP_CHECK(check_ld(op, "x", ld_x, d));
+  EOGP_CHECK(check_ld(op, "y", ld_y, d + (ones_column ? 1 : 0)));
+  if (n == 0) return EOGP_OK;
+  if (!x || !y) return fail(EOGP_ERR_INVALID, "layer_norm: NULL pointer");
+  EOGP_CHECK(check_aligned(op, "x", x, x_dtype));
+  EOGP_CHECK(check_aligned(op, "y", y, y_dtype));
+  EOGP_CHECK(check_aligned(op, "gamma", gamma, w_dtype));
+  EOGP_CHECK(check_aligned(op, "beta", beta, w_dtype));
+  return layer_norm(x, x_dtype, ld_x, gamma, beta, w_dtype, eps, token_mask, n, d, y, y_dtype, ld_y,
+                    ones_column != 0, mean, rstd, S(stream));
+}
+
+size_t eogp_layer_norm_backward_workspace_size(int64_t groups, int64_t rows, int64_t d,
+                                               eogp_dtype dtype) {
+  if (groups < 1 || rows < 0 || d < 1 || d > norm_max_width() || !model_type(dtype)) return 0;
+  if (groups >= kMaxFlat || rows >= kMaxFlat || groups * rows >= kMaxFlat) return 0;
+  return layer_norm_back_ws(groups, rows, d, dtype);
+}
+
+eogp_status eogp_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                                     eogp_dtype dtype, const void* gamma, eogp_dtype w_dtype,
+                                     const float* mean, const float* rstd, const uint8_t* token_mask,
+                                     const void* residual, int64_t ld_residual, int64_t groups,
+                                     int64_t rows, int64_t d, void* dx, int64_t ld_dx, float* d_gamma,
+                                     float* d_beta, void* ws, size_t ws_bytes, void* stream) {
+  const char* op = "layer_norm_backward";
+  if (groups < 0 || rows < 0 || groups >= kMaxFlat || rows >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, "layer_norm_backward: bad sizes");
+  const int64_t n = groups * rows;
+  EOGP_CHECK(check_norm(op, n, d, dtype, w_dtype));
+  EOGP_CHECK(check_ld(op, "dy", ld_dy, d));
+  EOGP_CHECK(check_ld(op, "x", ld_x, d));
+  EOGP_CHECK(check_ld(op, "dx", ld_dx, d));
+  if (residual) EOGP_CHECK(check_ld(op, "residual", ld_residual, d));
+  if (groups == 0) return EOGP_OK;
+  if (n > 0 && (!dy || !x || !mean || !rstd || !dx))
+    return fail(EOGP_ERR_INVALID, "layer_norm_backward: NULL pointer");
+  if (n > 0) {
+    EOGP_CHECK(check_aligned(op, "dy", dy, dtype));
+    EOGP_CHECK(check_aligned(op, "x", x, dtype));
+    EOGP_CHECK(check_aligned(op, "dx", dx, dtype));
+    EOGP_CHECK(check_aligned(op, "residual", residual, dtype));
+    EOGP_CHECK(check_aligned(op, "gamma", gamma, w_dtype));
+  }
+  if (!ws || ws_bytes < layer_norm_back_ws(groups, rows, d, dtype))
+    return fail(EOGP_ERR_WORKSPACE, "layer_norm_backward: workspace too small");
+  return layer_norm_back(dy, ld_dy, x, ld_x, dtype, gamma, w_dtype, mean, rstd, token_mask, residual,
+                         ld_residual, groups, rows, d, dx, ld_dx, d_gamma, d_beta, ws, S(stream));
+}
+
+eogp_status eogp_softmax_xent(const void* logits, eogp_dtype dtype, int64_t ld_logits,
+                              const int64_t* labels, const uint8_t* token_mask, int64_t n, int64_t V,
+                              float grad_scale, float* loss, void* d_logits, int64_t ld_d_logits,
+                              void* stream) {
+  const char* op = "softmax_xent";
+  EOGP_CHECK(check_rows(op, n, V));
+  if (!model_type(dtype)) return fail(EOGP_ERR_INVALID, "softmax_xent: unknown element type");
+  EOGP_CHECK(check_ld(op, "logits", ld_logits, V));
+  if (d_logits) EOGP_CHECK(check_ld(op, "d_logits", ld_d_logits, V));
+  if (n == 0) return EOGP_OK;
+  if (!logits || !labels || (!loss && !d_logits)) return fail(EOGP_ERR_INVALID, "softmax_xent: NULL pointer");
+  if (d_logits == logits && ld_d_logits != ld_logits)
+    return fail(EOGP_ERR_INVALID, "softmax_xent: gradients over the logits need their row stride");
+  EOGP_CHECK(check_aligned(op, "logits", logits, dtype));
+  EOGP_CHECK(check_aligned(op, "d_logits", d_logits, dtype));
+  return softmax_xent(logits, dtype, ld_logits, labels, token_mask, n, V, grad_scale, loss, d_logits,
+                      ld_d_logits, S(stream));
+}
+
+eogp_status eogp_sample_tokens(const void* logits, eogp_dtype dtype, int64_t ld_logits, int64_t n,
+                               int64_t V, const float* uniforms, const uint8_t* token_mask,
+                               double temperature, int64_t top_k, double top_p, double min_p,
+                               int64_t* tokens, void* stream) {
+  const char* op = "sample_tokens";
+  EOGP_CHECK(check_rows(op, n, V));
+  if (!model_type(dtype)) return fail(EOGP_ERR_INVALID, "sample_tokens: unknown element type");
+  if (V > sample_max_vocab())
+    return fail(EOGP_ERR_UNSUPPORTED, "sample_tokens: V > 2^20 is not supported");
+  if (!(temperature >= 0.0) || std::isinf(temperature))
+    return fail(EOGP_ERR_INVALID, "sample_tokens: temperature must be finite and >= 0");
+  if (top_k < 0) return fail(EOGP_ERR_INVALID, "sample_tokens: top_k must be >= 0 (0: no limit)");
+  if (!(top_p >= 0.0 && top_p <= 1.0) || !(min_p >= 0.0 && min_p <= 1.0))
+    return fail(EOGP_ERR_INVALID, "sample_tokens: top_p and min_p must lie in [0, 1]");
+  EOGP_CHECK(check_ld(op, "logits", ld_logits, V));
+  if (n == 0) return EOGP_OK;
+  if (!logits || !tokens || (!uniforms && temperature > 0.0))
+    return fail(EOGP_ERR_INVALID, "sample_tokens: NULL pointer");
+  EOGP_CHECK(check_aligned(op, "logits", logits, dtype));
+  return sample_tokens(logits, dtype, ld_logits, n, V, uniforms, token_mask, temperature, top_k, top_p,
+                       min_p, tokens, S(stream));
 }
 
 }  // extern "C"

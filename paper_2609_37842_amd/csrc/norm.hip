@@ -1,0 +1,339 @@
+// Layer norm over the width of each row, forward and backward.
+#include <algorithm>
+
+#include "rows.h"
+#include "timing.h"
+
+namespace eogp {
+namespace {
+
+// WPR waves share a row: sum of v over the row, in every lane of its waves. `slot` is LDS of the
+// block for 2 x 16 floats, used alternately so that one barrier per sum is enough.
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float* slot) {
+  v = wave_sum(v);
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = slot[0];
+#pragma unroll
+    for (int w = 1; w < WPR; ++w) v += slot[w];
+  }
+  return v;
+}
+
+// y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
+// bytes per lane), so mean and the centred second moment are two exact passes over registers and
+// HBM sees one read and one write. gamma and beta are read once per wave.
+template <typename TI, typename TO, int WPR, int P>
+__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm(
+    const TI* __restrict__ x, int64_t ldx, const void* __restrict__ gamma, const void* __restrict__ beta,
+    eogp_dtype wt, float eps, const uint8_t* __restrict__ mask, int64_t n, int64_t d, TO* __restrict__ y,
+    int64_t ldy, int ones, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
+  constexpr int E = kPiece<TI>;
+  constexpr int kWaves = WPR > 4 ? WPR : 4, kRows = kWaves / WPR;   // of a block
+  __shared__ float slot[2][16];
+  const int wid = threadIdx.x >> 6;
+  const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;   // place among the row's lanes
+  float g[P][E], b[P][E];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E + e;
+      g[p][e] = gamma && c < d ? load_any(gamma, wt, c) : 1.f;
+      b[p][e] = beta && c < d ? load_any(beta, wt, c) : 0.f;
+    }
+  const float width = (float)d;               // sums are divided by it: a constant row's mean is exact
+  for (int64_t row = (int64_t)blockIdx.x * kRows + (WPR == 1 ? wid : 0); row < n;
+       row += (int64_t)gridDim.x * kRows) {
+    TO* yr = y + row * ldy;
+    if (mask && mask[row] == 0) {            // not read; zeros
+      float zero[E] = {};
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+        if (c < d) store_piece<TO, E>(yr, c, d, zero);
+      }
+      if (t == 0) {
+        if (ones) yr[d] = (TO)0.f;
+        if (mean_out) mean_out[row] = 0.f;
+        if (rstd_out) rstd_out[row] = 0.f;
+      }
+      continue;
+    }
+    const TI* xr = x + row * ldx;
+    float v[P][E];
+    float s = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      load_piece<TI, E>(xr, c, d, 0.f, v[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += v[p][e];
+    const float mean = row_sum<WPR>(s, slot[0]) / width;
+    s = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int64_t c = (int64_t)(p * 64 * WPR + t) * E + e;
+        v[p][e] = c < d ? v[p][e] - mean : 0.f;
+        s += v[p][e] * v[p][e];
+      }
+    const float rstd = 1.f / sqrtf(row_sum<WPR>(s, slot[1]) / width + eps);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[p][e] = v[p][e] * rstd * g[p][e] + b[p][e];
+      if (c < d) store_piece<TO, E>(yr, c, d, v[p]);
+    }
+    if (t == 0) {
+      if (ones) yr[d] = (TO)1.f;
+      if (mean_out) mean_out[row] = mean;
+      if (rstd_out) rstd_out[row] = rstd;
+    }
+  }
+}
+
+// dx = rstd (t - mean(t) - xh mean(t xh)) [+ residual gradient], t = dy gamma, xh = (x - mean) rstd,
+// and the column sums of dy xh and dy over the block's rows, kept in registers from row to row.
+// Group k (of rows_per_group rows) has `splits` blocks; block j takes its rows j, j + splits, ...
+// (times the rows a block holds at once) and writes its sums to part[k][j][2][d].
+template <typename T, int WPR, int P>
+__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm_back(
+    const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,
+    const void* __restrict__ gamma, eogp_dtype wt, const float* __restrict__ mean_in,
+    const float* __restrict__ rstd_in, const uint8_t* __restrict__ mask, const T* res,
+    int64_t ldres, int64_t rows_per_group, int64_t d, int splits, T* dx, int64_t lddx,
+    float* __restrict__ part) {
+  constexpr int E = kPiece<T>;
+  constexpr int kWaves = WPR > 4 ? WPR : 4, kRows = kWaves / WPR;
+  __shared__ float slot[2][2][16];
+  __shared__ float fold[WPR == 1 ? 3 * 64 * E : 1];
+  const int wid = threadIdx.x >> 6;
+  const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+  float g[P][E], ag[P][E], ab[P][E];
+#pragma unroll
+  for (int p = 0; p < P; ++p)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E + e;
+      g[p][e] = gamma && c < d ? load_any(gamma, wt, c) : 1.f;
+      ag[p][e] = ab[p][e] = 0.f;
+    }
+  const float width = (float)d;
+  const int64_t group = blockIdx.x / splits, split = blockIdx.x % splits;
+  int turn = 0;
+  for (int64_t i = split * kRows + (WPR == 1 ? wid : 0); i < rows_per_group; i += (int64_t)splits * kRows) {
+    const int64_t row = group * rows_per_group + i;
+    T* out = dx + row * lddx;
+    if (mask && mask[row] == 0) {            // not read; zeros
+      float zero[E] = {};
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+        if (c < d) store_piece<T, E>(out, c, d, zero);
+      }
+      continue;
+    }
+    const float mean = mean_in[row], rstd = rstd_in[row];
+    float xv[P][E], gy[P][E];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      load_piece<T, E>(x + row * ldx, c, d, mean, xv[p]);
+      load_piece<T, E>(dy + row * lddy, c, d, 0.f, gy[p]);
+    }
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        xv[p][e] = (xv[p][e] - mean) * rstd;
+        ag[p][e] += gy[p][e] * xv[p][e];
+        ab[p][e] += gy[p][e];
+        gy[p][e] *= g[p][e];
+        s1 += gy[p][e];
+        s2 += gy[p][e] * xv[p][e];
+      }
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if constexpr (WPR > 1) {
+      float* q = &slot[turn][0][0];
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) {
+        q[wid] = s1;
+        q[16 + wid] = s2;
+      }
+      __syncthreads();
+      s1 = q[0];
+      s2 = q[16];
+#pragma unroll
+      for (int w = 1; w < WPR; ++w) {
+        s1 += q[w];
+        s2 += q[16 + w];
+      }
+    }
+    s1 /= width;
+    s2 /= width;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      float r[E] = {};
+      if (res) load_piece<T, E>(res + row * ldres, c, d, 0.f, r);
+#pragma unroll
+      for (int e = 0; e < E; ++e) r[e] += rstd * (gy[p][e] - s1 - xv[p][e] * s2);
+      if (c < d) store_piece<T, E>(out, c, d, r);
+    }
+  }
+  float* pg = part + (int64_t)blockIdx.x * 2 * d;
+  float* pb = pg + d;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+    if constexpr (WPR == 1) {                // the block's four rows at a time, in order of their waves
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        float(&a)[E] = which ? ab[p] : ag[p];
+        __syncthreads();
+        if (wid > 0)
+#pragma unroll
+          for (int e = 0; e < E; ++e) fold[((wid - 1) * 64 + t) * E + e] = a[e];
+        __syncthreads();
+        if (wid == 0)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            a[e] += fold[t * E + e] + fold[(64 + t) * E + e] + fold[(128 + t) * E + e];
+      }
+      if (wid > 0) continue;
+    }
+    if (c < d) {
+      store_piece<float, E>(pg, c, d, ag[p]);
+      store_piece<float, E>(pb, c, d, ab[p]);
+    }
+  }
+}
+
+// Column sums of the blocks' partial sums, in a fixed order: 16 columns x 16 slices per block.
+__global__ __launch_bounds__(256) void k_norm_fold(const float* __restrict__ part, int64_t groups, int splits,
+                                                   int64_t d, float* __restrict__ dgamma,
+                                                   float* __restrict__ dbeta) {
+  __shared__ float sum[16][17];
+  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int64_t col_blocks = (2 * d + 15) / 16;
+  for (int64_t unit = blockIdx.x; unit < groups * col_blocks; unit += gridDim.x) {
+    const int64_t group = unit / col_blocks, c = unit % col_blocks * 16 + col;   // of the 2 d columns
+    float s = 0.f;
+    if (c < 2 * d)
+      for (int j = slice; j < splits; j += 16) s += part[(group * splits + j) * 2 * d + c];
+    sum[slice][col] = s;
+    __syncthreads();
+    if (slice == 0 && c < 2 * d) {
+      for (int k = 1; k < 16; ++k) s += sum[k][col];
+      float* out = c < d ? dgamma : dbeta;
+      if (out) out[group * d + (c < d ? c : c - d)] = s;
+    }
+    __syncthreads();
+  }
+}
+
+// Waves per row and pieces per lane for a row of `pieces` 16-byte pieces: one wave while four
+// pieces a lane hold the row, then four waves, then sixteen.
+template <typename T, typename F>
+eogp_status with_shape(int64_t pieces, F&& f) {
+  using std::integral_constant;
+  if (pieces <= 64) return f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  if (pieces <= 128) return f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  if (pieces <= 192) return f(integral_constant<int, 1>{}, integral_constant<int, 3>{});
+  if (pieces <= 256) return f(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+  if (pieces <= 512) return f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  if (pieces <= 768) return f(integral_constant<int, 4>{}, integral_constant<int, 3>{});
+  if (pieces <= 1024) return f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  if constexpr (sizeof(T) == 4)              // (16-bit rows of up to 16,384 elements have 2,048 pieces)
+    if (pieces > 2048) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+}
+
+int rows_per_block(int64_t pieces) { return pieces <= 256 ? 4 : 1; }
+
+int64_t row_pieces(int64_t d, eogp_dtype t) { return ceil_div(d, t == EOGP_F32 ? 4 : 8); }
+
+}  // namespace
+
+int64_t norm_max_width() { return 16384; }   // 16 waves x 64 lanes x 4 pieces of 4 fp32
+
+eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* gamma, const void* beta,
+                       eogp_dtype wt, float eps, const uint8_t* mask, int64_t n, int64_t d, void* y,
+                       eogp_dtype yt, int64_t ldy, int ones, float* mean, float* rstd, hipStream_t s) {
+  if (n == 0) return EOGP_OK;
+  const int64_t pieces = row_pieces(d, xt);
+  timing::Scope ts(EOGP_KT_LAYER_NORM, s);
+  return with_type(xt, [&](auto ti) {
+    using TI = decltype(ti);
+    auto go = [&](auto to) {
+      using TO = decltype(to);
+      return with_shape<TI>(pieces, [&](auto wpr, auto p) {
+        constexpr int W = decltype(wpr)::value;
+        const int64_t blocks = std::min<int64_t>(ceil_div(n, rows_per_block(pieces)), W > 4 ? 512 : 2048);
+        hipLaunchKernelGGL((k_layer_norm<TI, TO, W, decltype(p)::value>), dim3((unsigned)blocks),
+                           dim3(W > 4 ? 64 * W : 256), 0, s, static_cast<const TI*>(x), ldx, gamma, beta,
+                           wt, eps, mask, n, d, static_cast<TO*>(y), ldy, ones, mean, rstd);
+        EOGP_LAUNCH_CHECK("layer_norm");
+        return EOGP_OK;
+      });
+    };
+    return yt == xt ? go(TI{}) : go(float{});
+  });
+}
+
+namespace {
+// Blocks of a group: enough to fill the chip four times over, no more than its rows need.
+int back_splits(int64_t groups, int64_t rows, int64_t pieces) {
+  const int64_t most = ceil_div(rows, rows_per_block(pieces));
+  const int64_t want = ceil_div(pieces <= 1024 ? 4 * kCus : 2 * kCus, groups);
+  return (int)std::max<int64_t>(1, std::min(most, want));
+}
+}  // namespace
+
+size_t layer_norm_back_ws(int64_t groups, int64_t rows, int64_t d, eogp_dtype t) {
+  return align256((size_t)groups * back_splits(groups, rows, row_pieces(d, t)) * 2 * d * sizeof(float));
+}
+
+eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t ldx, eogp_dtype t,
+                            const void* gamma, eogp_dtype wt, const float* mean, const float* rstd,
+                            const uint8_t* mask, const void* res, int64_t ldres, int64_t groups,
+                            int64_t rows, int64_t d, void* dx, int64_t lddx, float* dgamma,
+                            float* dbeta, void* ws, hipStream_t s) {
+  if (groups == 0) return EOGP_OK;
+  const int64_t pieces = row_pieces(d, t);
+  const int splits = back_splits(groups, rows, pieces);
+  float* part = static_cast<float*>(ws);
+  timing::Scope ts(EOGP_KT_LAYER_NORM, s);
+  const eogp_status st = with_type(t, [&](auto el) {
+    using T = decltype(el);
+    return with_shape<T>(pieces, [&](auto wpr, auto p) {
+      constexpr int W = decltype(wpr)::value, P = decltype(p)::value;
+      hipLaunchKernelGGL((k_layer_norm_back<T, W, P>), dim3((unsigned)(groups * splits)),
+                         dim3(W > 4 ? 64 * W : 256), 0, s, static_cast<const T*>(dy), lddy,
+                         static_cast<const T*>(x), ldx, gamma, wt, mean, rstd, mask,
+                         static_cast<const T*>(res), ldres, rows, d, splits, static_cast<T*>(dx), lddx,
+                         part);
+      EOGP_LAUNCH_CHECK("layer_norm_backward");
+      return EOGP_OK;
+    });
+  });
+  if (st != EOGP_OK) return st;
+  if (!dgamma && !dbeta) return EOGP_OK;
+  const int64_t fold_blocks = std::min<int64_t>(groups * ceil_div(2 * d, 16), 1 << 20);
+  hipLaunchKernelGGL(k_norm_fold, dim3((unsigned)fold_blocks), dim3(256), 0, s, part, groups, splits, d, dgamma,
+                     dbeta);
+  EOGP_LAUNCH_CHECK("layer_norm_backward (fold)");
+  return EOGP_OK;
+}
+
+}  // namespace eogp

@@ -1,0 +1,96 @@
+// Rows of fp32, bf16 or fp16 elements taken 16 bytes ("a piece") per lane, for the kernels that
+// pass over rows once: embedding, layer norm, cross-entropy, sampling. Rows may start at any
+// element; a row's last piece may be short.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace eogp {
+
+template <eogp_dtype D> struct ElemOf;
+template <> struct ElemOf<EOGP_F32> { using type = float; };
+template <> struct ElemOf<EOGP_BF16> { using type = __bf16; };
+template <> struct ElemOf<EOGP_F16> { using type = _Float16; };
+
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);   // elements of a piece
+
+// E elements at any element's address
+template <typename T, int E>
+using AnyVec = T __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+
+// Elements c .. c + E - 1 of a row of d as fp32; `pad` in the place of those past the end.
+template <typename T, int E>
+__device__ __forceinline__ void load_piece(const T* __restrict__ row, int64_t c, int64_t d, float pad,
+                                           float (&v)[E]) {
+  if (c + E <= d) {
+    const AnyVec<T, E> x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = (float)x[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = c + e < d ? (float)row[c + e] : pad;
+  }
+}
+
+// The same elements rounded to T and stored; none past the end.
+template <typename T, int E>
+__device__ __forceinline__ void store_piece(T* __restrict__ row, int64_t c, int64_t d, const float (&v)[E]) {
+  if (c + E <= d) {
+    AnyVec<T, E> x;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = (T)v[e];
+    *reinterpret_cast<AnyVec<T, E>*>(row + c) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (c + e < d) row[c + e] = (T)v[e];
+  }
+}
+
+// Element c of an array whose type is known at run time (weights read once per wave).
+__device__ __forceinline__ float load_any(const void* p, eogp_dtype t, int64_t c) {
+  if (t == EOGP_F32) return static_cast<const float*>(p)[c];
+  if (t == EOGP_BF16) return (float)static_cast<const __bf16*>(p)[c];
+  return (float)static_cast<const _Float16*>(p)[c];
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
+  return v;
+}
+
+// Calls f with the element type of a run-time dtype: f(T{}).
+template <typename F>
+inline eogp_status with_type(eogp_dtype t, F&& f) {
+  if (t == EOGP_F32) return f(float{});
+  if (t == EOGP_BF16) return f(__bf16{});
+  return f(_Float16{});
+}
+
+}  // namespace eogp
+
+namespace eogp {
+// Threads of the block that holds a row of `pieces` 16-byte pieces in registers, and pieces per
+// thread; none (0) for rows longer than 1,024 threads x 16 pieces, which are read again instead.
+template <typename F>
+inline eogp_status with_row_shape(int64_t pieces, F&& f) {
+  using std::integral_constant;
+  using N256 = integral_constant<int, 256>;
+  using N1024 = integral_constant<int, 1024>;
+  if (pieces <= 256) return f(N256{}, integral_constant<int, 1>{});
+  if (pieces <= 512) return f(N256{}, integral_constant<int, 2>{});
+  if (pieces <= 1024) return f(N256{}, integral_constant<int, 4>{});
+  if (pieces <= 2048) return f(N1024{}, integral_constant<int, 2>{});
+  if (pieces <= 4096) return f(N1024{}, integral_constant<int, 4>{});
+  if (pieces <= 8192) return f(N1024{}, integral_constant<int, 8>{});
+  if (pieces <= 12288) return f(N1024{}, integral_constant<int, 12>{});
+  if (pieces <= 16384) return f(N1024{}, integral_constant<int, 16>{});
+  return f(N1024{}, integral_constant<int, 0>{});
+}
+}  // namespace eogp

@@ -53,6 +53,9 @@ EXPORTED = (
     "eogp_ekfac_workspace_size", "eogp_ekfac_eigenvalues",
     "eogp_score_topk_workspace_size", "eogp_score_topk", "eogp_score_topk_tiled",
     "eogp_score_topk_noalloc",
+    "eogp_embed_tokens", "eogp_embed_backward_workspace_size", "eogp_embed_backward",
+    "eogp_layer_norm", "eogp_layer_norm_backward_workspace_size", "eogp_layer_norm_backward",
+    "eogp_softmax_xent", "eogp_sample_tokens",
     "eogp_timing_enable", "eogp_timing_read",
     "eogp_status_string", "eogp_last_error", "eogp_version",
 )
@@ -110,6 +113,22 @@ def load(path: str | None = None):
                                           c_i64, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
         "eogp_score_topk_noalloc": (c_i32, [c_vp, c_i64, c_vp, c_i64, c_i32, ctypes.POINTER(c_i64),
                                             c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp]),
+        "eogp_embed_tokens": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, c_vp, c_vp, c_i64,
+                                      ctypes.c_float, c_i32, c_vp, c_i32, c_i64, c_vp]),
+        "eogp_embed_backward_workspace_size": (c_sz, [c_i64, c_i64]),
+        "eogp_embed_backward": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_vp, c_i64, c_i64, c_i64,
+                                        ctypes.c_float, c_i32, c_vp, c_i64, c_vp, c_sz, c_vp]),
+        "eogp_layer_norm": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_vp, c_i32, ctypes.c_float, c_vp,
+                                    c_i64, c_i64, c_vp, c_i32, c_i64, c_i32, c_vp, c_vp, c_vp]),
+        "eogp_layer_norm_backward_workspace_size": (c_sz, [c_i64, c_i64, c_i64, c_i32]),
+        "eogp_layer_norm_backward": (c_i32, [c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_i32, c_vp,
+                                             c_vp, c_vp, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp,
+                                             c_i64, c_vp, c_vp, c_vp, c_sz, c_vp]),
+        "eogp_softmax_xent": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_vp, c_i64, c_i64, ctypes.c_float,
+                                      c_vp, c_vp, c_i64, c_vp]),
+        "eogp_sample_tokens": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, c_vp, c_vp,
+                                       ctypes.c_double, c_i64, ctypes.c_double, ctypes.c_double,
+                                       c_vp, c_vp]),
         "eogp_timing_enable": (c_i32, [c_i32]),
         "eogp_timing_read": (c_i32, [c_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(c_i64)]),
         "eogp_status_string": (ctypes.c_char_p, [c_i32]),
@@ -584,6 +603,255 @@ def eogp_score_topk(codes, scales, k_per_module, Y, topk, full_scores=False, out
     return out_idx, out_score, full
 
 
+# ---------------------------------------------------------------------------
+# The ends of a language model: embedding, layer norm, cross-entropy, sampling
+# ---------------------------------------------------------------------------
+def _empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows_of(x, name):
+    """(rows, width, row stride) of a [n, d] or [N, T, d] tensor whose rows have
+    unit column stride and lie at one constant stride."""
+    if x.dim() not in (2, 3):
+        raise ValueError(f"{name} must be [n, d] or [N, T, d]")
+    d = x.shape[-1]
+    if x.dim() == 2:
+        n, T = x.shape[0], 1
+        ld = x.stride(0)
+    else:
+        N, T = x.shape[0], x.shape[1]
+        n = N * T
+        ld = x.stride(1) if T > 1 else x.stride(0)
+        if N > 1 and T > 1 and x.stride(0) != T * ld:
+            raise ValueError(f"{name} must have its rows at a constant row stride")
+    if d > 1 and x.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    if n > 1 and ld < d:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return n, d, (ld if n > 1 else max(ld, d))
+
+
+def _model_dtype(x, name):
+    if x.dtype not in _DTYPE_CODE:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    return _DTYPE_CODE[x.dtype]
+
+
+def _per_row(x, lead, dtype, name):
+    """A contiguous tensor with one element per row, or None."""
+    if x is not None and (x.dtype != dtype or tuple(x.shape) != tuple(lead) or not x.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous {str(dtype)[6:]} {list(lead)}")
+    return x
+
+
+def _weight(w, d, x, name):
+    if w is None:
+        return None
+    if tuple(w.shape) != (d,) or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32):
+        raise ValueError(f"{name} must be contiguous [{d}] of the rows' type or float32")
+    return w
+
+
+def _same_shape(x, like, name):
+    if x.shape != like.shape or x.dtype != like.dtype:
+        raise ValueError(f"{name} must have the shape and type of its counterpart")
+
+
+def eogp_embed_tokens(table, tokens, scale=1.0, token_mask=None, out=None, accumulate=False,
+                      stream=None):
+    """out [*tokens.shape, d] = scale * table[tokens] (table [V, d]; tokens int64 [n]
+    or [N, T]), added to `out` if accumulate; see eogp_embed_tokens in eogp.h."""
+    L = load()
+    _need_cuda(table, tokens, token_mask, out)
+    V, d, ldt = _rows_of(table, "table")
+    if table.dim() != 2 or tokens.dim() not in (1, 2):
+        raise ValueError("table must be [V, d] and tokens [n] or [N, T]")
+    lead = tokens.shape
+    _per_row(tokens, lead, torch.int64, "tokens")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a caller's out")
+        out = _empty((*lead, d), table.dtype, table.device, stream)
+    if tuple(out.shape) != (*lead, d) or out.dtype not in (table.dtype, torch.float32):
+        raise ValueError("out must be [*tokens.shape, d] of the table's type or float32")
+    n, _, ldo = _rows_of(out, "out")
+    _check(L.eogp_embed_tokens(_ptr(table), _model_dtype(table, "table"), ldt, V, d, _ptr(tokens),
+                               _ptr(token_mask), n, float(scale), 1 if accumulate else 0, _ptr(out),
+                               _DTYPE_CODE[out.dtype], ldo, _stream(stream)))
+    return out
+
+
+def eogp_embed_backward_workspace_size(n: int, d: int) -> int:
+    return int(load().eogp_embed_backward_workspace_size(n, d))
+
+
+def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=None, accumulate=False,
+                        ws=None, stream=None):
+    """dtable [V, d] (float32) = scale * sum of d_out's rows by token, added to
+    `dtable` if accumulate; see eogp_embed_backward in eogp.h."""
+    L = load()
+    _need_cuda(d_out, tokens, token_mask, dtable)
+    n, d, ldd = _rows_of(d_out, "d_out")
+    lead = d_out.shape[:-1]
+    _per_row(tokens, lead, torch.int64, "tokens")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a caller's dtable")
+        dtable = _empty((V, d), torch.float32, d_out.device, stream)
+    if dtable.dtype != torch.float32 or tuple(dtable.shape) != (V, d):
+        raise ValueError("dtable must be float32 [V, d]")
+    _, _, ldt = _rows_of(dtable, "dtable")
+    need = eogp_embed_backward_workspace_size(n, d)
+    if ws is None and need:
+        ws = _empty((need,), torch.uint8, d_out.device, stream)
+    ws, wsb = _workspace(need, d_out.device, ws)
+    _check(L.eogp_embed_backward(_ptr(d_out), _model_dtype(d_out, "d_out"), ldd, _ptr(tokens),
+                                 _ptr(token_mask), n, V, d, float(scale), 1 if accumulate else 0,
+                                 _ptr(dtable), ldt, _ptr(ws), wsb, _stream(stream)))
+    return dtable
+
+
+def eogp_layer_norm(x, gamma=None, beta=None, eps=1e-5, token_mask=None, ones_column=False, out=None,
+                    mean=None, rstd=None, stream=None):
+    """(y, mean, rstd) of x [n, d] or [N, T, d]; with ones_column y has d + 1
+    columns, the last 1 in valid rows (a new y then has rows of a multiple of 16
+    elements); see eogp_layer_norm in eogp.h."""
+    L = load()
+    _need_cuda(x, gamma, beta, token_mask, out, mean, rstd)
+    n, d, ldx = _rows_of(x, "x")
+    lead, width = x.shape[:-1], d + (1 if ones_column else 0)
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    _weight(gamma, d, x, "gamma")
+    _weight(beta, d, x, "beta")
+    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+        raise ValueError("gamma and beta must have one type")
+    if out is None:
+        ld = -(-width // 16) * 16 if ones_column else width
+        out = _empty((*lead, ld), x.dtype, x.device, stream)[..., :width]
+    if tuple(out.shape) != (*lead, width) or out.dtype not in (x.dtype, torch.float32):
+        raise ValueError("out must be [..., d (+ 1 with ones_column)] of x's type or float32")
+    _, _, ldy = _rows_of(out, "out")
+    if mean is None:
+        mean = _empty(lead, torch.float32, x.device, stream)
+    if rstd is None:
+        rstd = _empty(lead, torch.float32, x.device, stream)
+    _per_row(mean, lead, torch.float32, "mean")
+    _per_row(rstd, lead, torch.float32, "rstd")
+    w = gamma if gamma is not None else beta
+    _check(L.eogp_layer_norm(_ptr(x), _model_dtype(x, "x"), ldx, _ptr(gamma), _ptr(beta),
+                             F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _ptr(token_mask), n,
+                             d, _ptr(out), _DTYPE_CODE[out.dtype], ldy, 1 if ones_column else 0,
+                             _ptr(mean), _ptr(rstd), _stream(stream)))
+    return out, mean, rstd
+
+
+def eogp_layer_norm_backward_workspace_size(groups: int, rows: int, d: int, dtype: int) -> int:
+    return int(load().eogp_layer_norm_backward_workspace_size(groups, rows, d, dtype))
+
+
+def eogp_layer_norm_backward(dy, x, gamma, mean, rstd, token_mask=None, residual=None,
+                             per_example=False, dx=None, dgamma=None, dbeta=None, ws=None, stream=None):
+    """(dx, dgamma, dbeta): gradient at x (plus `residual`), and the weight and bias
+    gradients, float32 [d] or with per_example [N, d] (x [N, T, d]); see
+    eogp_layer_norm_backward in eogp.h."""
+    L = load()
+    _need_cuda(dy, x, gamma, mean, rstd, token_mask, residual, dx, dgamma, dbeta)
+    n, d, ldx = _rows_of(x, "x")
+    lead = x.shape[:-1]
+    _same_shape(dy, x, "dy")
+    _, _, lddy = _rows_of(dy, "dy")
+    _weight(gamma, d, x, "gamma")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is None:
+            raise ValueError(f"the backward pass reads the forward pass's {name}")
+        _per_row(t, lead, torch.float32, name)
+    ldr = 0
+    if residual is not None:
+        _same_shape(residual, x, "residual")
+        _, _, ldr = _rows_of(residual, "residual")
+    if dx is None:
+        dx = _empty(tuple(x.shape), x.dtype, x.device, stream)
+    _same_shape(dx, x, "dx")
+    _, _, lddx = _rows_of(dx, "dx")
+    if per_example and x.dim() != 3:
+        raise ValueError("per-example gradients need x [N, T, d]")
+    groups = x.shape[0] if per_example else 1
+    rows = x.shape[1] if per_example else n
+    shape = (groups, d) if per_example else (d,)
+    if dgamma is None:
+        dgamma = _empty(shape, torch.float32, x.device, stream)
+    if dbeta is None:
+        dbeta = _empty(shape, torch.float32, x.device, stream)
+    _per_row(dgamma, shape, torch.float32, "dgamma")
+    _per_row(dbeta, shape, torch.float32, "dbeta")
+    code = _model_dtype(x, "x")
+    need = eogp_layer_norm_backward_workspace_size(groups, rows, d, code)
+    if ws is None and need:
+        ws = _empty((need,), torch.uint8, x.device, stream)
+    ws, wsb = _workspace(need, x.device, ws)
+    _check(L.eogp_layer_norm_backward(_ptr(dy), lddy, _ptr(x), ldx, code, _ptr(gamma),
+                                      F32 if gamma is None else _DTYPE_CODE[gamma.dtype], _ptr(mean),
+                                      _ptr(rstd), _ptr(token_mask), _ptr(residual), ldr, groups, rows, d,
+                                      _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), _ptr(ws), wsb,
+                                      _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+def eogp_softmax_xent(logits, labels, token_mask=None, grad_scale=1.0, grad=True, loss=None,
+                      dlogits=None, stream=None):
+    """(loss float32, dlogits) of logits [n, V] or [N, T, V] and labels int64 [n] or
+    [N, T]; grad=False leaves dlogits out (None); dlogits may be the logits; see
+    eogp_softmax_xent in eogp.h."""
+    L = load()
+    _need_cuda(logits, labels, token_mask, loss, dlogits)
+    n, V, ldl = _rows_of(logits, "logits")
+    lead = logits.shape[:-1]
+    _per_row(labels, lead, torch.int64, "labels")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    if loss is None:
+        loss = _empty(lead, torch.float32, logits.device, stream)
+    _per_row(loss, lead, torch.float32, "loss")
+    if not grad and dlogits is not None:
+        raise ValueError("dlogits without grad")
+    ldd = 0
+    if grad:
+        if dlogits is None:
+            dlogits = _empty(tuple(logits.shape), logits.dtype, logits.device, stream)
+        _same_shape(dlogits, logits, "dlogits")
+        _, _, ldd = _rows_of(dlogits, "dlogits")
+    _check(L.eogp_softmax_xent(_ptr(logits), _model_dtype(logits, "logits"), ldl, _ptr(labels),
+                               _ptr(token_mask), n, V, float(grad_scale), _ptr(loss), _ptr(dlogits), ldd,
+                               _stream(stream)))
+    return loss, dlogits
+
+
+def eogp_sample_tokens(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                       token_mask=None, out=None, stream=None):
+    """Tokens int64 drawn from logits [n, V] or [N, T, V] with uniforms float32 [n] or
+    [N, T] in [0, 1); see eogp_sample_tokens in eogp.h."""
+    L = load()
+    _need_cuda(logits, uniforms, token_mask, out)
+    n, V, ldl = _rows_of(logits, "logits")
+    lead = logits.shape[:-1]
+    _per_row(uniforms, lead, torch.float32, "uniforms")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
+    if out is None:
+        out = _empty(lead, torch.int64, logits.device, stream)
+    _per_row(out, lead, torch.int64, "out")
+    _check(L.eogp_sample_tokens(_ptr(logits), _model_dtype(logits, "logits"), ldl, n, V, _ptr(uniforms),
+                                _ptr(token_mask), float(temperature), int(top_k), float(top_p),
+                                float(min_p), _ptr(out), _stream(stream)))
+    return out
+
+
 def eogp_version() -> int:
     return int(load().eogp_version())
 
@@ -594,9 +862,11 @@ def eogp_version() -> int:
 KT_ROTATION_GEMM, KT_RETAINED, KT_PCA_GEMM, KT_SIGN_PACK = 0, 1, 2, 3
 KT_SCORE_PASS, KT_SCORE_MERGE, KT_SCORE_PREP, KT_COMPACTION = 4, 5, 6, 7
 KT_SRHT, KT_EKFAC, KT_PCA_FIT = 8, 9, 10
+KT_EMBED, KT_LAYER_NORM, KT_XENT, KT_SAMPLE = 11, 12, 13, 14
 KERNEL_CLASSES = {"rotation_gemm": 0, "retained": 1, "pca_gemm": 2, "sign_pack": 3,
                   "score_pass": 4, "score_merge": 5, "score_prep": 6, "compaction": 7,
-                  "srht": 8, "ekfac": 9, "pca_fit": 10}
+                  "srht": 8, "ekfac": 9, "pca_fit": 10, "embed": 11, "layer_norm": 12,
+                  "xent": 13, "sample": 14}
 
 
 def eogp_timing_enable(on: bool = True):
