@@ -65,21 +65,6 @@ __device__ __forceinline__ uint64_t share_of(uint64_t total, uint32_t part) {
   return (total >> 24) * part + (((total & 0xFFFFFF) * part) >> 24);
 }
 
-// What is kept so far: every element before (bin, key, index) in the order, that one included.
-struct Bound {
-  int bin = kBins;
-  uint32_t key = 0xFFFFFFFFu, index = 0xFFFFFFFFu;
-  __device__ __forceinline__ bool keeps(int b, uint32_t k, uint32_t i) const {
-    return b < bin || (b == bin && (k < key || (k == key && i <= index)));
-  }
-  __device__ __forceinline__ Bound least(const Bound& o) const { return keeps(o.bin, o.key, o.index) ? o : *this; }
-};
-
-struct Found {
-  uint32_t digit, count_before, count;
-  uint64_t mass_before, mass;
-};
-
 // Inclusive sum over a wave.
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   const int lane = threadIdx.x & 63;
@@ -90,275 +75,421 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   return v;
 }
 
+__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor((unsigned long long)v, off);
+  return v;
+}
+
+// Sum over the block, in every thread; `slot` is free again after the next barrier.
 template <int NT>
-struct Shared {
-  uint32_t count[kBins];
-  unsigned long long mass[kBins];
-  uint64_t wave_count[NT / 64], wave_mass[NT / 64];
-  float slot[NT / 64];
+__device__ __forceinline__ uint64_t block_total(uint64_t v, uint64_t* slot) {
+  v = wave_total(v);
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = slot[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) v += slot[w];
+  return v;
+}
+
+// floor(u * total), u in steps of 2^-24 and clamped to [0, 1)
+__device__ __forceinline__ uint64_t target_of(uint64_t total, float u) {
+  return share_of(total, (uint32_t)fminf(fmaxf(floorf(u * 16777216.f), 0.f), 16777215.f));
+}
+
+// The largest logit of the row, in every thread (-inf if there is none); `mine`: this thread's.
+template <typename Row, int NT>
+__device__ __forceinline__ float row_max(Row& r, int64_t V, float* slot, float& mine) {
+  float m = -INFINITY;
+  r.each(V, [&](int, int64_t, const auto& v) {
+#pragma unroll
+    for (int e = 0; e < Row::E; ++e) m = fmaxf(m, v[e]);   // (passes over NaN)
+  });
+  mine = m;
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) m = fmaxf(m, slot[w]);
+  return m;
+}
+
+// A row of up to 2^20 logits has this many turns of its block (one piece per thread each).
+template <typename T, int NT, int P>
+constexpr int kTurns = P > 0 ? P : (int)(kMaxVocab / (NT * kPiece<T>));
+
+// Draws from the weights kept(logit, index): each wave's sum of each turn (turns, then waves, are in
+// index order) shows the wave and turn of the drawn token; that wave reads its pieces again.
+template <typename T, int NT, typename Row, typename Kept>
+__device__ void draw(Row& r, const T* l, int64_t V, float u, uint64_t* turn_mass, int64_t* out, Kept&& kept) {
+  constexpr int E = kPiece<T>, kWaves = NT / 64;
+  const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  r.each(V, [&](int p, int64_t c, const auto& v) {
+    uint64_t s = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += kept(v[e], (uint32_t)c + e);
+    s = wave_total(s);
+    if (lane == 0) turn_mass[p * kWaves + wid] = s;
+  });
+  __syncthreads();
+  const int sums = (int)((V + NT * E - 1) / (NT * E)) * kWaves;
+  uint64_t total = 0;
+  for (int b = lane; b < sums; b += 64) total += turn_mass[b];
+  const uint64_t target = target_of(wave_total(total), u);   // below the total
+  uint64_t before = 0;
+  int hit = -1;
+  for (int b = 0; b < sums && hit < 0; b += 64) {
+    const uint64_t v = b + lane < sums ? turn_mass[b + lane] : 0;
+    const uint64_t incl = before + wave_scan(v);
+    const uint64_t over = __ballot(incl > target);
+    const int at = over ? __builtin_ctzll(over) : 63;
+    if (over) hit = b + at;
+    before = __shfl((unsigned long long)(over ? incl - v : incl), at);
+  }
+  if (hit < 0 || hit % kWaves != wid) return;
+  const int64_t c = ((int64_t)(hit / kWaves) * NT + threadIdx.x) * E;
+  float v[E];
+  load_piece<T, E>(l, c, V, -INFINITY, v);
+  uint64_t w[E], s = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) s += w[e] = kept(v[e], (uint32_t)c + e);
+  uint64_t run = before + wave_scan(s) - s;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (run <= target && target < run + w[e]) *out = c + e;
+    run += w[e];
+  }
+}
+
+// From the whole distribution (or its w >= min_w): one block per row. P > 0: the row stays in
+// registers as read; P = 0: it is read in both passes.
+template <typename T, int NT, int P>
+__global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ logits, int64_t ldl, int64_t V,
+                                               const float* __restrict__ uniforms,
+                                               const uint8_t* __restrict__ mask, float c, uint32_t min_w,
+                                               int64_t* __restrict__ out) {
+  __shared__ uint64_t turn_mass[kTurns<T, NT, P> * (NT / 64)];
+  __shared__ float slot[NT / 64];
+  const int64_t row = blockIdx.x;
+  if (mask && mask[row] == 0) {
+    if (threadIdx.x == 0) out[row] = -1;
+    return;
+  }
+  const T* l = logits + row * ldl;
+  RegisterRow<T, NT, P> r;
+  r.load(l, V);
+  float mine;
+  const float m = row_max<RegisterRow<T, NT, P>, NT>(r, V, slot, mine);
+  if (m == -INFINITY) {                                // nothing to draw from
+    if (threadIdx.x == 0) out[row] = -1;
+    return;
+  }
+  draw<T, NT>(r, l, V, uniforms[row], turn_mass, out + row, [&](float v, uint32_t) -> uint32_t {
+    const uint32_t w = weight_of(exponent_of(fmaxf(v, -INFINITY), m, c));
+    return w >= min_w ? w : 0;
+  });
+}
+
+// ---- with top_k or top_p -------------------------------------------------------------
+constexpr int kList = 1024;        // candidates that are settled against each other in LDS
+
+// What is kept: every element up to this one in the order.
+struct Bound {
+  uint32_t key, index;
+  __device__ __forceinline__ bool keeps(uint32_t k, uint32_t i) const {
+    return k < key || (k == key && i <= index);
+  }
+};
+
+struct Found {
+  uint32_t digit;
+  uint64_t before, amount;
+};
+
+template <int NT>
+struct SelectLds {
+  unsigned long long hist[kBins];
+  uint32_t key[kList], index[kList], weight[kList];
+  uint64_t sum[NT / 64], sum2[NT / 64];
+  uint32_t listed;
+  float slot[NT / 64], cut;
+  Bound bound;
   Found found;
 };
 
-// The digit at which the running count reaches `want` (BY_MASS: the running mass), starting from
-// (count0, mass0) before the first digit. One exists by the caller's choice of `want`.
-template <int NT, bool BY_MASS>
-__device__ Found find_digit(Shared<NT>& sh, int digits, uint32_t count0, uint64_t mass0, uint64_t want) {
+// The digit at which the running sum of hist, from `before` on, reaches `want`. One exists.
+template <int NT>
+__device__ Found find_digit(SelectLds<NT>& sh, int digits, uint64_t before, uint64_t want) {
   constexpr int kMost = kBins / NT;
   const int per = std::max(1, digits / NT), wid = threadIdx.x >> 6;
-  uint32_t cn[kMost];
-  uint64_t ms[kMost], cs = 0, mm = 0;
+  uint64_t h[kMost], s = 0;
   __syncthreads();                                     // the histogram is complete
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     const int b = threadIdx.x * per + k;
-    const bool in = k < per && b < digits;
-    cn[k] = in ? sh.count[b] : 0;
-    ms[k] = in ? sh.mass[b] : 0;
-    cs += cn[k];
-    mm += ms[k];
+    s += h[k] = k < per && b < digits ? sh.hist[b] : 0;
   }
-  const uint64_t ci = wave_scan(cs), mi = wave_scan(mm);
-  if ((threadIdx.x & 63) == 63) {
-    sh.wave_count[wid] = ci;
-    sh.wave_mass[wid] = mi;
-  }
+  const uint64_t incl = wave_scan(s);
+  if ((threadIdx.x & 63) == 63) sh.sum[wid] = incl;
   __syncthreads();
-  uint64_t c = count0 + ci - cs, m = mass0 + mi - mm;
-  for (int w = 0; w < wid; ++w) {
-    c += sh.wave_count[w];
-    m += sh.wave_mass[w];
-  }
+  uint64_t run = before + incl - s;
+  for (int w = 0; w < wid; ++w) run += sh.sum[w];
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
-    const uint64_t b0 = BY_MASS ? m : c, b1 = b0 + (BY_MASS ? ms[k] : (uint64_t)cn[k]);
-    if (b0 < want && want <= b1) sh.found = Found{(uint32_t)(threadIdx.x * per + k), (uint32_t)c, cn[k], m, ms[k]};
-    c += cn[k];
-    m += ms[k];
+    if (run < want && want <= run + h[k]) sh.found = Found{(uint32_t)(threadIdx.x * per + k), run, h[k]};
+    run += h[k];
   }
   __syncthreads();
   return sh.found;
 }
 
-// One block per row. P > 0: the row stays in registers as read; P = 0: it is read in every pass.
-template <typename T, int NT, int P, bool SELECT>
-__global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ logits, int64_t ldl, int64_t V,
-                                               const float* __restrict__ uniforms,
-                                               const uint8_t* __restrict__ mask, float c, uint32_t top_k,
-                                               uint32_t top_p24, uint32_t min_w, int64_t* __restrict__ out) {
+template <int NT>
+__device__ void clear_hist(SelectLds<NT>& sh, int digits) {
+  __syncthreads();
+  for (int b = threadIdx.x; b < digits; b += NT) sh.hist[b] = 0;
+  __syncthreads();
+}
+
+template <int NT>
+__device__ void clear_list(SelectLds<NT>& sh) {
+  __syncthreads();
+  if (threadIdx.x == 0) sh.listed = 0;
+  __syncthreads();
+}
+
+template <int NT>
+__device__ __forceinline__ void append(SelectLds<NT>& sh, uint32_t key, uint32_t index, uint32_t weight) {
+  const uint32_t at = atomicAdd(&sh.listed, 1u);
+  if (at < kList) {
+    sh.key[at] = key;
+    sh.index[at] = index;
+    sh.weight[at] = weight;
+  }
+}
+
+// Place and mass before element i of the list among its n elements.
+template <int NT>
+__device__ __forceinline__ void settle(const SelectLds<NT>& sh, int n, int i, uint32_t& rank, uint64_t& mass) {
+  const uint32_t k = sh.key[i], x = sh.index[i];
+  rank = 0;
+  mass = 0;
+  for (int j = 0; j < n; ++j) {
+    const bool first = sh.key[j] < k || (sh.key[j] == k && sh.index[j] < x);
+    rank += first;
+    mass += first ? sh.weight[j] : 0;
+  }
+}
+
+// The draw when the list holds every element that can be kept: top_k by rank (0: all of them),
+// top_p of `mass` (of the top_k's own mass if there is a top_k), min_w, then the running mass by
+// index; each element against all others.
+template <int NT>
+__device__ void draw_from_list(SelectLds<NT>& sh, uint32_t top_k, uint32_t top_p24, uint32_t min_w, uint64_t mass,
+                               float u, int64_t* out) {
+  constexpr int kMine = kList / NT;
+  const int n = (int)sh.listed;
+  uint32_t rank[kMine];
+  uint64_t before[kMine], s = 0;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = k * NT + threadIdx.x;
+    if (i >= n) break;
+    settle(sh, n, i, rank[k], before[k]);
+    if (!top_k || rank[k] < top_k) s += sh.weight[i];
+  }
+  s = block_total<NT>(s, sh.sum);
+  if (top_k) mass = s;
+  const uint64_t want = std::max<uint64_t>(1, share_of(mass, top_p24));
+  uint64_t kept = 0;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = k * NT + threadIdx.x;
+    if (i >= n) break;
+    const uint32_t w = sh.weight[i];
+    if ((top_k && rank[k] >= top_k) || before[k] >= want || w < min_w) sh.weight[i] = 0;   // all have read it
+    kept += sh.weight[i];
+  }
+  const uint64_t target = target_of(block_total<NT>(kept, sh.sum2), u);
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const uint32_t w = sh.weight[i], x = sh.index[i];
+    uint64_t run = 0;
+    for (int j = 0; j < n; ++j) run += sh.index[j] < x ? sh.weight[j] : 0;
+    if (run <= target && target < run + w) *out = x;
+  }
+}
+
+// The last kept element when more of a bin's elements tie than the list holds: the bin is split by the
+// key's four digits, then the index's. `row` is read once per digit.
+template <typename T, int NT>
+__device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0>& row, int64_t V, float m, float c, Bound within,
+                           bool by_mass, Found f, uint64_t want) {
   constexpr int E = kPiece<T>;
-  constexpr bool kResident = P > 0;
-  constexpr int kTurns = kResident ? P : (int)(kMaxVocab / (NT * E));
-  __shared__ Shared<NT> sh;
-  __shared__ uint64_t turn_mass[kTurns][NT / 64];      // kept mass of a wave's 64 pieces, in index order
+  const int bin = (int)f.digit;
+  Bound b{0, 0};
+  uint64_t before = f.before;
+  for (int level = 0; level < 8; ++level) {
+    const int shift = 24 - 8 * (level & 3);
+    clear_hist(sh, 256);
+    row.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t i = (uint32_t)i0 + e;
+        const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
+        if (i >= V || bin_of(t) != bin) continue;
+        const uint32_t k = order_key(x);
+        if (!within.keeps(k, i)) continue;
+        uint32_t dig;
+        if (level < 4) {
+          if (level > 0 && ((k ^ b.key) >> (shift + 8)) != 0) continue;
+          dig = (k >> shift) & 255;
+        } else {
+          if (k != b.key || (level > 4 && ((i ^ b.index) >> (shift + 8)) != 0)) continue;
+          dig = (i >> shift) & 255;
+        }
+        atomicAdd(&sh.hist[dig], by_mass ? (unsigned long long)weight_of(t) : 1ull);
+      }
+    });
+    f = find_digit<NT>(sh, 256, before, want);
+    before = f.before;
+    if (level < 4)
+      b.key |= f.digit << shift;
+    else
+      b.index |= f.digit << shift;
+    if (level == 3 && !by_mass && f.before + f.amount == want) {   // all of the last key's elements
+      b.index = 0xFFFFFFFFu;
+      break;
+    }
+  }
+  return b;
+}
+
+// One block per row.
+// 1. top_k up to the block's threads: the top_k-th largest of the threads' own maxima is a lower
+//    bound of the top_k-th largest logit, so the elements at or above it (few more than top_k) hold
+//    all that is kept; they are settled in LDS.
+// 2. Otherwise the row is read again: a histogram over bins of t (monotone in the logit) shows the
+//    bin in which the count or the mass is reached. The elements up to that bin, if the list holds
+//    them, are settled as in 1; if not, only that bin's are, which gives the last kept element; if
+//    even those are too many (ties), the bin is split digit by digit.
+// t_cut: elements below it weigh so little together that top_p is reached before them.
+template <typename T, int NT, int P>
+__global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logits, int64_t ldl, int64_t V,
+                                                      const float* __restrict__ uniforms,
+                                                      const uint8_t* __restrict__ mask, float c, uint32_t top_k,
+                                                      uint32_t top_p24, uint32_t min_w, float t_cut,
+                                                      int64_t* __restrict__ out) {
+  constexpr int E = kPiece<T>;
+  __shared__ SelectLds<NT> sh;
+  __shared__ uint64_t turn_mass[kTurns<T, NT, P> * (NT / 64)];
   const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x, wid = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x;
   if (mask && mask[row] == 0) {
     if (tid == 0) out[row] = -1;
     return;
   }
   const T* l = logits + row * ldl;
-  AnyVec<T, E> raw[kResident ? P : 1];
-  auto load_raw = [&](int64_t at) {
-    AnyVec<T, E> r;
-    if (at + E <= V) {
-      r = *reinterpret_cast<const AnyVec<T, E>*>(l + at);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) r[e] = at + e < V ? l[at + e] : (T)-INFINITY;
+  const float u = uniforms[row];
+  float m, mine;
+  {
+    RegisterRow<T, NT, P> r;
+    r.load(l, V);
+    m = row_max<RegisterRow<T, NT, P>, NT>(r, V, sh.slot, mine);
+    if (m == -INFINITY) {                              // nothing to draw from
+      if (tid == 0) out[row] = -1;
+      return;
     }
-    return r;
-  };
-  if constexpr (kResident) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) raw[p] = load_raw((int64_t)(p * NT + tid) * E);
-  }
-  const int turns = kResident ? P : (int)((V + NT * E - 1) / (NT * E));
-  // f(turn, index of the piece's first element, its logits with NaN as -inf)
-  auto each = [&](auto&& f) {
-    auto one = [&](int p, const AnyVec<T, E>& r) {
-      float v[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = fmaxf((float)r[e], -INFINITY);
-      f(p, (uint32_t)(p * NT + tid) * E, v);
-    };
-    if constexpr (kResident) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) one(p, raw[p]);
-    } else {
-      for (int p = 0; p < turns; ++p) one(p, load_raw((int64_t)(p * NT + tid) * E));
-    }
-  };
-  float m = -INFINITY;
-  each([&](int, uint32_t, const float(&v)[E]) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
-  });
-  m = wave_max(m);
-  if (lane == 0) sh.slot[wid] = m;
-  __syncthreads();
-  for (int w = 0; w < NT / 64; ++w) m = fmaxf(m, sh.slot[w]);
-  if (m == -INFINITY) {                                // nothing to draw from
-    if (tid == 0) out[row] = -1;
-    return;
-  }
-  Bound bound;
-  if constexpr (SELECT) {
-    const uint32_t n_el = (uint32_t)V;
-    auto clear = [&](int digits) {
+    if (top_k && top_k <= NT) {
+      const uint32_t own = order_key(mine);
+      sh.key[tid] = own;
+      if (tid == 0) sh.listed = 0;
       __syncthreads();
-      for (int b = tid; b < digits; b += NT) {
-        sh.count[b] = 0;
-        sh.mass[b] = 0;
-      }
+      uint32_t rank = 0;
+      for (int j = 0; j < NT; ++j) rank += sh.key[j] < own || (sh.key[j] == own && j < tid);
+      if (rank == top_k - 1) sh.cut = mine;
       __syncthreads();
-    };
-    // The last kept element when `want` elements (or that mass) are to be reached, given the
-    // histogram over the bins; `within` limits the candidates. Each pass splits the boundary digit
-    // by the next one: the bits of the key, then of the index. A digit that is taken whole, or
-    // holds one element, ends it. Returns the bound and adds up the mass kept.
-    auto refine = [&](auto by_mass, Found f, const Bound& within, uint64_t want, uint64_t& kept_mass) {
-      constexpr bool kByMass = decltype(by_mass)::value;
-      Bound b;
-      b.bin = (int)f.digit;
-      uint32_t key = 0, index = 0;                     // digits found so far
-      for (int level = 0; level < 8; ++level) {
-        const bool whole = kByMass ? f.count == 1 : f.count_before + f.count == want;
-        if (whole) break;
-        clear(256);
-        const int shift = 24 - 8 * (level & 3);
-        each([&](int, uint32_t i0, const float(&v)[E]) {
+      const float cut = sh.cut;
+      r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+        if (mine < cut) return;
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const uint32_t i = i0 + e;
-            const float t = exponent_of(v[e], m, c);
-            if (i >= n_el || bin_of(t) != b.bin) continue;
-            const uint32_t k = order_key(v[e]);
-            if (!within.keeps(b.bin, k, i)) continue;
-            uint32_t dig;
-            if (level < 4) {
-              if (level > 0 && ((k ^ key) >> (shift + 8)) != 0) continue;
-              dig = (k >> shift) & 255;
-            } else {
-              if (k != key || (level > 4 && ((i ^ index) >> (shift + 8)) != 0)) continue;
-              dig = (i >> shift) & 255;
-            }
-            atomicAdd(&sh.count[dig], 1u);
-            atomicAdd(&sh.mass[dig], (unsigned long long)weight_of(t));
-          }
-        });
-        f = find_digit<NT, kByMass>(sh, 256, f.count_before, f.mass_before, want);
-        if (level < 4) {
-          key |= f.digit << shift;
-          b.key = key | ((1u << shift) - 1);
-        } else {
-          index |= f.digit << shift;
-          b.index = index | ((1u << shift) - 1);
+        for (int e = 0; e < E; ++e) {
+          const float x = fmaxf(v[e], -INFINITY);
+          if (x >= cut && i0 + e < V) append(sh, order_key(x), (uint32_t)i0 + e, weight_of(exponent_of(x, m, c)));
         }
+      });
+      __syncthreads();
+      if (sh.listed <= kList) {
+        draw_from_list<NT>(sh, top_k, top_p24, min_w, 0, u, out + row);
+        return;
       }
-      kept_mass = f.mass_before + f.mass;
-      return b.least(within);
-    };
-    clear(kBins);
-    each([&](int, uint32_t i0, const float(&v)[E]) {
+    }
+  }
+  RegisterRow<T, NT, 0> r;
+  r.load(l, V);
+  Bound bound{0xFFFFFFFFu, 0xFFFFFFFFu};               // everything
+  for (int by_mass = 0; by_mass < 2; ++by_mass) {
+    if (by_mass ? top_p24 == 1u << 24 : top_k == 0) continue;
+    clear_hist(sh, kBins);
+    uint64_t mass = 0;
+    r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        if (i0 + e >= n_el) continue;
-        const float t = exponent_of(v[e], m, c);
-        const int b = bin_of(t);
-        atomicAdd(&sh.count[b], 1u);
-        atomicAdd(&sh.mass[b], (unsigned long long)weight_of(t));
+        const uint32_t i = (uint32_t)i0 + e;
+        const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
+        if (i >= V || !bound.keeps(order_key(x), i)) continue;
+        const uint32_t w = by_mass ? weight_of(t) : 1;
+        mass += w;
+        if (!by_mass || t >= t_cut) atomicAdd(&sh.hist[bin_of(t)], (unsigned long long)w);
       }
     });
-    uint64_t mass = 0;
-    Found fk{}, fp{};
-    if (top_k) fk = find_digit<NT, false>(sh, kBins, 0, 0, top_k);
-    if (top_k && top_p24 == 1u << 24) bound = refine(std::false_type{}, fk, bound, top_k, mass);
-    if (top_p24 < 1u << 24) {
-      if (top_k) {                                     // the bins' sums once more, of what top_k keeps
-        bound = refine(std::false_type{}, fk, bound, top_k, mass);
-        clear(kBins);
-        each([&](int, uint32_t i0, const float(&v)[E]) {
+    mass = block_total<NT>(mass, sh.sum2);
+    const uint64_t want = by_mass ? std::max<uint64_t>(1, share_of(mass, top_p24)) : top_k;
+    const Found f = find_digit<NT>(sh, kBins, 0, want);
+    const int last = (int)f.digit;
+    bool all = true;                                   // elements up to the bin, then of the bin alone
+    for (int only = 0; only < 2; ++only) {
+      all = !only;
+      clear_list(sh);
+      r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            if (i0 + e >= n_el) continue;
-            const float t = exponent_of(v[e], m, c);
-            const int b = bin_of(t);
-            if (!bound.keeps(b, order_key(v[e]), i0 + e)) continue;
-            atomicAdd(&sh.count[b], 1u);
-            atomicAdd(&sh.mass[b], (unsigned long long)weight_of(t));
-          }
-        });
-      } else {
-        uint64_t part = 0;
-        __syncthreads();
-        for (int b = tid; b < kBins; b += NT) part += sh.mass[b];
-        part = wave_scan(part);
-        if (lane == 63) sh.wave_mass[wid] = part;
-        __syncthreads();
-        for (int w = 0; w < NT / 64; ++w) mass += sh.wave_mass[w];
-        __syncthreads();
-      }
-      const uint64_t want = std::max<uint64_t>(1, share_of(mass, top_p24));
-      fp = find_digit<NT, true>(sh, kBins, 0, 0, want);
-      const Bound within = bound;
-      bound = refine(std::true_type{}, fp, within, want, mass);
+        for (int e = 0; e < E; ++e) {
+          const uint32_t i = (uint32_t)i0 + e;
+          const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
+          const int b = bin_of(t);
+          if (b > last || (only && b < last) || i >= V) continue;
+          const uint32_t k = order_key(x);
+          if (bound.keeps(k, i)) append(sh, k, i, weight_of(t));
+        }
+      });
+      __syncthreads();
+      if (sh.listed <= kList) break;
+      if (!only) __syncthreads();                      // all have seen the count before it is cleared
     }
+    const int n = (int)sh.listed;
+    if (n > kList) {
+      bound = split_bin<T, NT>(sh, r, V, m, c, bound, by_mass, f, want);
+      continue;
+    }
+    if (all) {
+      draw_from_list<NT>(sh, by_mass ? 0 : top_k, top_p24, min_w, mass, u, out + row);
+      return;
+    }
+    for (int i = tid; i < n; i += NT) {
+      uint32_t rank;
+      uint64_t before;
+      settle(sh, n, i, rank, before);
+      const bool is_last = by_mass ? f.before + before < want && want <= f.before + before + sh.weight[i]
+                                   : f.before + rank == want - 1;
+      if (is_last) sh.bound = Bound{sh.key[i], sh.index[i]};
+    }
+    __syncthreads();
+    bound = sh.bound;
   }
-  // Kept mass of each wave's pieces, turn by turn; turns and waves are in index order.
-  auto kept_weight = [&](float v, uint32_t i) -> uint32_t {
-    const float t = exponent_of(v, m, c);
-    if constexpr (SELECT) {
-      if (!bound.keeps(bin_of(t), order_key(v), i)) return 0;
-    }
-    const uint32_t w = weight_of(t);
-    return w >= min_w ? w : 0;
-  };
-  each([&](int p, uint32_t i0, const float(&v)[E]) {
-    uint64_t s = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += kept_weight(v[e], i0 + e);
-    for (int off = 32; off > 0; off >>= 1) s += __shfl_xor((unsigned long long)s, off);
-    if (lane == 0) turn_mass[p][wid] = s;
-  });
   __syncthreads();
-  // Every wave finds the turn and the wave that hold the drawn element: 64 sums at a time.
-  const uint64_t* flat = &turn_mass[0][0];
-  const int sums = turns * (NT / 64);
-  uint64_t total = 0;
-  for (int b = lane; b < sums; b += 64) total += flat[b];
-  for (int off = 32; off > 0; off >>= 1) total += __shfl_xor((unsigned long long)total, off);
-  const float u24 = floorf(uniforms[row] * 16777216.f);
-  const uint32_t r = (uint32_t)fminf(fmaxf(u24, 0.f), 16777215.f);
-  const uint64_t target = share_of(total, r);          // below total
-  uint64_t before = 0;
-  int hit = -1;
-  for (int b = 0; b < sums; b += 64) {
-    const uint64_t v = b + lane < sums ? flat[b + lane] : 0;
-    const uint64_t incl = before + wave_scan(v);
-    const uint64_t over = __ballot(incl > target);
-    if (over) {
-      const int at = __builtin_ctzll(over);
-      hit = b + at;
-      before = __shfl((unsigned long long)(incl - v), at);
-      break;
-    }
-    before = __shfl((unsigned long long)incl, 63);
-  }
-  if (hit < 0 || hit % (NT / 64) != wid) return;
-  const int turn = hit / (NT / 64);
-  each([&](int p, uint32_t i0, const float(&v)[E]) {
-    if (p != turn) return;
-    uint64_t w[E], s = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += w[e] = kept_weight(v[e], i0 + e);
-    uint64_t run = before + wave_scan(s) - s;
-    if (run <= target && target < run + s) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (run <= target && target < run + w[e]) out[row] = i0 + e;
-        run += w[e];
-      }
-    }
+  draw<T, NT>(r, l, V, u, turn_mass, out + row, [&](float v, uint32_t i) -> uint32_t {
+    const float x = fmaxf(v, -INFINITY);
+    if (!bound.keeps(order_key(x), i)) return 0;
+    const uint32_t w = weight_of(exponent_of(x, m, c));
+    return w >= min_w ? w : 0;
   });
 }
 
@@ -413,9 +544,15 @@ eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t
     }
     return with_row_shape(ceil_div(V, kPiece<T>), [&](auto nt, auto p) {
       constexpr int NT = decltype(nt)::value, P = decltype(p)::value;
-      auto* kfn = k || p24 < 1u << 24 ? k_sample<T, NT, P, true> : k_sample<T, NT, P, false>;
-      hipLaunchKernelGGL(kfn, dim3((unsigned)n), dim3(NT), 0, s, static_cast<const T*>(logits), ldl, V, uniforms,
-                         mask, c, k, p24, min_w, out);
+      if (k || p24 < 1u << 24) {
+        // V weights of at most 2^(30 + t_cut) each come to less than the (1 - top_p) 2^30 beyond top_p
+        const float t_cut = (float)(std::log2((16777216.0 - p24) / 16777216.0 / (double)V) - 0.01);
+        hipLaunchKernelGGL((k_sample_select<T, NT, P>), dim3((unsigned)n), dim3(NT), 0, s,
+                           static_cast<const T*>(logits), ldl, V, uniforms, mask, c, k, p24, min_w, t_cut, out);
+      } else {
+        hipLaunchKernelGGL((k_sample<T, NT, P>), dim3((unsigned)n), dim3(NT), 0, s, static_cast<const T*>(logits),
+                           ldl, V, uniforms, mask, c, min_w, out);
+      }
       EOGP_LAUNCH_CHECK("sample_tokens");
       return EOGP_OK;
     });

@@ -40,7 +40,6 @@ __global__ __launch_bounds__(NT) void k_xent(const T* logits, int64_t ldl, const
                                              const uint8_t* __restrict__ mask, int64_t V, float gscale,
                                              float* __restrict__ loss, T* dlogits, int64_t ldd) {
   constexpr int E = kPiece<T>;
-  constexpr bool kResident = P > 0;
   __shared__ float slot[2][NT / 64];
   const int64_t row = blockIdx.x;
   const T* l = logits + row * ldl;
@@ -54,45 +53,17 @@ __global__ __launch_bounds__(NT) void k_xent(const T* logits, int64_t ldl, const
     return;
   }
   const float at_label = threadIdx.x == 0 ? (float)l[label] : 0.f;
-  AnyVec<T, E> raw[kResident ? P : 1];
-  if constexpr (kResident) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int64_t c = (int64_t)(p * NT + threadIdx.x) * E;
-      if (c + E <= V) {
-        raw[p] = *reinterpret_cast<const AnyVec<T, E>*>(l + c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) raw[p][e] = c + e < V ? l[c + e] : (T)-INFINITY;
-      }
-    }
-  }
-  auto each = [&](auto&& f) {
-    if constexpr (kResident) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        float v[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = (float)raw[p][e];
-        f((int64_t)(p * NT + threadIdx.x) * E, v);
-      }
-    } else {
-      for (int64_t c = (int64_t)threadIdx.x * E; c < V; c += NT * E) {
-        float v[E];
-        load_piece<T, E>(l, c, V, -INFINITY, v);
-        f(c, v);
-      }
-    }
-  };
+  RegisterRow<T, NT, P> r;
+  r.load(l, V);
   // A NaN among the logits shows in the sum (fmaxf passes over it).
   float m = -INFINITY;
-  each([&](int64_t, const float(&v)[E]) {
+  r.each(V, [&](int, int64_t, const float(&v)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
   });
   m = block_max<NT>(m, slot[0]);
   float s = 0.f;
-  each([&](int64_t, const float(&v)[E]) {
+  r.each(V, [&](int, int64_t, const float(&v)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
   });
@@ -100,7 +71,7 @@ __global__ __launch_bounds__(NT) void k_xent(const T* logits, int64_t ldl, const
   if (threadIdx.x == 0 && loss) loss[row] = logf(s) - (at_label - m);
   if (!dl) return;
   const float log2s = log2f(s);
-  each([&](int64_t c, const float(&v)[E]) {
+  r.each(V, [&](int, int64_t c, const float(&v)[E]) {
     if (c >= V) return;
     float g[E];
 #pragma unroll
