@@ -3,6 +3,7 @@
 // element; a row's last piece may be short.
 #pragma once
 #include <type_traits>
+#include <utility>
 
 #include "common.h"
 
@@ -55,15 +56,60 @@ __device__ __forceinline__ float load_any(const void* p, eogp_dtype t, int64_t c
   return (float)static_cast<const _Float16*>(p)[c];
 }
 
+// Lane moves inside the vector unit (DPP): the value of the lane 1, 2, 4, 8 places before in a row of
+// 16 lanes, then the last lane of the row before (rows 1 and 3), then lane 31 (rows 2 and 3); `other`
+// where there is none. Six such steps make an inclusive scan of a wave, whose total is in lane 63.
+template <int STEP>
+__device__ __forceinline__ uint32_t lane_before(uint32_t x, uint32_t other) {
+  constexpr int kCtrl[6] = {0x111, 0x112, 0x114, 0x118, 0x142, 0x143}, kRows[6] = {15, 15, 15, 15, 10, 12};
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)x, kCtrl[STEP], kRows[STEP], 0xF, false);
+}
+
+template <typename F>
+__device__ __forceinline__ uint32_t scan_steps(uint32_t v, F&& f) {
+  v = f(v, std::integral_constant<int, 0>{});
+  v = f(v, std::integral_constant<int, 1>{});
+  v = f(v, std::integral_constant<int, 2>{});
+  v = f(v, std::integral_constant<int, 3>{});
+  v = f(v, std::integral_constant<int, 4>{});
+  return f(v, std::integral_constant<int, 5>{});
+}
+
+__device__ __forceinline__ float last_lane(uint32_t v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)v, 63));
+}
+
+// Sum and maximum over a wave, in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+  return last_lane(scan_steps(__float_as_uint(v), [](uint32_t x, auto step) {
+    return __float_as_uint(__uint_as_float(x) + __uint_as_float(lane_before<decltype(step)::value>(x, 0)));
+  }));
 }
 
 __device__ __forceinline__ float wave_max(float v) {
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-  return v;
+  return last_lane(scan_steps(__float_as_uint(v), [](uint32_t x, auto step) {
+    return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(lane_before<decltype(step)::value>(x, x))));
+  }));
 }
+
+// Inclusive sums over a wave.
+template <int STEP>
+__device__ __forceinline__ uint64_t add_before(uint64_t v) {
+  return v + ((uint64_t)lane_before<STEP>((uint32_t)(v >> 32), 0) << 32 | lane_before<STEP>((uint32_t)v, 0));
+}
+
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
+  v = add_before<1>(add_before<0>(v));
+  v = add_before<3>(add_before<2>(v));
+  return add_before<5>(add_before<4>(v));
+}
+
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+__device__ __forceinline__ uint64_t wave_total(uint64_t v) { return lane_value(wave_scan(v), 63); }
 
 // Calls f with the element type of a run-time dtype: f(T{}).
 template <typename F>
@@ -77,84 +123,166 @@ inline eogp_status with_type(eogp_dtype t, F&& f) {
 
 namespace eogp {
 
-// A row that a block of NT threads keeps in registers as read: P pieces of 16 bytes per thread, piece
-// p of thread t at element (p NT + t) E; past the row's end the elements are -inf. The passes over it
-// (each) take one piece at a time: pieces past the end cost a scalar branch, and the compiler neither
-// keeps one pass's conversions for the next nor interleaves pieces, both of which cost more registers
-// than the row has left.
-template <typename T, int NT, int P>
+// f(integral_constant<int, 0>), ..., f(integral_constant<int, N - 1>)
+template <int... I, typename F>
+__device__ __forceinline__ void unroll(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// A row that a block of NT threads keeps in registers as read: P pieces of 16 bytes per thread. In
+// index order come groups of G pieces per thread, in a group the waves, in a wave its G pieces of 64
+// lanes. A piece that would pass the end is taken E elements before the end instead, and its elements
+// that other pieces hold read as -inf: so every load is whole and unconditional (a row has at least E
+// elements). The passes over a row (each) take one piece at a time: groups past the end cost a scalar
+// branch, and the compiler neither keeps one pass's conversions for the next nor interleaves pieces,
+// both of which cost more registers than the row has left. The last pass over a row (each_then_load)
+// requests each piece of the next row into the registers that it has just finished with, so that the
+// next row arrives while this one's pass, sums and stores go on.
+template <typename T, int NT, int P, int G = 1>
 struct RegisterRow {
   static constexpr int E = kPiece<T>;
+  static constexpr int kGroup = NT * G * E;                // elements of a group
+  static_assert(P % G == 0, "whole groups");
   AnyVec<T, E> raw[P];
 
-  __device__ __forceinline__ void load(const T* row, int64_t width) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int64_t c = (int64_t)(p * NT + threadIdx.x) * E;
-      if (c + E <= width) {
-        raw[p] = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) raw[p][e] = c + e < width ? row[c + e] : (T)-INFINITY;
-      }
-    }
+  // First element of piece p, from the thread's place (here). The place is hidden from the compiler
+  // in each pass: it would keep the addresses of all pieces in registers from row to row.
+  static __device__ __forceinline__ uint32_t here() {
+    uint32_t b = ((threadIdx.x >> 6) * (G * 64) + (threadIdx.x & 63)) * E;
+    asm volatile("" : "+v"(b));
+    return b;
+  }
+  static __device__ __forceinline__ uint32_t at(uint32_t place, int p) {
+    return place + (uint32_t)((p / G) * kGroup + (p % G) * 64 * E);
   }
 
-  // f(p, index of the piece's first element, its elements as fp32)
+  static __device__ __forceinline__ AnyVec<T, E> fetch(const T* row, uint32_t c, uint32_t width) {
+    return *reinterpret_cast<const AnyVec<T, E>*>(row + (c < width - E ? c : width - E));
+  }
+
+  // f(p, c, first, v) with the elements v of indices c ..; those below `first` read as -inf.
   template <typename F>
-  __device__ __forceinline__ void each(int64_t width, F&& f) {
+  static __device__ __forceinline__ void take(int p, uint32_t c, uint32_t width, const AnyVec<T, E>& x, F&& f) {
+    float v[E];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if ((int64_t)p * NT * E >= width) break;             // uniform
-      asm volatile("" : "+v"(raw[p]));
-      float v[E];
+    for (int e = 0; e < E; ++e) v[e] = (float)x[e];
+    const uint32_t from = c < width - E ? c : width - E;
+    if (from != c) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = (float)raw[p][e];
-      f(p, (int64_t)(p * NT + threadIdx.x) * E, v);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < E; ++e)
+        if (from + e < c) v[e] = -INFINITY;
     }
+    f(p, from, c, v);
+  }
+
+  __device__ __forceinline__ void load(const T* row, uint32_t width) {
+    const uint32_t place = here();
+#pragma unroll
+    for (int p = 0; p < P; ++p) raw[p] = fetch(row, at(place, p), width);
+  }
+
+  template <typename F>
+  __device__ __forceinline__ void each(uint32_t width, F&& f) {
+    const uint32_t place = here();
+    unroll(std::make_integer_sequence<int, P>{}, [&](auto piece) {
+      constexpr int p = decltype(piece)::value;
+      if ((uint32_t)((p / G) * kGroup) < width) {          // uniform
+        AnyVec<T, E> x = raw[p];
+        asm volatile("" : "+v"(x));
+        take(p, at(place, p), width, x, f);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  }
+
+  template <typename F>
+  __device__ __forceinline__ void each_then_load(uint32_t width, F&& f, const T* next) {
+    const uint32_t place = here();
+    unroll(std::make_integer_sequence<int, P>{}, [&](auto piece) {
+      constexpr int p = decltype(piece)::value;
+      if ((uint32_t)((p / G) * kGroup) < width) {          // uniform
+        AnyVec<T, E> x = raw[p];
+        asm volatile("" : "+v"(x));
+        take(p, at(place, p), width, x, f);
+      }
+      raw[p] = fetch(next, at(place, p), width);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
 };
 
-// The same passes over a row that is too long for the registers: it is read in each.
-template <typename T, int NT>
-struct RegisterRow<T, NT, 0> {
-  static constexpr int E = kPiece<T>;
+// The same passes over a row that is too long for the registers, or shorter than a piece: it is read
+// in each.
+template <typename T, int NT, int G>
+struct RegisterRow<T, NT, 0, G> {
+  using Shape = RegisterRow<T, NT, G, G>;
+  static constexpr int E = kPiece<T>, kGroup = Shape::kGroup;
   const T* row;
 
-  __device__ __forceinline__ void load(const T* r, int64_t) { row = r; }
+  static __device__ __forceinline__ AnyVec<T, E> fetch(const T* row, uint32_t c, uint32_t width) {
+    AnyVec<T, E> x;
+    if (c + E <= width) {
+      x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = c + e < width ? row[c + e] : (T)-INFINITY;
+    }
+    return x;
+  }
+
+  __device__ __forceinline__ void load(const T* r, uint32_t) { row = r; }
 
   template <typename F>
-  __device__ __forceinline__ void each(int64_t width, F&& f) {
-    auto piece = [&](int64_t c) {
-      AnyVec<T, E> x;
-      if (c + E <= width) {
-        x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = c + e < width ? row[c + e] : (T)-INFINITY;
-      }
-      return x;
-    };
-    int64_t c = (int64_t)threadIdx.x * E;
-    AnyVec<T, E> next = piece(c);                          // the next piece is on its way while one is taken
-    for (int p = 0; (int64_t)p * NT * E < width; ++p, c += NT * E) {
+  __device__ __forceinline__ void each(uint32_t width, F&& f) {
+    const uint32_t place = Shape::here();
+    auto at = [&](int p) { return (uint32_t)(p / G) * kGroup + Shape::at(place, p % G); };
+    AnyVec<T, E> next = fetch(row, place, width);          // one piece is on its way while another is taken
+    for (int p = 0; (uint64_t)(p / G) * kGroup < width; ++p) {
       float v[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] = (float)next[e];
-      if ((int64_t)(p + 1) * NT * E < width) next = piece(c + NT * E);
-      f(p, c, v);
+      if ((uint64_t)((p + 1) / G) * kGroup < width) next = fetch(row, at(p + 1), width);
+      f(p, at(p), at(p), v);
     }
+  }
+
+  template <typename F>
+  __device__ __forceinline__ void each_then_load(uint32_t width, F&& f, const T* next) {
+    each(width, f);
+    row = next;
   }
 };
 
+// The rows of a block that stays for many: round i takes row i * blocks + (block + 97 i) mod blocks,
+// so that rows that cost nothing (masked ends of examples of a power of two tokens) do not all fall to
+// the same blocks. f(row): whether the row has work; rows without are passed over. -1 at the end.
+struct RowWalk {
+  uint32_t round = 0;
+  template <typename F>
+  __device__ __forceinline__ int64_t next(int64_t n, F&& f) {
+    while ((int64_t)round * gridDim.x < n) {
+      const int64_t row = (int64_t)round * gridDim.x + (blockIdx.x + 97u * round) % gridDim.x;
+      ++round;
+      if (row < n && f(row)) return row;
+    }
+    return -1;
+  }
+};
+
+// Blocks per CU by their registers (threads, pieces per thread); a kernel that holds its row so
+// asks for as many waves per SIMD (NT / 256 of a block).
+constexpr int row_blocks_per_cu(int nt, int p) { return nt == 256 ? 6 : p >= 1 && p <= 4 ? 2 : 1; }
+
 // Threads of the block that holds a row of `pieces` 16-byte pieces in registers, and pieces per
-// thread; none (0) for rows longer than 1,024 threads x 16 pieces, which are read again instead.
-template <typename F>
-inline eogp_status with_row_shape(int64_t pieces, F&& f) {
+// thread; none (0) for rows longer than 1,024 threads x 16 pieces, which are read again instead, and
+// for rows shorter than a piece.
+template <typename T, typename F>
+inline eogp_status with_row_shape(int64_t width, F&& f) {
   using std::integral_constant;
   using N256 = integral_constant<int, 256>;
   using N1024 = integral_constant<int, 1024>;
+  const int64_t pieces = ceil_div(width, kPiece<T>);
+  if (width < kPiece<T>) return f(N256{}, integral_constant<int, 0>{});
   if (pieces <= 512) return f(N256{}, integral_constant<int, 2>{});
   if (pieces <= 1024) return f(N256{}, integral_constant<int, 4>{});
   if (pieces <= 4096) return f(N1024{}, integral_constant<int, 4>{});

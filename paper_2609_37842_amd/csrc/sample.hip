@@ -65,21 +65,6 @@ __device__ __forceinline__ uint64_t share_of(uint64_t total, uint32_t part) {
   return (total >> 24) * part + (((total & 0xFFFFFF) * part) >> 24);
 }
 
-// Inclusive sum over a wave.
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
-  const int lane = threadIdx.x & 63;
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint64_t o = __shfl_up((unsigned long long)v, off);
-    if (lane >= off) v += o;
-  }
-  return v;
-}
-
-__device__ __forceinline__ uint64_t wave_total(uint64_t v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor((unsigned long long)v, off);
-  return v;
-}
-
 // Sum over the block, in every thread; `slot` is free again after the next barrier.
 template <int NT>
 __device__ __forceinline__ uint64_t block_total(uint64_t v, uint64_t* slot) {
@@ -101,7 +86,7 @@ __device__ __forceinline__ uint64_t target_of(uint64_t total, float u) {
 template <typename Row, int NT>
 __device__ __forceinline__ float row_max(Row& r, int64_t V, float* slot, float& mine) {
   float m = -INFINITY;
-  r.each(V, [&](int, int64_t, const auto& v) {
+  r.each((uint32_t)V, [&](int, uint32_t, uint32_t, const auto& v) {
 #pragma unroll
     for (int e = 0; e < Row::E; ++e) m = fmaxf(m, v[e]);   // (passes over NaN)
   });
@@ -114,80 +99,111 @@ __device__ __forceinline__ float row_max(Row& r, int64_t V, float* slot, float& 
   return m;
 }
 
-// A row of up to 2^20 logits has this many turns of its block (one piece per thread each).
+// Pieces of a wave whose weights are summed at once, and how many such groups a row has at most.
+constexpr int group_of(int p) { return p == 2 ? 2 : 4; }
 template <typename T, int NT, int P>
-constexpr int kTurns = P > 0 ? P : (int)(kMaxVocab / (NT * kPiece<T>));
+constexpr int kGroups = P > 0 ? P / group_of(P) : (int)(kMaxVocab / (NT * group_of(P) * kPiece<T>));
 
-// Draws from the weights kept(logit, index): each wave's sum of each turn (turns, then waves, are in
-// index order) shows the wave and turn of the drawn token; that wave reads its pieces again.
-template <typename T, int NT, typename Row, typename Kept>
-__device__ void draw(Row& r, const T* l, int64_t V, float u, uint64_t* turn_mass, int64_t* out, Kept&& kept) {
-  constexpr int E = kPiece<T>, kWaves = NT / 64;
+// The token drawn from the weights kept(logit, index), of which group_mass holds each wave's sums,
+// group by group (in index order come groups, then waves): the wave that holds it reads its group's
+// pieces again.
+template <typename T, int NT, int G, typename Kept>
+__device__ void find_token(const T* l, int64_t V, float u, const uint64_t* group_mass, int64_t* out, Kept&& kept) {
+  constexpr int E = kPiece<T>, kWaves = NT / 64, kGroup = NT * G * E;
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  r.each(V, [&](int p, int64_t c, const auto& v) {
-    uint64_t s = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += kept(v[e], (uint32_t)c + e);
-    s = wave_total(s);
-    if (lane == 0) turn_mass[p * kWaves + wid] = s;
-  });
-  __syncthreads();
-  const int sums = (int)((V + NT * E - 1) / (NT * E)) * kWaves;
+  const int sums = (int)((V + kGroup - 1) / kGroup) * kWaves;
   uint64_t total = 0;
-  for (int b = lane; b < sums; b += 64) total += turn_mass[b];
+  for (int b = lane; b < sums; b += 64) total += group_mass[b];
   const uint64_t target = target_of(wave_total(total), u);   // below the total
   uint64_t before = 0;
   int hit = -1;
   for (int b = 0; b < sums && hit < 0; b += 64) {
-    const uint64_t v = b + lane < sums ? turn_mass[b + lane] : 0;
+    const uint64_t v = b + lane < sums ? group_mass[b + lane] : 0;
     const uint64_t incl = before + wave_scan(v);
     const uint64_t over = __ballot(incl > target);
     const int at = over ? __builtin_ctzll(over) : 63;
     if (over) hit = b + at;
-    before = __shfl((unsigned long long)(over ? incl - v : incl), at);
+    before = lane_value(over ? incl - v : incl, at);
   }
   if (hit < 0 || hit % kWaves != wid) return;
-  const int64_t c = ((int64_t)(hit / kWaves) * NT + threadIdx.x) * E;
-  float v[E];
-  load_piece<T, E>(l, c, V, -INFINITY, v);
-  uint64_t w[E], s = 0;
+  for (int q = 0; q < G; ++q) {
+    const int64_t c = (int64_t)(hit / kWaves) * kGroup + ((int64_t)(wid * G + q) * 64 + lane) * E;
+    float v[E];
+    load_piece<T, E>(l, c, V, -INFINITY, v);
+    uint64_t w[E], s = 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) s += w[e] = kept(v[e], (uint32_t)c + e);
-  uint64_t run = before + wave_scan(s) - s;
+    for (int e = 0; e < E; ++e) s += w[e] = kept(v[e], (uint32_t)c + e);
+    const uint64_t incl = before + wave_scan(s);
+    uint64_t run = incl - s;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if (run <= target && target < run + w[e]) *out = c + e;
-    run += w[e];
+    for (int e = 0; e < E; ++e) {
+      if (run <= target && target < run + w[e]) *out = c + e;
+      run += w[e];
+    }
+    before = lane_value(incl, 63);
   }
 }
 
-// From the whole distribution (or its w >= min_w): one block per row. P > 0: the row stays in
-// registers as read; P = 0: it is read in both passes.
+// Adds a piece's weights to its group's sum; the group's last piece stores the wave's.
+template <int NT, int G, int E, typename Kept>
+__device__ __forceinline__ void add_piece(int p, uint32_t c, const float (&v)[E], uint64_t& sum, uint64_t* group_mass,
+                                          Kept&& kept) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum += kept(v[e], c + e);
+  if (p % G == G - 1) {
+    const uint64_t total = wave_scan(sum);
+    if ((threadIdx.x & 63) == 63) group_mass[(p / G) * (NT / 64) + (threadIdx.x >> 6)] = total;
+    sum = 0;
+  }
+}
+
+// From the whole distribution (or its w >= min_w). A block takes a row at a time. P > 0: the row stays
+// in registers as read, and the next one is requested piece by piece as the weights' pass lets go of
+// this one; P = 0: it is read in both passes.
 template <typename T, int NT, int P>
-__global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ logits, int64_t ldl, int64_t V,
-                                               const float* __restrict__ uniforms,
-                                               const uint8_t* __restrict__ mask, float c, uint32_t min_w,
-                                               int64_t* __restrict__ out) {
-  __shared__ uint64_t turn_mass[kTurns<T, NT, P> * (NT / 64)];
-  __shared__ float slot[NT / 64];
-  const int64_t row = blockIdx.x;
-  if (mask && mask[row] == 0) {
+__global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_sample(
+    const T* __restrict__ logits, int64_t ldl, int64_t n, int64_t V, const float* __restrict__ uniforms,
+    const uint8_t* __restrict__ mask, float c, uint32_t min_w, int64_t* __restrict__ out) {
+  constexpr int E = kPiece<T>, G = group_of(P);
+  __shared__ uint64_t group_mass[2][kGroups<T, NT, P> * (NT / 64)];
+  __shared__ float slot[2][NT / 64];
+  using Row = RegisterRow<T, NT, P, G>;
+  RowWalk walk;
+  auto live = [&](int64_t row) {
+    if (!mask || mask[row] != 0) return true;
     if (threadIdx.x == 0) out[row] = -1;
-    return;
+    return false;
+  };
+  Row r;
+  int64_t row = walk.next(n, live);
+  if (row < 0) return;
+  r.load(logits + row * ldl, (uint32_t)V);
+  for (int turn = 0;; turn ^= 1) {                     // rows alternate between the two sets of sums
+    const T* l = logits + row * ldl;
+    float mine;
+    const float m = row_max<Row, NT>(r, V, slot[turn], mine);
+    const int64_t after = walk.next(n, live);
+    auto kept = [&](float v, uint32_t) -> uint32_t {
+      const uint32_t w = weight_of(exponent_of(fmaxf(v, -INFINITY), m, c));
+      return w >= min_w ? w : 0;
+    };
+    uint64_t sum = 0;
+    auto add = [&](int p, uint32_t i0, uint32_t, const float(&v)[E]) {
+      add_piece<NT, G, E>(p, i0, v, sum, group_mass[turn], kept);
+    };
+    if (after < 0)
+      r.each((uint32_t)V, add);
+    else
+      r.each_then_load((uint32_t)V, add, logits + after * ldl);
+    __syncthreads();
+    if (m == -INFINITY) {                              // nothing to draw from
+      if (threadIdx.x == 0) out[row] = -1;
+    } else {
+      find_token<T, NT, G>(l, V, uniforms[row], group_mass[turn], out + row, kept);
+    }
+    if (after < 0) return;
+    row = after;
   }
-  const T* l = logits + row * ldl;
-  RegisterRow<T, NT, P> r;
-  r.load(l, V);
-  float mine;
-  const float m = row_max<RegisterRow<T, NT, P>, NT>(r, V, slot, mine);
-  if (m == -INFINITY) {                                // nothing to draw from
-    if (threadIdx.x == 0) out[row] = -1;
-    return;
-  }
-  draw<T, NT>(r, l, V, uniforms[row], turn_mass, out + row, [&](float v, uint32_t) -> uint32_t {
-    const uint32_t w = weight_of(exponent_of(fmaxf(v, -INFINITY), m, c));
-    return w >= min_w ? w : 0;
-  });
 }
 
 // ---- with top_k or top_p -------------------------------------------------------------
@@ -209,6 +225,7 @@ struct Found {
 template <int NT>
 struct SelectLds {
   unsigned long long hist[kBins];
+  uint32_t reach[8][3];
   uint32_t key[kList], index[kList], weight[kList];
   uint64_t sum[NT / 64], sum2[NT / 64];
   uint32_t listed;
@@ -318,10 +335,37 @@ __device__ void draw_from_list(SelectLds<NT>& sh, uint32_t top_k, uint32_t top_p
   }
 }
 
+// A lower bound of the top_k-th largest logit (1 <= top_k <= NT): of the upper 16 bits of the threads'
+// own largest logits (as order keys), the least that top_k of them reach; the logit with that key and
+// its lower bits set. Two bits are found at a time, by the threads below each of three candidates.
+template <int NT>
+__device__ float lower_bound_of(SelectLds<NT>& sh, uint32_t key, uint32_t top_k) {
+  if (threadIdx.x < 24) sh.reach[threadIdx.x / 3][threadIdx.x % 3] = 0;
+  if (threadIdx.x == 0) sh.listed = 0;
+  __syncthreads();
+  uint32_t found = 0;
+  for (int step = 0; step < 8; ++step) {
+    const int shift = 14 - 2 * step;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      const uint64_t below = __ballot(key >> 16 < found + ((uint32_t)(q + 1) << shift));
+      if ((threadIdx.x & 63) == 0) atomicAdd(&sh.reach[step][q], (uint32_t)__popcll(below));
+    }
+    __syncthreads();
+    uint32_t take = 0;                                 // the most with fewer than top_k threads below
+    for (int q = 0; q < 3; ++q)
+      if (sh.reach[step][q] < top_k) take = q + 1;
+    found += take << shift;
+  }
+  const uint32_t last = found << 16 | 0xFFFFu;
+  const uint32_t bits = last & 0x80000000u ? last : ~last & 0x7FFFFFFFu;
+  return last >= 0xFF800000u ? -INFINITY : __uint_as_float(bits);   // (-inf's own key, or beyond)
+}
+
 // The last kept element when more of a bin's elements tie than the list holds: the bin is split by the
 // key's four digits, then the index's. `row` is read once per digit.
 template <typename T, int NT>
-__device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0>& row, int64_t V, float m, float c, Bound within,
+__device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0, 4>& row, int64_t V, float m, float c, Bound within,
                            bool by_mass, Found f, uint64_t want) {
   constexpr int E = kPiece<T>;
   const int bin = (int)f.digit;
@@ -330,10 +374,10 @@ __device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0>& row, int64_
   for (int level = 0; level < 8; ++level) {
     const int shift = 24 - 8 * (level & 3);
     clear_hist(sh, 256);
-    row.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+    row.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t i = (uint32_t)i0 + e;
+        const uint32_t i = i0 + e;
         const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
         if (i >= V || bin_of(t) != bin) continue;
         const uint32_t k = order_key(x);
@@ -380,7 +424,8 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
                                                       int64_t* __restrict__ out) {
   constexpr int E = kPiece<T>;
   __shared__ SelectLds<NT> sh;
-  __shared__ uint64_t turn_mass[kTurns<T, NT, P> * (NT / 64)];
+  constexpr int kSums = (int)(((P > 0 ? P * NT * E : kMaxVocab) + NT * 4 * E - 1) / (NT * 4 * E)) * (NT / 64);
+  __shared__ uint64_t group_mass[kSums];
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
   if (mask && mask[row] == 0) {
@@ -392,28 +437,21 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
   float m, mine;
   {
     RegisterRow<T, NT, P> r;
-    r.load(l, V);
+    r.load(l, (uint32_t)V);
     m = row_max<RegisterRow<T, NT, P>, NT>(r, V, sh.slot, mine);
     if (m == -INFINITY) {                              // nothing to draw from
       if (tid == 0) out[row] = -1;
       return;
     }
     if (top_k && top_k <= NT) {
-      const uint32_t own = order_key(mine);
-      sh.key[tid] = own;
-      if (tid == 0) sh.listed = 0;
-      __syncthreads();
-      uint32_t rank = 0;
-      for (int j = 0; j < NT; ++j) rank += sh.key[j] < own || (sh.key[j] == own && j < tid);
-      if (rank == top_k - 1) sh.cut = mine;
-      __syncthreads();
-      const float cut = sh.cut;
-      r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+      const float cut = lower_bound_of<NT>(sh, order_key(mine), top_k);
+      r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t first, const float(&v)[E]) {
         if (mine < cut) return;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float x = fmaxf(v[e], -INFINITY);
-          if (x >= cut && i0 + e < V) append(sh, order_key(x), (uint32_t)i0 + e, weight_of(exponent_of(x, m, c)));
+          const uint32_t i = i0 + e;
+          if (x >= cut && i >= first && i < V) append(sh, order_key(x), i, weight_of(exponent_of(x, m, c)));
         }
       });
       __syncthreads();
@@ -423,17 +461,17 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
       }
     }
   }
-  RegisterRow<T, NT, 0> r;
-  r.load(l, V);
+  RegisterRow<T, NT, 0, 4> r;
+  r.load(l, (uint32_t)V);
   Bound bound{0xFFFFFFFFu, 0xFFFFFFFFu};               // everything
   for (int by_mass = 0; by_mass < 2; ++by_mass) {
     if (by_mass ? top_p24 == 1u << 24 : top_k == 0) continue;
     clear_hist(sh, kBins);
     uint64_t mass = 0;
-    r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+    r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t i = (uint32_t)i0 + e;
+        const uint32_t i = i0 + e;
         const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
         if (i >= V || !bound.keeps(order_key(x), i)) continue;
         const uint32_t w = by_mass ? weight_of(t) : 1;
@@ -449,10 +487,10 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
     for (int only = 0; only < 2; ++only) {
       all = !only;
       clear_list(sh);
-      r.each(V, [&](int, int64_t i0, const float(&v)[E]) {
+      r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const uint32_t i = (uint32_t)i0 + e;
+          const uint32_t i = i0 + e;
           const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
           const int b = bin_of(t);
           if (b > last || (only && b < last) || i >= V) continue;
@@ -484,13 +522,18 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
     __syncthreads();
     bound = sh.bound;
   }
-  __syncthreads();
-  draw<T, NT>(r, l, V, u, turn_mass, out + row, [&](float v, uint32_t i) -> uint32_t {
+  auto kept = [&](float v, uint32_t i) -> uint32_t {
     const float x = fmaxf(v, -INFINITY);
     if (!bound.keeps(order_key(x), i)) return 0;
     const uint32_t w = weight_of(exponent_of(x, m, c));
     return w >= min_w ? w : 0;
+  };
+  uint64_t sum = 0;
+  r.each((uint32_t)V, [&](int p, uint32_t i0, uint32_t, const float(&v)[E]) {
+    add_piece<NT, 4, E>(p, i0, v, sum, group_mass, kept);
   });
+  __syncthreads();
+  find_token<T, NT, 4>(l, V, u, group_mass, out + row, kept);
 }
 
 // Temperature 0: the lowest index of the largest logit.
@@ -542,7 +585,7 @@ eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t
       EOGP_LAUNCH_CHECK("sample_tokens (argmax)");
       return EOGP_OK;
     }
-    return with_row_shape(ceil_div(V, kPiece<T>), [&](auto nt, auto p) {
+    return with_row_shape<T>(V, [&](auto nt, auto p) {
       constexpr int NT = decltype(nt)::value, P = decltype(p)::value;
       if (k || p24 < 1u << 24) {
         // V weights of at most 2^(30 + t_cut) each come to less than the (1 - top_p) 2^30 beyond top_p
@@ -550,8 +593,9 @@ eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t
         hipLaunchKernelGGL((k_sample_select<T, NT, P>), dim3((unsigned)n), dim3(NT), 0, s,
                            static_cast<const T*>(logits), ldl, V, uniforms, mask, c, k, p24, min_w, t_cut, out);
       } else {
-        hipLaunchKernelGGL((k_sample<T, NT, P>), dim3((unsigned)n), dim3(NT), 0, s, static_cast<const T*>(logits),
-                           ldl, V, uniforms, mask, c, min_w, out);
+        const int64_t blocks = std::min<int64_t>(n, kCus * row_blocks_per_cu(NT, P));
+        hipLaunchKernelGGL((k_sample<T, NT, P>), dim3((unsigned)blocks), dim3(NT), 0, s,
+                           static_cast<const T*>(logits), ldl, n, V, uniforms, mask, c, min_w, out);
       }
       EOGP_LAUNCH_CHECK("sample_tokens");
       return EOGP_OK;

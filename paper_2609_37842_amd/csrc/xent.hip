@@ -31,57 +31,76 @@ __device__ __forceinline__ float block_sum(float v, float* slot) {
   return v;
 }
 
-// One block per row. loss = ln sum_i exp(l_i - m) - (l_label - m), m = max l;
+// loss = ln sum_i exp(l_i - m) - (l_label - m), m = max l;
 // dl_i = g (exp(l_i - m) / sum - [i = label]) = g (2^((l_i - m) log2 e - log2 sum) - [i = label]).
-// With P > 0 the row stays in registers as read (P pieces of 16 bytes per lane), so HBM sees one
-// read and one write; P = 0 reads it three times, for rows longer than the registers hold.
-template <typename T, int NT, int P>
-__global__ __launch_bounds__(NT) void k_xent(const T* logits, int64_t ldl, const int64_t* __restrict__ labels,
-                                             const uint8_t* __restrict__ mask, int64_t V, float gscale,
-                                             float* __restrict__ loss, T* dlogits, int64_t ldd) {
+// A block takes a row at a time. With P > 0 the row stays in registers as read, so HBM sees one read
+// and one write, and the next row is requested piece by piece as the gradient's pass lets go of this
+// one; P = 0 reads the row three times, for rows longer than the registers hold.
+template <typename T, int NT, int P, bool GRAD>
+__global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_xent(
+    const T* logits, int64_t ldl, const int64_t* __restrict__ labels, const uint8_t* __restrict__ mask, int64_t n,
+    int64_t V, float gscale, float* __restrict__ loss, T* dlogits, int64_t ldd) {
   constexpr int E = kPiece<T>;
   __shared__ float slot[2][NT / 64];
-  const int64_t row = blockIdx.x;
-  const T* l = logits + row * ldl;
-  T* dl = dlogits ? dlogits + row * ldd : nullptr;
-  const int64_t label = labels[row];
-  if ((mask && mask[row] == 0) || label < 0 || label >= V) {   // no loss; not read
+  RowWalk walk;
+  auto live = [&](int64_t row) {                       // rows without a loss are not read
+    const int64_t label = labels[row];
+    if ((!mask || mask[row] != 0) && label >= 0 && label < V) return true;
     if (threadIdx.x == 0 && loss) loss[row] = 0.f;
     float zero[E] = {};
-    if (dl)
-      for (int64_t c = (int64_t)threadIdx.x * E; c < V; c += NT * E) store_piece<T, E>(dl, c, V, zero);
-    return;
-  }
-  const float at_label = threadIdx.x == 0 ? (float)l[label] : 0.f;
+    if (GRAD)
+      for (int64_t c = (int64_t)threadIdx.x * E; c < V; c += NT * E)
+        store_piece<T, E>(dlogits + row * ldd, c, V, zero);
+    return false;
+  };
   RegisterRow<T, NT, P> r;
-  r.load(l, V);
-  // A NaN among the logits shows in the sum (fmaxf passes over it).
-  float m = -INFINITY;
-  r.each(V, [&](int, int64_t, const float(&v)[E]) {
+  int64_t row = walk.next(n, live);
+  if (row < 0) return;
+  r.load(logits + row * ldl, V);
+  for (;;) {
+    const uint32_t label = (uint32_t)labels[row];
+    const float at_label = threadIdx.x == 0 ? (float)logits[row * ldl + label] : 0.f;
+    // A NaN among the logits shows in the sum (fmaxf passes over it).
+    float m = -INFINITY;
+    r.each(V, [&](int, uint32_t, uint32_t, const float(&v)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
-  });
-  m = block_max<NT>(m, slot[0]);
-  float s = 0.f;
-  r.each(V, [&](int, int64_t, const float(&v)[E]) {
+      for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);
+    });
+    m = block_max<NT>(m, slot[0]);
+    float s = 0.f;
+    r.each(V, [&](int, uint32_t, uint32_t, const float(&v)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
-  });
-  s = block_sum<NT>(s, slot[1]);
-  if (threadIdx.x == 0 && loss) loss[row] = logf(s) - (at_label - m);
-  if (!dl) return;
-  const float log2s = log2f(s);
-  r.each(V, [&](int, int64_t c, const float(&v)[E]) {
-    if (c >= V) return;
-    float g[E];
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((v[e] - m) * kLog2e);
+    });
+    s = block_sum<NT>(s, slot[1]);
+    if (threadIdx.x == 0 && loss) loss[row] = logf(s) - (at_label - m);
+    const int64_t after = walk.next(n, live);
+    T* dl = dlogits + row * ldd;
+    const float log2s = log2f(s);
+    auto gradient = [&](int, uint32_t c, uint32_t first, const float(&v)[E]) {
+      if constexpr (GRAD) {
+        AnyVec<T, E> g;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      g[e] = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e - log2s);
-      if (c + e == label) g[e] -= 1.f;
-      g[e] *= gscale;
+        for (int e = 0; e < E; ++e) {
+          const float p = __builtin_amdgcn_exp2f((v[e] - m) * kLog2e - log2s);
+          g[e] = (T)((c + e == label ? p - 1.f : p) * gscale);
+        }
+        if (P > 0 ? c == first : c + E <= V) {
+          *reinterpret_cast<AnyVec<T, E>*>(dl + c) = g;
+        } else {                                       // other pieces hold what lies before `first`
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (c + e >= first && c + e < V) dl[c + e] = g[e];
+        }
+      }
+    };
+    if (after < 0) {
+      r.each(V, gradient);
+      return;
     }
-    store_piece<T, E>(dl, c, V, g);
-  });
+    r.each_then_load(V, gradient, logits + after * ldl);
+    row = after;
+  }
 }
 
 }  // namespace
@@ -93,16 +112,17 @@ eogp_status softmax_xent(const void* logits, eogp_dtype t, int64_t ldl, const in
   timing::Scope ts(EOGP_KT_XENT, s);
   return with_type(t, [&](auto el) {
     using T = decltype(el);
-    const int64_t pieces = ceil_div(V, kPiece<T>);
     auto go = [&](auto nt, auto p) {
       constexpr int NT = decltype(nt)::value;
-      hipLaunchKernelGGL((k_xent<T, NT, decltype(p)::value>), dim3((unsigned)n), dim3(NT), 0, s,
-                         static_cast<const T*>(logits), ldl, labels, mask, V, gscale, loss,
-                         static_cast<T*>(dlogits), ldd);
+      constexpr int P = decltype(p)::value;
+      const int64_t blocks = std::min<int64_t>(n, kCus * row_blocks_per_cu(NT, P));
+      auto* kfn = dlogits ? k_xent<T, NT, P, true> : k_xent<T, NT, P, false>;
+      hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(NT), 0, s, static_cast<const T*>(logits), ldl, labels, mask,
+                         n, V, gscale, loss, static_cast<T*>(dlogits), ldd);
       EOGP_LAUNCH_CHECK("softmax_xent");
       return EOGP_OK;
     };
-    return with_row_shape(pieces, go);
+    return with_row_shape<T>(V, go);
   });
 }
 
