@@ -22,33 +22,50 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
   return v;
 }
 
+// A block's weights in LDS, fp32 (gamma 1 and beta 0 where there is none): as registers they would
+// cost the kernels half of their waves.
+template <int NT>
+__device__ __forceinline__ void stage_weights(float* lds, const void* w, eogp_dtype wt, int64_t d, float none) {
+  for (int c = threadIdx.x; c < d; c += NT) lds[c] = w ? load_any(w, wt, c) : none;
+}
+
+constexpr int norm_threads(int wpr) { return wpr > 4 ? 64 * wpr : 256; }
+
 // y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
 // bytes per lane), so mean and the centred second moment are two exact passes over registers and
-// HBM sees one read and one write. gamma and beta are read once per wave.
+// HBM sees one read and one write.
 template <typename TI, typename TO, int WPR, int P>
-__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm(
+__global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
     const TI* __restrict__ x, int64_t ldx, const void* __restrict__ gamma, const void* __restrict__ beta,
     eogp_dtype wt, float eps, const uint8_t* __restrict__ mask, int64_t n, int64_t d, TO* __restrict__ y,
     int64_t ldy, int ones, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
-  constexpr int E = kPiece<TI>;
-  constexpr int kWaves = WPR > 4 ? WPR : 4, kRows = kWaves / WPR;   // of a block
+  constexpr int E = kPiece<TI>, NT = norm_threads(WPR);
+  constexpr int kRows = NT / 64 / WPR;                 // of a block at once
+  extern __shared__ __align__(16) float weights[];     // gamma, beta: round_up(d, E) each
   __shared__ float slot[2][16];
   const int wid = threadIdx.x >> 6;
   const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;   // place among the row's lanes
-  float g[P][E], b[P][E];
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int64_t c = (int64_t)(p * 64 * WPR + t) * E + e;
-      g[p][e] = gamma && c < d ? load_any(gamma, wt, c) : 1.f;
-      b[p][e] = beta && c < d ? load_any(beta, wt, c) : 0.f;
-    }
+  float *g = weights, *b = weights + (d + E - 1) / E * E;
   const float width = (float)d;               // sums are divided by it: a constant row's mean is exact
-  for (int64_t row = (int64_t)blockIdx.x * kRows + (WPR == 1 ? wid : 0); row < n;
-       row += (int64_t)gridDim.x * kRows) {
+  bool staged = false;
+  for (int64_t first = (int64_t)blockIdx.x * kRows; first < n; first += (int64_t)gridDim.x * kRows) {
+    const int64_t row = first + (WPR == 1 ? wid : 0);
+    const bool live = row < n && (!mask || mask[row] != 0);   // uniform across the row's waves
+    AnyVec<TI, E> raw[P];
+    if (live) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        raw[p] = fetch_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d, (TI)0.f);
+    }
+    if (!staged) {                            // while the first rows are on their way
+      stage_weights<NT>(g, gamma, wt, d, 1.f);
+      stage_weights<NT>(b, beta, wt, d, 0.f);
+      __syncthreads();
+      staged = true;
+    }
+    if (row >= n) continue;
     TO* yr = y + row * ldy;
-    if (mask && mask[row] == 0) {            // not read; zeros
+    if (!live) {                              // not read; zeros
       float zero[E] = {};
 #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -62,18 +79,14 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm(
       }
       continue;
     }
-    const TI* xr = x + row * ldx;
     float v[P][E];
     float s = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      load_piece<TI, E>(xr, c, d, 0.f, v[p]);
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
+      widen<TI, E>(raw[p], v[p]);
 #pragma unroll
       for (int e = 0; e < E; ++e) s += v[p][e];
+    }
     const float mean = row_sum<WPR>(s, slot[0]) / width;
     s = 0.f;
 #pragma unroll
@@ -88,9 +101,12 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      if (c >= d) break;
+      const AnyVec<float, E> gp = *reinterpret_cast<const AlignedVec<float, E>*>(g + c);
+      const AnyVec<float, E> bp = *reinterpret_cast<const AlignedVec<float, E>*>(b + c);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[p][e] = v[p][e] * rstd * g[p][e] + b[p][e];
-      if (c < d) store_piece<TO, E>(yr, c, d, v[p]);
+      for (int e = 0; e < E; ++e) v[p][e] = v[p][e] * rstd * gp[e] + bp[e];
+      store_piece<TO, E>(yr, c, d, v[p]);
     }
     if (t == 0) {
       if (ones) yr[d] = (TO)1.f;
@@ -103,29 +119,30 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm(
 // dx = rstd (t - mean(t) - xh mean(t xh)) [+ residual gradient], t = dy gamma, xh = (x - mean) rstd,
 // and the column sums of dy xh and dy over the block's rows, kept in registers from row to row.
 // Group k (of rows_per_group rows) has `splits` blocks; block j takes its rows j, j + splits, ...
-// (times the rows a block holds at once) and writes its sums to part[k][j][2][d].
+// (times the rows a block holds at once) and writes its sums to part[k][j][2][d]. A row's three
+// inputs are requested together and stay as read (16-bit rows in half the registers); xh and t are
+// formed twice, once for the sums and once for dx.
 template <typename T, int WPR, int P>
-__global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm_back(
+__global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,
     const void* __restrict__ gamma, eogp_dtype wt, const float* __restrict__ mean_in,
     const float* __restrict__ rstd_in, const uint8_t* __restrict__ mask, const T* res,
     int64_t ldres, int64_t rows_per_group, int64_t d, int splits, T* dx, int64_t lddx,
     float* __restrict__ part) {
-  constexpr int E = kPiece<T>;
-  constexpr int kWaves = WPR > 4 ? WPR : 4, kRows = kWaves / WPR;
+  constexpr int E = kPiece<T>, NT = norm_threads(WPR);
+  constexpr int kRows = NT / 64 / WPR;
+  extern __shared__ __align__(16) float weights[];     // gamma: round_up(d, E)
   __shared__ float slot[2][2][16];
   __shared__ float fold[WPR == 1 ? 3 * 64 * E : 1];
   const int wid = threadIdx.x >> 6;
   const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
-  float g[P][E], ag[P][E], ab[P][E];
+  float ag[P][E], ab[P][E];
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int64_t c = (int64_t)(p * 64 * WPR + t) * E + e;
-      g[p][e] = gamma && c < d ? load_any(gamma, wt, c) : 1.f;
-      ag[p][e] = ab[p][e] = 0.f;
-    }
+    for (int e = 0; e < E; ++e) ag[p][e] = ab[p][e] = 0.f;
+  stage_weights<NT>(weights, gamma, wt, d, 1.f);
+  __syncthreads();
   const float width = (float)d;
   const int64_t group = blockIdx.x / splits, split = blockIdx.x % splits;
   int turn = 0;
@@ -142,25 +159,35 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm_back(
       continue;
     }
     const float mean = mean_in[row], rstd = rstd_in[row];
-    float xv[P][E], gy[P][E];
+    AnyVec<T, E> xr[P], dr[P], rr[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      load_piece<T, E>(x + row * ldx, c, d, mean, xv[p]);
-      load_piece<T, E>(dy + row * lddy, c, d, 0.f, gy[p]);
+      xr[p] = fetch_piece<T, E>(x + row * ldx, c, d, (T)0.f);
+      dr[p] = fetch_piece<T, E>(dy + row * lddy, c, d, (T)0.f);   // (0 past the end: no sum sees x there)
+    }
+    if (res) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        rr[p] = fetch_piece<T, E>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d, (T)0.f);
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int p = 0; p < P; ++p)
+    for (int p = 0; p < P; ++p) {
+      const int c = (p * 64 * WPR + t) * E;
+      AnyVec<float, E> gp;
+      if (c < d) gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        xv[p][e] = (xv[p][e] - mean) * rstd;
-        ag[p][e] += gy[p][e] * xv[p][e];
-        ab[p][e] += gy[p][e];
-        gy[p][e] *= g[p][e];
-        s1 += gy[p][e];
-        s2 += gy[p][e] * xv[p][e];
+        const float xh = ((float)xr[p][e] - mean) * rstd, g = (float)dr[p][e];
+        ag[p][e] += g * xh;
+        ab[p][e] += g;
+        const float tv = c < d ? g * gp[e] : 0.f;
+        s1 += tv;
+        s2 += tv * xh;
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     s1 = wave_sum(s1);
     s2 = wave_sum(s2);
     if constexpr (WPR > 1) {
@@ -184,11 +211,18 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm_back(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      float r[E] = {};
-      if (res) load_piece<T, E>(res + row * ldres, c, d, 0.f, r);
+      if (c >= d) break;
+      const AnyVec<float, E> gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
+      AnyVec<T, E> xc = xr[p], dc = dr[p];
+      asm volatile("" : "+v"(xc), "+v"(dc));           // formed again, not kept from the sums' pass
+      float r[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) r[e] += rstd * (gy[p][e] - s1 - xv[p][e] * s2);
-      if (c < d) store_piece<T, E>(out, c, d, r);
+      for (int e = 0; e < E; ++e) {
+        const float xh = ((float)xc[e] - mean) * rstd;
+        r[e] = rstd * ((float)dc[e] * gp[e] - s1 - xh * s2) + (res ? (float)rr[p][e] : 0.f);
+      }
+      store_piece<T, E>(out, c, d, r);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   float* pg = part + (int64_t)blockIdx.x * 2 * d;
@@ -219,22 +253,36 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void k_layer_norm_back(
   }
 }
 
-// Column sums of the blocks' partial sums, in a fixed order: 16 columns x 16 slices per block.
-__global__ __launch_bounds__(256) void k_norm_fold(const float* __restrict__ part, int64_t groups, int splits,
-                                                   int64_t d, float* __restrict__ dgamma,
-                                                   float* __restrict__ dbeta) {
-  __shared__ float sum[16][17];
-  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
-  const int64_t col_blocks = (2 * d + 15) / 16;
+// Column sums of the blocks' partial sums, in a fixed order: 32 columns x SLICES slices of the blocks
+// per block, eight requests of a thread at a time.
+template <int SLICES>
+__global__ __launch_bounds__(32 * SLICES) void k_norm_fold(const float* __restrict__ part, int64_t groups, int splits,
+                                                           int64_t d, float* __restrict__ dgamma,
+                                                           float* __restrict__ dbeta) {
+  __shared__ float sum[SLICES][33];
+  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t col_blocks = (2 * d + 31) / 32;
   for (int64_t unit = blockIdx.x; unit < groups * col_blocks; unit += gridDim.x) {
-    const int64_t group = unit / col_blocks, c = unit % col_blocks * 16 + col;   // of the 2 d columns
+    const int64_t group = unit / col_blocks, c = unit % col_blocks * 32 + col;   // of the 2 d columns
+    const float* from = part + group * splits * 2 * d + c;
     float s = 0.f;
-    if (c < 2 * d)
-      for (int j = slice; j < splits; j += 16) s += part[(group * splits + j) * 2 * d + c];
+    if (c < 2 * d) {
+      for (int j = slice; j < splits; j += 8 * SLICES) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = j + k * SLICES;
+          v[k] = at < splits ? from[(int64_t)at * 2 * d] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[k];
+      }
+    }
     sum[slice][col] = s;
     __syncthreads();
     if (slice == 0 && c < 2 * d) {
-      for (int k = 1; k < 16; ++k) s += sum[k][col];
+#pragma unroll
+      for (int k = 1; k < SLICES; ++k) s += sum[k][col];
       float* out = c < d ? dgamma : dbeta;
       if (out) out[group * d + (c < d ? c : c - d)] = s;
     }
@@ -261,6 +309,10 @@ eogp_status with_shape(int64_t pieces, F&& f) {
 
 int rows_per_block(int64_t pieces) { return pieces <= 256 ? 4 : 1; }
 
+constexpr int kStaticLds = 48 << 10;         // dynamic LDS that needs no permission
+
+int64_t weight_bytes(int64_t d, eogp_dtype t) { return round_up(d, t == EOGP_F32 ? 4 : 8) * (int64_t)sizeof(float); }
+
 int64_t row_pieces(int64_t d, eogp_dtype t) { return ceil_div(d, t == EOGP_F32 ? 4 : 8); }
 
 }  // namespace
@@ -280,9 +332,14 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
       return with_shape<TI>(pieces, [&](auto wpr, auto p) {
         constexpr int W = decltype(wpr)::value;
         const int64_t blocks = std::min<int64_t>(ceil_div(n, rows_per_block(pieces)), W > 4 ? 512 : 2048);
-        hipLaunchKernelGGL((k_layer_norm<TI, TO, W, decltype(p)::value>), dim3((unsigned)blocks),
-                           dim3(W > 4 ? 64 * W : 256), 0, s, static_cast<const TI*>(x), ldx, gamma, beta,
-                           wt, eps, mask, n, d, static_cast<TO*>(y), ldy, ones, mean, rstd);
+        auto* kfn = k_layer_norm<TI, TO, W, decltype(p)::value>;
+        const int lds = 2 * (int)weight_bytes(d, xt);
+        if (lds > kStaticLds) {
+          const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);
+          if (st != EOGP_OK) return st;
+        }
+        hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(norm_threads(W)), lds, s, static_cast<const TI*>(x), ldx,
+                           gamma, beta, wt, eps, mask, n, d, static_cast<TO*>(y), ldy, ones, mean, rstd);
         EOGP_LAUNCH_CHECK("layer_norm");
         return EOGP_OK;
       });
@@ -318,20 +375,25 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
     using T = decltype(el);
     return with_shape<T>(pieces, [&](auto wpr, auto p) {
       constexpr int W = decltype(wpr)::value, P = decltype(p)::value;
-      hipLaunchKernelGGL((k_layer_norm_back<T, W, P>), dim3((unsigned)(groups * splits)),
-                         dim3(W > 4 ? 64 * W : 256), 0, s, static_cast<const T*>(dy), lddy,
-                         static_cast<const T*>(x), ldx, gamma, wt, mean, rstd, mask,
-                         static_cast<const T*>(res), ldres, rows, d, splits, static_cast<T*>(dx), lddx,
-                         part);
+      auto* kfn = k_layer_norm_back<T, W, P>;
+      const int lds = (int)weight_bytes(d, t);
+      if (lds > kStaticLds) {
+        const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);
+        if (st != EOGP_OK) return st;
+      }
+      hipLaunchKernelGGL(kfn, dim3((unsigned)(groups * splits)), dim3(norm_threads(W)), lds, s,
+                         static_cast<const T*>(dy), lddy, static_cast<const T*>(x), ldx, gamma, wt, mean, rstd, mask,
+                         static_cast<const T*>(res), ldres, rows, d, splits, static_cast<T*>(dx), lddx, part);
       EOGP_LAUNCH_CHECK("layer_norm_backward");
       return EOGP_OK;
     });
   });
   if (st != EOGP_OK) return st;
   if (!dgamma && !dbeta) return EOGP_OK;
-  const int64_t fold_blocks = std::min<int64_t>(groups * ceil_div(2 * d, 16), 1 << 20);
-  hipLaunchKernelGGL(k_norm_fold, dim3((unsigned)fold_blocks), dim3(256), 0, s, part, groups, splits, d, dgamma,
-                     dbeta);
+  const int64_t fold_blocks = std::min<int64_t>(groups * ceil_div(2 * d, 32), 1 << 20);
+  const bool many = splits > 64;
+  hipLaunchKernelGGL(many ? k_norm_fold<32> : k_norm_fold<8>, dim3((unsigned)fold_blocks), dim3(many ? 1024 : 256), 0,
+                     s, part, groups, splits, d, dgamma, dbeta);
   EOGP_LAUNCH_CHECK("layer_norm_backward (fold)");
   return EOGP_OK;
 }

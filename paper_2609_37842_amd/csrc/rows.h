@@ -20,6 +20,10 @@ template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);   // elements 
 template <typename T, int E>
 using AnyVec = T __attribute__((ext_vector_type(E), aligned(sizeof(T))));
 
+// E elements at a 16-byte boundary (LDS)
+template <typename T, int E>
+using AlignedVec = T __attribute__((ext_vector_type(E), aligned(16)));
+
 // Elements c .. c + E - 1 of a row of d as fp32; `pad` in the place of those past the end.
 template <typename T, int E>
 __device__ __forceinline__ void load_piece(const T* __restrict__ row, int64_t c, int64_t d, float pad,
@@ -32,6 +36,26 @@ __device__ __forceinline__ void load_piece(const T* __restrict__ row, int64_t c,
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = c + e < d ? (float)row[c + e] : pad;
   }
+}
+
+// The same elements as they are, and their fp32 values: loads of several pieces go out together when
+// their conversions come after all of them.
+template <typename T, int E>
+__device__ __forceinline__ AnyVec<T, E> fetch_piece(const T* __restrict__ row, int64_t c, int64_t d, T pad) {
+  AnyVec<T, E> x;
+  if (c + E <= d) {
+    x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = c + e < d ? row[c + e] : pad;
+  }
+  return x;
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void widen(const AnyVec<T, E>& x, float (&v)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = (float)x[e];
 }
 
 // The same elements rounded to T and stored; none past the end.
@@ -220,14 +244,7 @@ struct RegisterRow<T, NT, 0, G> {
   const T* row;
 
   static __device__ __forceinline__ AnyVec<T, E> fetch(const T* row, uint32_t c, uint32_t width) {
-    AnyVec<T, E> x;
-    if (c + E <= width) {
-      x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = c + e < width ? row[c + e] : (T)-INFINITY;
-    }
-    return x;
+    return fetch_piece<T, E>(row, c, width, (T)-INFINITY);
   }
 
   __device__ __forceinline__ void load(const T* r, uint32_t) { row = r; }

@@ -614,12 +614,31 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+# The stream and the addresses as plain integers: calls of a few microseconds (a decoding step's
+# norm, a short query) are as long as their marshalling, and a Stream object alone costs 2.8 us.
+_raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_handle(stream, device):
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_current_stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_current_stream(device.index)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def _rows_of(x, name):
     """(rows, width, row stride) of a [n, d] or [N, T, d] tensor whose rows have
     unit column stride and lie at one constant stride."""
     if x.dim() not in (2, 3):
         raise ValueError(f"{name} must be [n, d] or [N, T, d]")
     d = x.shape[-1]
+    if d > 0 and x.is_contiguous():
+        return x.numel() // d, d, d
     if x.dim() == 2:
         n, T = x.shape[0], 1
         ld = x.stride(0)
@@ -637,24 +656,22 @@ def _rows_of(x, name):
 
 
 def _model_dtype(x, name):
-    if x.dtype not in _DTYPE_CODE:
+    code = _DTYPE_CODE.get(x.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16")
-    return _DTYPE_CODE[x.dtype]
+    return code
 
 
 def _per_row(x, lead, dtype, name):
     """A contiguous tensor with one element per row, or None."""
-    if x is not None and (x.dtype != dtype or tuple(x.shape) != tuple(lead) or not x.is_contiguous()):
+    if x is not None and (x.dtype != dtype or x.shape != lead or not x.is_contiguous()):
         raise ValueError(f"{name} must be contiguous {str(dtype)[6:]} {list(lead)}")
-    return x
 
 
 def _weight(w, d, x, name):
-    if w is None:
-        return None
-    if tuple(w.shape) != (d,) or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32):
+    if w is not None and (w.dim() != 1 or w.shape[0] != d or not w.is_contiguous()
+                          or (w.dtype != x.dtype and w.dtype != torch.float32)):
         raise ValueError(f"{name} must be contiguous [{d}] of the rows' type or float32")
-    return w
 
 
 def _same_shape(x, like, name):
@@ -681,9 +698,9 @@ def eogp_embed_tokens(table, tokens, scale=1.0, token_mask=None, out=None, accum
     if tuple(out.shape) != (*lead, d) or out.dtype not in (table.dtype, torch.float32):
         raise ValueError("out must be [*tokens.shape, d] of the table's type or float32")
     n, _, ldo = _rows_of(out, "out")
-    _check(L.eogp_embed_tokens(_ptr(table), _model_dtype(table, "table"), ldt, V, d, _ptr(tokens),
-                               _ptr(token_mask), n, float(scale), 1 if accumulate else 0, _ptr(out),
-                               _DTYPE_CODE[out.dtype], ldo, _stream(stream)))
+    _check(L.eogp_embed_tokens(_at(table), _model_dtype(table, "table"), ldt, V, d, _at(tokens),
+                               _at(token_mask), n, float(scale), 1 if accumulate else 0, _at(out),
+                               _DTYPE_CODE[out.dtype], ldo, _stream_handle(stream, out.device)))
     return out
 
 
@@ -712,9 +729,10 @@ def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=Non
     if ws is None and need:
         ws = _empty((need,), torch.uint8, d_out.device, stream)
     ws, wsb = _workspace(need, d_out.device, ws)
-    _check(L.eogp_embed_backward(_ptr(d_out), _model_dtype(d_out, "d_out"), ldd, _ptr(tokens),
-                                 _ptr(token_mask), n, V, d, float(scale), 1 if accumulate else 0,
-                                 _ptr(dtable), ldt, _ptr(ws), wsb, _stream(stream)))
+    _check(L.eogp_embed_backward(_at(d_out), _model_dtype(d_out, "d_out"), ldd, _at(tokens),
+                                 _at(token_mask), n, V, d, float(scale), 1 if accumulate else 0,
+                                 _at(dtable), ldt, _at(ws), wsb,
+                                 _stream_handle(stream, dtable.device)))
     return dtable
 
 
@@ -745,10 +763,10 @@ def eogp_layer_norm(x, gamma=None, beta=None, eps=1e-5, token_mask=None, ones_co
     _per_row(mean, lead, torch.float32, "mean")
     _per_row(rstd, lead, torch.float32, "rstd")
     w = gamma if gamma is not None else beta
-    _check(L.eogp_layer_norm(_ptr(x), _model_dtype(x, "x"), ldx, _ptr(gamma), _ptr(beta),
-                             F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _ptr(token_mask), n,
-                             d, _ptr(out), _DTYPE_CODE[out.dtype], ldy, 1 if ones_column else 0,
-                             _ptr(mean), _ptr(rstd), _stream(stream)))
+    _check(L.eogp_layer_norm(_at(x), _model_dtype(x, "x"), ldx, _at(gamma), _at(beta),
+                             F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _at(token_mask), n,
+                             d, _at(out), _DTYPE_CODE[out.dtype], ldy, 1 if ones_column else 0,
+                             _at(mean), _at(rstd), _stream_handle(stream, x.device)))
     return out, mean, rstd
 
 
@@ -797,11 +815,11 @@ def eogp_layer_norm_backward(dy, x, gamma, mean, rstd, token_mask=None, residual
     if ws is None and need:
         ws = _empty((need,), torch.uint8, x.device, stream)
     ws, wsb = _workspace(need, x.device, ws)
-    _check(L.eogp_layer_norm_backward(_ptr(dy), lddy, _ptr(x), ldx, code, _ptr(gamma),
-                                      F32 if gamma is None else _DTYPE_CODE[gamma.dtype], _ptr(mean),
-                                      _ptr(rstd), _ptr(token_mask), _ptr(residual), ldr, groups, rows, d,
-                                      _ptr(dx), lddx, _ptr(dgamma), _ptr(dbeta), _ptr(ws), wsb,
-                                      _stream(stream)))
+    _check(L.eogp_layer_norm_backward(_at(dy), lddy, _at(x), ldx, code, _at(gamma),
+                                      F32 if gamma is None else _DTYPE_CODE[gamma.dtype], _at(mean),
+                                      _at(rstd), _at(token_mask), _at(residual), ldr, groups, rows, d,
+                                      _at(dx), lddx, _at(dgamma), _at(dbeta), _at(ws), wsb,
+                                      _stream_handle(stream, x.device)))
     return dx, dgamma, dbeta
 
 
@@ -827,9 +845,9 @@ def eogp_softmax_xent(logits, labels, token_mask=None, grad_scale=1.0, grad=True
             dlogits = _empty(tuple(logits.shape), logits.dtype, logits.device, stream)
         _same_shape(dlogits, logits, "dlogits")
         _, _, ldd = _rows_of(dlogits, "dlogits")
-    _check(L.eogp_softmax_xent(_ptr(logits), _model_dtype(logits, "logits"), ldl, _ptr(labels),
-                               _ptr(token_mask), n, V, float(grad_scale), _ptr(loss), _ptr(dlogits), ldd,
-                               _stream(stream)))
+    _check(L.eogp_softmax_xent(_at(logits), _model_dtype(logits, "logits"), ldl, _at(labels),
+                               _at(token_mask), n, V, float(grad_scale), _at(loss), _at(dlogits), ldd,
+                               _stream_handle(stream, logits.device)))
     return loss, dlogits
 
 
@@ -846,9 +864,9 @@ def eogp_sample_tokens(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.
     if out is None:
         out = _empty(lead, torch.int64, logits.device, stream)
     _per_row(out, lead, torch.int64, "out")
-    _check(L.eogp_sample_tokens(_ptr(logits), _model_dtype(logits, "logits"), ldl, n, V, _ptr(uniforms),
-                                _ptr(token_mask), float(temperature), int(top_k), float(top_p),
-                                float(min_p), _ptr(out), _stream(stream)))
+    _check(L.eogp_sample_tokens(_at(logits), _model_dtype(logits, "logits"), ldl, n, V, _at(uniforms),
+                                _at(token_mask), float(temperature), int(top_k), float(top_p),
+                                float(min_p), _at(out), _stream_handle(stream, logits.device)))
     return out
 
 
