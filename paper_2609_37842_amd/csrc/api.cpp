@@ -73,7 +73,7 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
 eogp_status embed_tokens(const void* table, eogp_dtype tt, int64_t ldt, int64_t V, int64_t d,
                          const int64_t* tokens, const uint8_t* mask, int64_t n, float scale, int accumulate,
                          void* out, eogp_dtype ot, int64_t ldo, hipStream_t s);
-size_t embed_back_ws(int64_t n, int64_t d);
+size_t embed_back_ws(int64_t n, int64_t V, int64_t d);
 eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_t* tokens, const uint8_t* mask,
                        int64_t n, int64_t V, int64_t d, float scale, int accumulate, float* dtable, int64_t ldt,
                        void* ws, hipStream_t s);
@@ -599,9 +599,9 @@ eogp_status eogp_embed_tokens(const void* table, eogp_dtype table_dtype, int64_t
                       out_dtype, ld_out, S(stream));
 }
 
-size_t eogp_embed_backward_workspace_size(int64_t n, int64_t d) {
-  if (n < 1 || n >= kMaxFlat || d < 1 || d >= kMaxFlat) return 0;
-  return embed_back_ws(n, d);
+size_t eogp_embed_backward_workspace_size(int64_t n, int64_t V, int64_t d) {
+  if (n < 1 || n >= kMaxFlat || V < 1 || V >= kMaxFlat || d < 1 || d >= kMaxFlat) return 0;
+  return embed_back_ws(n, V, d);
 }
 
 eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_d_out,
@@ -618,7 +618,7 @@ eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_
     return fail(EOGP_ERR_INVALID, "embed_backward: NULL pointer");
   if (n > 0) EOGP_CHECK(check_aligned(op, "d_out", d_out, dtype));
   EOGP_CHECK(check_aligned(op, "d_table", d_table, EOGP_F32));
-  if (n > 0 && (!ws || ws_bytes < embed_back_ws(n, d)))
+  if (n > 0 && (!ws || ws_bytes < embed_back_ws(n, V, d)))
     return fail(EOGP_ERR_WORKSPACE, "embed_backward: workspace too small");
   return embed_back(d_out, dtype, ld_d_out, tokens, token_mask, n, V, d, scale, accumulate, d_table,
                     ld_d_table, ws, S(stream));

@@ -63,12 +63,30 @@ __device__ __forceinline__ uint32_t token_key(const int64_t* tokens, const uint8
   return t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;
 }
 
-// Digit counts of each tile: hist[digit][tile].
+// Zeros `words` words of flags and one counter.
+__global__ __launch_bounds__(256) void k_clear(uint32_t* __restrict__ flags, int64_t words, uint32_t* __restrict__ counter) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) flags[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0;
+}
+
+// Zeros rows row0 .. row1 - 1 of the table but for flagged ones (their sums are written later).
+__device__ void fill_zero(float* __restrict__ dtable, int64_t ldt, int64_t d, const uint8_t* __restrict__ flags,
+                          int64_t block, int64_t blocks, int64_t row0, int64_t row1) {
+  const int lane = threadIdx.x & 63;
+  const float z[4] = {};
+  for (int64_t r = row0 + block * 4 + (threadIdx.x >> 6); r < row1; r += blocks * 4) {
+    if (flags && flags[r]) continue;
+    for (int64_t c = 4 * lane; c < d; c += 256) store_piece<float, 4>(dtable + r * ldt, c, d, z);
+  }
+}
+
+// Digit counts of each tile: hist[digit][tile]. The first pass flags the tokens that have rows.
 template <bool FIRST>
 __global__ __launch_bounds__(256) void k_sort_count(const int64_t* __restrict__ tokens,
                                                     const uint8_t* __restrict__ mask, int64_t V,
                                                     const uint32_t* __restrict__ keys, int64_t n, int shift,
-                                                    int bits, uint32_t* __restrict__ hist, int64_t tiles) {
+                                                    int bits, uint32_t* __restrict__ hist, int64_t tiles,
+                                                    uint8_t* __restrict__ flags) {
   __shared__ uint32_t count[1 << kMaxDigit];
   const uint32_t dmask = (1u << bits) - 1;
   for (int b = threadIdx.x; b <= (int)dmask; b += 256) count[b] = 0;
@@ -76,6 +94,7 @@ __global__ __launch_bounds__(256) void k_sort_count(const int64_t* __restrict__ 
   const int64_t base = (int64_t)blockIdx.x * kTile;
   for (int64_t i = base + threadIdx.x; i < std::min<int64_t>(base + kTile, n); i += 256) {
     const uint32_t k = FIRST ? token_key(tokens, mask, i, V) : keys[i];
+    if (FIRST && flags && k < V) flags[k] = 1;         // (whoever writes it, it is 1)
     atomicAdd(&count[(k >> shift) & dmask], 1u);
   }
   __syncthreads();
@@ -109,7 +128,13 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
                                                       int bits, const uint32_t* __restrict__ hist, int64_t tiles,
                                                       const uint32_t* __restrict__ totals,
                                                       uint32_t* __restrict__ keys_out,
-                                                      uint32_t* __restrict__ rows_out) {
+                                                      uint32_t* __restrict__ rows_out, float* __restrict__ dtable,
+                                                      int64_t ldt, int64_t d, const uint8_t* __restrict__ flags,
+                                                      int64_t row0, int64_t row1) {
+  if (blockIdx.x >= tiles) {                            // blocks beside the sort's: its latency hides the zeros
+    fill_zero(dtable, ldt, d, flags, blockIdx.x - tiles, gridDim.x - tiles, row0, row1);
+    return;
+  }
   __shared__ uint32_t at[kSortWaves][1 << kMaxDigit];   // next place of a digit for a wave
   __shared__ uint32_t wave_total[kSortWaves];
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -180,34 +205,59 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
     }
 }
 
-// ---- sums over the sorted rows -----------------------------------------------------
-__global__ __launch_bounds__(256) void k_zero(float* __restrict__ p, int64_t ld, int64_t rows, int64_t d) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
-    float z[4] = {};
-    for (int64_t c = 4 * lane; c < d; c += 256) store_piece<float, 4>(p + r * ld, c, d, z);
+// Few rows: each one's place is the number of rows before it, found by comparing it with all of them
+// (a quarter of them per thread); one launch instead of the radix sort's six. Blocks beside them write
+// the table's zeros.
+constexpr int kFew = 8192;
+
+__global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens, const uint8_t* __restrict__ mask,
+                                              int64_t V, int n, uint32_t* __restrict__ keys_out,
+                                              uint32_t* __restrict__ rows_out, uint32_t* __restrict__ counter,
+                                              int rank_blocks, float* __restrict__ dtable, int64_t ldt, int64_t d) {
+  __shared__ __align__(16) uint32_t key[kFew];
+  if ((int)blockIdx.x >= rank_blocks) {
+    fill_zero(dtable, ldt, d, nullptr, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, 0, V);
+    return;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0;
+  for (int i = threadIdx.x; i < (n + 15) / 16 * 16; i += 256) key[i] = i < n ? token_key(tokens, mask, i, V) : 0xFFFFFFFFu;
+  __syncthreads();
+  const int i = blockIdx.x * 64 + (threadIdx.x >> 2), part = threadIdx.x & 3;
+  const uint32_t mine = i < n ? key[i] : 0;
+  uint32_t before = 0;
+  for (int j = 4 * part; j < n; j += 16) {
+    const uint4 k = *reinterpret_cast<const uint4*>(key + j);
+    before += (k.x < mine || (k.x == mine && j < i)) + (k.y < mine || (k.y == mine && j + 1 < i)) +
+              (k.z < mine || (k.z == mine && j + 2 < i)) + (k.w < mine || (k.w == mine && j + 3 < i));
+  }
+  before += __shfl_xor(before, 1);
+  before += __shfl_xor(before, 2);
+  if (i < n && part == 0) {
+    keys_out[before] = mine;
+    rows_out[before] = (uint32_t)i;
   }
 }
 
-// A wave sums the rows of a chunk of sorted places, for 64 pieces of their columns, eight rows in
+// ---- sums over the sorted rows -----------------------------------------------------
+// A wave sums the rows of a chunk of CHUNK sorted places, for 64 pieces of their columns, eight rows in
 // flight, token by token. A token whose rows all lie in the chunk is finished here; the sum of one
 // that goes on beyond an end of the chunk is written to part[chunk][0] (it began in an earlier
-// chunk) or part[chunk][1] (it begins here and goes on), and k_embed_join adds those in order.
-constexpr int kChunk = 64;
-
-template <typename T>
+// chunk) or part[chunk][1] (it begins here and goes on), and k_embed_join adds those in order: the
+// chunks where such tokens begin are listed for it.
+template <typename T, int CHUNK>
 __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, int64_t ldd, int64_t d,
                                                    const uint32_t* __restrict__ keys,
                                                    const uint32_t* __restrict__ rows, int64_t n, uint32_t V,
                                                    float scale, int accumulate, float* __restrict__ dtable,
-                                                   int64_t ldt, float* __restrict__ part, int64_t col_units) {
+                                                   int64_t ldt, float* __restrict__ part, int64_t col_units,
+                                                   uint32_t* __restrict__ listed, uint32_t* __restrict__ list) {
   constexpr int E = kPiece<T>, U = 8;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t chunk = unit / col_units, p0 = chunk * kChunk;
+  const int64_t chunk = unit / col_units, p0 = chunk * CHUNK;
   if (p0 >= n) return;
   const int64_t c = (unit % col_units * 64 + lane) * E;
-  const int count = (int)std::min<int64_t>(kChunk, n - p0);
+  const int count = (int)std::min<int64_t>(CHUNK, n - p0);
   // lane l holds place p0 + l
   const uint32_t mykey = lane < count ? keys[p0 + lane] : V;
   const uint32_t myrow = lane < count ? rows[p0 + lane] : 0;
@@ -216,6 +266,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
   uint32_t cur = __builtin_amdgcn_readlane(mykey, 0);
   bool from_before = cur == before;
   auto flush = [&](bool goes_on) {
+    if (goes_on && !from_before && unit % col_units == 0 && lane == 0) list[atomicAdd(listed, 1u)] = (uint32_t)chunk;
     if (c >= d) return;
     if (from_before || goes_on) {
       store_piece<float, E>(part + (chunk * 2 + (from_before ? 0 : 1)) * d, c, d, acc);
@@ -229,12 +280,12 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
     }
   };
   for (int i = 0; i < count; i += U) {
-    float v[U][E];
+    AnyVec<T, E> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = std::min(i + u, count - 1);
       const uint32_t k = __builtin_amdgcn_readlane(mykey, j), r = __builtin_amdgcn_readlane(myrow, j);
-      if (k < V) load_piece<T, E>(dout + (int64_t)r * ldd, c, d, 0.f, v[u]);
+      if (k < V) v[u] = fetch_piece<T, E, true>(dout + (int64_t)r * ldd, c, d, (T)0.f);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -249,41 +300,63 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
       }
       if (k >= V) return;                      // the rows that count for no token are last
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += v[u][e];
+      for (int e = 0; e < E; ++e) acc[e] += (float)v[u][e];
     }
   }
   flush(cur == after);
 }
 
-// One block per chunk and 256 columns: if a token's rows begin in the chunk and go on beyond it, the
-// sums of its chunks are added (its four waves take every fourth following chunk) and the row is
-// finished.
-__global__ __launch_bounds__(256) void k_embed_join(const uint32_t* __restrict__ keys, int64_t n, uint32_t V,
-                                                    const float* __restrict__ part, int64_t d, float scale,
-                                                    int accumulate, float* __restrict__ dtable, int64_t ldt,
-                                                    int64_t col_blocks) {
+// One block per listed chunk and 256 columns: the sums of the chunks of the token that begins there and
+// goes on are added, a quarter of them per wave, and its row is finished. (Small blocks: most such tokens
+// span two or three chunks, so a unit is a chain of waits; of 196,000 rows of 2048 with
+// Zipf-distributed tokens 16 waves per block took 105 us where 4 take 36.)
+template <int CHUNK>
+__global__ __launch_bounds__(256) void k_embed_join(const uint32_t* __restrict__ keys, int64_t n,
+                                                     const float* __restrict__ part, int64_t d, float scale,
+                                                     int accumulate, float* __restrict__ dtable, int64_t ldt,
+                                                     int64_t col_blocks, const uint32_t* __restrict__ listed,
+                                                     const uint32_t* __restrict__ list) {
   __shared__ float fold[4][256];
-  const int64_t chunk = blockIdx.x / col_blocks, p1 = (chunk + 1) * kChunk;
-  if (p1 >= n) return;
-  const uint32_t k = keys[p1 - 1];
-  if (k >= V || keys[p1] != k || (chunk > 0 && keys[chunk * kChunk] == k && keys[chunk * kChunk - 1] == k)) return;
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t c = (blockIdx.x % col_blocks) * 256 + lane * 4;
-  float acc[4] = {};
-  if (wid == 0 && c < d) load_piece<float, 4>(part + (chunk * 2 + 1) * d, c, d, 0.f, acc);
-  for (int64_t j = chunk + 1 + wid; j * kChunk < n && keys[j * kChunk] == k; j += 4) {
-    float v[4];
-    load_piece<float, 4>(part + j * 2 * d, c, d, 0.f, v);
-    for (int e = 0; e < 4; ++e) acc[e] += v[e];
+  const int64_t units = (int64_t)*listed * col_blocks;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t first = list[unit / col_blocks];
+    const uint32_t k = keys[(first + 1) * CHUNK - 1];
+    int64_t more = 0;                                  // chunks after the first that begin with its rows
+    for (;;) {
+      const int64_t at = (first + 1 + more + lane) * CHUNK;
+      const uint64_t same = __ballot(at < n && keys[at < n ? at : 0] == k);
+      const int run = ~same ? __builtin_ctzll(~same) : 64;
+      more += run;
+      if (run < 64) break;
+    }
+    const int64_t c = unit % col_blocks * 256 + lane * 4;
+    float acc[4] = {};
+    for (int64_t j = wid; j <= more; j += 4 * 8) {    // chunk first + j: its own part 1, the others' part 0
+      AnyVec<float, 4> v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t q = j + u * 4;
+        v[u] = fetch_piece<float, 4>(part + ((first + q) * 2 + (q == 0)) * d, c, q <= more ? d : 0, 0.f);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += v[u][e];
+    }
+    __syncthreads();                                   // the unit before has been read
+#pragma unroll
+    for (int e = 0; e < 4; ++e) fold[wid][lane * 4 + e] = acc[e];
+    __syncthreads();
+    const int64_t col = unit % col_blocks * 256 + threadIdx.x;
+    if (col < d) {
+      float s = fold[0][threadIdx.x];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) s += fold[w][threadIdx.x];
+      float* t = dtable + (int64_t)k * ldt + col;
+      *t = (accumulate ? *t : 0.f) + s * scale;
+    }
   }
-  for (int e = 0; e < 4; ++e) fold[wid][lane * 4 + e] = acc[e];
-  __syncthreads();
-  const int64_t col = (blockIdx.x % col_blocks) * 256 + threadIdx.x;
-  if (col >= d) return;
-  float s = fold[0][threadIdx.x];
-  for (int w = 1; w < 4; ++w) s += fold[w][threadIdx.x];
-  float* t = dtable + (int64_t)k * ldt + col;
-  *t = (accumulate ? *t : 0.f) + s * scale;
 }
 
 struct SortShape {
@@ -297,24 +370,56 @@ SortShape sort_shape(int64_t V) {
   return {passes, (b + passes - 1) / passes};
 }
 
+constexpr int kChunk = 64, kFewChunk = 8;    // sorted places per wave; few rows: one load's latency each
+
 struct BackWs {
-  uint32_t *keys[2], *rows[2], *hist, *totals;
+  uint32_t *keys[2], *rows[2], *hist, *totals, *listed, *list;
+  uint8_t* flags;
   float* part;
   size_t bytes;
 };
 
-BackWs carve_back(void* ws, int64_t n, int64_t d) {
+BackWs carve_back(void* ws, int64_t n, int64_t V, int64_t d) {
   Carve cv(ws, ~(size_t)0);
+  const bool few = n <= kFew;
+  const int64_t chunks = ceil_div(n, few ? kFewChunk : kChunk);
   BackWs w;
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < (few ? 1 : 2); ++k) {
     w.keys[k] = cv.take<uint32_t>(n);
     w.rows[k] = cv.take<uint32_t>(n);
   }
-  w.hist = cv.take<uint32_t>((size_t)ceil_div(n, kTile) << kMaxDigit);
-  w.totals = cv.take<uint32_t>(1 << kMaxDigit);
-  w.part = cv.take<float>((size_t)ceil_div(n, kChunk) * 2 * d);
+  w.hist = cv.take<uint32_t>(few ? 0 : (size_t)ceil_div(n, kTile) << kMaxDigit);
+  w.totals = cv.take<uint32_t>(few ? 0 : 1 << kMaxDigit);
+  w.flags = cv.take<uint8_t>(few ? 0 : round_up(V, 4));
+  w.listed = cv.take<uint32_t>(1);
+  w.list = cv.take<uint32_t>(chunks);
+  w.part = cv.take<float>((size_t)chunks * 2 * d);
   w.bytes = cv.used;
   return w;
+}
+
+// Sums of the sorted rows, then of the tokens that several chunks hold.
+template <int CHUNK>
+eogp_status sum_sorted(const BackWs& w, const uint32_t* keys, const uint32_t* rows, const void* dout, eogp_dtype t,
+                       int64_t ldd, int64_t n, int64_t V, int64_t d, float scale, int accumulate, float* dtable,
+                       int64_t ldt, hipStream_t s) {
+  const int64_t chunks = ceil_div(n, CHUNK);
+  const eogp_status st = with_type(t, [&](auto el) {
+    using T = decltype(el);
+    const int64_t col_units = ceil_div(d, 64 * kPiece<T>);
+    hipLaunchKernelGGL((k_embed_sum<T, CHUNK>), dim3((unsigned)ceil_div(chunks * col_units, 4)), dim3(256), 0, s,
+                       static_cast<const T*>(dout), ldd, d, keys, rows, n, (uint32_t)V, scale, accumulate, dtable,
+                       ldt, w.part, col_units, w.listed, w.list);
+    EOGP_LAUNCH_CHECK("embed_backward (sums)");
+    return EOGP_OK;
+  });
+  if (st != EOGP_OK || chunks == 1) return st;
+  const int64_t col_blocks = ceil_div(d, 256);
+  hipLaunchKernelGGL(k_embed_join<CHUNK>, dim3((unsigned)std::min<int64_t>((chunks - 1) * col_blocks, 8 * kCus)),
+                     dim3(256), 0, s, keys, n, w.part, d, scale, accumulate, dtable, ldt, col_blocks, w.listed,
+                     w.list);
+  EOGP_LAUNCH_CHECK("embed_backward (join)");
+  return EOGP_OK;
 }
 
 }  // namespace
@@ -348,50 +453,44 @@ eogp_status embed_tokens(const void* table, eogp_dtype tt, int64_t ldt, int64_t 
   });
 }
 
-size_t embed_back_ws(int64_t n, int64_t d) { return carve_back(nullptr, n, d).bytes; }
+size_t embed_back_ws(int64_t n, int64_t V, int64_t d) { return carve_back(nullptr, n, V, d).bytes; }
 
 eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_t* tokens, const uint8_t* mask,
                        int64_t n, int64_t V, int64_t d, float scale, int accumulate, float* dtable, int64_t ldt,
                        void* ws, hipStream_t s) {
   timing::Scope ts(EOGP_KT_EMBED, s);
-  if (!accumulate) {
-    hipLaunchKernelGGL(k_zero, dim3((unsigned)std::min<int64_t>(ceil_div(V, 4), 8 * kCus)), dim3(256), 0, s, dtable,
-                       ldt, V, d);
-    EOGP_LAUNCH_CHECK("embed_backward (zeros)");
+  const unsigned fill_blocks = accumulate ? 0 : (unsigned)std::min<int64_t>(ceil_div(V, 4), 4 * kCus);
+  const BackWs w = n > 0 ? carve_back(ws, n, V, d) : BackWs{};
+  if (n <= kFew) {
+    const int rank_blocks = (int)ceil_div(n, 64);
+    if (rank_blocks + fill_blocks == 0) return EOGP_OK;
+    hipLaunchKernelGGL(k_rank, dim3(rank_blocks + fill_blocks), dim3(256), 0, s, tokens, mask, V, (int)n, w.keys[0],
+                       w.rows[0], w.listed, rank_blocks, dtable, ldt, d);
+    EOGP_LAUNCH_CHECK("embed_backward (ranks)");
+    if (n == 0) return EOGP_OK;
+    return sum_sorted<kFewChunk>(w, w.keys[0], w.rows[0], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
   }
-  if (n == 0) return EOGP_OK;
-  const BackWs w = carve_back(ws, n, d);
-  const int64_t tiles = ceil_div(n, kTile);
+  const int64_t tiles = ceil_div(n, kTile), words = accumulate ? 0 : round_up(V, 4) / 4;
   const SortShape sh = sort_shape(V);
+  hipLaunchKernelGGL(k_clear, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(words, 256), kCus))),
+                     dim3(256), 0, s, reinterpret_cast<uint32_t*>(w.flags), words, w.listed);
+  EOGP_LAUNCH_CHECK("embed_backward (flags)");
   for (int p = 0; p < sh.passes; ++p) {
     const int shift = p * sh.bits;
     const uint32_t *ki = w.keys[(p + 1) & 1], *ri = w.rows[(p + 1) & 1];
     auto* count = p == 0 ? k_sort_count<true> : k_sort_count<false>;
     auto* scatter = p == 0 ? k_sort_scatter<true> : k_sort_scatter<false>;
     hipLaunchKernelGGL(count, dim3((unsigned)tiles), dim3(256), 0, s, tokens, mask, V, ki, n, shift, sh.bits, w.hist,
-                       tiles);
+                       tiles, accumulate ? nullptr : w.flags);
     hipLaunchKernelGGL(k_sort_scan, dim3(1u << sh.bits), dim3(64), 0, s, w.hist, tiles, w.totals);
-    hipLaunchKernelGGL(scatter, dim3((unsigned)tiles), dim3(256), 0, s, tokens, mask, V, ki, ri, n, shift, sh.bits,
-                       w.hist, tiles, w.totals, w.keys[p & 1], w.rows[p & 1]);
+    // an equal share of the table's zeros beside each pass
+    hipLaunchKernelGGL(scatter, dim3((unsigned)tiles + fill_blocks), dim3(256), 0, s, tokens, mask, V, ki, ri, n,
+                       shift, sh.bits, w.hist, tiles, w.totals, w.keys[p & 1], w.rows[p & 1], dtable, ldt, d, w.flags,
+                       V * p / sh.passes, V * (p + 1) / sh.passes);
     EOGP_LAUNCH_CHECK("embed_backward (sort)");
   }
-  const uint32_t *keys = w.keys[(sh.passes - 1) & 1], *rows = w.rows[(sh.passes - 1) & 1];
-  const int64_t chunks = ceil_div(n, kChunk);
-  const eogp_status st = with_type(t, [&](auto el) {
-    using T = decltype(el);
-    const int64_t col_units = ceil_div(d, 64 * kPiece<T>);
-    hipLaunchKernelGGL(k_embed_sum<T>, dim3((unsigned)ceil_div(chunks * col_units, 4)), dim3(256), 0, s,
-                       static_cast<const T*>(dout), ldd, d, keys, rows, n, (uint32_t)V, scale, accumulate, dtable,
-                       ldt, w.part, col_units);
-    EOGP_LAUNCH_CHECK("embed_backward (sums)");
-    return EOGP_OK;
-  });
-  if (st != EOGP_OK || chunks == 1) return st;
-  const int64_t col_blocks = ceil_div(d, 256);
-  hipLaunchKernelGGL(k_embed_join, dim3((unsigned)(chunks * col_blocks)), dim3(256), 0, s, keys, n, (uint32_t)V,
-                     w.part, d, scale, accumulate, dtable, ldt, col_blocks);
-  EOGP_LAUNCH_CHECK("embed_backward (join)");
-  return EOGP_OK;
+  const int last = (sh.passes - 1) & 1;
+  return sum_sorted<kChunk>(w, w.keys[last], w.rows[last], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
 }
 
 }  // namespace eogp

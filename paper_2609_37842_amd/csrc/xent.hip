@@ -86,7 +86,7 @@ __global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_xen
           g[e] = (T)((c + e == label ? p - 1.f : p) * gscale);
         }
         if (P > 0 ? c == first : c + E <= V) {
-          *reinterpret_cast<AnyVec<T, E>*>(dl + c) = g;
+          __builtin_nontemporal_store(g, reinterpret_cast<AnyVec<T, E>*>(dl + c));
         } else {                                       // other pieces hold what lies before `first`
 #pragma unroll
           for (int e = 0; e < E; ++e)

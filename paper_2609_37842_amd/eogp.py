@@ -115,7 +115,7 @@ def load(path: str | None = None):
                                             c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp]),
         "eogp_embed_tokens": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, c_vp, c_vp, c_i64,
                                       ctypes.c_float, c_i32, c_vp, c_i32, c_i64, c_vp]),
-        "eogp_embed_backward_workspace_size": (c_sz, [c_i64, c_i64]),
+        "eogp_embed_backward_workspace_size": (c_sz, [c_i64, c_i64, c_i64]),
         "eogp_embed_backward": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_vp, c_i64, c_i64, c_i64,
                                         ctypes.c_float, c_i32, c_vp, c_i64, c_vp, c_sz, c_vp]),
         "eogp_layer_norm": (c_i32, [c_vp, c_i32, c_i64, c_vp, c_vp, c_i32, ctypes.c_float, c_vp,
@@ -704,8 +704,8 @@ def eogp_embed_tokens(table, tokens, scale=1.0, token_mask=None, out=None, accum
     return out
 
 
-def eogp_embed_backward_workspace_size(n: int, d: int) -> int:
-    return int(load().eogp_embed_backward_workspace_size(n, d))
+def eogp_embed_backward_workspace_size(n: int, V: int, d: int) -> int:
+    return int(load().eogp_embed_backward_workspace_size(n, V, d))
 
 
 def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=None, accumulate=False,
@@ -725,7 +725,7 @@ def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=Non
     if dtable.dtype != torch.float32 or tuple(dtable.shape) != (V, d):
         raise ValueError("dtable must be float32 [V, d]")
     _, _, ldt = _rows_of(dtable, "dtable")
-    need = eogp_embed_backward_workspace_size(n, d)
+    need = eogp_embed_backward_workspace_size(n, V, d)
     if ws is None and need:
         ws = _empty((need,), torch.uint8, d_out.device, stream)
     ws, wsb = _workspace(need, d_out.device, ws)

@@ -94,8 +94,9 @@ def test_abi_refusals_without_device():
     back = lambda **k: L.eogp_embed_backward(*(k.get(a, b) for a, b in dict(   # noqa: E731
         dout=FAKE, t=0, ldd=8, tok=FAKE, mask=None, n=3, V=4, d=8, scale=1.0, acc=0, dt=FAKE, ldt=8, ws=FAKE,
         wsb=1 << 30, s=None).items()))
-    need = L.eogp_embed_backward_workspace_size(3, 8)
-    assert need > 0 and L.eogp_embed_backward_workspace_size(0, 8) == 0
+    need = L.eogp_embed_backward_workspace_size(3, 4, 8)
+    assert need > 0 and L.eogp_embed_backward_workspace_size(0, 4, 8) == 0
+    assert L.eogp_embed_backward_workspace_size(3, 0, 8) == 0
     assert back(n=-1) == -1 and back(V=0) == -1 and back(ldd=7) == -1 and back(ldt=7) == -1 and back(t=3) == -1
     assert back(dout=None) == -1 and back(dt=None) == -1
     assert back(wsb=need - 1) == -4 and back(ws=None) == -4
