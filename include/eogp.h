@@ -495,7 +495,8 @@ eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, con
  *   mean, rstd            [groups * rows] fp32 of the forward pass.
  *   d_gamma, d_beta       [groups, d] fp32, or NULL.
  *   ws                    eogp_layer_norm_backward_workspace_size bytes.
- * Errors as for eogp_layer_norm; EOGP_ERR_WORKSPACE if ws is too small. */
+ * Errors as for eogp_layer_norm, and EOGP_ERR_INVALID for more than 2^21 groups;
+ * EOGP_ERR_WORKSPACE if ws is too small. */
 size_t eogp_layer_norm_backward_workspace_size(int64_t groups, int64_t rows, int64_t d,
                                                eogp_dtype dtype);
 eogp_status eogp_layer_norm_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,

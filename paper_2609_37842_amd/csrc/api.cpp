@@ -123,6 +123,7 @@ using namespace eogp;
 namespace {
 inline hipStream_t S(void* s) { return static_cast<hipStream_t>(s); }
 constexpr int64_t kMaxFlat = (int64_t)1 << 31;
+constexpr int64_t kMaxGroups = (int64_t)1 << 21;   // a block each, of up to 1,024 threads
 
 eogp_status check_plan_args(const float* eigvals, int64_t d_out, int64_t d_in, double damping,
                             int64_t m, const float* Q_A, const float* Q_S) {
@@ -662,7 +663,7 @@ eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, con
 size_t eogp_layer_norm_backward_workspace_size(int64_t groups, int64_t rows, int64_t d,
                                                eogp_dtype dtype) {
   if (groups < 1 || rows < 0 || d < 1 || d > norm_max_width() || !model_type(dtype)) return 0;
-  if (groups >= kMaxFlat || rows >= kMaxFlat || groups * rows >= kMaxFlat) return 0;
+  if (groups > kMaxGroups || rows >= kMaxFlat || groups * rows >= kMaxFlat) return 0;
   return layer_norm_back_ws(groups, rows, d, dtype);
 }
 
@@ -673,8 +674,8 @@ eogp_status eogp_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
                                      int64_t rows, int64_t d, void* dx, int64_t ld_dx, float* d_gamma,
                                      float* d_beta, void* ws, size_t ws_bytes, void* stream) {
   const char* op = "layer_norm_backward";
-  if (groups < 0 || rows < 0 || groups >= kMaxFlat || rows >= kMaxFlat)
-    return fail(EOGP_ERR_INVALID, "layer_norm_backward: bad sizes");
+  if (groups < 0 || rows < 0 || groups > kMaxGroups || rows >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, "layer_norm_backward: bad sizes (at most 2^21 groups)");
   const int64_t n = groups * rows;
   EOGP_CHECK(check_norm(op, n, d, dtype, w_dtype));
   EOGP_CHECK(check_ld(op, "dy", ld_dy, d));

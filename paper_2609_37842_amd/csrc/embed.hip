@@ -69,14 +69,17 @@ __global__ __launch_bounds__(256) void k_clear(uint32_t* __restrict__ flags, int
   if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0;
 }
 
-// Zeros rows row0 .. row1 - 1 of the table but for flagged ones (their sums are written later).
+// Zeros rows row0 .. row1 - 1 of the table but for flagged ones (their sums are written later). Plain
+// stores: nothing else is in the L2s' way (154 MB: 25 us, 29 with streaming stores).
 __device__ void fill_zero(float* __restrict__ dtable, int64_t ldt, int64_t d, const uint8_t* __restrict__ flags,
                           int64_t block, int64_t blocks, int64_t row0, int64_t row1) {
   const int lane = threadIdx.x & 63;
-  const float z[4] = {};
+  const AnyVec<float, 4> z = {};
   for (int64_t r = row0 + block * 4 + (threadIdx.x >> 6); r < row1; r += blocks * 4) {
     if (flags && flags[r]) continue;
-    for (int64_t c = 4 * lane; c < d; c += 256) store_piece<float, 4>(dtable + r * ldt, c, d, z);
+    float* row = dtable + r * ldt;
+    for (int64_t c = 4 * lane; c + 4 <= d; c += 256) *reinterpret_cast<AnyVec<float, 4>*>(row + c) = z;
+    if (lane < (d & 3)) row[(d & ~(int64_t)3) + lane] = 0.f;
   }
 }
 
@@ -307,9 +310,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
 }
 
 // One block per listed chunk and 256 columns: the sums of the chunks of the token that begins there and
-// goes on are added, a quarter of them per wave, and its row is finished. (Small blocks: most such tokens
-// span two or three chunks, so a unit is a chain of waits; of 196,000 rows of 2048 with
-// Zipf-distributed tokens 16 waves per block took 105 us where 4 take 36.)
+// goes on are added, a quarter of them per wave, and its row is finished. Most such tokens span two or
+// three chunks, so a unit is a chain of waits and as many units as fit are wanted: for 196,000 rows of
+// 2048 with Zipf-distributed tokens 16 waves per block take 105 us, 4 waves with eight requests each
+// 36, with four (fewer registers) 25.
 template <int CHUNK>
 __global__ __launch_bounds__(256) void k_embed_join(const uint32_t* __restrict__ keys, int64_t n,
                                                      const float* __restrict__ part, int64_t d, float scale,
@@ -332,15 +336,15 @@ __global__ __launch_bounds__(256) void k_embed_join(const uint32_t* __restrict__
     }
     const int64_t c = unit % col_blocks * 256 + lane * 4;
     float acc[4] = {};
-    for (int64_t j = wid; j <= more; j += 4 * 8) {    // chunk first + j: its own part 1, the others' part 0
-      AnyVec<float, 4> v[8];
+    for (int64_t j = wid; j <= more; j += 4 * 4) {    // chunk first + j: its own part 1, the others' part 0
+      AnyVec<float, 4> v[4];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < 4; ++u) {
         const int64_t q = j + u * 4;
         v[u] = fetch_piece<float, 4>(part + ((first + q) * 2 + (q == 0)) * d, c, q <= more ? d : 0, 0.f);
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += v[u][e];
     }

@@ -2,6 +2,7 @@
 // pass over rows once: embedding, layer norm, cross-entropy, sampling. Rows may start at any
 // element; a row's last piece may be short.
 #pragma once
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -279,23 +280,30 @@ struct RegisterRow<T, NT, 0, G> {
 
 // The rows of a block that stays for many: round i takes row i * blocks + (block + 97 i) mod blocks,
 // so that rows that cost nothing (masked ends of examples of a power of two tokens) do not all fall to
-// the same blocks. f(row): whether the row has work; rows without are passed over. -1 at the end.
+// the same blocks. (Numbering the valid rows by a scan over the mask and dealing those out evenly took
+// 4096 rows of 100,352 bf16 from 323 to 315 us and 24 rows of 50,257 fp32 from 11.8 to 14.8.)
 struct RowWalk {
   uint32_t round = 0;
-  template <typename F>
-  __device__ __forceinline__ int64_t next(int64_t n, F&& f) {
+  // The next row for which work(row) holds, -1 at the end.
+  template <typename Work>
+  __device__ __forceinline__ int64_t next(int64_t n, Work&& work) {
     while ((int64_t)round * gridDim.x < n) {
       const int64_t row = (int64_t)round * gridDim.x + (blockIdx.x + 97u * round) % gridDim.x;
       ++round;
-      if (row < n && f(row)) return row;
+      if (row < n && work(row)) return row;
     }
     return -1;
   }
 };
 
-// Blocks per CU by their registers (threads, pieces per thread); a kernel that holds its row so
-// asks for as many waves per SIMD (NT / 256 of a block).
-constexpr int row_blocks_per_cu(int nt, int p) { return nt == 256 ? 6 : p >= 1 && p <= 4 ? 2 : 1; }
+// Blocks of a launch that has one per row (a launch holds fewer than 2^32 threads).
+constexpr int64_t kMostBlocks = 1 << 21;
+
+// Blocks for n rows: those of 256 threads have one row each, the others stay, `per_cu` of them to a CU
+// by their registers.
+inline int64_t row_blocks(int64_t n, int nt, int per_cu) {
+  return std::min<int64_t>(n, nt == 256 ? kMostBlocks : kCus * per_cu);
+}
 
 // Threads of the block that holds a row of `pieces` 16-byte pieces in registers, and pieces per
 // thread; none (0) for rows longer than 1,024 threads x 16 pieces, which are read again instead, and

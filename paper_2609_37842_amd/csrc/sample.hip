@@ -27,17 +27,30 @@ constexpr float kC1 = 0.6931470036506653f * kTwo30, kC2 = 0.24022242426872253f *
                 kC3 = 0.05550733581185341f * kTwo30, kC4 = 0.009671512991189957f * kTwo30,
                 kC5 = 0.001326472731307149f * kTwo30;
 
-// t in [-31, 0]; below -31 the weight is 0 as it is at -31. fminf takes the NaN of inf - inf to 0.
-__device__ __forceinline__ float exponent_of(float l, float m, float c) {
-#pragma clang fp contract(off)
-  const float diff = l - m;
-  const float t = diff * c;
-  return fmaxf(fminf(t, 0.f), -31.f);
+// A row's largest logit and the scale of the differences from it. With a largest of +inf only the
+// logits of +inf count: inf - FLT_MAX is inf, every other difference times inf is -inf or NaN.
+struct Scale {
+  float most, c;
+};
+
+__device__ __forceinline__ Scale scale_of(float most, float c) {
+  return most == INFINITY ? Scale{3.4028234663852886e38f, INFINITY} : Scale{most, c};
 }
 
+// t in [-31, 0]; below -31 the weight is 0 as it is at -31. The median of a NaN (a NaN logit) and two
+// numbers is the lesser number, so it weighs nothing.
+__device__ __forceinline__ float exponent_of(float l, Scale s) {
+#pragma clang fp contract(off)
+  const float diff = l - s.most;
+  return __builtin_amdgcn_fmed3f(diff * s.c, -31.f, 0.f);
+}
+
+// Adding 1.5 * 2^23 rounds t to a whole number k (nearest, ties to even) and leaves it in the sum's low
+// bits, which go to the exponent of 2^30 2^f as they are (k >= -31: it stays a normal number).
 __device__ __forceinline__ uint32_t weight_of(float t) {
 #pragma clang fp contract(off)
-  const float k = rintf(t);
+  const float shifted = t + 12582912.f;
+  const float k = shifted - 12582912.f;
   const float f = t - k;
   float p = f * kC5;
   p = p + kC4;
@@ -49,7 +62,14 @@ __device__ __forceinline__ uint32_t weight_of(float t) {
   p = p + kC1;
   p = p * f;
   p = p + kTwo30;
-  return (uint32_t)p >> (uint32_t)(int)-k;
+  return (uint32_t)__uint_as_float(__float_as_uint(p) + (__float_as_uint(shifted) << 23));
+}
+
+// Sum of up to eight weights of at most 2^30 each: three fit 32 bits, four might not.
+template <int E>
+__device__ __forceinline__ uint64_t sum_weights(const uint32_t (&w)[E]) {
+  if constexpr (E == 4) return (uint64_t)(w[0] + w[1] + w[2]) + w[3];
+  return (uint64_t)(w[0] + w[1] + w[2]) + (w[3] + w[4] + w[5]) + (w[6] + w[7]);
 }
 
 __device__ __forceinline__ int bin_of(float t) { return std::min((int)(t * -kBinsPerOctave), kBins - 1); }
@@ -112,28 +132,32 @@ __device__ void find_token(const T* l, int64_t V, float u, const uint64_t* group
   constexpr int E = kPiece<T>, kWaves = NT / 64, kGroup = NT * G * E;
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int sums = (int)((V + kGroup - 1) / kGroup) * kWaves;
-  uint64_t total = 0;
-  for (int b = lane; b < sums; b += 64) total += group_mass[b];
-  const uint64_t target = target_of(wave_total(total), u);   // below the total
+  const uint64_t mine = lane < sums ? group_mass[lane] : 0, scan = wave_scan(mine);
+  uint64_t total = lane_value(scan, 63);
+  for (int b = 64; b < sums; b += 64) total += wave_total(b + lane < sums ? group_mass[b + lane] : 0);
+  const uint64_t target = target_of(total, u);         // below the total
   uint64_t before = 0;
   int hit = -1;
   for (int b = 0; b < sums && hit < 0; b += 64) {
-    const uint64_t v = b + lane < sums ? group_mass[b + lane] : 0;
-    const uint64_t incl = before + wave_scan(v);
+    const uint64_t v = b == 0 ? mine : b + lane < sums ? group_mass[b + lane] : 0;
+    const uint64_t incl = before + (b == 0 ? scan : wave_scan(v));
     const uint64_t over = __ballot(incl > target);
     const int at = over ? __builtin_ctzll(over) : 63;
     if (over) hit = b + at;
     before = lane_value(over ? incl - v : incl, at);
   }
   if (hit < 0 || hit % kWaves != wid) return;
-  for (int q = 0; q < G; ++q) {
-    const int64_t c = (int64_t)(hit / kWaves) * kGroup + ((int64_t)(wid * G + q) * 64 + lane) * E;
-    float v[E];
-    load_piece<T, E>(l, c, V, -INFINITY, v);
-    uint64_t w[E], s = 0;
+  const int64_t c0 = (int64_t)(hit / kWaves) * kGroup + ((int64_t)wid * G * 64 + lane) * E;
+  AnyVec<T, E> raw[G];                                 // requested together
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += w[e] = kept(v[e], (uint32_t)c + e);
-    const uint64_t incl = before + wave_scan(s);
+  for (int q = 0; q < G; ++q) raw[q] = fetch_piece<T, E>(l, c0 + q * 64 * E, V, (T)-INFINITY);
+#pragma unroll
+  for (int q = 0; q < G; ++q) {
+    const int64_t c = c0 + q * 64 * E;
+    uint32_t w[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = kept((float)raw[q][e], (uint32_t)c + e);
+    const uint64_t s = sum_weights<E>(w), incl = before + wave_scan(s);
     uint64_t run = incl - s;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -148,8 +172,10 @@ __device__ void find_token(const T* l, int64_t V, float u, const uint64_t* group
 template <int NT, int G, int E, typename Kept>
 __device__ __forceinline__ void add_piece(int p, uint32_t c, const float (&v)[E], uint64_t& sum, uint64_t* group_mass,
                                           Kept&& kept) {
+  uint32_t w[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) sum += kept(v[e], c + e);
+  for (int e = 0; e < E; ++e) w[e] = kept(v[e], c + e);
+  sum += sum_weights<E>(w);
   if (p % G == G - 1) {
     const uint64_t total = wave_scan(sum);
     if ((threadIdx.x & 63) == 63) group_mass[(p / G) * (NT / 64) + (threadIdx.x >> 6)] = total;
@@ -160,8 +186,9 @@ __device__ __forceinline__ void add_piece(int p, uint32_t c, const float (&v)[E]
 // From the whole distribution (or its w >= min_w). A block takes a row at a time. P > 0: the row stays
 // in registers as read, and the next one is requested piece by piece as the weights' pass lets go of
 // this one; P = 0: it is read in both passes.
-template <typename T, int NT, int P>
-__global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_sample(
+// MIN: only weights of at least min_w count.
+template <typename T, int NT, int P, bool MIN>
+__global__ __launch_bounds__(NT) void k_sample(
     const T* __restrict__ logits, int64_t ldl, int64_t n, int64_t V, const float* __restrict__ uniforms,
     const uint8_t* __restrict__ mask, float c, uint32_t min_w, int64_t* __restrict__ out) {
   constexpr int E = kPiece<T>, G = group_of(P);
@@ -183,9 +210,10 @@ __global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_sam
     float mine;
     const float m = row_max<Row, NT>(r, V, slot[turn], mine);
     const int64_t after = walk.next(n, live);
+    const Scale scale = scale_of(m, c);
     auto kept = [&](float v, uint32_t) -> uint32_t {
-      const uint32_t w = weight_of(exponent_of(fmaxf(v, -INFINITY), m, c));
-      return w >= min_w ? w : 0;
+      const uint32_t w = weight_of(exponent_of(v, scale));
+      return !MIN || w >= min_w ? w : 0;
     };
     uint64_t sum = 0;
     auto add = [&](int p, uint32_t i0, uint32_t, const float(&v)[E]) {
@@ -207,7 +235,9 @@ __global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_sam
 }
 
 // ---- with top_k or top_p -------------------------------------------------------------
-constexpr int kList = 1024;        // candidates that are settled against each other in LDS
+// Candidates that are settled against each other in LDS, each against all (1,024: some 40 us): at most,
+// with top_k, and when the alternative is one bin's and a pass over the row (about 10 us of 50,257).
+constexpr int kList = 1024, kListTopK = 512, kListAll = 256;
 
 // What is kept: every element up to this one in the order.
 struct Bound {
@@ -290,6 +320,7 @@ __device__ __forceinline__ void settle(const SelectLds<NT>& sh, int n, int i, ui
   const uint32_t k = sh.key[i], x = sh.index[i];
   rank = 0;
   mass = 0;
+#pragma unroll 4
   for (int j = 0; j < n; ++j) {
     const bool first = sh.key[j] < k || (sh.key[j] == k && sh.index[j] < x);
     rank += first;
@@ -330,6 +361,7 @@ __device__ void draw_from_list(SelectLds<NT>& sh, uint32_t top_k, uint32_t top_p
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint32_t w = sh.weight[i], x = sh.index[i];
     uint64_t run = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) run += sh.index[j] < x ? sh.weight[j] : 0;
     if (run <= target && target < run + w) *out = x;
   }
@@ -365,7 +397,7 @@ __device__ float lower_bound_of(SelectLds<NT>& sh, uint32_t key, uint32_t top_k)
 // The last kept element when more of a bin's elements tie than the list holds: the bin is split by the
 // key's four digits, then the index's. `row` is read once per digit.
 template <typename T, int NT>
-__device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0, 4>& row, int64_t V, float m, float c, Bound within,
+__device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0, 4>& row, int64_t V, Scale scale, Bound within,
                            bool by_mass, Found f, uint64_t want) {
   constexpr int E = kPiece<T>;
   const int bin = (int)f.digit;
@@ -378,7 +410,7 @@ __device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0, 4>& row, int
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const uint32_t i = i0 + e;
-        const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
+        const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, scale);
         if (i >= V || bin_of(t) != bin) continue;
         const uint32_t k = order_key(x);
         if (!within.keeps(k, i)) continue;
@@ -434,28 +466,43 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
   }
   const T* l = logits + row * ldl;
   const float u = uniforms[row];
-  float m, mine;
+  Scale scale;
   {
     RegisterRow<T, NT, P> r;
     r.load(l, (uint32_t)V);
-    m = row_max<RegisterRow<T, NT, P>, NT>(r, V, sh.slot, mine);
+    float mine;
+    const float m = row_max<RegisterRow<T, NT, P>, NT>(r, V, sh.slot, mine);
     if (m == -INFINITY) {                              // nothing to draw from
       if (tid == 0) out[row] = -1;
       return;
     }
+    scale = scale_of(m, c);
     if (top_k && top_k <= NT) {
       const float cut = lower_bound_of<NT>(sh, order_key(mine), top_k);
-      r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t first, const float(&v)[E]) {
-        if (mine < cut) return;
+      // Which of the thread's pieces reach the bound; those few are read again and taken apart.
+      uint64_t hits = 0;
+      if (mine >= cut)
+        r.each((uint32_t)V, [&](int p, uint32_t, uint32_t, const float(&v)[E]) {
+          float top = v[0];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float x = fmaxf(v[e], -INFINITY);
-          const uint32_t i = i0 + e;
-          if (x >= cut && i >= first && i < V) append(sh, order_key(x), i, weight_of(exponent_of(x, m, c)));
+          for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+          if (top >= cut) hits |= 1ull << (P > 0 ? p : p & 63);
+        });
+      using Shape = RegisterRow<T, NT, 1>;
+      const uint32_t place = Shape::here();
+      for (; hits; hits &= hits - 1) {
+        for (int64_t i0 = place + (int64_t)__builtin_ctzll(hits) * NT * E; i0 < V; i0 += 64 * NT * E) {
+          float v[E];
+          load_piece<T, E>(l, i0, V, -INFINITY, v);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (v[e] >= cut && i0 + e < V)
+              append(sh, order_key(v[e]), (uint32_t)i0 + e, weight_of(exponent_of(v[e], scale)));
+          if (P > 0) break;
         }
-      });
+      }
       __syncthreads();
-      if (sh.listed <= kList) {
+      if (sh.listed <= kListTopK) {
         draw_from_list<NT>(sh, top_k, top_p24, min_w, 0, u, out + row);
         return;
       }
@@ -467,44 +514,53 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
   for (int by_mass = 0; by_mass < 2; ++by_mass) {
     if (by_mass ? top_p24 == 1u << 24 : top_k == 0) continue;
     clear_hist(sh, kBins);
+    const bool bounded = by_mass && top_k;
     uint64_t mass = 0;
     r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const uint32_t i = i0 + e;
-        const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
-        if (i >= V || !bound.keeps(order_key(x), i)) continue;
-        const uint32_t w = by_mass ? weight_of(t) : 1;
-        mass += w;
-        if (!by_mass || t >= t_cut) atomicAdd(&sh.hist[bin_of(t)], (unsigned long long)w);
+        const float t = exponent_of(v[e], scale);
+        if (by_mass) {
+          uint32_t w = weight_of(t);                   // (0 past the row's end)
+          if (bounded && !bound.keeps(order_key(fmaxf(v[e], -INFINITY)), i)) w = 0;
+          mass += w;
+          if (t >= t_cut && w) atomicAdd(&sh.hist[bin_of(t)], (unsigned long long)w);
+        } else if (i < V) {
+          atomicAdd(&sh.hist[bin_of(t)], 1ull);
+        }
       }
     });
     mass = block_total<NT>(mass, sh.sum2);
     const uint64_t want = by_mass ? std::max<uint64_t>(1, share_of(mass, top_p24)) : top_k;
     const Found f = find_digit<NT>(sh, kBins, 0, want);
-    const int last = (int)f.digit;
-    bool all = true;                                   // elements up to the bin, then of the bin alone
+    // Elements up to the bin, then of the bin alone; the bin's t are above `low` and at most `high`.
+    const float low = -((float)f.digit + 1.f) / kBinsPerOctave, high = -(float)f.digit / kBinsPerOctave;
+    bool all = true;
     for (int only = 0; only < 2; ++only) {
       all = !only;
       clear_list(sh);
       r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
+        float top = v[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) top = fmaxf(top, v[e]);
+        if (exponent_of(top, scale) <= low) return;    // none of the piece
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const uint32_t i = i0 + e;
-          const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, m, c);
-          const int b = bin_of(t);
-          if (b > last || (only && b < last) || i >= V) continue;
+          const float x = fmaxf(v[e], -INFINITY), t = exponent_of(x, scale);
+          if (t <= low || (only && t > high) || i >= V) continue;
           const uint32_t k = order_key(x);
           if (bound.keeps(k, i)) append(sh, k, i, weight_of(t));
         }
       });
       __syncthreads();
-      if (sh.listed <= kList) break;
+      if (sh.listed <= (only ? kList : kListAll)) break;
       if (!only) __syncthreads();                      // all have seen the count before it is cleared
     }
     const int n = (int)sh.listed;
     if (n > kList) {
-      bound = split_bin<T, NT>(sh, r, V, m, c, bound, by_mass, f, want);
+      bound = split_bin<T, NT>(sh, r, V, scale, bound, by_mass, f, want);
       continue;
     }
     if (all) {
@@ -525,7 +581,7 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
   auto kept = [&](float v, uint32_t i) -> uint32_t {
     const float x = fmaxf(v, -INFINITY);
     if (!bound.keeps(order_key(x), i)) return 0;
-    const uint32_t w = weight_of(exponent_of(x, m, c));
+    const uint32_t w = weight_of(exponent_of(x, scale));
     return w >= min_w ? w : 0;
   };
   uint64_t sum = 0;
@@ -577,26 +633,36 @@ eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t
   const uint32_t k = top_k >= V ? 0 : (uint32_t)top_k;           // all of them: no limit
   const uint32_t p24 = (uint32_t)std::floor(top_p * 16777216.0 + 0.5);
   const uint32_t min_w = (uint32_t)std::ceil(min_p * 1073741824.0);
+  const bool select = k || p24 < 1u << 24;
   return with_type(t, [&](auto el) {
     using T = decltype(el);
-    if (temperature == 0) {
-      hipLaunchKernelGGL(k_argmax<T>, dim3((unsigned)n), dim3(1024), 0, s, static_cast<const T*>(logits), ldl, V,
-                         mask, out);
-      EOGP_LAUNCH_CHECK("sample_tokens (argmax)");
+    const T* l = static_cast<const T*>(logits);
+    // f(first row, rows) for launches with a block per row
+    auto in_parts = [&](auto&& f) {
+      for (int64_t r = 0; r < n; r += kMostBlocks) {
+        f(r, (unsigned)std::min<int64_t>(n - r, kMostBlocks));
+        EOGP_LAUNCH_CHECK("sample_tokens");
+      }
       return EOGP_OK;
-    }
-    return with_row_shape<T>(V, [&](auto nt, auto p) {
+    };
+    if (temperature == 0)
+      return in_parts([&](int64_t r, unsigned rows) {
+        hipLaunchKernelGGL(k_argmax<T>, dim3(rows), dim3(1024), 0, s, l + r * ldl, ldl, V, mask ? mask + r : nullptr,
+                           out + r);
+      });
+    return with_row_shape<T>(V, [&](auto nt, auto p) -> eogp_status {
       constexpr int NT = decltype(nt)::value, P = decltype(p)::value;
-      if (k || p24 < 1u << 24) {
+      if (select) {
         // V weights of at most 2^(30 + t_cut) each come to less than the (1 - top_p) 2^30 beyond top_p
         const float t_cut = (float)(std::log2((16777216.0 - p24) / 16777216.0 / (double)V) - 0.01);
-        hipLaunchKernelGGL((k_sample_select<T, NT, P>), dim3((unsigned)n), dim3(NT), 0, s,
-                           static_cast<const T*>(logits), ldl, V, uniforms, mask, c, k, p24, min_w, t_cut, out);
-      } else {
-        const int64_t blocks = std::min<int64_t>(n, kCus * row_blocks_per_cu(NT, P));
-        hipLaunchKernelGGL((k_sample<T, NT, P>), dim3((unsigned)blocks), dim3(NT), 0, s,
-                           static_cast<const T*>(logits), ldl, n, V, uniforms, mask, c, min_w, out);
+        return in_parts([&](int64_t r, unsigned rows) {
+          hipLaunchKernelGGL((k_sample_select<T, NT, P>), dim3(rows), dim3(NT), 0, s, l + r * ldl, ldl, V,
+                             uniforms + r, mask ? mask + r : nullptr, c, k, p24, min_w, t_cut, out + r);
+        });
       }
+      auto* kfn = min_w > 1 ? k_sample<T, NT, P, true> : k_sample<T, NT, P, false>;
+      hipLaunchKernelGGL(kfn, dim3((unsigned)row_blocks(n, NT, 1)), dim3(NT), 0, s, l, ldl, n, V, uniforms, mask, c,
+                         min_w, out);
       EOGP_LAUNCH_CHECK("sample_tokens");
       return EOGP_OK;
     });

@@ -31,21 +31,22 @@ __device__ __forceinline__ float block_sum(float v, float* slot) {
   return v;
 }
 
+constexpr int xent_per_cu(int nt, int p) { return nt == 256 ? 6 : p >= 1 && p <= 4 ? 2 : 1; }
+
 // loss = ln sum_i exp(l_i - m) - (l_label - m), m = max l;
 // dl_i = g (exp(l_i - m) / sum - [i = label]) = g (2^((l_i - m) log2 e - log2 sum) - [i = label]).
 // A block takes a row at a time. With P > 0 the row stays in registers as read, so HBM sees one read
 // and one write, and the next row is requested piece by piece as the gradient's pass lets go of this
 // one; P = 0 reads the row three times, for rows longer than the registers hold.
 template <typename T, int NT, int P, bool GRAD>
-__global__ __launch_bounds__(NT, row_blocks_per_cu(NT, P) * NT / 256) void k_xent(
+__global__ __launch_bounds__(NT, xent_per_cu(NT, P) * NT / 256) void k_xent(
     const T* logits, int64_t ldl, const int64_t* __restrict__ labels, const uint8_t* __restrict__ mask, int64_t n,
     int64_t V, float gscale, float* __restrict__ loss, T* dlogits, int64_t ldd) {
   constexpr int E = kPiece<T>;
   __shared__ float slot[2][NT / 64];
   RowWalk walk;
   auto live = [&](int64_t row) {                       // rows without a loss are not read
-    const int64_t label = labels[row];
-    if ((!mask || mask[row] != 0) && label >= 0 && label < V) return true;
+    if ((!mask || mask[row] != 0) && labels[row] >= 0 && labels[row] < V) return true;
     if (threadIdx.x == 0 && loss) loss[row] = 0.f;
     float zero[E] = {};
     if (GRAD)
@@ -115,7 +116,7 @@ eogp_status softmax_xent(const void* logits, eogp_dtype t, int64_t ldl, const in
     auto go = [&](auto nt, auto p) {
       constexpr int NT = decltype(nt)::value;
       constexpr int P = decltype(p)::value;
-      const int64_t blocks = std::min<int64_t>(n, kCus * row_blocks_per_cu(NT, P));
+      const int64_t blocks = row_blocks(n, NT, xent_per_cu(NT, P));
       auto* kfn = dlogits ? k_xent<T, NT, P, true> : k_xent<T, NT, P, false>;
       hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(NT), 0, s, static_cast<const T*>(logits), ldl, labels, mask,
                          n, V, gscale, loss, static_cast<T*>(dlogits), ldd);
