@@ -136,6 +136,10 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
   return add_before<5>(add_before<4>(v));
 }
 
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  return scan_steps(v, [](uint32_t x, auto step) { return x + lane_before<decltype(step)::value>(x, 0); });
+}
+
 __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
@@ -260,14 +264,25 @@ struct RegisterRow<T, NT, 0, G> {
   template <typename F>
   __device__ __forceinline__ void each(uint32_t width, F&& f) {
     const uint32_t place = Shape::here();
-    auto at = [&](int p) { return (uint32_t)(p / G) * kGroup + Shape::at(place, p % G); };
-    AnyVec<T, E> next = fetch(row, place, width);          // one piece is on its way while another is taken
-    for (int p = 0; (uint64_t)(p / G) * kGroup < width; ++p) {
-      float v[E];
+    AnyVec<T, E> next[G];                                  // one group is on its way while another is taken
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = (float)next[e];
-      if ((uint64_t)((p + 1) / G) * kGroup < width) next = fetch(row, at(p + 1), width);
-      f(p, at(p), at(p), v);
+    for (int q = 0; q < G; ++q) next[q] = fetch(row, Shape::at(place, q), width);
+    int p = 0;
+    for (uint64_t base = 0; base < width; base += kGroup) {
+      AnyVec<T, E> now[G];
+#pragma unroll
+      for (int q = 0; q < G; ++q) now[q] = next[q];
+      if (base + kGroup < width) {
+#pragma unroll
+        for (int q = 0; q < G; ++q) next[q] = fetch(row, (uint32_t)(base + kGroup) + Shape::at(place, q), width);
+      }
+#pragma unroll
+      for (int q = 0; q < G; ++q, ++p) {
+        float v[E];
+        widen<T, E>(now[q], v);
+        const uint32_t c = (uint32_t)base + Shape::at(place, q);
+        f(p, c, c, v);
+      }
     }
   }
 

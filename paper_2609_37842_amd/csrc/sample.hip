@@ -255,8 +255,8 @@ struct Found {
 template <int NT>
 struct SelectLds {
   unsigned long long hist[kBins];
-  uint32_t reach[8][3];
-  uint32_t key[kList], index[kList], weight[kList];
+  alignas(16) uint32_t reach[2][256];
+  alignas(16) uint32_t key[kList + 4], index[kList + 4], weight[kList + 4];
   uint64_t sum[NT / 64], sum2[NT / 64];
   uint32_t listed;
   float slot[NT / 64], cut;
@@ -280,7 +280,11 @@ __device__ Found find_digit(SelectLds<NT>& sh, int digits, uint64_t before, uint
   if ((threadIdx.x & 63) == 63) sh.sum[wid] = incl;
   __syncthreads();
   uint64_t run = before + incl - s;
-  for (int w = 0; w < wid; ++w) run += sh.sum[w];
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    const uint64_t others = sh.sum[w];
+    run += w < wid ? others : 0;
+  }
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {
     if (run < want && want <= run + h[k]) sh.found = Found{(uint32_t)(threadIdx.x * per + k), run, h[k]};
@@ -314,17 +318,34 @@ __device__ __forceinline__ void append(SelectLds<NT>& sh, uint32_t key, uint32_t
   }
 }
 
+// Four places past the list's n elements that are read with them and stand for nothing.
+template <int NT>
+__device__ __forceinline__ void end_list(SelectLds<NT>& sh, int n) {
+  if (threadIdx.x < 4) {
+    sh.key[n + threadIdx.x] = sh.index[n + threadIdx.x] = 0xFFFFFFFFu;
+    sh.weight[n + threadIdx.x] = 0;
+  }
+  __syncthreads();
+}
+
 // Place and mass before element i of the list among its n elements.
 template <int NT>
 __device__ __forceinline__ void settle(const SelectLds<NT>& sh, int n, int i, uint32_t& rank, uint64_t& mass) {
-  const uint32_t k = sh.key[i], x = sh.index[i];
+  const uint64_t mine = (uint64_t)sh.key[i] << 32 | sh.index[i];
   rank = 0;
   mass = 0;
-#pragma unroll 4
-  for (int j = 0; j < n; ++j) {
-    const bool first = sh.key[j] < k || (sh.key[j] == k && sh.index[j] < x);
-    rank += first;
-    mass += first ? sh.weight[j] : 0;
+  for (int j = 0; j < n; j += 4) {
+    const uint4 k = *reinterpret_cast<const uint4*>(sh.key + j), x = *reinterpret_cast<const uint4*>(sh.index + j),
+                w = *reinterpret_cast<const uint4*>(sh.weight + j);
+    auto one = [&](uint32_t kj, uint32_t xj, uint32_t wj) {
+      const bool first = ((uint64_t)kj << 32 | xj) < mine;
+      rank += first;
+      mass += first ? wj : 0;
+    };
+    one(k.x, x.x, w.x);
+    one(k.y, x.y, w.y);
+    one(k.z, x.z, w.z);
+    one(k.w, x.w, w.w);
   }
 }
 
@@ -336,6 +357,7 @@ __device__ void draw_from_list(SelectLds<NT>& sh, uint32_t top_k, uint32_t top_p
                                float u, int64_t* out) {
   constexpr int kMine = kList / NT;
   const int n = (int)sh.listed;
+  end_list(sh, n);
   uint32_t rank[kMine];
   uint64_t before[kMine], s = 0;
 #pragma unroll
@@ -361,33 +383,45 @@ __device__ void draw_from_list(SelectLds<NT>& sh, uint32_t top_k, uint32_t top_p
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint32_t w = sh.weight[i], x = sh.index[i];
     uint64_t run = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) run += sh.index[j] < x ? sh.weight[j] : 0;
+    for (int j = 0; j < n; j += 4) {
+      const uint4 xs = *reinterpret_cast<const uint4*>(sh.index + j),
+                  ws = *reinterpret_cast<const uint4*>(sh.weight + j);
+      run += (uint64_t)((xs.x < x ? ws.x : 0) + (xs.y < x ? ws.y : 0) + (xs.z < x ? ws.z : 0)) +
+             (xs.w < x ? ws.w : 0);
+    }
     if (run <= target && target < run + w) *out = x;
   }
 }
 
 // A lower bound of the top_k-th largest logit (1 <= top_k <= NT): of the upper 16 bits of the threads'
 // own largest logits (as order keys), the least that top_k of them reach; the logit with that key and
-// its lower bits set. Two bits are found at a time, by the threads below each of three candidates.
+// its lower bits set. Found a byte at a time: every wave scans the counts of the byte's 256 values.
 template <int NT>
 __device__ float lower_bound_of(SelectLds<NT>& sh, uint32_t key, uint32_t top_k) {
-  if (threadIdx.x < 24) sh.reach[threadIdx.x / 3][threadIdx.x % 3] = 0;
+  const int lane = threadIdx.x & 63;
+  for (int i = threadIdx.x; i < 512; i += NT) (&sh.reach[0][0])[i] = 0;
   if (threadIdx.x == 0) sh.listed = 0;
   __syncthreads();
-  uint32_t found = 0;
-  for (int step = 0; step < 8; ++step) {
-    const int shift = 14 - 2 * step;
+  uint32_t found = 0, below = 0;                       // below: threads whose key is below the bytes found
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      const uint64_t below = __ballot(key >> 16 < found + ((uint32_t)(q + 1) << shift));
-      if ((threadIdx.x & 63) == 0) atomicAdd(&sh.reach[step][q], (uint32_t)__popcll(below));
-    }
+  for (int byte = 0; byte < 2; ++byte) {
+    if (byte == 0 || key >> 24 == found >> 8) atomicAdd(&sh.reach[byte][(key >> (24 - 8 * byte)) & 255], 1u);
     __syncthreads();
-    uint32_t take = 0;                                 // the most with fewer than top_k threads below
-    for (int q = 0; q < 3; ++q)
-      if (sh.reach[step][q] < top_k) take = q + 1;
-    found += take << shift;
+    const uint4 c = *reinterpret_cast<const uint4*>(&sh.reach[byte][4 * lane]);
+    const uint32_t sum = c.x + c.y + c.z + c.w, incl = below + wave_scan(sum);
+    const int at = __builtin_ctzll(__ballot(incl >= top_k));        // (all NT threads reach it at the latest)
+    uint32_t run = (uint32_t)__builtin_amdgcn_readlane((int)(incl - sum), at), digit = 4 * at;
+    const uint32_t part[3] = {(uint32_t)__builtin_amdgcn_readlane((int)c.x, at),
+                              (uint32_t)__builtin_amdgcn_readlane((int)c.y, at),
+                              (uint32_t)__builtin_amdgcn_readlane((int)c.z, at)};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (digit == 4u * at + k && run + part[k] < top_k) {
+        run += part[k];
+        ++digit;
+      }
+    below = run;
+    found |= digit << (8 - 8 * byte);
   }
   const uint32_t last = found << 16 | 0xFFFFu;
   const uint32_t bits = last & 0x80000000u ? last : ~last & 0x7FFFFFFFu;
@@ -517,6 +551,7 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
     const bool bounded = by_mass && top_k;
     uint64_t mass = 0;
     r.each((uint32_t)V, [&](int, uint32_t i0, uint32_t, const float(&v)[E]) {
+      if ((uint32_t)__builtin_amdgcn_readfirstlane((int)i0) >= V) return;   // past the end for the whole wave
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const uint32_t i = i0 + e;
@@ -567,6 +602,7 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
       draw_from_list<NT>(sh, by_mass ? 0 : top_k, top_p24, min_w, mass, u, out + row);
       return;
     }
+    end_list(sh, n);
     for (int i = tid; i < n; i += NT) {
       uint32_t rank;
       uint64_t before;
