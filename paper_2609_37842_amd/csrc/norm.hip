@@ -29,6 +29,46 @@ __device__ __forceinline__ void stage_weights(float* lds, const void* w, eogp_dt
   for (int c = threadIdx.x; c < d; c += NT) lds[c] = w ? load_any(w, wt, c) : none;
 }
 
+// The valid rows among first, first + step, ... of a wave, in order. The masks (and the means
+// and reciprocal deviations) of 64 rows are read at once, a row per lane, so that a row costs no wait
+// for them. VALUES: 1 for the mask alone, 3 with the statistics.
+template <int VALUES>
+struct RowQueue {
+  const uint8_t* mask;
+  const float *means, *rstds;
+  int64_t first, step, n;
+  uint64_t live = 0, masked = 0;               // bits of the 64 rows from `first` on that are left
+  float lane_mean = 0.f, lane_rstd = 0.f;
+
+  __device__ __forceinline__ RowQueue(const uint8_t* m, const float* me, const float* rs, int64_t f, int64_t st,
+                                      int64_t rows)
+      : mask(m), means(me), rstds(rs), first(f - 64 * st), step(st), n(rows) {}
+
+  // The next valid row, -1 at the end; skip(row) for the masked ones of a batch when it is taken up.
+  template <typename Skip>
+  __device__ __forceinline__ int64_t next(Skip&& skip) {
+    while (!live) {
+      first += 64 * step;
+      if (first >= n) return -1;
+      const int64_t mine = first + (threadIdx.x & 63) * step;
+      const bool in = mine < n, ok = in && (!mask || mask[mine] != 0);
+      live = __ballot(ok);
+      masked = __ballot(in && !ok);
+      if constexpr (VALUES > 1) {
+        lane_mean = ok ? means[mine] : 0.f;
+        lane_rstd = ok ? rstds[mine] : 0.f;
+      }
+      for (; masked; masked &= masked - 1) skip(first + __builtin_ctzll(masked) * step);
+    }
+    const int at = __builtin_ctzll(live);
+    live &= live - 1;
+    mean = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_uint(lane_mean), at));
+    rstd = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_uint(lane_rstd), at));
+    return first + at * step;
+  }
+  float mean = 0.f, rstd = 0.f;                // of the row that next returned
+};
+
 constexpr int norm_threads(int wpr) { return wpr > 4 ? 64 * wpr : 256; }
 
 // y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
@@ -47,38 +87,34 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
   const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;   // place among the row's lanes
   float *g = weights, *b = weights + (d + E - 1) / E * E;
   const float width = (float)d;               // sums are divided by it: a constant row's mean is exact
-  bool staged = false;
-  for (int64_t first = (int64_t)blockIdx.x * kRows; first < n; first += (int64_t)gridDim.x * kRows) {
-    const int64_t row = first + (WPR == 1 ? wid : 0);
-    const bool live = row < n && (!mask || mask[row] != 0);   // uniform across the row's waves
-    AnyVec<TI, E> raw[P];
-    if (live) {
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-        raw[p] = fetch_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d, (TI)0.f);
-    }
-    if (!staged) {                            // while the first rows are on their way
-      stage_weights<NT>(g, gamma, wt, d, 1.f);
-      stage_weights<NT>(b, beta, wt, d, 0.f);
-      __syncthreads();
-      staged = true;
-    }
-    if (row >= n) continue;
+  RowQueue<1> queue(mask, nullptr, nullptr, (int64_t)blockIdx.x * kRows + (WPR == 1 ? wid : 0),
+                    (int64_t)gridDim.x * kRows, n);
+  auto none = [&](int64_t row) {              // not read; zeros
     TO* yr = y + row * ldy;
-    if (!live) {                              // not read; zeros
-      float zero[E] = {};
+    float zero[E] = {};
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-        if (c < d) store_piece<TO, E>(yr, c, d, zero);
-      }
-      if (t == 0) {
-        if (ones) yr[d] = (TO)0.f;
-        if (mean_out) mean_out[row] = 0.f;
-        if (rstd_out) rstd_out[row] = 0.f;
-      }
-      continue;
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      if (c < d) store_piece<TO, E>(yr, c, d, zero);
     }
+    if (t == 0) {
+      if (ones) yr[d] = (TO)0.f;
+      if (mean_out) mean_out[row] = 0.f;
+      if (rstd_out) rstd_out[row] = 0.f;
+    }
+  };
+  AnyVec<TI, E> raw[P];
+  auto load = [&](int64_t row) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      raw[p] = fetch_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d, (TI)0.f);
+  };
+  int64_t row = queue.next(none);
+  if (row >= 0) load(row);
+  stage_weights<NT>(g, gamma, wt, d, 1.f);    // while the first row is on its way
+  stage_weights<NT>(b, beta, wt, d, 0.f);
+  __syncthreads();
+  while (row >= 0) {
     float v[P][E];
     float s = 0.f;
 #pragma unroll
@@ -87,6 +123,8 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
 #pragma unroll
       for (int e = 0; e < E; ++e) s += v[p][e];
     }
+    const int64_t after = queue.next(none);
+    if (after >= 0) load(after);              // the next row, while this one is summed and written
     const float mean = row_sum<WPR>(s, slot[0]) / width;
     s = 0.f;
 #pragma unroll
@@ -98,6 +136,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
         s += v[p][e] * v[p][e];
       }
     const float rstd = 1.f / sqrtf(row_sum<WPR>(s, slot[1]) / width + eps);
+    TO* yr = y + row * ldy;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
@@ -113,6 +152,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
       if (mean_out) mean_out[row] = mean;
       if (rstd_out) rstd_out[row] = rstd;
     }
+    row = after;
   }
 }
 
@@ -128,7 +168,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     const void* __restrict__ gamma, eogp_dtype wt, const float* __restrict__ mean_in,
     const float* __restrict__ rstd_in, const uint8_t* __restrict__ mask, const T* res,
     int64_t ldres, int64_t rows_per_group, int64_t d, int splits, T* dx, int64_t lddx,
-    float* __restrict__ part) {
+    float* __restrict__ part, float* __restrict__ dgamma, float* __restrict__ dbeta) {
   constexpr int E = kPiece<T>, NT = norm_threads(WPR);
   constexpr int kRows = NT / 64 / WPR;
   extern __shared__ __align__(16) float weights[];     // gamma: round_up(d, E)
@@ -145,32 +185,53 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
   __syncthreads();
   const float width = (float)d;
   const int64_t group = blockIdx.x / splits, split = blockIdx.x % splits;
-  int turn = 0;
-  for (int64_t i = split * kRows + (WPR == 1 ? wid : 0); i < rows_per_group; i += (int64_t)splits * kRows) {
-    const int64_t row = group * rows_per_group + i;
-    T* out = dx + row * lddx;
-    if (mask && mask[row] == 0) {            // not read; zeros
-      float zero[E] = {};
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-        if (c < d) store_piece<T, E>(out, c, d, zero);
-      }
-      continue;
-    }
-    const float mean = mean_in[row], rstd = rstd_in[row];
-    // (streaming loads: 32,768 rows of 5120 bf16 in 303 us, 316 without)
-    AnyVec<T, E> xr[P], dr[P], rr[P];
+  const int64_t row0 = group * rows_per_group;
+  RowQueue<3> queue(mask ? mask + row0 : nullptr, mean_in + row0, rstd_in + row0,
+                    split * kRows + (WPR == 1 ? wid : 0), (int64_t)splits * kRows, rows_per_group);
+  auto none = [&](int64_t i) {               // not read; zeros
+    float zero[E] = {};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      xr[p] = fetch_piece<T, E, true>(x + row * ldx, c, d, (T)0.f);
-      dr[p] = fetch_piece<T, E, true>(dy + row * lddy, c, d, (T)0.f);   // (0 past the end: no sum sees x there)
+      if (c < d) store_piece<T, E>(dx + (row0 + i) * lddx, c, d, zero);
+    }
+  };
+  // Rows ahead of their turn where two fit the registers (else the block's other waves and the CU's
+  // other blocks have theirs on the way).
+  constexpr bool kAhead = WPR <= 4 && P * E <= 16;
+  struct Inputs {
+    AnyVec<T, E> x[P], dy[P], res[P];
+  };
+  auto load = [&](int64_t i, Inputs& in) {
+    const int64_t row = row0 + i;
+    // (streaming loads: 32,768 rows of 5120 bf16 in 303 us, 316 without)
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
+      in.x[p] = fetch_piece<T, E, true>(x + row * ldx, c, d, (T)0.f);
+      in.dy[p] = fetch_piece<T, E, true>(dy + row * lddy, c, d, (T)0.f);   // (0 past the end: no sum sees x there)
     }
     if (res) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        rr[p] = fetch_piece<T, E, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d, (T)0.f);
+        in.res[p] = fetch_piece<T, E, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d, (T)0.f);
+    }
+  };
+  int turn = 0;
+  Inputs now, ahead;
+  int64_t i = queue.next(none);
+  if (kAhead && i >= 0) load(i, ahead);
+  while (i >= 0) {
+    const float mean = queue.mean, rstd = queue.rstd;
+    T* out = dx + (row0 + i) * lddx;
+    int64_t after;
+    if constexpr (kAhead) {
+      now = ahead;
+      after = queue.next(none);
+      if (after >= 0) load(after, ahead);
+    } else {
+      load(i, now);
+      after = queue.next(none);
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -180,7 +241,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
       if (c < d) gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float xh = ((float)xr[p][e] - mean) * rstd, g = (float)dr[p][e];
+        const float xh = ((float)now.x[p][e] - mean) * rstd, g = (float)now.dy[p][e];
         ag[p][e] += g * xh;
         ab[p][e] += g;
         const float tv = c < d ? g * gp[e] : 0.f;
@@ -214,20 +275,25 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
       if (c >= d) break;
       const AnyVec<float, E> gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
-      AnyVec<T, E> xc = xr[p], dc = dr[p];
+      AnyVec<T, E> xc = now.x[p], dc = now.dy[p];
       asm volatile("" : "+v"(xc), "+v"(dc));           // formed again, not kept from the sums' pass
       float r[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float xh = ((float)xc[e] - mean) * rstd;
-        r[e] = rstd * ((float)dc[e] * gp[e] - s1 - xh * s2) + (res ? (float)rr[p][e] : 0.f);
+        r[e] = rstd * ((float)dc[e] * gp[e] - s1 - xh * s2) + (res ? (float)now.res[p][e] : 0.f);
       }
       store_piece<T, E>(out, c, d, r);
       __builtin_amdgcn_sched_barrier(0);
     }
+    i = after;
   }
-  float* pg = part + (int64_t)blockIdx.x * 2 * d;
-  float* pb = pg + d;
+  // a group's only block writes its gradients, others their sums for k_norm_fold
+  float *pg = part + (int64_t)blockIdx.x * 2 * d, *pb = pg + d;
+  if (splits == 1) {
+    pg = dgamma ? dgamma + group * d : nullptr;
+    pb = dbeta ? dbeta + group * d : nullptr;
+  }
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
@@ -248,8 +314,8 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
       if (wid > 0) continue;
     }
     if (c < d) {
-      store_piece<float, E>(pg, c, d, ag[p]);
-      store_piece<float, E>(pb, c, d, ab[p]);
+      if (pg) store_piece<float, E>(pg, c, d, ag[p]);
+      if (pb) store_piece<float, E>(pb, c, d, ab[p]);
     }
   }
 }
@@ -350,8 +416,10 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
 }
 
 namespace {
-// Blocks of a group: enough to fill the chip four times over, no more than its rows need.
+// Blocks of a group: enough to fill the chip four times over, no more than its rows need; one for so
+// few rows that a second launch would cost more than their turns.
 int back_splits(int64_t groups, int64_t rows, int64_t pieces) {
+  if (rows <= 4 * rows_per_block(pieces)) return 1;
   const int64_t most = ceil_div(rows, rows_per_block(pieces));
   const int64_t want = ceil_div(pieces <= 1024 ? 4 * kCus : 2 * kCus, groups);
   return (int)std::max<int64_t>(1, std::min(most, want));
@@ -384,13 +452,14 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
       }
       hipLaunchKernelGGL(kfn, dim3((unsigned)(groups * splits)), dim3(norm_threads(W)), lds, s,
                          static_cast<const T*>(dy), lddy, static_cast<const T*>(x), ldx, gamma, wt, mean, rstd, mask,
-                         static_cast<const T*>(res), ldres, rows, d, splits, static_cast<T*>(dx), lddx, part);
+                         static_cast<const T*>(res), ldres, rows, d, splits, static_cast<T*>(dx), lddx, part, dgamma,
+                         dbeta);
       EOGP_LAUNCH_CHECK("layer_norm_backward");
       return EOGP_OK;
     });
   });
   if (st != EOGP_OK) return st;
-  if (!dgamma && !dbeta) return EOGP_OK;
+  if (splits == 1 || (!dgamma && !dbeta)) return EOGP_OK;
   const int64_t fold_blocks = std::min<int64_t>(groups * ceil_div(2 * d, 32), 1 << 20);
   const bool many = splits > 64;
   hipLaunchKernelGGL(many ? k_norm_fold<32> : k_norm_fold<8>, dim3((unsigned)fold_blocks), dim3(many ? 1024 : 256), 0,

@@ -17,31 +17,44 @@ template <> struct ElemOf<EOGP_F16> { using type = _Float16; };
 
 template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);   // elements of a piece
 
-// E elements at any element's address
+// E elements at any element's address. (Plain typedefs: an alignment that depends on a template's
+// parameters is dropped, and the compiler would take 16-byte boundaries for granted.)
+template <typename T, int E> struct AnyVecOf;
+#define EOGP_ANY_VEC(T, E)                                                  \
+  template <> struct AnyVecOf<T, E> {                                       \
+    typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T)))); \
+  };
+EOGP_ANY_VEC(float, 2)
+EOGP_ANY_VEC(float, 4)
+EOGP_ANY_VEC(float, 8)
+EOGP_ANY_VEC(__bf16, 2)
+EOGP_ANY_VEC(__bf16, 4)
+EOGP_ANY_VEC(__bf16, 8)
+EOGP_ANY_VEC(_Float16, 2)
+EOGP_ANY_VEC(_Float16, 4)
+EOGP_ANY_VEC(_Float16, 8)
+#undef EOGP_ANY_VEC
 template <typename T, int E>
-using AnyVec = T __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+using AnyVec = typename AnyVecOf<T, E>::type;
 
 // E elements at a 16-byte boundary (LDS)
 template <typename T, int E>
 using AlignedVec = T __attribute__((ext_vector_type(E), aligned(16)));
 
-// Elements c .. c + E - 1 of a row of d as fp32; `pad` in the place of those past the end.
-template <typename T, int E>
-__device__ __forceinline__ void load_piece(const T* __restrict__ row, int64_t c, int64_t d, float pad,
-                                           float (&v)[E]) {
-  if (c + E <= d) {
-    const AnyVec<T, E> x = *reinterpret_cast<const AnyVec<T, E>*>(row + c);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = (float)x[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = c + e < d ? (float)row[c + e] : pad;
-  }
+// A piece as four words, moved down by a number of bytes with `fill` coming in above. (Only a row's last
+// piece is ever short, by the same bytes in every row, so the tests are uniform.)
+__device__ __forceinline__ uint4 words_down(uint4 x, uint32_t bytes, uint32_t fill) {
+  if (bytes & 8) x = uint4{x.z, x.w, fill, fill};
+  if (bytes & 4) x = uint4{x.y, x.z, x.w, fill};
+  if (bytes & 2)
+    x = uint4{__builtin_amdgcn_alignbit(x.y, x.x, 16), __builtin_amdgcn_alignbit(x.z, x.y, 16),
+              __builtin_amdgcn_alignbit(x.w, x.z, 16), __builtin_amdgcn_alignbit(fill, x.w, 16)};
+  return x;
 }
 
-// The same elements as they are, and their fp32 values: loads of several pieces go out together when
-// their conversions come after all of them.
-// STREAM: rows that are read this once, past the L2s' other lines.
+// Elements c .. c + E - 1 of a row of d; `pad` in the place of those past the end, which are not read.
+// The short last piece is one load of the row's last E elements, moved down. STREAM: rows that are read
+// this once, past the L2s' other lines.
 template <typename T, int E, bool STREAM = false>
 __device__ __forceinline__ AnyVec<T, E> fetch_piece(const T* __restrict__ row, int64_t c, int64_t d, T pad) {
   AnyVec<T, E> x;
@@ -53,7 +66,23 @@ __device__ __forceinline__ AnyVec<T, E> fetch_piece(const T* __restrict__ row, i
       x = *p;
   } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = c + e < d ? row[c + e] : pad;
+    for (int e = 0; e < E; ++e) x[e] = pad;
+    if (c < d) {
+      if constexpr (E * sizeof(T) == 16) {
+        if (d >= E) {
+          uint32_t fill;
+          if constexpr (sizeof(T) == 4)
+            fill = __builtin_bit_cast(uint32_t, pad);
+          else
+            fill = __builtin_bit_cast(uint16_t, pad) * 0x10001u;
+          const uint4 last = __builtin_bit_cast(uint4, *reinterpret_cast<const AnyVec<T, E>*>(row + d - E));
+          return __builtin_bit_cast(AnyVec<T, E>, words_down(last, (uint32_t)(c + E - d) * (uint32_t)sizeof(T), fill));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (c + e < d) x[e] = row[c + e];
+    }
   }
   return x;
 }
@@ -64,20 +93,50 @@ __device__ __forceinline__ void widen(const AnyVec<T, E>& x, float (&v)[E]) {
   for (int e = 0; e < E; ++e) v[e] = (float)x[e];
 }
 
-// The same elements rounded to T and stored, none past the end. The stores are streaming: what these
-// kernels write is not read again by them, and lines that go to HBM at once leave the L2s to what is
-// (131,072 embedded rows of 768 fp32: 116 -> 75 us; layer norm of 65,536: 80 -> 71).
+// The same elements as fp32.
+template <typename T, int E>
+__device__ __forceinline__ void load_piece(const T* __restrict__ row, int64_t c, int64_t d, float pad,
+                                           float (&v)[E]) {
+  widen<T, E>(fetch_piece<T, E>(row, c, d, (T)pad), v);
+}
+
+// The same elements rounded to T and stored, none past the end (a short piece in up to three stores).
+// The stores are streaming: what these kernels write is not read again by them, and lines that go to HBM
+// at once leave the L2s to what is (131,072 embedded rows of 768 fp32: 116 -> 75 us; layer norm of
+// 65,536: 80 -> 71).
 template <typename T, int E>
 __device__ __forceinline__ void store_piece(T* __restrict__ row, int64_t c, int64_t d, const float (&v)[E]) {
+  AnyVec<T, E> x;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = (T)v[e];
   if (c + E <= d) {
-    AnyVec<T, E> x;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = (T)v[e];
     __builtin_nontemporal_store(x, reinterpret_cast<AnyVec<T, E>*>(row + c));
-  } else {
+  } else if (c < d) {
+    if constexpr (E * sizeof(T) == 16) {
+      uint4 w = __builtin_bit_cast(uint4, x);
+      T* to = row + c;
+      const uint32_t bytes = (uint32_t)(d - c) * (uint32_t)sizeof(T);
+      if (bytes & 8) {
+        using Half = AnyVec<T, 8 / (int)sizeof(T)>;
+        *reinterpret_cast<Half*>(to) = __builtin_bit_cast(Half, uint2{w.x, w.y});
+        to += 8 / sizeof(T);
+        w = words_down(w, 8, 0);
+      }
+      if constexpr (sizeof(T) == 4) {
+        if (bytes & 4) *to = __builtin_bit_cast(T, w.x);
+      } else {
+        if (bytes & 4) {
+          *reinterpret_cast<AnyVec<T, 2>*>(to) = __builtin_bit_cast(AnyVec<T, 2>, w.x);
+          to += 2;
+          w = words_down(w, 4, 0);
+        }
+        if (bytes & 2) *to = __builtin_bit_cast(T, (uint16_t)w.x);
+      }
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (c + e < d) row[c + e] = (T)v[e];
+      for (int e = 0; e < E; ++e)
+        if (c + e < d) row[c + e] = x[e];
+    }
   }
 }
 
