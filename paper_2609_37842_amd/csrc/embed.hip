@@ -18,34 +18,36 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
   constexpr int E = kPiece<TT>;
   const int lane = threadIdx.x & 63;
   const int64_t units = n * col_units;
-  for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
+  for (int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units;
+       u += (int64_t)gridDim.x * 4) {
     const int64_t row = u / col_units, c0 = (u % col_units) * (64 * P * E);
     const bool live = !mask || mask[row] != 0;
     const int64_t tok = live ? tokens[row] : 0;
     const bool inside = tok >= 0 && tok < V;
     const TT* src = table + (live && inside ? tok : 0) * ldt;
     TO* dst = out + row * ldo;
-    float v[P][E];
+    AnyVec<TT, E> raw[P];
+    if (live && inside) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int64_t c = c0 + (int64_t)(p * 64 + lane) * E;
-      if (live && inside) {
-        load_piece<TT, E>(src, c, d, 0.f, v[p]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[p][e] = live ? __builtin_nanf("") : 0.f;
-      }
+      for (int p = 0; p < P; ++p) raw[p] = request_piece<TT, E>(src, c0 + (int64_t)(p * 64 + lane) * E, d);
     }
     if (!live && accumulate) continue;         // nothing to add
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = c0 + (int64_t)(p * 64 + lane) * E;
       if (c >= d) break;
-      float old[E] = {};
+      float v[E], old[E] = {};
+      if (live && inside) {
+        settle_piece<TT, E>(raw[p], c, d);
+        widen<TT, E>(raw[p], v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = live ? __builtin_nanf("") : 0.f;
+      }
       if (accumulate) load_piece<TO, E>(dst, c, d, 0.f, old);
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[p][e] = accumulate ? old[e] + v[p][e] * scale : v[p][e] * scale;
-      store_piece<TO, E>(dst, c, d, v[p]);
+      for (int e = 0; e < E; ++e) v[e] = accumulate ? old[e] + v[e] * scale : v[e] * scale;
+      store_piece<TO, E>(dst, c, d, v);
     }
   }
 }
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
                                                    uint32_t* __restrict__ listed, uint32_t* __restrict__ list) {
   constexpr int E = kPiece<T>, U = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t chunk = unit / col_units, p0 = chunk * CHUNK;
   if (p0 >= n) return;
   const int64_t c = (unit % col_units * 64 + lane) * E;
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
     for (int u = 0; u < U; ++u) {
       const int j = std::min(i + u, count - 1);
       const uint32_t k = __builtin_amdgcn_readlane(mykey, j), r = __builtin_amdgcn_readlane(myrow, j);
-      if (k < V) v[u] = fetch_piece<T, E, true>(dout + (int64_t)r * ldd, c, d, (T)0.f);
+      if (k < V) v[u] = request_piece<T, E, true>(dout + (int64_t)r * ldd, c, d);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -302,6 +304,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
       }
       if (k >= V) return;                      // the rows that count for no token are last
+      settle_piece<T, E>(v[u], c, d);
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += (float)v[u][e];
     }

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
   constexpr int kRows = NT / 64 / WPR;                 // of a block at once
   extern __shared__ __align__(16) float weights[];     // gamma, beta: round_up(d, E) each
   __shared__ float slot[2][16];
-  const int wid = threadIdx.x >> 6;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (rows and their addresses are scalar)
   const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;   // place among the row's lanes
   float *g = weights, *b = weights + (d + E - 1) / E * E;
   const float width = (float)d;               // sums are divided by it: a constant row's mean is exact
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
   auto load = [&](int64_t row) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      raw[p] = fetch_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d, (TI)0.f);
+      raw[p] = request_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d);
   };
   int64_t row = queue.next(none);
   if (row >= 0) load(row);
@@ -119,6 +119,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
     float s = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
+      settle_piece<TI, E>(raw[p], (int64_t)(p * 64 * WPR + t) * E, d);
       widen<TI, E>(raw[p], v[p]);
 #pragma unroll
       for (int e = 0; e < E; ++e) s += v[p][e];
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
   extern __shared__ __align__(16) float weights[];     // gamma: round_up(d, E)
   __shared__ float slot[2][2][16];
   __shared__ float fold[WPR == 1 ? 3 * 64 * E : 1];
-  const int wid = threadIdx.x >> 6;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (rows and their addresses are scalar)
   const int t = WPR == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
   float ag[P][E], ab[P][E];
 #pragma unroll
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     for (int e = 0; e < E; ++e) ag[p][e] = ab[p][e] = 0.f;
   stage_weights<NT>(weights, gamma, wt, d, 1.f);
   __syncthreads();
-  const float width = (float)d;
+  const float inv_width = 1.f / (float)d;
   const int64_t group = blockIdx.x / splits, split = blockIdx.x % splits;
   const int64_t row0 = group * rows_per_group;
   RowQueue<3> queue(mask ? mask + row0 : nullptr, mean_in + row0, rstd_in + row0,
@@ -208,13 +209,13 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      in.x[p] = fetch_piece<T, E, true>(x + row * ldx, c, d, (T)0.f);
-      in.dy[p] = fetch_piece<T, E, true>(dy + row * lddy, c, d, (T)0.f);   // (0 past the end: no sum sees x there)
+      in.x[p] = request_piece<T, E, true>(x + row * ldx, c, d);
+      in.dy[p] = request_piece<T, E, true>(dy + row * lddy, c, d);
     }
     if (res) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        in.res[p] = fetch_piece<T, E, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d, (T)0.f);
+        in.res[p] = request_piece<T, E, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d);
     }
   };
   int turn = 0;
@@ -237,6 +238,9 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * 64 * WPR + t) * E;
+      settle_piece<T, E>(now.x[p], c, d);
+      settle_piece<T, E>(now.dy[p], c, d);             // (0 past the end: no sum sees x there)
+      if (res) settle_piece<T, E>(now.res[p], c, d);
       AnyVec<float, E> gp;
       if (c < d) gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
 #pragma unroll
@@ -268,8 +272,8 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
         s2 += q[16 + w];
       }
     }
-    s1 /= width;
-    s2 /= width;
+    s1 *= inv_width;
+    s2 *= inv_width;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;

@@ -87,6 +87,29 @@ __device__ __forceinline__ AnyVec<T, E> fetch_piece(const T* __restrict__ row, i
   return x;
 }
 
+// The same in two steps, for several pieces at once: whole unconditional loads (a piece that would pass
+// the end is taken E elements before it), then what such lanes hold put right. With the two in one step
+// a wave that has such lanes waits for each load before it requests the next: the lanes' other value
+// goes to the registers that the load is about to fill.
+template <typename T, int E, bool STREAM = false>
+__device__ __forceinline__ AnyVec<T, E> request_piece(const T* __restrict__ row, int64_t c, int64_t d) {
+  static_assert(E * sizeof(T) == 16, "one piece");
+  if (d < E) return fetch_piece<T, E>(row, c, d, (T)0.f);      // (uniform)
+  const auto* p = reinterpret_cast<const AnyVec<T, E>*>(row + (c < d - E ? c : d - E));
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  return *p;
+}
+
+// Zero past the row's end.
+template <typename T, int E>
+__device__ __forceinline__ void settle_piece(AnyVec<T, E>& x, int64_t c, int64_t d) {
+  if (c + E > d && d >= E) {
+    const uint4 w = __builtin_bit_cast(uint4, x);
+    x = __builtin_bit_cast(AnyVec<T, E>, c < d ? words_down(w, (uint32_t)(c + E - d) * (uint32_t)sizeof(T), 0)
+                                               : uint4{0, 0, 0, 0});
+  }
+}
+
 template <typename T, int E>
 __device__ __forceinline__ void widen(const AnyVec<T, E>& x, float (&v)[E]) {
 #pragma unroll
