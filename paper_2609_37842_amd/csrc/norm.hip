@@ -71,11 +71,18 @@ struct RowQueue {
 
 constexpr int norm_threads(int wpr) { return wpr > 4 ? 64 * wpr : 256; }
 
+// Blocks of the forward pass on a CU, by its registers (elements of a lane).
+constexpr int norm_per_cu(int wpr, int elements) {
+  if (wpr > 4) return elements <= 8 ? 2 : 1;
+  return elements <= 8 ? 8 : elements <= 12 ? 7 : elements <= 16 ? 6 : 4;
+}
+
 // y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
 // bytes per lane), so mean and the centred second moment are two exact passes over registers and
 // HBM sees one read and one write.
 template <typename TI, typename TO, int WPR, int P>
-__global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm(
+__global__ __launch_bounds__(norm_threads(WPR), norm_per_cu(WPR, P * kPiece<TI>) * norm_threads(WPR) / 256)
+void k_layer_norm(
     const TI* __restrict__ x, int64_t ldx, const void* __restrict__ gamma, const void* __restrict__ beta,
     eogp_dtype wt, float eps, const uint8_t* __restrict__ mask, int64_t n, int64_t d, TO* __restrict__ y,
     int64_t ldy, int ones, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
@@ -199,7 +206,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
   };
   // Rows ahead of their turn where two fit the registers (else the block's other waves and the CU's
   // other blocks have theirs on the way).
-  constexpr bool kAhead = WPR <= 4 && P * E <= 16;
+  constexpr bool kAhead = P * E <= (WPR <= 4 ? 16 : 8);
   struct Inputs {
     AnyVec<T, E> x[P], dy[P], res[P];
   };
@@ -361,21 +368,28 @@ __global__ __launch_bounds__(32 * SLICES) void k_norm_fold(const float* __restri
   }
 }
 
-// Waves per row and pieces per lane for a row of `pieces` 16-byte pieces: one wave while four
-// pieces a lane hold the row, then four waves, then sixteen.
-template <typename T, typename F>
+// Waves per row and pieces per lane for a row of `pieces` 16-byte pieces: one wave while four pieces a
+// lane hold the row (no barrier per row), then four waves, then sixteen. The backward pass goes over to
+// sixteen waves at 512 pieces, the forward pass at 768: its three rows and two sums take a lane of three
+// pieces too many registers, and blocks of many waves leave fewer partial sums (3,906 rows of 5120
+// bf16 47 us, with four waves and three pieces 63; 18,310 of 8192 212 us, with four pieces 326).
+template <typename T, bool BACK, typename F>
 eogp_status with_shape(int64_t pieces, F&& f) {
   using std::integral_constant;
-  if (pieces <= 64) return f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  if (pieces <= 128) return f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-  if (pieces <= 192) return f(integral_constant<int, 1>{}, integral_constant<int, 3>{});
-  if (pieces <= 256) return f(integral_constant<int, 1>{}, integral_constant<int, 4>{});
-  if (pieces <= 512) return f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  if (pieces <= 768) return f(integral_constant<int, 4>{}, integral_constant<int, 3>{});
-  if (pieces <= 1024) return f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  using One = integral_constant<int, 1>;
+  using Four = integral_constant<int, 4>;
+  using Sixteen = integral_constant<int, 16>;
+  if (pieces <= 64) return f(One{}, integral_constant<int, 1>{});
+  if (pieces <= 128) return f(One{}, integral_constant<int, 2>{});
+  if (pieces <= 192) return f(One{}, integral_constant<int, 3>{});
+  if (pieces <= 256) return f(One{}, integral_constant<int, 4>{});
+  if (pieces <= 512) return f(Four{}, integral_constant<int, 2>{});
+  if constexpr (!BACK)
+    if (pieces <= 768) return f(Four{}, integral_constant<int, 3>{});
+  if (pieces <= 1024) return f(Sixteen{}, integral_constant<int, 1>{});
   if constexpr (sizeof(T) == 4)              // (16-bit rows of up to 16,384 elements have 2,048 pieces)
-    if (pieces > 2048) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-  return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    if (pieces > 2048) return f(Sixteen{}, integral_constant<int, 4>{});
+  return f(Sixteen{}, integral_constant<int, 2>{});
 }
 
 int rows_per_block(int64_t pieces) { return pieces <= 256 ? 4 : 1; }
@@ -400,11 +414,14 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
     using TI = decltype(ti);
     auto go = [&](auto to) {
       using TO = decltype(to);
-      return with_shape<TI>(pieces, [&](auto wpr, auto p) {
+      return with_shape<TI, false>(pieces, [&](auto wpr, auto p) {
         constexpr int W = decltype(wpr)::value;
-        const int64_t blocks = std::min<int64_t>(ceil_div(n, rows_per_block(pieces)), W > 4 ? 512 : 2048);
         auto* kfn = k_layer_norm<TI, TO, W, decltype(p)::value>;
         const int lds = 2 * (int)weight_bytes(d, xt);
+        // no more blocks than are there at once: rows are dealt out to them, and each reads the weights
+        const int64_t per_cu = std::min<int64_t>(norm_per_cu(W, decltype(p)::value * kPiece<TI>),
+                                                 std::max<int64_t>(1, (160 << 10) / (lds + 256)));
+        const int64_t blocks = std::min<int64_t>(ceil_div(n, rows_per_block(pieces)), per_cu * kCus);
         if (lds > kStaticLds) {
           const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);
           if (st != EOGP_OK) return st;
@@ -420,12 +437,12 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
 }
 
 namespace {
-// Blocks of a group: enough to fill the chip four times over, no more than its rows need; one for so
+// Blocks of a group: as many as are there at once, no more than its rows need; one for so
 // few rows that a second launch would cost more than their turns.
 int back_splits(int64_t groups, int64_t rows, int64_t pieces) {
   if (rows <= 4 * rows_per_block(pieces)) return 1;
   const int64_t most = ceil_div(rows, rows_per_block(pieces));
-  const int64_t want = ceil_div(pieces <= 1024 ? 4 * kCus : 2 * kCus, groups);
+  const int64_t want = ceil_div(pieces <= 512 ? 4 * kCus : kCus, groups);
   return (int)std::max<int64_t>(1, std::min(most, want));
 }
 }  // namespace
@@ -446,7 +463,7 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
   timing::Scope ts(EOGP_KT_LAYER_NORM, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
-    return with_shape<T>(pieces, [&](auto wpr, auto p) {
+    return with_shape<T, true>(pieces, [&](auto wpr, auto p) {
       constexpr int W = decltype(wpr)::value, P = decltype(p)::value;
       auto* kfn = k_layer_norm_back<T, W, P>;
       const int lds = (int)weight_bytes(d, t);
