@@ -9,13 +9,14 @@ namespace {
 
 // One wave per row and 64 P pieces of it; a lane's P pieces are requested together. A token
 // outside [0, V) gives NaN, a masked row zeros (neither reads the table).
-template <typename TT, typename TO, int P>
+template <typename TT, typename TO, int SHAPE>
 __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int64_t ldt, int64_t V, int64_t d,
                                                const int64_t* __restrict__ tokens,
                                                const uint8_t* __restrict__ mask, int64_t n, float scale,
                                                int accumulate, TO* __restrict__ out, int64_t ldo,
                                                int64_t col_units) {
-  constexpr int E = kPiece<TT>;
+  constexpr int E = kPiece<TT>, P = SHAPE ? SHAPE : 1;      // SHAPE 0: rows shorter than a piece
+  constexpr bool kNarrow = SHAPE == 0;
   const int lane = threadIdx.x & 63;
   const int64_t units = n * col_units;
   for (int64_t u = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units;
@@ -29,7 +30,7 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
     AnyVec<TT, E> raw[P];
     if (live && inside) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) raw[p] = request_piece<TT, E>(src, c0 + (int64_t)(p * 64 + lane) * E, d);
+      for (int p = 0; p < P; ++p) raw[p] = request_piece<TT, E, kNarrow>(src, c0 + (int64_t)(p * 64 + lane) * E, d);
     }
     if (!live && accumulate) continue;         // nothing to add
 #pragma unroll
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
       if (c >= d) break;
       float v[E], old[E] = {};
       if (live && inside) {
-        settle_piece<TT, E>(raw[p], c, d);
+        settle_piece<TT, E, kNarrow>(raw[p], c, d);
         widen<TT, E>(raw[p], v);
       } else {
 #pragma unroll
@@ -65,14 +66,13 @@ __device__ __forceinline__ uint32_t token_key(const int64_t* tokens, const uint8
   return t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;
 }
 
-// Zeros `words` words of flags and one counter.
-__global__ __launch_bounds__(256) void k_clear(uint32_t* __restrict__ flags, int64_t words, uint32_t* __restrict__ counter) {
+// Zeros `words` words of flags.
+__global__ __launch_bounds__(256) void k_clear(uint32_t* __restrict__ flags, int64_t words) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) flags[i] = 0;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0;
 }
 
-// Zeros rows row0 .. row1 - 1 of the table but for flagged ones (their sums are written later). Plain
-// stores: nothing else is in the L2s' way (154 MB: 25 us, 29 with streaming stores).
+// Zeros rows row0 .. row1 - 1 of the table but for flagged ones (their sums are written later). Streaming
+// stores: call after call, 154 MB of zeros and 512 rows take 38 us so, 42 with plain ones.
 __device__ void fill_zero(float* __restrict__ dtable, int64_t ldt, int64_t d, const uint8_t* __restrict__ flags,
                           int64_t block, int64_t blocks, int64_t row0, int64_t row1) {
   const int lane = threadIdx.x & 63;
@@ -80,7 +80,8 @@ __device__ void fill_zero(float* __restrict__ dtable, int64_t ldt, int64_t d, co
   for (int64_t r = row0 + block * 4 + (threadIdx.x >> 6); r < row1; r += blocks * 4) {
     if (flags && flags[r]) continue;
     float* row = dtable + r * ldt;
-    for (int64_t c = 4 * lane; c + 4 <= d; c += 256) *reinterpret_cast<AnyVec<float, 4>*>(row + c) = z;
+    for (int64_t c = 4 * lane; c + 4 <= d; c += 256)
+      __builtin_nontemporal_store(z, reinterpret_cast<AnyVec<float, 4>*>(row + c));
     if (lane < (d & 3)) row[(d & ~(int64_t)3) + lane] = 0.f;
   }
 }
@@ -176,11 +177,25 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
   __syncthreads();
   // at[w][dig]: the first place of wave w's rows with this digit. Exclusive sum over the digits'
   // totals (each thread holds nd / 256 or fewer neighbouring digits), plus earlier tiles and waves.
+  // Without `totals` the counts are as k_sort_count left them, and the block sums the tiles itself.
   const int per = nd > 256 ? nd / 256 : 1;
-  uint32_t mine = 0, tot[2] = {0, 0};
+  uint32_t mine = 0, tot[2] = {0, 0}, earlier[2] = {0, 0};
   const int d0 = threadIdx.x * per;
   for (int k = 0; k < per; ++k)
-    if (d0 + k < nd) mine += tot[k] = totals[d0 + k];
+    if (d0 + k < nd) {
+      const uint32_t* h = hist + (int64_t)(d0 + k) * tiles;
+      if (totals) {
+        tot[k] = totals[d0 + k];
+        earlier[k] = h[blockIdx.x];
+      } else {
+        for (int64_t j = 0; j < tiles; ++j) {
+          const uint32_t c = h[j];
+          tot[k] += c;
+          earlier[k] += j < blockIdx.x ? c : 0;
+        }
+      }
+      mine += tot[k];
+    }
   uint32_t incl = mine;
   for (int off = 1; off < 64; off <<= 1) {
     const uint32_t o = __shfl_up(incl, off);
@@ -192,7 +207,7 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
   for (int w = 0; w < wid; ++w) first += wave_total[w];
   for (int k = 0; k < per; ++k)
     if (d0 + k < nd) {
-      uint32_t run = first + hist[(int64_t)(d0 + k) * tiles + blockIdx.x];
+      uint32_t run = first + earlier[k];
       for (int w = 0; w < kSortWaves; ++w) {
         const uint32_t c = at[w][d0 + k];
         at[w][d0 + k] = run;
@@ -213,18 +228,16 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
 // Few rows: each one's place is the number of rows before it, found by comparing it with all of them
 // (a quarter of them per thread); one launch instead of the radix sort's six. Blocks beside them write
 // the table's zeros.
-constexpr int kFew = 8192;
+constexpr int kFew = 2048;
 
 __global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens, const uint8_t* __restrict__ mask,
                                               int64_t V, int n, uint32_t* __restrict__ keys_out,
-                                              uint32_t* __restrict__ rows_out, uint32_t* __restrict__ counter,
-                                              int rank_blocks, float* __restrict__ dtable, int64_t ldt, int64_t d) {
+                                              uint32_t* __restrict__ rows_out, int rank_blocks, float* __restrict__ dtable, int64_t ldt, int64_t d) {
   __shared__ __align__(16) uint32_t key[kFew];
   if ((int)blockIdx.x >= rank_blocks) {
     fill_zero(dtable, ldt, d, nullptr, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, 0, V);
     return;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *counter = 0;
   for (int i = threadIdx.x; i < (n + 15) / 16 * 16; i += 256) key[i] = i < n ? token_key(tokens, mask, i, V) : 0xFFFFFFFFu;
   __syncthreads();
   const int i = blockIdx.x * 64 + (threadIdx.x >> 2), part = threadIdx.x & 3;
@@ -247,15 +260,15 @@ __global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens
 // A wave sums the rows of a chunk of CHUNK sorted places, for 64 pieces of their columns, eight rows in
 // flight, token by token. A token whose rows all lie in the chunk is finished here; the sum of one
 // that goes on beyond an end of the chunk is written to part[chunk][0] (it began in an earlier
-// chunk) or part[chunk][1] (it begins here and goes on), and k_embed_join adds those in order: the
-// chunks where such tokens begin are listed for it.
-template <typename T, int CHUNK>
+// chunk) or part[chunk][1] (it begins here and goes on: begins[chunk]), and k_embed_join adds those in
+// order.
+template <typename T, int CHUNK, bool NARROW>
 __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, int64_t ldd, int64_t d,
                                                    const uint32_t* __restrict__ keys,
                                                    const uint32_t* __restrict__ rows, int64_t n, uint32_t V,
                                                    float scale, int accumulate, float* __restrict__ dtable,
                                                    int64_t ldt, float* __restrict__ part, int64_t col_units,
-                                                   uint32_t* __restrict__ listed, uint32_t* __restrict__ list) {
+                                                   uint8_t* __restrict__ begins) {
   constexpr int E = kPiece<T>, U = 8;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -269,9 +282,13 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
   const uint32_t before = p0 > 0 ? keys[p0 - 1] : V, after = p0 + count < n ? keys[p0 + count] : V;
   float acc[E] = {};
   uint32_t cur = __builtin_amdgcn_readlane(mykey, 0);
+  const uint32_t row0 = __builtin_amdgcn_readlane(myrow, 0);
+  if (cur >= V) {                              // the rows that count for no token are last
+    if (unit % col_units == 0 && lane == 0) begins[chunk] = 0;
+    return;
+  }
   bool from_before = cur == before;
   auto flush = [&](bool goes_on) {
-    if (goes_on && !from_before && unit % col_units == 0 && lane == 0) list[atomicAdd(listed, 1u)] = (uint32_t)chunk;
     if (c >= d) return;
     if (from_before || goes_on) {
       store_piece<float, E>(part + (chunk * 2 + (from_before ? 0 : 1)) * d, c, d, acc);
@@ -290,7 +307,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
     for (int u = 0; u < U; ++u) {
       const int j = std::min(i + u, count - 1);
       const uint32_t k = __builtin_amdgcn_readlane(mykey, j), r = __builtin_amdgcn_readlane(myrow, j);
-      if (k < V) v[u] = request_piece<T, E, true>(dout + (int64_t)r * ldd, c, d);
+      v[u] = request_piece<T, E, NARROW, true>(dout + (int64_t)(k < V ? r : row0) * ldd, c, d);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -303,39 +320,53 @@ __global__ __launch_bounds__(256) void k_embed_sum(const T* __restrict__ dout, i
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
       }
-      if (k >= V) return;                      // the rows that count for no token are last
-      settle_piece<T, E>(v[u], c, d);
+      if (k >= V) {                            // (the requests of such rows were the first row's again)
+        if (unit % col_units == 0 && lane == 0) begins[chunk] = 0;
+        return;
+      }
+      settle_piece<T, E, NARROW>(v[u], c, d);
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += (float)v[u][e];
     }
   }
+  if (unit % col_units == 0 && lane == 0) begins[chunk] = cur == after && !from_before;
   flush(cur == after);
 }
 
-// One block per listed chunk and 256 columns: the sums of the chunks of the token that begins there and
-// goes on are added, a quarter of them per wave, and its row is finished. Most such tokens span two or
-// three chunks, so a unit is a chain of waits and as many units as fit are wanted: for 196,000 rows of
-// 2048 with Zipf-distributed tokens 16 waves per block take 105 us, 4 waves with eight requests each
-// 36, with four (fewer registers) 25.
+// A block takes chunks in which a token begins that goes on, 256 columns at a time (a unit; the flags of
+// 64 units are read at once): the sums of that token's chunks are added, a quarter of them per wave, and
+// its row is finished. Most such tokens span two or three chunks, so a unit is a chain of waits and as
+// many units as fit are wanted: for 196,000 rows of 2048 with Zipf-distributed tokens 16 waves per block
+// take 105 us, 4 waves with eight requests each 36, with four (fewer registers) 25.
 template <int CHUNK>
 __global__ __launch_bounds__(256) void k_embed_join(const uint32_t* __restrict__ keys, int64_t n,
-                                                     const float* __restrict__ part, int64_t d, float scale,
-                                                     int accumulate, float* __restrict__ dtable, int64_t ldt,
-                                                     int64_t col_blocks, const uint32_t* __restrict__ listed,
-                                                     const uint32_t* __restrict__ list) {
+                                                    const float* __restrict__ part, int64_t d, float scale,
+                                                    int accumulate, float* __restrict__ dtable, int64_t ldt,
+                                                    int64_t col_blocks, const uint8_t* __restrict__ begins) {
   __shared__ float fold[4][256];
   const int wid = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t units = (int64_t)*listed * col_blocks;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t first = list[unit / col_blocks];
+  const int64_t units = (n + CHUNK - 1) / CHUNK * col_blocks;
+  uint64_t todo = 0;
+  int64_t base = blockIdx.x - 64 * (int64_t)gridDim.x;
+  for (;;) {
+    while (!todo) {                                    // (uniform across the block)
+      base += 64 * (int64_t)gridDim.x;
+      if (base >= units) return;
+      const int64_t u = base + lane * (int64_t)gridDim.x;
+      todo = __ballot(u < units && begins[u < units ? u / col_blocks : 0]);
+    }
+    const int64_t unit = base + __builtin_ctzll(todo) * (int64_t)gridDim.x;
+    todo &= todo - 1;
+    const int64_t first = unit / col_blocks;
     const uint32_t k = keys[(first + 1) * CHUNK - 1];
-    int64_t more = 0;                                  // chunks after the first that begin with its rows
-    for (;;) {
-      const int64_t at = (first + 1 + more + lane) * CHUNK;
-      const uint64_t same = __ballot(at < n && keys[at < n ? at : 0] == k);
-      const int run = ~same ? __builtin_ctzll(~same) : 64;
-      more += run;
-      if (run < 64) break;
+    // Chunks after the first that begin with its rows: 64 ends of equal parts are looked at at a time.
+    int64_t more = 0, end = (n + CHUNK - 1) / CHUNK - first - 1;
+    while (more < end) {
+      const int64_t part_len = (end - more + 63) / 64, at = more + (lane + 1) * part_len - 1;
+      const bool same = at < end && keys[(first + 1 + at) * CHUNK] == k;
+      more += __popcll(__ballot(same)) * part_len;
+      if (part_len == 1) break;
+      end = std::min(end, more + part_len - 1);
     }
     const int64_t c = unit % col_blocks * 256 + lane * 4;
     float acc[4] = {};
@@ -377,11 +408,21 @@ SortShape sort_shape(int64_t V) {
   return {passes, (b + passes - 1) / passes};
 }
 
-constexpr int kChunk = 64, kFewChunk = 8;    // sorted places per wave; few rows: one load's latency each
+constexpr int64_t kFlagBytes = 256 << 20;
+constexpr int64_t kTilesInline = 64;         // tiles whose counts a scatter block sums itself
+
+// Sorted places per wave: 64, fewer where those would leave most of the chip's waves without rows.
+constexpr int kChunk = 64, kShortChunk = 16, kFewChunk = 8;
+
+int chunk_of(int64_t n, int64_t d, eogp_dtype t) {
+  if (n <= kFew) return kFewChunk;
+  const int64_t waves = ceil_div(n, kChunk) * ceil_div(d, t == EOGP_F32 ? 256 : 512);
+  return waves >= 16 * kCus ? kChunk : kShortChunk;
+}
 
 struct BackWs {
-  uint32_t *keys[2], *rows[2], *hist, *totals, *listed, *list;
-  uint8_t* flags;
+  uint32_t *keys[2], *rows[2], *hist, *totals;
+  uint8_t *flags, *begins;
   float* part;
   size_t bytes;
 };
@@ -389,7 +430,7 @@ struct BackWs {
 BackWs carve_back(void* ws, int64_t n, int64_t V, int64_t d) {
   Carve cv(ws, ~(size_t)0);
   const bool few = n <= kFew;
-  const int64_t chunks = ceil_div(n, few ? kFewChunk : kChunk);
+  const int64_t chunks = ceil_div(n, chunk_of(n, d, EOGP_BF16));     // (no other type has more)
   BackWs w;
   for (int k = 0; k < (few ? 1 : 2); ++k) {
     w.keys[k] = cv.take<uint32_t>(n);
@@ -398,8 +439,7 @@ BackWs carve_back(void* ws, int64_t n, int64_t V, int64_t d) {
   w.hist = cv.take<uint32_t>(few ? 0 : (size_t)ceil_div(n, kTile) << kMaxDigit);
   w.totals = cv.take<uint32_t>(few ? 0 : 1 << kMaxDigit);
   w.flags = cv.take<uint8_t>(few ? 0 : round_up(V, 4));
-  w.listed = cv.take<uint32_t>(1);
-  w.list = cv.take<uint32_t>(chunks);
+  w.begins = cv.take<uint8_t>(chunks);
   w.part = cv.take<float>((size_t)chunks * 2 * d);
   w.bytes = cv.used;
   return w;
@@ -414,17 +454,17 @@ eogp_status sum_sorted(const BackWs& w, const uint32_t* keys, const uint32_t* ro
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
     const int64_t col_units = ceil_div(d, 64 * kPiece<T>);
-    hipLaunchKernelGGL((k_embed_sum<T, CHUNK>), dim3((unsigned)ceil_div(chunks * col_units, 4)), dim3(256), 0, s,
+    auto* kfn = d < kPiece<T> ? k_embed_sum<T, CHUNK, true> : k_embed_sum<T, CHUNK, false>;
+    hipLaunchKernelGGL(kfn, dim3((unsigned)ceil_div(chunks * col_units, 4)), dim3(256), 0, s,
                        static_cast<const T*>(dout), ldd, d, keys, rows, n, (uint32_t)V, scale, accumulate, dtable,
-                       ldt, w.part, col_units, w.listed, w.list);
+                       ldt, w.part, col_units, w.begins);
     EOGP_LAUNCH_CHECK("embed_backward (sums)");
     return EOGP_OK;
   });
   if (st != EOGP_OK || chunks == 1) return st;
   const int64_t col_blocks = ceil_div(d, 256);
   hipLaunchKernelGGL(k_embed_join<CHUNK>, dim3((unsigned)std::min<int64_t>((chunks - 1) * col_blocks, 8 * kCus)),
-                     dim3(256), 0, s, keys, n, w.part, d, scale, accumulate, dtable, ldt, col_blocks, w.listed,
-                     w.list);
+                     dim3(256), 0, s, keys, n, w.part, d, scale, accumulate, dtable, ldt, col_blocks, w.begins);
   EOGP_LAUNCH_CHECK("embed_backward (join)");
   return EOGP_OK;
 }
@@ -441,7 +481,7 @@ eogp_status embed_tokens(const void* table, eogp_dtype tt, int64_t ldt, int64_t 
     auto go = [&](auto to, auto pp) {
       using TO = decltype(to);
       constexpr int P = decltype(pp)::value;
-      const int64_t col_units = ceil_div(d, 64 * P * kPiece<TT>);
+      const int64_t col_units = ceil_div(d, 64 * std::max(P, 1) * kPiece<TT>);
       const int64_t blocks = std::min<int64_t>(ceil_div(n * col_units, 4), 8 * kCus * 4);
       hipLaunchKernelGGL((k_embed<TT, TO, P>), dim3((unsigned)blocks), dim3(256), 0, s,
                          static_cast<const TT*>(table), ldt, V, d, tokens, mask, n, scale, accumulate,
@@ -451,7 +491,8 @@ eogp_status embed_tokens(const void* table, eogp_dtype tt, int64_t ldt, int64_t 
     };
     auto pick = [&](auto to) {
       const int64_t pieces = ceil_div(d, kPiece<TT>);
-      return pieces <= 64    ? go(to, std::integral_constant<int, 1>{})
+      return d < kPiece<TT> ? go(to, std::integral_constant<int, 0>{})
+             : pieces <= 64  ? go(to, std::integral_constant<int, 1>{})
              : pieces <= 128 ? go(to, std::integral_constant<int, 2>{})
              : pieces <= 192 ? go(to, std::integral_constant<int, 3>{})
                              : go(to, std::integral_constant<int, 4>{});
@@ -472,32 +513,39 @@ eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_
     const int rank_blocks = (int)ceil_div(n, 64);
     if (rank_blocks + fill_blocks == 0) return EOGP_OK;
     hipLaunchKernelGGL(k_rank, dim3(rank_blocks + fill_blocks), dim3(256), 0, s, tokens, mask, V, (int)n, w.keys[0],
-                       w.rows[0], w.listed, rank_blocks, dtable, ldt, d);
+                       w.rows[0], rank_blocks, dtable, ldt, d);
     EOGP_LAUNCH_CHECK("embed_backward (ranks)");
     if (n == 0) return EOGP_OK;
     return sum_sorted<kFewChunk>(w, w.keys[0], w.rows[0], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
   }
-  const int64_t tiles = ceil_div(n, kTile), words = accumulate ? 0 : round_up(V, 4) / 4;
+  const int64_t tiles = ceil_div(n, kTile);
   const SortShape sh = sort_shape(V);
-  hipLaunchKernelGGL(k_clear, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(words, 256), kCus))),
-                     dim3(256), 0, s, reinterpret_cast<uint32_t*>(w.flags), words, w.listed);
-  EOGP_LAUNCH_CHECK("embed_backward (flags)");
+  // Zeros of a table of up to 256 MB cost less beside the sort than knowing which rows need none.
+  const bool flagged = !accumulate && V * d * (int64_t)sizeof(float) > kFlagBytes;
+  if (flagged) {
+    const int64_t words = round_up(V, 4) / 4;
+    hipLaunchKernelGGL(k_clear, dim3((unsigned)std::min<int64_t>(ceil_div(words, 256), kCus)), dim3(256), 0, s,
+                       reinterpret_cast<uint32_t*>(w.flags), words);
+    EOGP_LAUNCH_CHECK("embed_backward (flags)");
+  }
+  const bool scan = tiles > kTilesInline;
   for (int p = 0; p < sh.passes; ++p) {
     const int shift = p * sh.bits;
     const uint32_t *ki = w.keys[(p + 1) & 1], *ri = w.rows[(p + 1) & 1];
     auto* count = p == 0 ? k_sort_count<true> : k_sort_count<false>;
     auto* scatter = p == 0 ? k_sort_scatter<true> : k_sort_scatter<false>;
     hipLaunchKernelGGL(count, dim3((unsigned)tiles), dim3(256), 0, s, tokens, mask, V, ki, n, shift, sh.bits, w.hist,
-                       tiles, accumulate ? nullptr : w.flags);
-    hipLaunchKernelGGL(k_sort_scan, dim3(1u << sh.bits), dim3(64), 0, s, w.hist, tiles, w.totals);
+                       tiles, flagged ? w.flags : nullptr);
+    if (scan) hipLaunchKernelGGL(k_sort_scan, dim3(1u << sh.bits), dim3(64), 0, s, w.hist, tiles, w.totals);
     // an equal share of the table's zeros beside each pass
     hipLaunchKernelGGL(scatter, dim3((unsigned)tiles + fill_blocks), dim3(256), 0, s, tokens, mask, V, ki, ri, n,
-                       shift, sh.bits, w.hist, tiles, w.totals, w.keys[p & 1], w.rows[p & 1], dtable, ldt, d, w.flags,
-                       V * p / sh.passes, V * (p + 1) / sh.passes);
+                       shift, sh.bits, w.hist, tiles, scan ? w.totals : nullptr, w.keys[p & 1], w.rows[p & 1], dtable,
+                       ldt, d, flagged ? w.flags : nullptr, V * p / sh.passes, V * (p + 1) / sh.passes);
     EOGP_LAUNCH_CHECK("embed_backward (sort)");
   }
   const int last = (sh.passes - 1) & 1;
-  return sum_sorted<kChunk>(w, w.keys[last], w.rows[last], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
+  const auto sum = chunk_of(n, d, t) == kChunk ? sum_sorted<kChunk> : sum_sorted<kShortChunk>;
+  return sum(w, w.keys[last], w.rows[last], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
 }
 
 }  // namespace eogp

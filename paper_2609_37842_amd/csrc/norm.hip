@@ -80,13 +80,14 @@ constexpr int norm_per_cu(int wpr, int elements) {
 // y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
 // bytes per lane), so mean and the centred second moment are two exact passes over registers and
 // HBM sees one read and one write.
-template <typename TI, typename TO, int WPR, int P>
-__global__ __launch_bounds__(norm_threads(WPR), norm_per_cu(WPR, P * kPiece<TI>) * norm_threads(WPR) / 256)
+template <typename TI, typename TO, int WPR, int SHAPE>
+__global__ __launch_bounds__(norm_threads(WPR), norm_per_cu(WPR, SHAPE * kPiece<TI>) * norm_threads(WPR) / 256)
 void k_layer_norm(
     const TI* __restrict__ x, int64_t ldx, const void* __restrict__ gamma, const void* __restrict__ beta,
     eogp_dtype wt, float eps, const uint8_t* __restrict__ mask, int64_t n, int64_t d, TO* __restrict__ y,
     int64_t ldy, int ones, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
-  constexpr int E = kPiece<TI>, NT = norm_threads(WPR);
+  constexpr int E = kPiece<TI>, NT = norm_threads(WPR), P = SHAPE ? SHAPE : 1;
+  constexpr bool kNarrow = SHAPE == 0;
   constexpr int kRows = NT / 64 / WPR;                 // of a block at once
   extern __shared__ __align__(16) float weights[];     // gamma, beta: round_up(d, E) each
   __shared__ float slot[2][16];
@@ -114,7 +115,7 @@ void k_layer_norm(
   auto load = [&](int64_t row) {
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      raw[p] = request_piece<TI, E>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d);
+      raw[p] = request_piece<TI, E, kNarrow>(x + row * ldx, (int64_t)(p * 64 * WPR + t) * E, d);
   };
   int64_t row = queue.next(none);
   if (row >= 0) load(row);
@@ -126,7 +127,7 @@ void k_layer_norm(
     float s = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      settle_piece<TI, E>(raw[p], (int64_t)(p * 64 * WPR + t) * E, d);
+      settle_piece<TI, E, kNarrow>(raw[p], (int64_t)(p * 64 * WPR + t) * E, d);
       widen<TI, E>(raw[p], v[p]);
 #pragma unroll
       for (int e = 0; e < E; ++e) s += v[p][e];
@@ -170,14 +171,15 @@ void k_layer_norm(
 // (times the rows a block holds at once) and writes its sums to part[k][j][2][d]. A row's three
 // inputs are requested together and stay as read (16-bit rows in half the registers); xh and t are
 // formed twice, once for the sums and once for dx.
-template <typename T, int WPR, int P>
+template <typename T, int WPR, int SHAPE>
 __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,
     const void* __restrict__ gamma, eogp_dtype wt, const float* __restrict__ mean_in,
     const float* __restrict__ rstd_in, const uint8_t* __restrict__ mask, const T* res,
     int64_t ldres, int64_t rows_per_group, int64_t d, int splits, T* dx, int64_t lddx,
     float* __restrict__ part, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  constexpr int E = kPiece<T>, NT = norm_threads(WPR);
+  constexpr int E = kPiece<T>, NT = norm_threads(WPR), P = SHAPE ? SHAPE : 1;
+  constexpr bool kNarrow = SHAPE == 0;
   constexpr int kRows = NT / 64 / WPR;
   extern __shared__ __align__(16) float weights[];     // gamma: round_up(d, E)
   __shared__ float slot[2][2][16];
@@ -216,13 +218,13 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int64_t c = (int64_t)(p * 64 * WPR + t) * E;
-      in.x[p] = request_piece<T, E, true>(x + row * ldx, c, d);
-      in.dy[p] = request_piece<T, E, true>(dy + row * lddy, c, d);
+      in.x[p] = request_piece<T, E, kNarrow, true>(x + row * ldx, c, d);
+      in.dy[p] = request_piece<T, E, kNarrow, true>(dy + row * lddy, c, d);
     }
     if (res) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
-        in.res[p] = request_piece<T, E, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d);
+        in.res[p] = request_piece<T, E, kNarrow, true>(res + row * ldres, (int64_t)(p * 64 * WPR + t) * E, d);
     }
   };
   int turn = 0;
@@ -245,9 +247,9 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * 64 * WPR + t) * E;
-      settle_piece<T, E>(now.x[p], c, d);
-      settle_piece<T, E>(now.dy[p], c, d);             // (0 past the end: no sum sees x there)
-      if (res) settle_piece<T, E>(now.res[p], c, d);
+      settle_piece<T, E, kNarrow>(now.x[p], c, d);
+      settle_piece<T, E, kNarrow>(now.dy[p], c, d);             // (0 past the end: no sum sees x there)
+      if (res) settle_piece<T, E, kNarrow>(now.res[p], c, d);
       AnyVec<float, E> gp;
       if (c < d) gp = *reinterpret_cast<const AlignedVec<float, E>*>(weights + c);
 #pragma unroll
@@ -368,17 +370,19 @@ __global__ __launch_bounds__(32 * SLICES) void k_norm_fold(const float* __restri
   }
 }
 
-// Waves per row and pieces per lane for a row of `pieces` 16-byte pieces: one wave while four pieces a
+// Waves per row and 16-byte pieces per lane (0: a row is shorter than a piece) for rows of d: one wave while four pieces a
 // lane hold the row (no barrier per row), then four waves, then sixteen. The backward pass goes over to
 // sixteen waves at 512 pieces, the forward pass at 768: its three rows and two sums take a lane of three
 // pieces too many registers, and blocks of many waves leave fewer partial sums (3,906 rows of 5120
 // bf16 47 us, with four waves and three pieces 63; 18,310 of 8192 212 us, with four pieces 326).
 template <typename T, bool BACK, typename F>
-eogp_status with_shape(int64_t pieces, F&& f) {
+eogp_status with_shape(int64_t d, F&& f) {
   using std::integral_constant;
   using One = integral_constant<int, 1>;
   using Four = integral_constant<int, 4>;
   using Sixteen = integral_constant<int, 16>;
+  const int64_t pieces = ceil_div(d, kPiece<T>);
+  if (d < kPiece<T>) return f(One{}, integral_constant<int, 0>{});
   if (pieces <= 64) return f(One{}, integral_constant<int, 1>{});
   if (pieces <= 128) return f(One{}, integral_constant<int, 2>{});
   if (pieces <= 192) return f(One{}, integral_constant<int, 3>{});
@@ -414,7 +418,7 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
     using TI = decltype(ti);
     auto go = [&](auto to) {
       using TO = decltype(to);
-      return with_shape<TI, false>(pieces, [&](auto wpr, auto p) {
+      return with_shape<TI, false>(d, [&](auto wpr, auto p) {
         constexpr int W = decltype(wpr)::value;
         auto* kfn = k_layer_norm<TI, TO, W, decltype(p)::value>;
         const int lds = 2 * (int)weight_bytes(d, xt);
@@ -463,9 +467,9 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
   timing::Scope ts(EOGP_KT_LAYER_NORM, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
-    return with_shape<T, true>(pieces, [&](auto wpr, auto p) {
-      constexpr int W = decltype(wpr)::value, P = decltype(p)::value;
-      auto* kfn = k_layer_norm_back<T, W, P>;
+    return with_shape<T, true>(d, [&](auto wpr, auto p) {
+      constexpr int W = decltype(wpr)::value;
+      auto* kfn = k_layer_norm_back<T, W, decltype(p)::value>;
       const int lds = (int)weight_bytes(d, t);
       if (lds > kStaticLds) {
         const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);

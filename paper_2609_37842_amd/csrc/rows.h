@@ -90,23 +90,26 @@ __device__ __forceinline__ AnyVec<T, E> fetch_piece(const T* __restrict__ row, i
 // The same in two steps, for several pieces at once: whole unconditional loads (a piece that would pass
 // the end is taken E elements before it), then what such lanes hold put right. With the two in one step
 // a wave that has such lanes waits for each load before it requests the next: the lanes' other value
-// goes to the registers that the load is about to fill.
-template <typename T, int E, bool STREAM = false>
+// goes to the registers that the load is about to fill. NARROW: rows shorter than a piece, element by
+// element (an instance of its own: a branch beside the loads would make them wait as well).
+template <typename T, int E, bool NARROW, bool STREAM = false>
 __device__ __forceinline__ AnyVec<T, E> request_piece(const T* __restrict__ row, int64_t c, int64_t d) {
   static_assert(E * sizeof(T) == 16, "one piece");
-  if (d < E) return fetch_piece<T, E>(row, c, d, (T)0.f);      // (uniform)
+  if constexpr (NARROW) return fetch_piece<T, E>(row, c, d, (T)0.f);
   const auto* p = reinterpret_cast<const AnyVec<T, E>*>(row + (c < d - E ? c : d - E));
   if constexpr (STREAM) return __builtin_nontemporal_load(p);
   return *p;
 }
 
 // Zero past the row's end.
-template <typename T, int E>
+template <typename T, int E, bool NARROW>
 __device__ __forceinline__ void settle_piece(AnyVec<T, E>& x, int64_t c, int64_t d) {
-  if (c + E > d && d >= E) {
-    const uint4 w = __builtin_bit_cast(uint4, x);
-    x = __builtin_bit_cast(AnyVec<T, E>, c < d ? words_down(w, (uint32_t)(c + E - d) * (uint32_t)sizeof(T), 0)
-                                               : uint4{0, 0, 0, 0});
+  if constexpr (!NARROW) {
+    if (c + E > d) {
+      const uint4 w = __builtin_bit_cast(uint4, x);
+      x = __builtin_bit_cast(AnyVec<T, E>, c < d ? words_down(w, (uint32_t)(c + E - d) * (uint32_t)sizeof(T), 0)
+                                                 : uint4{0, 0, 0, 0});
+    }
   }
 }
 
@@ -414,6 +417,7 @@ inline eogp_status with_row_shape(int64_t width, F&& f) {
   if (width < kPiece<T>) return f(N256{}, integral_constant<int, 0>{});
   if (pieces <= 512) return f(N256{}, integral_constant<int, 2>{});
   if (pieces <= 1024) return f(N256{}, integral_constant<int, 4>{});
+  if (pieces <= 2048) return f(N256{}, integral_constant<int, 8>{});
   if (pieces <= 4096) return f(N1024{}, integral_constant<int, 4>{});
   if (pieces <= 8192) return f(N1024{}, integral_constant<int, 8>{});
   if (pieces <= 16384) return f(N1024{}, integral_constant<int, 16>{});
