@@ -23,10 +23,11 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
 }
 
 // A block's weights in LDS, fp32 (gamma 1 and beta 0 where there is none): as registers they would
-// cost the kernels half of their waves.
-template <int NT>
+// cost the kernels half of their waves. The places up to a whole piece of E hold zeros: what LDS held
+// before may be a NaN, and 0 times it would be one.
+template <int NT, int E>
 __device__ __forceinline__ void stage_weights(float* lds, const void* w, eogp_dtype wt, int64_t d, float none) {
-  for (int c = threadIdx.x; c < d; c += NT) lds[c] = w ? load_any(w, wt, c) : none;
+  for (int c = threadIdx.x; c < (d + E - 1) / E * E; c += NT) lds[c] = c >= d ? 0.f : w ? load_any(w, wt, c) : none;
 }
 
 // The valid rows among first, first + step, ... of a wave, in order. The masks (and the means
@@ -119,8 +120,8 @@ void k_layer_norm(
   };
   int64_t row = queue.next(none);
   if (row >= 0) load(row);
-  stage_weights<NT>(g, gamma, wt, d, 1.f);    // while the first row is on its way
-  stage_weights<NT>(b, beta, wt, d, 0.f);
+  stage_weights<NT, E>(g, gamma, wt, d, 1.f);    // while the first row is on its way
+  stage_weights<NT, E>(b, beta, wt, d, 0.f);
   __syncthreads();
   while (row >= 0) {
     float v[P][E];
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
   for (int p = 0; p < P; ++p)
 #pragma unroll
     for (int e = 0; e < E; ++e) ag[p][e] = ab[p][e] = 0.f;
-  stage_weights<NT>(weights, gamma, wt, d, 1.f);
+  stage_weights<NT, E>(weights, gamma, wt, d, 1.f);
   __syncthreads();
   const float inv_width = 1.f / (float)d;
   const int64_t group = blockIdx.x / splits, split = blockIdx.x % splits;
