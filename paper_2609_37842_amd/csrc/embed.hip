@@ -66,10 +66,27 @@ __global__ __launch_bounds__(256) void k_embed(const TT* __restrict__ table, int
 // result does not depend on any race.
 constexpr int kTile = 2048, kSortWaves = 4, kMaxDigit = 9;
 
-__device__ __forceinline__ uint32_t token_key(const int64_t* tokens, const uint8_t* mask, int64_t i, int64_t V) {
-  if (mask && mask[i] == 0) return (uint32_t)V;
-  const int64_t t = tokens[i];
-  return t >= 0 && t < V ? (uint32_t)t : (uint32_t)V;
+// Keys of rows i0, i0 + step, ..., all requested together (rows past the end read the last one): with a branch at
+// the mask each row would wait for its mask and then for its token.
+template <bool FIRST, int R>
+__device__ __forceinline__ void load_keys(const int64_t* tokens, const uint8_t* mask, int64_t V, const uint32_t* keys,
+                                          int64_t n, int64_t i0, int64_t step, uint32_t (&key)[R]) {
+  if constexpr (FIRST) {
+    const uint8_t* live = mask ? mask : reinterpret_cast<const uint8_t*>(tokens);   // (some byte that is there)
+    int64_t t[R];
+    uint8_t m[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t i = std::min<int64_t>(i0 + r * step, n - 1);
+      t[r] = tokens[i];
+      m[r] = live[i];
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) key[r] = (!mask || m[r]) && t[r] >= 0 && t[r] < V ? (uint32_t)t[r] : (uint32_t)V;
+  } else {
+#pragma unroll
+    for (int r = 0; r < R; ++r) key[r] = keys[std::min<int64_t>(i0 + r * step, n - 1)];
+  }
 }
 
 // Zeros `words` words of flags.
@@ -109,8 +126,12 @@ __global__ __launch_bounds__(256) void k_sort_count(const int64_t* __restrict__ 
   for (int b = threadIdx.x; b <= (int)dmask; b += 256) count[b] = 0;
   __syncthreads();
   const int64_t base = (int64_t)blockIdx.x * kTile;
-  for (int64_t i = base + threadIdx.x; i < std::min<int64_t>(base + kTile, n); i += 256) {
-    const uint32_t k = FIRST ? token_key(tokens, mask, i, V) : keys[i];
+  uint32_t key[kTile / 256];
+  load_keys<FIRST>(tokens, mask, V, keys, n, base + threadIdx.x, 256, key);
+#pragma unroll
+  for (int r = 0; r < kTile / 256; ++r) {
+    if (base + r * 256 + threadIdx.x >= n) break;
+    const uint32_t k = key[r];
     if (FIRST && flags && k < V) flags[k] = 1;         // (whoever writes it, it is 1)
     atomicAdd(&count[(k >> shift) & dmask], 1u);
   }
@@ -162,12 +183,11 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
   constexpr int R = kTile / 256;                        // rounds of 64 rows per wave
   const int64_t base = (int64_t)blockIdx.x * kTile + (int64_t)wid * R * 64;
   uint32_t key[R], row[R], rank[R];
+  load_keys<FIRST>(tokens, mask, V, keys, n, base + lane, 64, key);
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int64_t i = base + r * 64 + lane;
-    const bool in = i < n;
-    key[r] = !in ? 0u : FIRST ? token_key(tokens, mask, i, V) : keys[i];
-    row[r] = !in ? 0u : FIRST ? (uint32_t)i : rows[i];
+    const int64_t i = std::min<int64_t>(base + r * 64 + lane, n - 1);
+    row[r] = FIRST ? (uint32_t)i : rows[i];
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -199,10 +219,16 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
         tot[k] = totals[d0 + k];
         earlier[k] = h[blockIdx.x];
       } else {
-        for (int64_t j = 0; j < tiles; ++j) {
-          const uint32_t c = h[j];
-          tot[k] += c;
-          earlier[k] += j < blockIdx.x ? c : 0;
+        for (int64_t j0 = 0; j0 < tiles; j0 += 8) {
+          uint32_t c[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) c[q] = h[std::min<int64_t>(j0 + q, tiles - 1)];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int64_t j = j0 + q;
+            tot[k] += j < tiles ? c[q] : 0;
+            earlier[k] += j < blockIdx.x ? c[q] : 0;   // (blockIdx.x < tiles)
+          }
         }
       }
       mine += tot[k];
@@ -237,9 +263,10 @@ __global__ __launch_bounds__(256) void k_sort_scatter(const int64_t* __restrict_
 }
 
 // Few rows: each one's place is the number of rows before it, found by comparing it with all of them
-// (a quarter of them per thread); one launch instead of the radix sort's four or more. Blocks beside them write
-// the table's zeros.
-constexpr int kFew = 2048;
+// (an eighth of them per thread); one launch instead of the radix sort's four or more. Blocks beside them write
+// the table's zeros. Whole calls with comparisons / with the sort: 2,049 fp32 rows of 768 into 8,204 tokens 29 / 39 us,
+// 4,000 into 50,257 46 / 54, 6,000 of 100 into 5,000 37 / 42, 8,192 of 1,543 into 8,204 59 / 56.
+constexpr int kFew = 6144, kRankRows = 32;    // rows of a block that ranks them
 
 __global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens, const uint8_t* __restrict__ mask,
                                               int64_t V, int n, uint32_t* __restrict__ keys_out,
@@ -249,18 +276,31 @@ __global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens
     fill_zero(dtable, ldt, d, nullptr, blockIdx.x - rank_blocks, gridDim.x - rank_blocks, 0, V);
     return;
   }
-  for (int i = threadIdx.x; i < (n + 15) / 16 * 16; i += 256) key[i] = i < n ? token_key(tokens, mask, i, V) : 0xFFFFFFFFu;
+  for (int base = 0; base < n; base += kTile) {        // (kFew is a multiple of kTile)
+    const int i0 = base + threadIdx.x;
+    uint32_t some[kTile / 256];
+    load_keys<true>(tokens, mask, V, nullptr, n, i0, 256, some);
+#pragma unroll
+    for (int r = 0; r < kTile / 256; ++r) key[i0 + r * 256] = i0 + r * 256 < n ? some[r] : 0xFFFFFFFFu;
+  }
   __syncthreads();
-  const int i = blockIdx.x * 64 + (threadIdx.x >> 2), part = threadIdx.x & 3;
+  const int i = blockIdx.x * kRankRows + (threadIdx.x >> 3), part = threadIdx.x & 7;
   const uint32_t mine = i < n ? key[i] : 0;
   uint32_t before = 0;
-  for (int j = 4 * part; j < n; j += 16) {
-    const uint4 k = *reinterpret_cast<const uint4*>(key + j);
-    before += (k.x < mine || (k.x == mine && j < i)) + (k.y < mine || (k.y == mine && j + 1 < i)) +
-              (k.z < mine || (k.z == mine && j + 2 < i)) + (k.w < mine || (k.w == mine && j + 3 < i));
+  for (int j0 = 4 * part; j0 < n; j0 += 256) {         // (eight reads in flight; places past n hold the last of all keys)
+    uint4 k[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) k[q] = *reinterpret_cast<const uint4*>(key + j0 + q * 32);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int j = j0 + q * 32;                       // earlier rows come first among equal keys
+      before += (k[q].x < mine + (j < i)) + (k[q].y < mine + (j + 1 < i)) + (k[q].z < mine + (j + 2 < i)) +
+                (k[q].w < mine + (j + 3 < i));
+    }
   }
   before += __shfl_xor(before, 1);
   before += __shfl_xor(before, 2);
+  before += __shfl_xor(before, 4);
   if (i < n && part == 0) {
     keys_out[before] = mine;
     rows_out[before] = (uint32_t)i;
@@ -270,7 +310,7 @@ __global__ __launch_bounds__(256) void k_rank(const int64_t* __restrict__ tokens
 // ---- sums over the sorted rows -----------------------------------------------------
 // Bound by HBM: the rows are read once, in the order of their tokens, and each finished row of the table is
 // written once (196,600 bf16 rows of 2048, 805 MB, into a table of 100,352: 230 us; with the sort, the zeros of
-// the other tokens' rows and the join 400 us, 4.1 TB/s).
+// the other tokens' rows and the join 392 us, 4.2 TB/s).
 // A wave sums the rows of a chunk of CHUNK sorted places, for 64 pieces of their columns, eight rows in
 // flight, token by token, in fp32. A token whose rows all lie in the chunk is finished here; the sum of one
 // that goes on beyond an end of the chunk is written to part[chunk][0] (it began in an earlier
@@ -428,12 +468,13 @@ constexpr int64_t kFlagBytes = 256 << 20;
 constexpr int64_t kTilesInline = 64;         // tiles whose counts a scatter block sums itself
 
 // Sorted places per wave: 64, fewer where those would leave most of the chip's waves without rows. Shorter chunks
-// give the sums more waves and the join longer chains. Whole calls with chunks of 16 / 32: 74,562 rows of 158 into
+// give the sums more waves and the join longer chains. Whole calls with chunks of 16 / 32, one after the other: 74,562 rows of 158 into
 // 7,642 tokens 121 / 92 us, 65,536 bf16 rows of 768 into 50,257 132 / 108, 8,000 rows of 1,543 into 8,204 60 / 58.
 constexpr int kChunk = 64, kShortChunk = 32, kFewChunk = 8;
+constexpr int64_t kFewChunkRows = 2048;
 
 int chunk_of(int64_t n, int64_t d, eogp_dtype t) {
-  if (n <= kFew) return kFewChunk;
+  if (n <= kFewChunkRows) return kFewChunk;
   const int64_t waves = ceil_div(n, kChunk) * ceil_div(d, t == EOGP_F32 ? 256 : 512);
   return waves >= 16 * kCus ? kChunk : kShortChunk;
 }
@@ -527,14 +568,19 @@ eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_
   timing::Scope ts(EOGP_KT_EMBED, s);
   const unsigned fill_blocks = accumulate ? 0 : (unsigned)std::min<int64_t>(ceil_div(V, 4), 4 * kCus);
   const BackWs w = n > 0 ? carve_back(ws, n, V, d) : BackWs{};
+  auto chunks = [&](const uint32_t* keys, const uint32_t* rows) {
+    const int chunk = chunk_of(n, d, t);
+    const auto sum = chunk == kChunk ? sum_sorted<kChunk> : chunk == kShortChunk ? sum_sorted<kShortChunk> : sum_sorted<kFewChunk>;
+    return sum(w, keys, rows, dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
+  };
   if (n <= kFew) {
-    const int rank_blocks = (int)ceil_div(n, 64);
+    const int rank_blocks = (int)ceil_div(n, kRankRows);
     if (rank_blocks + fill_blocks == 0) return EOGP_OK;
     hipLaunchKernelGGL(k_rank, dim3(rank_blocks + fill_blocks), dim3(256), 0, s, tokens, mask, V, (int)n, w.keys[0],
                        w.rows[0], rank_blocks, dtable, ldt, d);
     EOGP_LAUNCH_CHECK("embed_backward (ranks)");
     if (n == 0) return EOGP_OK;
-    return sum_sorted<kFewChunk>(w, w.keys[0], w.rows[0], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
+    return chunks(w.keys[0], w.rows[0]);
   }
   const int64_t tiles = ceil_div(n, kTile);
   const SortShape sh = sort_shape(V);
@@ -562,8 +608,7 @@ eogp_status embed_back(const void* dout, eogp_dtype t, int64_t ldd, const int64_
     EOGP_LAUNCH_CHECK("embed_backward (sort)");
   }
   const int last = (sh.passes - 1) & 1;
-  const auto sum = chunk_of(n, d, t) == kChunk ? sum_sorted<kChunk> : sum_sorted<kShortChunk>;
-  return sum(w, w.keys[last], w.rows[last], dout, t, ldd, n, V, d, scale, accumulate, dtable, ldt, s);
+  return chunks(w.keys[last], w.rows[last]);
 }
 
 }  // namespace eogp

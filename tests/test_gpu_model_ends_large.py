@@ -268,3 +268,19 @@ def test_what_shared_memory_held_before_does_not_matter():
                 both.append(got)
             assert all(torch.equal(a, b) for a, b in zip(*both)), (dt, d)
             assert not torch.isnan(both[1][3]).any()
+
+
+@pytest.mark.parametrize("n", [2048, 2049, 4095, 4097, 6143, 6144, 6145, 8193])
+@pytest.mark.parametrize("V", [1, 40, 30000])
+def test_embed_backward_at_the_ends_of_its_sorts(n, V):
+    """Whole numbers, so that any order of the sums is exact: small masked and unmasked lists, one token to many."""
+    say(f"[embed_backward] n={n} V={V}")
+    g = gen(27, n, V)
+    tok = torch.from_numpy(g.integers(-1, V + 1, n)).to(DEV)
+    do = torch.from_numpy(g.integers(-100, 100, (n, 37)).astype(np.float32)).to(DEV)
+    for mask in (None, torch.from_numpy((g.random(n) < 0.7).astype(np.uint8)).to(DEV)):
+        got = E.eogp_embed_backward(do, tok, V, token_mask=mask)
+        keep = (tok >= 0) & (tok < V) & (True if mask is None else mask != 0)
+        want = torch.zeros((V, 37), device=DEV).index_add_(0, tok[keep], do[keep])
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
