@@ -462,7 +462,9 @@ eogp_status eogp_embed_tokens(const void* table, eogp_dtype table_dtype, int64_t
  * d_table). The rows are sorted by token (stable) and summed in that order.
  * A token outside [0, V) counts for none.
  *   d_out    [n, ld_d_out >= d] of `dtype`;  d_table [V, ld_d_table >= d] fp32.
- *   ws       eogp_embed_backward_workspace_size bytes (none for n = 0). */
+ *   ws       eogp_embed_backward_workspace_size bytes (none for n = 0), which
+ *            are no fewer for a larger n, V or d: the workspace of the largest
+ *            batch serves every smaller one. */
 size_t eogp_embed_backward_workspace_size(int64_t n, int64_t V, int64_t d);
 eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_d_out,
                                 const int64_t* tokens, const uint8_t* token_mask, int64_t n, int64_t V,

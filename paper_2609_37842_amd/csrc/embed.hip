@@ -473,10 +473,27 @@ constexpr int64_t kTilesInline = 64;         // tiles whose counts a scatter blo
 constexpr int kChunk = 64, kShortChunk = 32, kFewChunk = 8;
 constexpr int64_t kFewChunkRows = 2048;
 
+constexpr int64_t kFullWaves = 16 * kCus;    // waves from which 64 places each keep the chip busy
+
 int chunk_of(int64_t n, int64_t d, eogp_dtype t) {
   if (n <= kFewChunkRows) return kFewChunk;
   const int64_t waves = ceil_div(n, kChunk) * ceil_div(d, t == EOGP_F32 ? 256 : 512);
-  return waves >= 16 * kCus ? kChunk : kShortChunk;
+  return waves >= kFullWaves ? kChunk : kShortChunk;
+}
+
+// The most chunks, and the most chunks times d, of any list of up to n rows of up to d elements: the
+// workspace for a batch holds that of every smaller one, though longer lists may have fewer chunks. Short
+// chunks are taken for fewer than kFullWaves chunks of 64 places and 512 (fp32: 256) columns, so no
+// such list has more than 2 kFullWaves of them, or more than that times 512 elements.
+struct ChunkRoom {
+  int64_t chunks, elements;
+};
+
+ChunkRoom chunk_room(int64_t n, int64_t d) {
+  const int64_t few = ceil_div(std::min(n, kFewChunkRows), kFewChunk), shorts = ceil_div(n, kShortChunk),
+                longs = ceil_div(n, kChunk);
+  return {std::max({few, std::min(shorts, 2 * kFullWaves), longs}),
+          std::max({few * d, std::min(shorts * d, 2 * kFullWaves * 512), longs * d})};
 }
 
 struct BackWs {
@@ -489,7 +506,7 @@ struct BackWs {
 BackWs carve_back(void* ws, int64_t n, int64_t V, int64_t d) {
   Carve cv(ws, ~(size_t)0);
   const bool few = n <= kFew;
-  const int64_t chunks = ceil_div(n, chunk_of(n, d, EOGP_BF16));     // (no other type has more)
+  const ChunkRoom room = chunk_room(n, d);
   BackWs w;
   for (int k = 0; k < (few ? 1 : 2); ++k) {
     w.keys[k] = cv.take<uint32_t>(n);
@@ -498,8 +515,8 @@ BackWs carve_back(void* ws, int64_t n, int64_t V, int64_t d) {
   w.hist = cv.take<uint32_t>(few ? 0 : (size_t)ceil_div(n, kTile) << kMaxDigit);
   w.totals = cv.take<uint32_t>(few ? 0 : 1 << kMaxDigit);
   w.flags = cv.take<uint8_t>(few ? 0 : round_up(V, 4));
-  w.begins = cv.take<uint8_t>(chunks);
-  w.part = cv.take<float>((size_t)chunks * 2 * d);
+  w.begins = cv.take<uint8_t>(room.chunks);
+  w.part = cv.take<float>((size_t)room.elements * 2);
   w.bytes = cv.used;
   return w;
 }

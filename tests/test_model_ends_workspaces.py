@@ -1,0 +1,40 @@
+"""Workspace sizes of the operators at the ends of a model (no GPU): a buffer sized for the largest batch has to
+serve every smaller one, so no size may fall as a batch grows."""
+import pytest
+
+from paper_2609_37842_amd import eogp as E
+
+
+def steps(most):
+    """Every length up to 5,000, then the neighbourhoods of multiples of 64 (chunks and tiles end there)."""
+    out = set(range(1, min(most, 5000) + 1))
+    for k in range(5000 // 64, most // 64 + 1):
+        out.update((64 * k, 64 * k + 1))
+    return sorted(out)
+
+
+def assert_rising(size, values):
+    last = 0
+    for v in values:
+        got = size(v)
+        assert got >= last, (v, got, last)
+        last = got
+
+
+@pytest.mark.parametrize("d", [1, 7, 64, 256, 257, 512, 513, 768, 1024, 1025, 2048, 5121, 16384])
+def test_embed_backward_size_rises_with_rows(d):
+    assert_rising(lambda n: E.eogp_embed_backward_workspace_size(n, 50257, d), steps(300_000))
+
+
+@pytest.mark.parametrize("n", [1, 100, 2048, 2049, 6144, 6145, 23808, 65472, 65473, 131009, 262144])
+def test_embed_backward_size_rises_with_width_and_vocabulary(n):
+    assert_rising(lambda d: E.eogp_embed_backward_workspace_size(n, 50257, d), range(1, 8300))
+    assert_rising(lambda V: E.eogp_embed_backward_workspace_size(n, V, 768), range(1, 140_000, 13))
+
+
+@pytest.mark.parametrize("n,d,chunk", [(1, 1, 8), (2048, 768, 8), (2049, 768, 32), (6145, 2048, 32), (65472, 2048, 32),
+                                       (65473, 2048, 64), (262144, 2048, 64), (4_000_000, 64, 64)])
+def test_embed_backward_size_holds_the_sums_of_its_chunks(n, d, chunk):
+    """Two partial rows of d fp32 for each chunk, and a sorted list of keys and rows."""
+    chunks = -(-n // chunk)
+    assert E.eogp_embed_backward_workspace_size(n, 50257, d) >= chunks * (8 * d + 1) + 8 * n
