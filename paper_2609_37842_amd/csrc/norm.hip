@@ -459,7 +459,9 @@ int back_splits(int64_t groups, int64_t rows, int64_t pieces) {
 }  // namespace
 
 size_t layer_norm_back_ws(int64_t groups, int64_t rows, int64_t d, eogp_dtype t) {
-  return align256((size_t)groups * back_splits(groups, rows, row_pieces(d, t)) * 2 * d * sizeof(float));
+  // A group's only block writes its gradients itself: no partial sums then, and the least workspace there is.
+  const int splits = back_splits(groups, rows, row_pieces(d, t));
+  return align256(std::max<size_t>(1, splits > 1 ? (size_t)groups * splits * 2 * d * sizeof(float) : 0));
 }
 
 eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t ldx, eogp_dtype t,

@@ -38,3 +38,17 @@ def test_embed_backward_size_holds_the_sums_of_its_chunks(n, d, chunk):
     """Two partial rows of d fp32 for each chunk, and a sorted list of keys and rows."""
     chunks = -(-n // chunk)
     assert E.eogp_embed_backward_workspace_size(n, 50257, d) >= chunks * (8 * d + 1) + 8 * n
+
+
+def test_layer_norm_backward_asks_for_partial_sums_only():
+    """Blocks that own an example write its gradients themselves: examples of few rows, or as many examples as
+    blocks, need no room for partial sums, whatever their number."""
+    size = E.eogp_layer_norm_backward_workspace_size
+    for d, rows in ((768, 16), (768, 1), (5120, 4), (1024, 16), (16384, 4)):
+        for code in (E.F32, E.BF16, E.F16):
+            for groups in (1, 2, 131_072, 1 << 21):
+                assert 0 < size(groups, rows, d, code) <= 256, (groups, rows, d)
+    # 2 d fp32 for each block of a launch, of which there are at most twice 4 x 256 with partial sums
+    for d in (768, 2048):
+        for groups in (1, 128, 1023, 1024, 131_072):
+            assert size(groups, 512, d, E.F32) <= 2048 * 2 * d * 4
