@@ -496,7 +496,8 @@ eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, con
  *                         itself, and overlaps nothing else.
  *   mean, rstd            [groups * rows] fp32 of the forward pass.
  *   d_gamma, d_beta       [groups, d] fp32, or NULL.
- *   ws                    eogp_layer_norm_backward_workspace_size bytes.
+ *   ws                    eogp_layer_norm_backward_workspace_size bytes, no
+ *                         fewer for more groups or rows of the same width and type.
  * Errors as for eogp_layer_norm, and EOGP_ERR_INVALID for more than 2^21 groups;
  * EOGP_ERR_WORKSPACE if ws is too small. */
 size_t eogp_layer_norm_backward_workspace_size(int64_t groups, int64_t rows, int64_t d,

@@ -448,20 +448,27 @@ eogp_status layer_norm(const void* x, eogp_dtype xt, int64_t ldx, const void* ga
 }
 
 namespace {
-// Blocks of a group: as many as are there at once, no more than its rows need; one for so
-// few rows that a second launch would cost more than their turns.
+// Blocks of a launch that sums columns, and the rows up to which a group has one block: so few that a second launch
+// would cost more than their turns.
+int64_t back_blocks(int64_t pieces) { return pieces <= 512 ? 4 * kCus : kCus; }
+bool one_block(int64_t rows, int64_t pieces) { return rows <= 4 * rows_per_block(pieces); }
+
+// Blocks of a group: as many as are there at once, no more than its rows need.
 int back_splits(int64_t groups, int64_t rows, int64_t pieces) {
-  if (rows <= 4 * rows_per_block(pieces)) return 1;
-  const int64_t most = ceil_div(rows, rows_per_block(pieces));
-  const int64_t want = ceil_div(pieces <= 512 ? 4 * kCus : kCus, groups);
-  return (int)std::max<int64_t>(1, std::min(most, want));
+  if (one_block(rows, pieces)) return 1;
+  return (int)std::min(ceil_div(rows, rows_per_block(pieces)), ceil_div(back_blocks(pieces), groups));
 }
 }  // namespace
 
 size_t layer_norm_back_ws(int64_t groups, int64_t rows, int64_t d, eogp_dtype t) {
-  // A group's only block writes its gradients itself: no partial sums then, and the least workspace there is.
-  const int splits = back_splits(groups, rows, row_pieces(d, t));
-  return align256(std::max<size_t>(1, splits > 1 ? (size_t)groups * splits * 2 * d * sizeof(float) : 0));
+  // The partial sums of as many blocks as any launch of up to `groups` groups of up to `rows` rows writes, so that
+  // the workspace for a batch serves every smaller one. A group's only block writes its gradients itself; those of
+  // several, ceil(most / g) each, are at most g + most - 1 for g groups, and less than most groups have several.
+  const int64_t pieces = row_pieces(d, t), most = back_blocks(pieces);
+  const int64_t blocks = one_block(rows, pieces) ? 0
+                                                 : std::min(groups * ceil_div(rows, rows_per_block(pieces)),
+                                                            std::min(groups, most - 1) + most - 1);
+  return align256(std::max<size_t>(1, (size_t)blocks * 2 * d * sizeof(float)));
 }
 
 eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t ldx, eogp_dtype t,

@@ -52,3 +52,28 @@ def test_layer_norm_backward_asks_for_partial_sums_only():
     for d in (768, 2048):
         for groups in (1, 128, 1023, 1024, 131_072):
             assert size(groups, 512, d, E.F32) <= 2048 * 2 * d * 4
+
+
+@pytest.mark.parametrize("code", [E.F32, E.BF16, E.F16])
+@pytest.mark.parametrize("d", [1, 5, 255, 768, 1025, 2047, 2049, 4097, 5120, 16384])
+def test_layer_norm_backward_size_rises_with_groups_and_rows(d, code):
+    size = E.eogp_layer_norm_backward_workspace_size
+    for rows in (0, 1, 4, 5, 16, 17, 100, 512, 4096):
+        assert_rising(lambda g: size(g, rows, d, code), range(1, 2200))
+    for groups in (1, 2, 5, 128, 255, 256, 257, 600, 1023, 1024, 5000):
+        assert_rising(lambda r: size(groups, r, d, code), range(0, 4200))
+
+
+@pytest.mark.parametrize("pieces_of", [(E.F32, 4), (E.BF16, 8)])
+def test_layer_norm_backward_size_holds_the_partial_sums(pieces_of):
+    """2 d fp32 for each block, where a group has several: a group's blocks take four rows at a time (one, beyond
+    256 pieces of 16 bytes), and 4 x 256 (256 beyond 512 pieces) fill the chip."""
+    code, e = pieces_of
+    for d in (64, 768, 1024, 1025, 2048, 2049, 4096, 4097, 16384):
+        pieces = -(-d // e)
+        per, fill = 4 if pieces <= 256 else 1, 1024 if pieces <= 512 else 256
+        for groups in [*range(1, 300), 511, 512, 513, 1023, 1024, 4000]:
+            for rows in (1, 5, 17, 40, 512, 3000):
+                splits = min(-(-rows // per), -(-fill // groups)) if rows > 4 * per else 1
+                need = groups * splits * 2 * d * 4 if splits > 1 else 0
+                assert E.eogp_layer_norm_backward_workspace_size(groups, rows, d, code) >= need, (d, groups, rows)
