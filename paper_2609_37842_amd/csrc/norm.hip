@@ -309,7 +309,7 @@ __global__ __launch_bounds__(norm_threads(WPR)) void k_layer_norm_back(
     i = after;
   }
   // a group's only block writes its gradients, others their sums for k_norm_fold
-  float *pg = part + (int64_t)blockIdx.x * 2 * d, *pb = pg + d;
+  float *pg = part ? part + (int64_t)blockIdx.x * 2 * d : nullptr, *pb = part ? pg + d : nullptr;
   if (splits == 1) {
     pg = dgamma ? dgamma + group * d : nullptr;
     pb = dbeta ? dbeta + group * d : nullptr;
@@ -479,7 +479,7 @@ eogp_status layer_norm_back(const void* dy, int64_t lddy, const void* x, int64_t
   if (groups == 0) return EOGP_OK;
   const int64_t pieces = row_pieces(d, t);
   const int splits = back_splits(groups, rows, pieces);
-  float* part = static_cast<float*>(ws);
+  float* part = dgamma || dbeta ? static_cast<float*>(ws) : nullptr;   // (NULL: nobody wants the sums)
   timing::Scope ts(EOGP_KT_LAYER_NORM, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
