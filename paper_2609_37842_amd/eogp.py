@@ -631,6 +631,40 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+# The device that kernels are launched on. (Asked for after a device tensor has been seen, so the
+# runtime is there; torch.cuda.current_device() would look for that again.)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _need_here(stream, first, *ts):
+    """Device tensors, and a stream if there is one, of the device that kernels are launched on."""
+    here = first.get_device()
+    if here >= 0 and here != _current_device():
+        _refuse_device(_current_device(), here)
+    for t in ts:
+        if t is not None and t.get_device() != here:
+            _refuse_device(here, t.get_device())
+    if here < 0:
+        _refuse_device(here, here)
+    if stream is not None and stream.device_index != here:
+        raise ValueError(f"stream must belong to the current device cuda:{here}, not cuda:{stream.device_index}")
+
+
+def _refuse_device(here, there):
+    if min(here, there) < 0:
+        raise ValueError("EOGP arguments must be device tensors")
+    raise ValueError(f"EOGP arguments must be on the current device cuda:{here}, not cuda:{there}")
+
+
+def _scratch(need, device, ws, stream):
+    """The caller's workspace, or a new one that belongs to the stream the call runs on."""
+    if ws is None:
+        return (_empty((need,), torch.uint8, device, stream), need) if need else (None, 0)
+    if not ws.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _workspace(need, device, ws)
+
+
 def _rows_of(x, name):
     """(rows, width, row stride) of a [n, d] or [N, T, d] tensor whose rows have
     unit column stride and lie at one constant stride."""
@@ -684,7 +718,7 @@ def eogp_embed_tokens(table, tokens, scale=1.0, token_mask=None, out=None, accum
     """out [*tokens.shape, d] = scale * table[tokens] (table [V, d]; tokens int64 [n]
     or [N, T]), added to `out` if accumulate; see eogp_embed_tokens in eogp.h."""
     L = load()
-    _need_cuda(table, tokens, token_mask, out)
+    _need_here(stream, table, tokens, token_mask, out)
     V, d, ldt = _rows_of(table, "table")
     if table.dim() != 2 or tokens.dim() not in (1, 2):
         raise ValueError("table must be [V, d] and tokens [n] or [N, T]")
@@ -713,7 +747,7 @@ def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=Non
     """dtable [V, d] (float32) = scale * sum of d_out's rows by token, added to
     `dtable` if accumulate; see eogp_embed_backward in eogp.h."""
     L = load()
-    _need_cuda(d_out, tokens, token_mask, dtable)
+    _need_here(stream, d_out, tokens, token_mask, dtable, ws)
     n, d, ldd = _rows_of(d_out, "d_out")
     lead = d_out.shape[:-1]
     _per_row(tokens, lead, torch.int64, "tokens")
@@ -726,9 +760,7 @@ def eogp_embed_backward(d_out, tokens, V, scale=1.0, token_mask=None, dtable=Non
         raise ValueError("dtable must be float32 [V, d]")
     _, _, ldt = _rows_of(dtable, "dtable")
     need = eogp_embed_backward_workspace_size(n, V, d)
-    if ws is None and need:
-        ws = _empty((need,), torch.uint8, d_out.device, stream)
-    ws, wsb = _workspace(need, d_out.device, ws)
+    ws, wsb = _scratch(need, d_out.device, ws, stream)
     _check(L.eogp_embed_backward(_at(d_out), _model_dtype(d_out, "d_out"), ldd, _at(tokens),
                                  _at(token_mask), n, V, d, float(scale), 1 if accumulate else 0,
                                  _at(dtable), ldt, _at(ws), wsb,
@@ -742,7 +774,7 @@ def eogp_layer_norm(x, gamma=None, beta=None, eps=1e-5, token_mask=None, ones_co
     columns, the last 1 in valid rows (a new y then has rows of a multiple of 16
     elements); see eogp_layer_norm in eogp.h."""
     L = load()
-    _need_cuda(x, gamma, beta, token_mask, out, mean, rstd)
+    _need_here(stream, x, gamma, beta, token_mask, out, mean, rstd)
     n, d, ldx = _rows_of(x, "x")
     lead, width = x.shape[:-1], d + (1 if ones_column else 0)
     _per_row(token_mask, lead, torch.uint8, "token_mask")
@@ -780,7 +812,7 @@ def eogp_layer_norm_backward(dy, x, gamma, mean, rstd, token_mask=None, residual
     gradients, float32 [d] or with per_example [N, d] (x [N, T, d]); see
     eogp_layer_norm_backward in eogp.h."""
     L = load()
-    _need_cuda(dy, x, gamma, mean, rstd, token_mask, residual, dx, dgamma, dbeta)
+    _need_here(stream, dy, x, gamma, mean, rstd, token_mask, residual, dx, dgamma, dbeta, ws)
     n, d, ldx = _rows_of(x, "x")
     lead = x.shape[:-1]
     _same_shape(dy, x, "dy")
@@ -812,9 +844,7 @@ def eogp_layer_norm_backward(dy, x, gamma, mean, rstd, token_mask=None, residual
     _per_row(dbeta, shape, torch.float32, "dbeta")
     code = _model_dtype(x, "x")
     need = eogp_layer_norm_backward_workspace_size(groups, rows, d, code)
-    if ws is None and need:
-        ws = _empty((need,), torch.uint8, x.device, stream)
-    ws, wsb = _workspace(need, x.device, ws)
+    ws, wsb = _scratch(need, x.device, ws, stream)
     _check(L.eogp_layer_norm_backward(_at(dy), lddy, _at(x), ldx, code, _at(gamma),
                                       F32 if gamma is None else _DTYPE_CODE[gamma.dtype], _at(mean),
                                       _at(rstd), _at(token_mask), _at(residual), ldr, groups, rows, d,
@@ -829,7 +859,7 @@ def eogp_softmax_xent(logits, labels, token_mask=None, grad_scale=1.0, grad=True
     [N, T]; grad=False leaves dlogits out (None); dlogits may be the logits; see
     eogp_softmax_xent in eogp.h."""
     L = load()
-    _need_cuda(logits, labels, token_mask, loss, dlogits)
+    _need_here(stream, logits, labels, token_mask, loss, dlogits)
     n, V, ldl = _rows_of(logits, "logits")
     lead = logits.shape[:-1]
     _per_row(labels, lead, torch.int64, "labels")
@@ -856,7 +886,7 @@ def eogp_sample_tokens(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.
     """Tokens int64 drawn from logits [n, V] or [N, T, V] with uniforms float32 [n] or
     [N, T] in [0, 1); see eogp_sample_tokens in eogp.h."""
     L = load()
-    _need_cuda(logits, uniforms, token_mask, out)
+    _need_here(stream, logits, uniforms, token_mask, out)
     n, V, ldl = _rows_of(logits, "logits")
     lead = logits.shape[:-1]
     _per_row(uniforms, lead, torch.float32, "uniforms")
