@@ -438,7 +438,8 @@ eogp_status eogp_srht_project(const float* Z, int64_t ldz, int64_t N, int64_t m,
  * of the attributed linear modules out of tokens and logits. Element types
  * are fp32, bf16 and fp16; sums, statistics and weight gradients are fp32.
  * Rows are tokens (n = examples * tokens of each), `ld_*` their strides in
- * elements, at any element's address. token_mask ([n] uint8 or NULL = all
+ * elements, at any element's address (arrays and workspaces at a multiple of
+ * their elements' size, the workspaces' 4 bytes). token_mask ([n] uint8 or NULL = all
  * valid) works as in the first stage: masked rows are never read, their
  * outputs are zero, and they count for no sum. Results do not depend on the
  * order in which the GPU runs blocks: repeated calls agree bit for bit.

@@ -566,10 +566,16 @@ eogp_status check_ld(const char* op, const char* what, int64_t ld, int64_t width
   return EOGP_OK;
 }
 
-eogp_status check_aligned(const char* op, const char* what, const void* p, eogp_dtype t) {
-  if ((uintptr_t)p % (t == EOGP_F32 ? 4 : 2))
+// Addresses have to be multiples of their elements' size: one value for a whole wave is read by a scalar load, which
+// drops an address's low bits.
+eogp_status check_address(const char* op, const char* what, const void* p, size_t element) {
+  if ((uintptr_t)p % element)
     return fail(EOGP_ERR_INVALID, std::string(op) + ": " + what + " must be aligned to its elements");
   return EOGP_OK;
+}
+
+eogp_status check_aligned(const char* op, const char* what, const void* p, eogp_dtype t) {
+  return check_address(op, what, p, t == EOGP_F32 ? 4 : 2);
 }
 }  // namespace
 
@@ -596,6 +602,7 @@ eogp_status eogp_embed_tokens(const void* table, eogp_dtype table_dtype, int64_t
   if (!table || !tokens || !out) return fail(EOGP_ERR_INVALID, "embed_tokens: NULL pointer");
   EOGP_CHECK(check_aligned(op, "table", table, table_dtype));
   EOGP_CHECK(check_aligned(op, "out", out, out_dtype));
+  EOGP_CHECK(check_address(op, "tokens", tokens, 8));
   return embed_tokens(table, table_dtype, ld_table, V, d, tokens, token_mask, n, scale, accumulate, out,
                       out_dtype, ld_out, S(stream));
 }
@@ -617,8 +624,12 @@ eogp_status eogp_embed_backward(const void* d_out, eogp_dtype dtype, int64_t ld_
   EOGP_CHECK(check_ld(op, "d_table", ld_d_table, d));
   if (!d_table || (n > 0 && (!d_out || !tokens)))
     return fail(EOGP_ERR_INVALID, "embed_backward: NULL pointer");
-  if (n > 0) EOGP_CHECK(check_aligned(op, "d_out", d_out, dtype));
-  EOGP_CHECK(check_aligned(op, "d_table", d_table, EOGP_F32));
+  if (n > 0) {
+    EOGP_CHECK(check_aligned(op, "d_out", d_out, dtype));
+    EOGP_CHECK(check_address(op, "tokens", tokens, 8));
+    EOGP_CHECK(check_address(op, "ws", ws, 4));
+  }
+  EOGP_CHECK(check_address(op, "d_table", d_table, 4));
   if (n > 0 && (!ws || ws_bytes < embed_back_ws(n, V, d)))
     return fail(EOGP_ERR_WORKSPACE, "embed_backward: workspace too small");
   return embed_back(d_out, dtype, ld_d_out, tokens, token_mask, n, V, d, scale, accumulate, d_table,
@@ -656,6 +667,8 @@ eogp_status eogp_layer_norm(const void* x, eogp_dtype x_dtype, int64_t ld_x, con
   EOGP_CHECK(check_aligned(op, "y", y, y_dtype));
   EOGP_CHECK(check_aligned(op, "gamma", gamma, w_dtype));
   EOGP_CHECK(check_aligned(op, "beta", beta, w_dtype));
+  EOGP_CHECK(check_address(op, "mean", mean, 4));
+  EOGP_CHECK(check_address(op, "rstd", rstd, 4));
   return layer_norm(x, x_dtype, ld_x, gamma, beta, w_dtype, eps, token_mask, n, d, y, y_dtype, ld_y,
                     ones_column != 0, mean, rstd, S(stream));
 }
@@ -691,7 +704,12 @@ eogp_status eogp_layer_norm_backward(const void* dy, int64_t ld_dy, const void* 
     EOGP_CHECK(check_aligned(op, "dx", dx, dtype));
     EOGP_CHECK(check_aligned(op, "residual", residual, dtype));
     EOGP_CHECK(check_aligned(op, "gamma", gamma, w_dtype));
+    EOGP_CHECK(check_address(op, "mean", mean, 4));
+    EOGP_CHECK(check_address(op, "rstd", rstd, 4));
   }
+  EOGP_CHECK(check_address(op, "d_gamma", d_gamma, 4));
+  EOGP_CHECK(check_address(op, "d_beta", d_beta, 4));
+  EOGP_CHECK(check_address(op, "ws", ws, 4));
   if (!ws || ws_bytes < layer_norm_back_ws(groups, rows, d, dtype))
     return fail(EOGP_ERR_WORKSPACE, "layer_norm_backward: workspace too small");
   return layer_norm_back(dy, ld_dy, x, ld_x, dtype, gamma, w_dtype, mean, rstd, token_mask, residual,
@@ -713,6 +731,8 @@ eogp_status eogp_softmax_xent(const void* logits, eogp_dtype dtype, int64_t ld_l
     return fail(EOGP_ERR_INVALID, "softmax_xent: gradients over the logits need their row stride");
   EOGP_CHECK(check_aligned(op, "logits", logits, dtype));
   EOGP_CHECK(check_aligned(op, "d_logits", d_logits, dtype));
+  EOGP_CHECK(check_address(op, "labels", labels, 8));
+  EOGP_CHECK(check_address(op, "loss", loss, 4));
   return softmax_xent(logits, dtype, ld_logits, labels, token_mask, n, V, grad_scale, loss, d_logits,
                       ld_d_logits, S(stream));
 }
@@ -736,6 +756,8 @@ eogp_status eogp_sample_tokens(const void* logits, eogp_dtype dtype, int64_t ld_
   if (!logits || !tokens || (!uniforms && temperature > 0.0))
     return fail(EOGP_ERR_INVALID, "sample_tokens: NULL pointer");
   EOGP_CHECK(check_aligned(op, "logits", logits, dtype));
+  EOGP_CHECK(check_address(op, "uniforms", uniforms, 4));
+  EOGP_CHECK(check_address(op, "tokens", tokens, 8));
   return sample_tokens(logits, dtype, ld_logits, n, V, uniforms, token_mask, temperature, top_k, top_p,
                        min_p, tokens, S(stream));
 }
