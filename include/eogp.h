@@ -443,11 +443,14 @@ eogp_status eogp_srht_project(const float* Z, int64_t ldz, int64_t N, int64_t m,
  * valid) works as in the first stage: masked rows are never read, their
  * outputs are zero, and they count for no sum. Results do not depend on the
  * order in which the GPU runs blocks: repeated calls agree bit for bit.
- * Every call is enqueued on `stream` and launches kernels only.
+ * Every call is enqueued on `stream`, of the current device, and launches
+ * kernels only. (The first stage takes fp32 and bf16 activations and
+ * output-gradients; fp16 rows have to be widened for it.)
  * ------------------------------------------------------------------------ */
 
 /* Token embedding: out[i] = scale * table[tokens[i]], added to out[i] if
- * accumulate != 0 (position rows, a second table). One rounding to out's type.
+ * accumulate != 0 (position rows, a second table; a masked row then stays as
+ * it is). One rounding to out's type.
  *   table   [V, ld_table >= d];  tokens [n];  out [n, ld_out >= d] of the
  *           table's type or fp32. A valid row whose token lies outside [0, V)
  *           gets NaN.
@@ -533,7 +536,7 @@ eogp_status eogp_softmax_xent(const void* logits, eogp_dtype dtype, int64_t ld_l
  *         degree-5 polynomial p in Horner's form, fp32, each operation rounded.
  * In the order (logit descending, index ascending), kept are the first top_k
  * (0: all); of those the shortest prefix whose mass reaches
- * floor(mass * rint(top_p 2^24) / 2^24), at least one; of those w_v >= min_p 2^30
+ * floor(mass * floor(top_p 2^24 + 1/2) / 2^24), at least one; of those w_v >= min_p 2^30
  * (the largest weight is 2^30). The token is the lowest index whose running
  * kept mass exceeds floor(floor(u 2^24) * kept mass / 2^24).
  *   uniforms      [n] fp32 (clamped to [0, 1)); may be NULL at temperature 0.

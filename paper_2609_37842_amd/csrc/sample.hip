@@ -21,7 +21,7 @@ constexpr float kBinsPerOctave = 64.f;
 constexpr int64_t kMaxVocab = (int64_t)1 << 20;
 
 // 2^30 2^f on [-1/2, 1/2]: a least-squares fit of (2^f - 1) / f reweighted until its relative error
-// was level (9e-8); scaling by 2^30 changes no rounding.
+// was level (1.1e-7, and 1.9e-7 with fp32's roundings); scaling by 2^30 changes no rounding.
 constexpr float kTwo30 = 1073741824.f;
 constexpr float kC1 = 0.6931470036506653f * kTwo30, kC2 = 0.24022242426872253f * kTwo30,
                 kC3 = 0.05550733581185341f * kTwo30, kC4 = 0.009671512991189957f * kTwo30,
@@ -187,9 +187,13 @@ __device__ __forceinline__ void add_piece(int p, uint32_t c, const float (&v)[E]
 // in registers as read, and the next one is requested piece by piece as the weights' pass lets go of
 // this one; P = 0: it is read in both passes.
 // MIN: only weights of at least min_w count (a compare and a select per logit that the plain draw is spared).
-// Bound by the vector ALU: the maximum is one operation a logit, the weight and its sum about 18 (an
-// integer weight of 30 bits; the hardware's exponential has no rounding that another machine repeats).
-// 1,536 fp32 rows of 50,257: 89 to 101 us, 3.1 to 3.5 TB/s; the first reading of the row is its only one.
+// Bound by the vector ALU of the blocks with the most rows: 37 vector instructions a logit (18 of them the
+// whole-number weight of 30 bits, since the hardware's exponential has no rounding that another machine repeats; the
+// others the maximum, 64-bit sums and addresses) keep it busy for 0.72 of the launch on average over the CUs, where the
+// mean block has 6.3 rows and those with the most 7 or 8. 2,048 fp32 places of 50,257, 75% of them valid: 93 to 101 us,
+// 3.1 to 3.3 TB/s; 1,536 unmasked rows, six a block: 91; the first reading of the row is its only one.
+// With P = 0 it is read twice (1,024 fp32 rows of 100,352: 145 us, 2.8 TB/s of one reading); 16-bit rows of 8,193 to
+// 16,384 pieces spill 4 registers, with MIN 11 (2,048 bf16 rows of 100,352: 174 and 183 us, 2.4 and 2.2 TB/s).
 template <typename T, int NT, int P, bool MIN>
 __global__ __launch_bounds__(NT) void k_sample(
     const T* __restrict__ logits, int64_t ldl, int64_t n, int64_t V, const float* __restrict__ uniforms,
@@ -478,9 +482,11 @@ __device__ Bound split_bin(SelectLds<NT>& sh, RegisterRow<T, NT, 0, 4>& row, int
 }
 
 // One block per row, since all its steps meet in one list. 256 bf16 rows of 100,352 (a row per CU) with
-// top_k 50, top_p 0.9 and min_p: 20 us, 2.6 TB/s of one reading; one fp16 row of 50,257 with top_p 0.95: 19 us,
-// seven dependent steps (maximum, histogram, its scan, list, order, draw) of one CU, where several CUs for the row
-// would pay a launch of 4 us or a wait between blocks for each.
+// top_k 50, top_p 0.9 and min_p: 20 us, 2.6 TB/s of one reading; one fp16 row of 50,257 with top_p 0.95: 19 us where
+// few tokens reach it (59 where thousands do), dependent steps (maximum, histogram, its scan, list, order, draw) of one
+// CU, where several CUs for the row would pay a launch of 4 us or a wait between blocks for each. The histogram
+// and the list read the row again, from the caches, and the bound and scale lie in scratch (64 to 72 bytes a lane). Wide filters read
+// it up to five times: 256 bf16 rows of 100,352 with a top_p that keeps thousands 124 us, top_k 2,000 101, both 167.
 // 1. top_k up to the block's threads: the top_k-th largest of the threads' own maxima is a lower
 //    bound of the top_k-th largest logit, so the elements at or above it (few more than top_k) hold
 //    all that is kept; they are settled in LDS.
@@ -636,7 +642,7 @@ __global__ __launch_bounds__(NT) void k_sample_select(const T* __restrict__ logi
 }
 
 // Temperature 0: the lowest index of the largest logit, one block per row (bound by HBM for many rows, by the
-// row's round trips for few).
+// row's round trips for few). 2,048 fp32 rows of 50,257: 75 us, 5.5 TB/s; 256 bf16 rows of 100,352 13 us, one row 7.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_argmax(const T* __restrict__ logits, int64_t ldl, int64_t V,
                                                  const uint8_t* __restrict__ mask, int64_t* __restrict__ out) {

@@ -39,9 +39,12 @@ constexpr int xent_per_cu(int nt, int p) { return nt == 256 ? 6 : p >= 1 && p <=
 // to the logits' type.
 // Bound by HBM. A block takes a row at a time. With P > 0 the row stays in registers as read, so HBM sees
 // one read and one write, and the next row is requested piece by piece as the gradient's pass lets go of
-// this one; P = 0 reads the row three times, for rows longer than the registers hold. 3,585 bf16 rows of
-// 100,352 with their gradients take 310 us, 4.6 TB/s; 24 fp32 rows of 50,257 take 12 us, three passes over a row's
-// registers by one CU (a row over several CUs would need a second launch, 4 us, or a wait between blocks).
+// this one; P = 0 reads the row three times, for rows longer than the registers hold. 4,096 bf16 places of
+// 100,352, 75% of them valid, with their gradients take 311 to 315 us, 4.6 TB/s; 24 fp32 rows of 50,257 take 12 us,
+// three passes over a row's registers by one CU (a row over several CUs would need a second launch, 4 us, or a wait
+// between blocks). With P = 0, 2,048 fp32 rows of 100,352: 510 us, 3.2 TB/s of one reading and the writing (6.4 of all
+// three), the loss alone 250. The six blocks of 16-bit rows of 1,025 to 2,048 pieces on a CU spill two registers each
+// (8,192 rows of 16,384: 101 us, 5.3 TB/s).
 template <typename T, int NT, int P, bool GRAD>
 __global__ __launch_bounds__(NT, xent_per_cu(NT, P) * NT / 256) void k_xent(
     const T* logits, int64_t ldl, const int64_t* __restrict__ labels, const uint8_t* __restrict__ mask, int64_t n,
