@@ -551,6 +551,132 @@ eogp_status eogp_sample_tokens(const void* logits, eogp_dtype dtype, int64_t ld_
                                int64_t* tokens, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The middle of a language model's block: what lies between the query, key and
+ * value projections and the output projection, so that these modules' inputs
+ * and output-gradients are made on the device too. Types, masks, streams,
+ * alignment and repeatability as for the ends of a model; scores, weights'
+ * sums and statistics are fp32.
+ * ------------------------------------------------------------------------ */
+
+/* A tensor of heads [N, T, heads, D]: element (n, t, h, c) lies at
+ * data[n * ld_example + t * ld_token + h * ld_head + c], strides in elements,
+ * at least 0 and below 2^40. Outputs may not overlap themselves; slices of one projection's
+ * rows and [N, heads, T, D] arrays are both such tensors. (heads = 0 or data =
+ * NULL where a call takes a tensor as optional.) */
+typedef struct {
+  void* data;
+  int64_t heads, ld_example, ld_token, ld_head;
+} eogp_heads;
+
+/* Table of rotary positions: for position p < positions and pair i < width / 2
+ *   table[p][i] = magnitude * (cos, sin)(p f_i),
+ *   f_i = base^(-2 i / width) (g_i + (1 - g_i) / factor).
+ * Without an original length (0) g_i is 0: every frequency is divided by
+ * `factor` (1: as it is). With one, frequencies that turn more than `high`
+ * times over it keep their value, those that turn fewer than `low` times are
+ * divided, and those between are interpolated:
+ *   g_i = clamp((original base^(-2 i / width) / 2 pi - low) / (high - low), 0, 1).
+ *   table   [positions, width / 2, 2] fp32. Angles are fp64.
+ * Errors: EOGP_ERR_INVALID for an odd or non-positive width, positions outside [0, 2^31),
+ * base <= 0, factor <= 0, original < 0, high <= low, values that are not finite, or NULL. */
+eogp_status eogp_rotary_table(int64_t positions, int64_t width, double base, double factor,
+                              double original, double low, double high, double magnitude, float* table,
+                              void* stream);
+
+/* Norm and rotation of queries and keys, in one pass: y = R_p (x rstd w), where
+ *   norm = EOGP_NORM_HEAD  rstd = (mean of x^2 over each head + eps)^-1/2, w [D];
+ *   norm = EOGP_NORM_ROW   the same over all heads of a token (heads * D elements), w [heads * D];
+ *   norm = EOGP_NORM_NONE  rstd = w = 1 (weights NULL).
+ * R_p turns pairs of the first `width` elements of each head by the table's row of the token's position:
+ * (a, b) -> (a cos - b sin, a sin + b cos), with a = element i and b = element width / 2 + i, or with
+ * interleaved != 0 elements 2 i and 2 i + 1. The elements behind `width` pass. One rounding at the end.
+ *   q, k          inputs of `dtype`; k NULL (or of no heads): queries alone.
+ *   q_out, k_out  of `dtype`; an output may be its input (same data and strides), else overlaps nothing.
+ *   q_weight, k_weight  of `dtype` or fp32 (w_dtype), or NULL (1).
+ *   table         [table_positions, width / 2, 2] fp32 of eogp_rotary_table; NULL with width 0: the norm alone.
+ *   positions     [N * T] int64, or NULL: the token's index in its example. A valid token whose position lies outside
+ *                 the table gets NaN in its turned elements.
+ *   token_mask    [N * T] uint8 or NULL; masked tokens count for nothing and get zeros.
+ * Errors: EOGP_ERR_INVALID for bad sizes, NULL pointers, an odd width or one above D, eps < 0;
+ * EOGP_ERR_UNSUPPORTED for D > 256, other weight types, or a row norm of more than 8,192 elements (2,048 of heads of
+ * fewer than 8). */
+#define EOGP_NORM_NONE 0
+#define EOGP_NORM_HEAD 1
+#define EOGP_NORM_ROW 2
+eogp_status eogp_rotate_heads(const eogp_heads* q, const eogp_heads* k, eogp_dtype dtype, int64_t N, int64_t T,
+                              int64_t D, int32_t norm, const void* q_weight, const void* k_weight,
+                              eogp_dtype w_dtype, float eps, const float* table, int64_t table_positions,
+                              int64_t width, int32_t interleaved, const int64_t* positions,
+                              const uint8_t* token_mask, const eogp_heads* q_out, const eogp_heads* k_out,
+                              void* stream);
+
+/* Its backward pass: with t = R_p^T dy and xh = x rstd,
+ *   dx = rstd (t w - xh mean(t w xh)),   d_w = sum of t xh
+ * over the tokens (and, for EOGP_NORM_HEAD, heads) of the batch, or with per_example != 0 of each example.
+ *   dq, dk        gradients of the outputs;  q, k the forward pass's inputs (not read, may be NULL, without a norm).
+ *   dq_in, dk_in  gradients of the inputs; may be dq and dk themselves, else overlap nothing.
+ *   dq_weight, dk_weight  fp32 [weight], or [N, weight] per example; NULL: left out (always without a norm).
+ *   ws            eogp_rotate_heads_backward_workspace_size bytes (0 without a norm), no fewer for more examples or
+ *                 tokens of the same heads, widths and types.
+ * A position outside the table gives NaN to the input gradients and weight gradients that it reaches.
+ * Errors as for eogp_rotate_heads, and EOGP_ERR_INVALID for more than 2^21 examples with per_example;
+ * EOGP_ERR_WORKSPACE if ws is too small. */
+size_t eogp_rotate_heads_backward_workspace_size(int64_t N, int64_t T, int64_t q_heads, int64_t k_heads, int64_t D,
+                                                 eogp_dtype dtype, int32_t norm, int64_t width,
+                                                 int32_t per_example);
+eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* dk, const eogp_heads* q,
+                                       const eogp_heads* k, eogp_dtype dtype, int64_t N, int64_t T, int64_t D,
+                                       int32_t norm, const void* q_weight, const void* k_weight,
+                                       eogp_dtype w_dtype, float eps, const float* table, int64_t table_positions,
+                                       int64_t width, int32_t interleaved, const int64_t* positions,
+                                       const uint8_t* token_mask, int32_t per_example, const eogp_heads* dq_in,
+                                       const eogp_heads* dk_in, float* dq_weight, float* dk_weight, void* ws,
+                                       size_t ws_bytes, void* stream);
+
+/* Softmax attention: out[i] = sum_j w_ij v[j], w_i = softmax over the keys that query i sees of scale q[i] . k[j].
+ * Query head h reads key head h / (heads of q / heads of k). With p = q_start[n] + i the query's position (q_start NULL:
+ * Tk - Tq + i, the last tokens of the keys) key j is seen if
+ *   k_mask[n, j] != 0 (or k_mask NULL),  j <= p if causal,  and  |p - j| < window or j < sinks if window > 0.
+ * A query that sees no key, and a masked one, gets zeros and a log-sum-exp of -inf.
+ *   q, out    [N, Tq, heads, D];  k, v [N, Tk, key heads, D], of `dtype`; out of `dtype` or fp32; it overlaps no input.
+ *   q_start   [N] int64 or NULL: chunks of new tokens and single ones over a cache whose rows from q_start[n] + Tq on
+ *             (causal) are not read, whatever they hold.
+ *   q_mask, k_mask  [N, Tq], [N, Tk] uint8 or NULL. Masked queries and keys count for nothing, whatever they hold; a
+ *             value that is not finite at a key that some query of the example sees may reach others of its queries.
+ *   lse       [N, Tq, heads of q] fp32: ln sum_j exp(scale q . k), for the backward pass, or NULL.
+ *   ws        eogp_attention_workspace_size bytes (0: none; NULL then), no fewer for more examples, queries, query heads
+ *             or keys.
+ * 16-bit weights enter the product with v rounded to `dtype` (their sum is that of the unrounded ones, fp32); fp32 runs
+ * in fp32 throughout. Errors: EOGP_ERR_INVALID for bad sizes (need key heads that divide the query heads; N * Tq * heads
+ * and N * Tk * key heads below 2^31), scale <= 0, window or sinks < 0, sinks without a window, NULL pointers;
+ * EOGP_ERR_UNSUPPORTED for D < 8 or D > 256 or another output type; EOGP_ERR_WORKSPACE if ws is too small. */
+size_t eogp_attention_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads, int64_t D,
+                                     eogp_dtype dtype);
+eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_heads* v, eogp_dtype dtype, int64_t N,
+                           int64_t Tq, int64_t Tk, int64_t D, float scale, int32_t causal, int64_t window,
+                           int64_t sinks, const int64_t* q_start, const uint8_t* q_mask, const uint8_t* k_mask,
+                           const eogp_heads* out, eogp_dtype out_dtype, float* lse, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* Its backward pass: with P the weights and dP = d_out v^T,
+ *   dv = P^T d_out,  dS = P (dP - rowsum(d_out out)),  dq = scale dS k,  dk = scale dS^T q,
+ * key heads summed over their query heads. Zeros at masked queries and keys and those that see, or are seen by, nothing.
+ *   d_out, dq, dk, dv  of `dtype`, shaped as out, q, k, v; the gradients overlap nothing else.
+ *   out, lse           of the forward pass (out of `dtype` or fp32), from the same arguments.
+ *   ws                 eogp_attention_backward_workspace_size bytes, no fewer for more examples, queries, heads or keys.
+ * Sums run in a fixed order. 16-bit weights and score gradients are rounded to `dtype` once, before the products that
+ * take them. Errors as for eogp_attention. */
+size_t eogp_attention_backward_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,
+                                              int64_t D, eogp_dtype dtype);
+eogp_status eogp_attention_backward(const eogp_heads* d_out, const eogp_heads* q, const eogp_heads* k,
+                                    const eogp_heads* v, eogp_dtype dtype, int64_t N, int64_t Tq, int64_t Tk,
+                                    int64_t D, float scale, int32_t causal, int64_t window, int64_t sinks,
+                                    const int64_t* q_start, const uint8_t* q_mask, const uint8_t* k_mask,
+                                    const eogp_heads* out, eogp_dtype out_dtype, const float* lse,
+                                    const eogp_heads* dq, const eogp_heads* dk, const eogp_heads* dv, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Kernel timing, for measurement harnesses. While enabled, each launch of a
  * kernel class below is bracketed by two HIP events recorded on the stream it
  * is launched on. eogp_timing_read waits for the recorded events of one class,
@@ -573,7 +699,9 @@ typedef enum {
   EOGP_KT_LAYER_NORM = 12,    /* layer norm, forward and backward                */
   EOGP_KT_XENT = 13,          /* cross-entropy and its gradient                  */
   EOGP_KT_SAMPLE = 14,        /* sampling                                        */
-  EOGP_KT_COUNT = 15
+  EOGP_KT_ROTARY = 15,        /* rotary tables, norms and rotation of heads      */
+  EOGP_KT_ATTENTION = 16,     /* attention, forward and backward                 */
+  EOGP_KT_COUNT = 17
 } eogp_kernel_class;
 eogp_status eogp_timing_enable(int32_t enable);
 eogp_status eogp_timing_read(int32_t kernel_class, double* total_ms, int64_t* launches);

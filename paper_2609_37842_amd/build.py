@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libeogp.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "timing.cpp", "select.hip", "gemm.hip", "retain.hip", "encode.hip", "score.hip",
-           "srht.hip", "pcafit.hip", "norm.hip", "embed.hip", "xent.hip", "sample.hip"]
+           "srht.hip", "pcafit.hip", "norm.hip", "embed.hip", "xent.hip", "sample.hip",
+           "rotary.hip", "attend.hip", "attend_back.hip"]
 # rocSOLVER (and its rocBLAS) serve the PCA fit's symmetric eigendecomposition.
 LIBS = ["-L/opt/rocm/lib", "-lrocsolver", "-lrocblas", "-Wl,-rpath,/opt/rocm/lib"]
 ARCH = "gfx950"

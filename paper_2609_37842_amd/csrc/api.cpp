@@ -84,6 +84,31 @@ int64_t sample_max_vocab();
 eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t n, int64_t V,
                           const float* uniforms, const uint8_t* mask, double temperature, int64_t top_k,
                           double top_p, double min_p, int64_t* out, hipStream_t s);
+eogp_status rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
+                         double high, double magnitude, float* table, hipStream_t s);
+int64_t rotate_max_row(int64_t D);
+eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype t, int norm, const void* qw,
+                         const void* kw, eogp_dtype wt, float eps, const float* table, int64_t positions, int64_t width,
+                         int interleaved, bool back, const int64_t* at, const uint8_t* mask, int64_t N, int64_t T_,
+                         int64_t D, hipStream_t s);
+size_t rotate_back_ws(eogp_dtype t, int norm, int64_t Hq, int64_t Hk, int64_t D, int64_t width, int64_t groups,
+                      int64_t tokens);
+eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, const eogp_heads* out, eogp_dtype t, int norm,
+                              const void* qw, const void* kw, eogp_dtype wt, float eps, const float* table,
+                              int64_t positions, int64_t width, int interleaved, const int64_t* at, const uint8_t* mask,
+                              int64_t N, int64_t T_, int64_t D, bool per_example, float* dqw, float* dkw, void* ws,
+                              hipStream_t s);
+size_t attention_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D);
+eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads& v, const eogp_heads& out,
+                      eogp_dtype t, eogp_dtype out_t, int64_t N, int64_t Tq, int64_t Tk, int64_t D, float scale,
+                      int causal, int64_t window, int64_t sinks, const int64_t* q_start, const uint8_t* q_mask,
+                      const uint8_t* k_mask, float* lse, void* ws, hipStream_t s);
+size_t attention_back_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D);
+eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eogp_heads& k, const eogp_heads& v,
+                           const eogp_heads& out, const eogp_heads& dq, const eogp_heads& dk, const eogp_heads& dv,
+                           eogp_dtype t, eogp_dtype out_t, int64_t N, int64_t Tq, int64_t Tk, int64_t D, float scale,
+                           int causal, int64_t window, int64_t sinks, const int64_t* q_start, const uint8_t* q_mask,
+                           const uint8_t* k_mask, const float* lse, void* ws, hipStream_t s);
 
 namespace {
 thread_local std::string g_last_error;
@@ -760,6 +785,254 @@ eogp_status eogp_sample_tokens(const void* logits, eogp_dtype dtype, int64_t ld_
   EOGP_CHECK(check_address(op, "tokens", tokens, 8));
   return sample_tokens(logits, dtype, ld_logits, n, V, uniforms, token_mask, temperature, top_k, top_p,
                        min_p, tokens, S(stream));
+}
+
+namespace {
+// Strides that the kernels multiply by indices below 2^31 without leaving 64 bits.
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+
+// A tensor of heads [N, T, heads, D] that a call reads or writes.
+eogp_status check_heads(const char* op, const char* what, const eogp_heads* x, int64_t heads, eogp_dtype t, int64_t N,
+                        int64_t T) {
+  if (!x) return fail(EOGP_ERR_INVALID, std::string(op) + ": NULL " + what);
+  if (x->heads != heads)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": " + what + " must have " + std::to_string(heads) + " heads");
+  for (int64_t ld : {x->ld_example, x->ld_token, x->ld_head})
+    if (ld < 0 || ld >= kMaxStride)
+      return fail(EOGP_ERR_INVALID, std::string(op) + ": strides of " + what + " outside [0, 2^40)");
+  if (N * T > 0 && heads > 0) {
+    if (!x->data) return fail(EOGP_ERR_INVALID, std::string(op) + ": NULL pointer (" + what + ")");
+    EOGP_CHECK(check_aligned(op, what, x->data, t));
+  }
+  return EOGP_OK;
+}
+
+// An output besides: its rows lie apart, in one order of the three strides or another.
+eogp_status check_out(const char* op, const char* what, const eogp_heads* x, int64_t heads, eogp_dtype t, int64_t N,
+                      int64_t T, int64_t D) {
+  EOGP_CHECK(check_heads(op, what, x, heads, t, N, T));
+  std::pair<int64_t, int64_t> axes[3] = {{x->ld_example, N}, {x->ld_token, T}, {x->ld_head, heads}};
+  std::sort(axes, axes + 3);
+  int64_t reach = D;                       // elements from the first to past the last of the axes before
+  if (N * T * heads == 0) return EOGP_OK;
+  for (const auto& [ld, count] : axes) {
+    if (count <= 1) continue;
+    if (ld < reach) return fail(EOGP_ERR_INVALID, std::string(op) + ": rows of " + what + " overlap");
+    if ((count - 1) >= ((int64_t)1 << 61) / ld)
+      return fail(EOGP_ERR_INVALID, std::string(op) + ": " + what + " is too large");
+    reach += (count - 1) * ld;
+  }
+  return EOGP_OK;
+}
+
+const eogp_heads kNoHeads = {nullptr, 0, 0, 0, 0};
+
+eogp_status check_batch(const char* op, int64_t N, int64_t T, int64_t heads) {
+  if (N < 0 || T < 0 || heads < 0 || N >= kMaxFlat || T >= kMaxFlat || heads >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": bad sizes");
+  if ((N > 0 && T >= kMaxFlat / N) || (N * T > 0 && heads >= kMaxFlat / (N * T)))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": examples x tokens x heads must be < 2^31");
+  return EOGP_OK;
+}
+
+eogp_status check_rotate(const char* op, eogp_dtype dtype, int64_t N, int64_t T, int64_t Hq, int64_t Hk, int64_t D,
+                         int32_t norm, const void* q_weight, const void* k_weight, eogp_dtype w_dtype, float eps,
+                         const float* table, int64_t table_positions, int64_t width, const int64_t* positions) {
+  if (!model_type(dtype) || !model_type(w_dtype))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": unknown element type");
+  if (w_dtype != dtype && w_dtype != EOGP_F32)
+    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": weights must have the heads' type or be fp32");
+  if (Hq < 1 || D < 1) return fail(EOGP_ERR_INVALID, std::string(op) + ": bad sizes");
+  if (D > 256) return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": D > 256 is not supported");
+  EOGP_CHECK(check_batch(op, N, T, Hq));
+  EOGP_CHECK(check_batch(op, N, T, Hk));
+  if (width < 0 || width % 2 || width > D)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": width must be even and at most D");
+  if (norm != EOGP_NORM_NONE && norm != EOGP_NORM_HEAD && norm != EOGP_NORM_ROW)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": unknown norm");
+  if (norm == EOGP_NORM_NONE && (q_weight || k_weight))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": weights without a norm");
+  if (norm != EOGP_NORM_NONE && (!(eps >= 0.f) || std::isinf(eps)))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": eps must be >= 0");
+  if (norm == EOGP_NORM_ROW && std::max(Hq, Hk) * D > rotate_max_row(D))
+    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": a norm over more than 8192 elements (2048 of heads below 8) is not supported");
+  if (table_positions < 0 || table_positions >= kMaxFlat)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": table positions outside [0, 2^31)");
+  if (width > 0 && table_positions > 0 && !table) return fail(EOGP_ERR_INVALID, std::string(op) + ": NULL table");
+  EOGP_CHECK(check_address(op, "table", table, 4));
+  EOGP_CHECK(check_address(op, "positions", positions, 8));
+  EOGP_CHECK(check_aligned(op, "q_weight", q_weight, w_dtype));
+  EOGP_CHECK(check_aligned(op, "k_weight", k_weight, w_dtype));
+  return EOGP_OK;
+}
+}  // namespace
+
+eogp_status eogp_rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
+                              double high, double magnitude, float* table, void* stream) {
+  const char* op = "rotary_table";
+  if (positions < 0 || positions >= kMaxFlat || width < 2 || width % 2 || width >= kMaxFlat / 64)
+    return fail(EOGP_ERR_INVALID, "rotary_table: need 0 <= positions < 2^31 and an even width >= 2");
+  for (double v : {base, factor, original, low, high, magnitude})
+    if (!std::isfinite(v)) return fail(EOGP_ERR_INVALID, "rotary_table: values must be finite");
+  if (!(base > 0.0) || !(factor > 0.0) || original < 0.0 || !(high > low))
+    return fail(EOGP_ERR_INVALID, "rotary_table: need base > 0, factor > 0, original >= 0 and high > low");
+  if (positions == 0) return EOGP_OK;
+  if (!table) return fail(EOGP_ERR_INVALID, "rotary_table: NULL pointer");
+  EOGP_CHECK(check_address(op, "table", table, 4));
+  return rotary_table(positions, width, base, factor, original, low, high, magnitude, table, S(stream));
+}
+
+eogp_status eogp_rotate_heads(const eogp_heads* q, const eogp_heads* k, eogp_dtype dtype, int64_t N, int64_t T,
+                              int64_t D, int32_t norm, const void* q_weight, const void* k_weight,
+                              eogp_dtype w_dtype, float eps, const float* table, int64_t table_positions,
+                              int64_t width, int32_t interleaved, const int64_t* positions,
+                              const uint8_t* token_mask, const eogp_heads* q_out, const eogp_heads* k_out,
+                              void* stream) {
+  const char* op = "rotate_heads";
+  if (!q) return fail(EOGP_ERR_INVALID, "rotate_heads: NULL q");
+  const eogp_heads in[2] = {*q, k ? *k : kNoHeads};
+  EOGP_CHECK(check_rotate(op, dtype, N, T, in[0].heads, in[1].heads, D, norm, q_weight, k_weight, w_dtype, eps, table,
+                          table_positions, width, positions));
+  EOGP_CHECK(check_heads(op, "q", &in[0], in[0].heads, dtype, N, T));
+  EOGP_CHECK(check_heads(op, "k", &in[1], in[1].heads, dtype, N, T));
+  const eogp_heads out[2] = {q_out ? *q_out : kNoHeads, k_out ? *k_out : kNoHeads};
+  EOGP_CHECK(check_out(op, "q_out", &out[0], in[0].heads, dtype, N, T, D));
+  EOGP_CHECK(check_out(op, "k_out", &out[1], in[1].heads, dtype, N, T, D));
+  return rotate_heads(in, out, dtype, norm, q_weight, k_weight, w_dtype, eps, table, table_positions, width,
+                      interleaved != 0, false, positions, token_mask, N, T, D, S(stream));
+}
+
+size_t eogp_rotate_heads_backward_workspace_size(int64_t N, int64_t T, int64_t q_heads, int64_t k_heads, int64_t D,
+                                                 eogp_dtype dtype, int32_t norm, int64_t width,
+                                                 int32_t per_example) {
+  if (norm == EOGP_NORM_NONE || (per_example && (N < 1 || N > kMaxGroups))) return 0;
+  if (check_rotate("rotate_heads_backward", dtype, N, T, q_heads, k_heads, D, norm, nullptr, nullptr, EOGP_F32, 0.f,
+                   nullptr, 0, width, nullptr) != EOGP_OK)
+    return 0;
+  return rotate_back_ws(dtype, norm, q_heads, k_heads, D, width, per_example ? N : 1, per_example ? T : N * T);
+}
+
+eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* dk, const eogp_heads* q,
+                                       const eogp_heads* k, eogp_dtype dtype, int64_t N, int64_t T, int64_t D,
+                                       int32_t norm, const void* q_weight, const void* k_weight,
+                                       eogp_dtype w_dtype, float eps, const float* table, int64_t table_positions,
+                                       int64_t width, int32_t interleaved, const int64_t* positions,
+                                       const uint8_t* token_mask, int32_t per_example, const eogp_heads* dq_in,
+                                       const eogp_heads* dk_in, float* dq_weight, float* dk_weight, void* ws,
+                                       size_t ws_bytes, void* stream) {
+  const char* op = "rotate_heads_backward";
+  if (!dq) return fail(EOGP_ERR_INVALID, "rotate_heads_backward: NULL dq");
+  const eogp_heads grad[2] = {*dq, dk ? *dk : kNoHeads};
+  EOGP_CHECK(check_rotate(op, dtype, N, T, grad[0].heads, grad[1].heads, D, norm, q_weight, k_weight, w_dtype, eps,
+                          table, table_positions, width, positions));
+  EOGP_CHECK(check_heads(op, "dq", &grad[0], grad[0].heads, dtype, N, T));
+  EOGP_CHECK(check_heads(op, "dk", &grad[1], grad[1].heads, dtype, N, T));
+  const eogp_heads out[2] = {dq_in ? *dq_in : kNoHeads, dk_in ? *dk_in : kNoHeads};
+  EOGP_CHECK(check_out(op, "dq_in", &out[0], grad[0].heads, dtype, N, T, D));
+  EOGP_CHECK(check_out(op, "dk_in", &out[1], grad[1].heads, dtype, N, T, D));
+  if (norm == EOGP_NORM_NONE) {
+    if (dq_weight || dk_weight) return fail(EOGP_ERR_INVALID, "rotate_heads_backward: weight gradients without a norm");
+    return rotate_heads(grad, out, dtype, norm, nullptr, nullptr, w_dtype, 0.f, table, table_positions, width,
+                        interleaved != 0, true, positions, token_mask, N, T, D, S(stream));
+  }
+  const eogp_heads in[2] = {q ? *q : kNoHeads, k ? *k : kNoHeads};
+  EOGP_CHECK(check_heads(op, "q", &in[0], grad[0].heads, dtype, N, T));
+  EOGP_CHECK(check_heads(op, "k", &in[1], grad[1].heads, dtype, N, T));
+  EOGP_CHECK(check_address(op, "dq_weight", dq_weight, 4));
+  EOGP_CHECK(check_address(op, "dk_weight", dk_weight, 4));
+  EOGP_CHECK(check_address(op, "ws", ws, 4));
+  if (per_example && N > kMaxGroups)
+    return fail(EOGP_ERR_INVALID, "rotate_heads_backward: at most 2^21 examples with gradients of their own");
+  if ((N > 0 || !per_example) && (!ws || ws_bytes < rotate_back_ws(dtype, norm, grad[0].heads, grad[1].heads, D, width,
+                                                 per_example ? N : 1, per_example ? T : N * T)))
+    return fail(EOGP_ERR_WORKSPACE, "rotate_heads_backward: workspace too small");
+  return rotate_heads_back(in, grad, out, dtype, norm, q_weight, k_weight, w_dtype, eps, table, table_positions, width,
+                           interleaved != 0, positions, token_mask, N, T, D, per_example != 0, dq_weight, dk_weight, ws,
+                           S(stream));
+}
+
+namespace {
+eogp_status check_attention(const char* op, int64_t Hq, int64_t Hkv, eogp_dtype dtype, eogp_dtype out_dtype, int64_t N,
+                            int64_t Tq, int64_t Tk, int64_t D, float scale, int64_t window, int64_t sinks) {
+  if (!model_type(dtype) || !model_type(out_dtype))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": unknown element type");
+  if (out_dtype != dtype && out_dtype != EOGP_F32)
+    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": out must have the type of q or be fp32");
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv)
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": the heads of k must divide those of q");
+  if (D < 1) return fail(EOGP_ERR_INVALID, std::string(op) + ": bad sizes");
+  if (D < 8 || D > 256) return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": D outside [8, 256] is not supported");
+  EOGP_CHECK(check_batch(op, N, Tq, Hq));
+  EOGP_CHECK(check_batch(op, N, Tk, Hkv));
+  EOGP_CHECK(check_batch(op, N, 1, Hq));
+  if (!(scale > 0.f) || std::isinf(scale)) return fail(EOGP_ERR_INVALID, std::string(op) + ": scale must be > 0");
+  if (window < 0 || sinks < 0 || (sinks > 0 && window == 0))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": need window >= 0, and sinks >= 0 with a window only");
+  return EOGP_OK;
+}
+}  // namespace
+
+size_t eogp_attention_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads, int64_t D,
+                                     eogp_dtype dtype) {
+  if (check_attention("attention", q_heads, k_heads, dtype, dtype, N, Tq, Tk, D, 1.f, 0, 0) != EOGP_OK) return 0;
+  return attention_ws(dtype, N, Tq, Tk, q_heads, k_heads, D);
+}
+
+eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_heads* v, eogp_dtype dtype, int64_t N,
+                           int64_t Tq, int64_t Tk, int64_t D, float scale, int32_t causal, int64_t window,
+                           int64_t sinks, const int64_t* q_start, const uint8_t* q_mask, const uint8_t* k_mask,
+                           const eogp_heads* out, eogp_dtype out_dtype, float* lse, void* ws, size_t ws_bytes,
+                           void* stream) {
+  const char* op = "attention";
+  if (!q || !k) return fail(EOGP_ERR_INVALID, "attention: NULL q or k");
+  EOGP_CHECK(check_attention(op, q->heads, k->heads, dtype, out_dtype, N, Tq, Tk, D, scale, window, sinks));
+  EOGP_CHECK(check_heads(op, "q", q, q->heads, dtype, N, Tq));
+  EOGP_CHECK(check_heads(op, "k", k, k->heads, dtype, N, Tk));
+  EOGP_CHECK(check_heads(op, "v", v, k->heads, dtype, N, Tk));
+  EOGP_CHECK(check_out(op, "out", out, q->heads, out_dtype, N, Tq, D));
+  EOGP_CHECK(check_address(op, "q_start", q_start, 8));
+  EOGP_CHECK(check_address(op, "lse", lse, 4));
+  EOGP_CHECK(check_address(op, "ws", ws, 4));
+  if (N == 0 || Tq == 0) return EOGP_OK;
+  const size_t need = attention_ws(dtype, N, Tq, Tk, q->heads, k->heads, D);
+  if (need > 0 && (!ws || ws_bytes < need)) return fail(EOGP_ERR_WORKSPACE, "attention: workspace too small");
+  return attention(*q, *k, *v, *out, dtype, out_dtype, N, Tq, Tk, D, scale, causal != 0, window, sinks, q_start, q_mask,
+                   k_mask, lse, ws, S(stream));
+}
+
+size_t eogp_attention_backward_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,
+                                              int64_t D, eogp_dtype dtype) {
+  if (check_attention("attention_backward", q_heads, k_heads, dtype, dtype, N, Tq, Tk, D, 1.f, 0, 0) != EOGP_OK) return 0;
+  return N == 0 ? 0 : attention_back_ws(dtype, N, Tq, Tk, q_heads, k_heads, D);
+}
+
+eogp_status eogp_attention_backward(const eogp_heads* d_out, const eogp_heads* q, const eogp_heads* k,
+                                    const eogp_heads* v, eogp_dtype dtype, int64_t N, int64_t Tq, int64_t Tk,
+                                    int64_t D, float scale, int32_t causal, int64_t window, int64_t sinks,
+                                    const int64_t* q_start, const uint8_t* q_mask, const uint8_t* k_mask,
+                                    const eogp_heads* out, eogp_dtype out_dtype, const float* lse,
+                                    const eogp_heads* dq, const eogp_heads* dk, const eogp_heads* dv, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  const char* op = "attention_backward";
+  if (!q || !k) return fail(EOGP_ERR_INVALID, "attention_backward: NULL q or k");
+  EOGP_CHECK(check_attention(op, q->heads, k->heads, dtype, out_dtype, N, Tq, Tk, D, scale, window, sinks));
+  EOGP_CHECK(check_heads(op, "d_out", d_out, q->heads, dtype, N, Tq));
+  EOGP_CHECK(check_heads(op, "q", q, q->heads, dtype, N, Tq));
+  EOGP_CHECK(check_heads(op, "k", k, k->heads, dtype, N, Tk));
+  EOGP_CHECK(check_heads(op, "v", v, k->heads, dtype, N, Tk));
+  EOGP_CHECK(check_heads(op, "out", out, q->heads, out_dtype, N, Tq));
+  EOGP_CHECK(check_out(op, "dq", dq, q->heads, dtype, N, Tq, D));
+  EOGP_CHECK(check_out(op, "dk", dk, k->heads, dtype, N, Tk, D));
+  EOGP_CHECK(check_out(op, "dv", dv, k->heads, dtype, N, Tk, D));
+  EOGP_CHECK(check_address(op, "q_start", q_start, 8));
+  EOGP_CHECK(check_address(op, "lse", lse, 4));
+  EOGP_CHECK(check_address(op, "ws", ws, 4));
+  if (N == 0) return EOGP_OK;
+  if (Tq > 0 && !lse) return fail(EOGP_ERR_INVALID, "attention_backward: NULL lse");
+  if (!ws || ws_bytes < attention_back_ws(dtype, N, Tq, Tk, q->heads, k->heads, D))
+    return fail(EOGP_ERR_WORKSPACE, "attention_backward: workspace too small");
+  return attention_back(*d_out, *q, *k, *v, *out, *dq, *dk, *dv, dtype, out_dtype, N, Tq, Tk, D, scale, causal != 0,
+                        window, sinks, q_start, q_mask, k_mask, lse, ws, S(stream));
 }
 
 }  // extern "C"

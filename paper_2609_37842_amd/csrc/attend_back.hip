@@ -1,0 +1,542 @@
+// The gradients of attention at queries, keys and values.
+#include <algorithm>
+
+#include "attend.h"
+#include "timing.h"
+
+namespace eogp {
+namespace {
+
+template <typename T>
+struct BackArgs {
+  Heads<const T> q, k, v, dout;
+  const void* out;                // the forward pass's output, rows of T or fp32
+  int64_t out_n, out_t, out_h;
+  int out_f32;
+  Heads<T> dq, dk, dv;
+  Sight sight;
+  int N, Hq, Hkv, D;
+  Divide by_group;                // query heads of a key head
+  float scale, scale_log2;
+  const float* lse;               // [N, Tq, Hq]
+  float *lse2, *delta;            // [N, Tq, Hq]: log-sum-exp in powers of two (+inf: the row counts for nothing), dout . out
+  uint32_t* norms;                // fp16: [N Hkv][2] largest squared norms of a row of dout and of v, as bits
+  int row_tiles, key_tiles, splits;
+  float* part;                    // splits > 1: [splits][N Hkv][Tk][2][D]
+};
+
+// Weights times 2^kLiftBack: fp16 holds small ones as precisely as large ones. (Weights are at most 1.)
+template <typename T> constexpr float kLiftBack = 0.f;
+template <> constexpr float kLiftBack<_Float16> = 15.f;
+
+// fp16 score gradients P (dP - delta) are small where many keys share a row, and lie below fp16's normal range where
+// the output gradients are small as well. They are held times 2^e, e from |dP - delta| <= 2 max |dout row| max |v row|
+// of the key head's rows, so that none passes 2^14.
+template <typename T>
+__device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit) {
+  if constexpr (sizeof(T) == 4 || kLiftBack<T> == 0.f) return 0;
+  const float bound = 2.f * sqrtf(__uint_as_float(a.norms[2 * unit])) * sqrtf(__uint_as_float(a.norms[2 * unit + 1]));
+  if (!(bound > 0.f) || isinf(bound)) return 0;
+  const int e = 14 - (ilogbf(bound) + 1);
+  return e < -100 ? -100 : e > 100 ? 100 : e;
+}
+
+__device__ __forceinline__ float sum_of(float v, int lanes) {
+  for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
+
+__global__ __launch_bounds__(256) void k_attend_zero(uint32_t* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
+// delta = dout . out of each row, its log-sum-exp in powers of two, and (fp16) the largest norms of rows of dout,
+// then of v. A row takes `lanes` lanes, 16 bytes each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_delta(const BackArgs<T> a, int lanes, int64_t rows, int of_v) {
+  constexpr int E = kPiece<T>;
+  const int lane = threadIdx.x & 63, per = 64 / lanes, c = (lane % lanes) * E;
+  const int H = of_v ? a.Hkv : a.Hq, Tn = of_v ? a.sight.Tk : a.sight.Tq;
+  for (int64_t id0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * per; id0 < rows; id0 += (int64_t)gridDim.x * 4 * per) {
+    const int64_t id = id0 + lane / lanes;
+    const bool in = id < rows;
+    const int64_t rc = in ? id : rows - 1;
+    const int hq = (int)(rc % H);
+    const int64_t i = rc / H % Tn, n = rc / H / Tn;
+    const uint8_t* mask = of_v ? a.sight.k_mask : a.sight.q_mask;
+    bool live = in && (!mask || mask[n * Tn + i]);
+    float dot = 0.f, square = 0.f;
+    if (of_v) {
+      if (live) {
+        float x[E];
+        load_piece<T, E>(a.v.row(n, i, hq), c, a.D, 0.f, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) square += x[e] * x[e];
+      }
+    } else {
+      const float s = in ? a.lse[id] : 0.f;
+      live = live && s != -INFINITY;
+      if (live) {
+        float x[E], y[E];
+        load_piece<T, E>(a.dout.row(n, i, hq), c, a.D, 0.f, x);
+        const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h;
+        if (a.out_f32)
+          load_piece<float, E>(static_cast<const float*>(a.out) + at, c, a.D, 0.f, y);
+        else
+          load_piece<T, E>(static_cast<const T*>(a.out) + at, c, a.D, 0.f, y);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          dot += x[e] * y[e];
+          square += x[e] * x[e];
+        }
+      }
+      dot = sum_of(dot, lanes);
+      if (in && lane % lanes == 0) {
+        a.delta[id] = live ? dot : 0.f;
+        a.lse2[id] = live ? s * 1.4426950408889634f : INFINITY;
+      }
+    }
+    if constexpr (kLiftBack<T> != 0.f) {
+      square = sum_of(square, lanes);
+      const int unit = (int)(n * a.Hkv) + hq / (H / a.Hkv);
+      // (the largest of a set does not depend on the order; a key that no query sees only makes the bound larger)
+      if (live && lane % lanes == 0) atomicMax(a.norms + 2 * unit + of_v, __float_as_uint(square == square ? square : 0.f));
+    }
+  }
+}
+
+// Gradients of keys and values: a wave has 32 keys, their rows of K and V and both gradients in registers; the
+// block's waves share tiles of 32 rows of queries and output gradients, over all query heads of the key head.
+// PARTS: 1 gradients of V, 2 of K, 3 both.
+template <typename T, int DP, int NW, int PARTS>
+__global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a) {
+  constexpr int NT = 64 * NW, kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+  constexpr int kKs = 32 / (2 * kPiece<T>);
+  constexpr bool kV = PARTS & 1, kK = PARTS & 2;
+  extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
+  __shared__ __align__(16) float row_f[2][2][RB];        // lse2, delta
+  __shared__ __align__(16) int row_i[2][3][RB];          // spans
+  __shared__ int slot[NW];
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+  const int units = a.N * a.Hkv, G = a.Hq / a.Hkv;
+  int b = blockIdx.x;
+  const int split = b % a.splits;
+  b /= a.splits;
+  const int unit = b % units, tile_key = b / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
+  const int64_t start = a.sight.start(n);
+  const int k0 = tile_key * 32 * NW, j0 = k0 + wid * 32, j = j0 + l;
+  const int k1 = min(k0 + 32 * NW, a.sight.Tk);
+  const bool key_live = j < a.sight.Tk && (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
+  const uint32_t key_bits = (uint32_t)__ballot(key_live);
+
+  // queries that can see one of the block's keys
+  constexpr int64_t kFar = (int64_t)1 << 40;
+  const int64_t st = start < -kFar ? -kFar : start > kFar ? kFar : start;
+  const bool sink = k0 < a.sight.sinks;
+  int64_t i_lo = a.sight.causal ? k0 - st : a.sight.window && !sink ? k0 - a.sight.window + 1 - st : 0;
+  int64_t i_hi = a.sight.window && !sink ? (int64_t)k1 - 1 + a.sight.window - st : a.sight.Tq;
+  int i0 = clamp_key(i_lo, a.sight.Tq), i1 = clamp_key(i_hi, a.sight.Tq);
+  const int any = __syncthreads_or(key_bits != 0);
+  if (!any) i1 = i0;
+  if (a.sight.q_mask && i0 < i1) {
+    const int2 r = set_range<NT>(a.sight.q_mask + (int64_t)n * a.sight.Tq, i0, i1, slot);
+    i0 = r.x;
+    i1 = r.y;
+  }
+  const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
+  int t = (int)((int64_t)row_tiles * split / a.splits);
+  const int t_end = (int)((int64_t)row_tiles * (split + 1) / a.splits);
+
+  RowPieces<T, DP> kf, vf;
+  const int jc = min(j, a.sight.Tk - 1);
+  kf.load(a.k.row(n, jc, kvh), key_live, a.D);
+  if constexpr (kK) vf.load(a.v.row(n, jc, kvh), key_live, a.D);
+  f32x16 dv[kV ? kDt : 1], dk[kK ? kDt : 1];
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt) {
+    if constexpr (kV) dv[dt] = zeros16();
+    if constexpr (kK) dk[dt] = zeros16();
+  }
+  const int lift = lift_of(a, unit);
+  const float ds_by = exp2f((float)lift - kLiftBack<T>);
+
+  Stage<T, DP, RB, NT> qs, os;
+  float r_lse2 = 0.f, r_delta = 0.f;
+  Span r_span{0, 0, 0};
+  bool r_live = false;
+  auto request = [&](int tile) {
+    const int r0 = rows_lo + tile * RB;
+    auto at = [&](const Heads<const T>& x) {
+      return [=](int r) {
+        const int row = min(r0 + r, rows_hi - 1);
+        const int i = a.by_group.quotient(row);
+        return x.row(n, i, kvh * G + a.by_group.rest(row, i));
+      };
+    };
+    qs.request(threadIdx.x, a.D, at(a.q));
+    os.request(threadIdx.x, a.D, at(a.dout));
+    const int row = r0 + l, rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
+    const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + kvh * G + a.by_group.rest(rc, i);
+    r_lse2 = row < rows_hi ? a.lse2[id] : INFINITY;
+    r_delta = a.delta[id];
+    r_live = r_lse2 != INFINITY;
+    r_span = span_of(a.sight, start + i);
+  };
+  if (t < t_end) request(t);
+  for (int turn = 0; t < t_end; ++t, turn ^= 1) {
+    char *qt = lds + turn * 2 * kTile, *ot = qt + kTile;
+    const uint64_t live = __ballot(r_live) & 0xFFFFFFFFull;
+    const int r0 = rows_lo + t * RB;
+    qs.store(threadIdx.x, a.D, qt, live);
+    os.store(threadIdx.x, a.D, ot, live);
+    if (threadIdx.x < RB) {
+      row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
+      row_f[turn][1][l] = r_delta;
+      row_i[turn][0][l] = r_span.lo;
+      row_i[turn][1][l] = r_span.hi;
+      row_i[turn][2][l] = r_span.sk;
+    }
+    __syncthreads();
+    if (t + 1 < t_end) request(t + 1);
+    if (live == 0 || key_bits == 0) continue;
+    const int last = min(r0 + RB, rows_hi) - 1;
+    const bool full = key_bits == 0xFFFFFFFFu && j0 >= span_of(a.sight, start + a.by_group.quotient(last)).lo &&
+                      j0 + 32 <= span_of(a.sight, start + a.by_group.quotient(r0)).hi;
+
+    f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      mma(s, row_frag<T, kROWB>(qt, l, k), kf.f[k]);
+      if constexpr (kK) mma(dp, row_frag<T, kROWB>(ot, l, k), vf.f[k]);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&row_f[turn][0][8 * g + 4 * h]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + i], a.scale_log2, -lse2[i]));
+    }
+    if (!full) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const i32x4 lo = *reinterpret_cast<const i32x4*>(&row_i[turn][0][8 * g + 4 * h]);
+        const i32x4 hi = *reinterpret_cast<const i32x4*>(&row_i[turn][1][8 * g + 4 * h]);
+        const i32x4 sk = *reinterpret_cast<const i32x4*>(&row_i[turn][2][8 * g + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // (dP as well: a key that the row does not see may hold anything)
+          const bool seen = key_live & sees(Span{lo[i], hi[i], sk[i]}, j);
+          s[4 * g + i] = seen ? s[4 * g + i] : 0.f;
+          dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+        }
+      }
+    }
+    if constexpr (kV) {
+      Frag<T> p[kKs];
+#pragma unroll
+      for (int k = 0; k < kKs; ++k) p[k] = acc_frag<T>(s, k);
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) mma(dv[dt], col_frag<T, kROWB>(ot, 0, k, dt), p[k]);
+    }
+    if constexpr (kK) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 delta = *reinterpret_cast<const f32x4*>(&row_f[turn][1][8 * g + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float d = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
+          if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
+          dp[4 * g + i] = d;
+        }
+      }
+      Frag<T> p[kKs];
+#pragma unroll
+      for (int k = 0; k < kKs; ++k) p[k] = acc_frag<T>(dp, k);
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) mma(dk[dt], col_frag<T, kROWB>(qt, 0, k, dt), p[k]);
+    }
+  }
+
+  if (j >= a.sight.Tk) return;
+  const float by_v = exp2f(-kLiftBack<T>), by_k = a.scale * exp2f(-(float)lift);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (!(which ? kK : kV)) continue;
+    const Heads<T>& to = which ? a.dk : a.dv;
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = dt * 32 + 8 * g + 4 * h;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (PARTS == 1) v[i] = dv[dt][4 * g + i] * by_v;
+          else if constexpr (PARTS == 2) v[i] = dk[dt][4 * g + i] * by_k;
+          else v[i] = which ? dk[dt][4 * g + i] * by_k : dv[dt][4 * g + i] * by_v;
+          if (!key_live) v[i] = 0.f;
+        }
+        if (a.part)
+          store_piece<float, 4>(a.part + ((((int64_t)split * units + unit) * a.sight.Tk + j) * 2 + which) * a.D, c, a.D, v);
+        else
+          store_piece<T, 4>(to.row(n, j, kvh), c, a.D, v);
+      }
+  }
+}
+
+// Sums of the splits' parts in their order, one element of both gradients per thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
+  const int64_t units = (int64_t)a.N * a.Hkv, all = units * a.sight.Tk * 2 * a.D;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += a.part[s * all + id];
+    const int c = (int)(id % a.D), which = (int)(id / a.D % 2);
+    const int64_t row = id / a.D / 2, j = row % a.sight.Tk, unit = row / a.sight.Tk;
+    (which ? a.dk : a.dv).row(unit / a.Hkv, j, unit % a.Hkv)[c] = (T)v;
+  }
+}
+
+// Gradients of queries: a wave has 32 rows of queries, output gradients and the result in registers; the block's
+// waves share tiles of keys and values.
+template <typename T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) {
+  constexpr int NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+  constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
+  extern __shared__ __align__(16) char lds[];            // [2][K, V]
+  __shared__ int slot[NW], all[3][NW];
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+  const int units = a.N * a.Hkv, G = a.Hq / a.Hkv, rows = G * a.sight.Tq;
+  const int unit = blockIdx.x % units, tile_row = a.row_tiles - 1 - blockIdx.x / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
+  const int64_t start = a.sight.start(n);
+  const int r = tile_row * kRows + wid * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
+            hq = kvh * G + a.by_group.rest(rc, i);
+  const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + hq;
+  const float lse2 = r < rows ? a.lse2[id] : INFINITY, delta = a.delta[id];
+  const bool live = lse2 != INFINITY;
+  const Span span = live ? span_of(a.sight, start + i) : Span{0, 0, 0};
+  Bounds bd;
+  bd.lo_min = wave_min_i(span.hi > span.lo ? span.lo : a.sight.Tk);
+  bd.hi_max = wave_max_i(span.hi > span.lo ? span.hi : 0);
+  bd.sk_max = wave_max_i(span.sk);
+  bd.lo_max = wave_max_i(span.lo);
+  bd.hi_min = wave_min_i(live ? span.hi : a.sight.Tk);
+  if (lane == 0) {
+    all[0][wid] = bd.lo_min;
+    all[1][wid] = bd.hi_max;
+    all[2][wid] = bd.sk_max;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    bd.lo_min = min(bd.lo_min, all[0][w]);
+    bd.hi_max = max(bd.hi_max, all[1][w]);
+    bd.sk_max = max(bd.sk_max, all[2][w]);
+  }
+  const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
+  if (kmask) {
+    const int from = bd.sk_max > 0 ? 0 : bd.lo_min, to = max(bd.hi_max, bd.sk_max);
+    const int2 m = set_range<NT>(kmask, min(from, to), to, slot);
+    bd.lo_min = max(bd.lo_min, m.x);
+    bd.hi_max = min(bd.hi_max, m.y);
+    bd.sk_max = bd.sk_max > m.x ? min(bd.sk_max, m.y) : 0;
+  }
+  const Tiles tiles = tiles_of(bd, KB);
+
+  RowPieces<T, DP> q, o;
+  q.load(a.q.row(n, i, hq), live, a.D);
+  o.load(a.dout.row(n, i, hq), live, a.D);
+  f32x16 dq[kDt];
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt) dq[dt] = zeros16();
+  const int lift = lift_of(a, unit);
+  const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
+
+  const T *kbase = a.k.row(n, 0, kvh), *vbase = a.v.row(n, 0, kvh);
+  Stage<T, DP, KB, NT> ks, vs;
+  bool key_live = false;
+  auto request = [&](int tile) {
+    const int j0 = tile * KB;
+    auto at = [&](const T* base, int64_t ld) {
+      return [=](int row) { return base + (int64_t)min(j0 + row, a.sight.Tk - 1) * ld; };
+    };
+    ks.request(threadIdx.x, a.D, at(kbase, a.k.ld_t));
+    vs.request(threadIdx.x, a.D, at(vbase, a.v.ld_t));
+    const int j = j0 + l;
+    key_live = ((j >= bd.lo_min && j < bd.hi_max) || j < bd.sk_max) && (!kmask || kmask[j]);
+  };
+  if (tiles.count > 0) request(tiles.at(0));
+  for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= 1) {
+    char *kt = lds + turn * 2 * kTile, *vt = kt + kTile;
+    const uint64_t bits = __ballot(key_live) & 0xFFFFFFFFull;
+    const int j0 = tiles.at(t) * KB;
+    ks.store(threadIdx.x, a.D, kt, bits);
+    vs.store(threadIdx.x, a.D, vt, bits);
+    __syncthreads();
+    if (t + 1 < tiles.count) request(tiles.at(t + 1));
+    if (bits == 0) continue;
+    f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      mma(s, row_frag<T, kROWB>(kt, l, k), q.f[k]);
+      mma(dp, row_frag<T, kROWB>(vt, l, k), o.f[k]);
+    }
+    const bool full = bits == 0xFFFFFFFFull && j0 >= bd.lo_max && j0 + KB <= bd.hi_min;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref));
+      if (!full) {
+        const int at = 8 * (e / 4) + 4 * h + e % 4;
+        p = ((bool)((bits >> at) & 1) & sees(span, j0 + at)) ? p : 0.f;
+      }
+      float d = p * (dp[e] - delta);
+      if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
+      s[e] = d;
+    }
+    Frag<T> ds[kKs];
+#pragma unroll
+    for (int k = 0; k < kKs; ++k) ds[k] = acc_frag<T>(s, k);
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+      for (int k = 0; k < kKs; ++k) mma(dq[dt], col_frag<T, kROWB>(kt, 0, k, dt), ds[k]);
+  }
+  if (r >= rows) return;
+  const float by = a.scale * exp2f(-(float)lift);
+  T* to = a.dq.row(n, i, hq);
+#pragma unroll
+  for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = live ? dq[dt][4 * g + e] * by : 0.f;
+      store_piece<T, 4>(to, dt * 32 + 8 * g + 4 * h, a.D, v);
+    }
+}
+
+constexpr int kBackWaves = 4;
+constexpr int64_t kSplitBlocks = 4 * kCus;
+
+// Workers that share a key tile's rows: as many as fill the chip a few times over, none with fewer than 8 tiles.
+int back_splits(int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv) {
+  const int64_t blocks = N * Hkv * ceil_div(Tk, 32 * kBackWaves), tiles = ceil_div(Hq / Hkv * Tq, 32);
+  return (int)std::min<int64_t>(std::max<int64_t>(1, tiles / 8), std::max<int64_t>(1, kSplitBlocks / std::max<int64_t>(1, blocks)));
+}
+
+}  // namespace
+
+// Bytes for any call of up to N examples, Tq queries and Tk keys: launches with several workers a key tile have at most
+// kSplitBlocks blocks, and a worker has no fewer than 8 tiles of 32 rows.
+size_t attention_back_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
+  size_t bytes = 2 * align256((size_t)(N * Tq * Hq) * sizeof(float)) + 256;
+  if (t == EOGP_F16) bytes += align256((size_t)(2 * N * Hkv) * sizeof(float));
+  const int64_t most = ceil_div(Hq / Hkv * Tq, 32) / 8;
+  if (most > 1)
+    bytes += align256((size_t)std::min(most * (N * Hkv * Tk), kSplitBlocks * 32 * kBackWaves) * (2 * D) * sizeof(float));
+  return bytes;
+}
+
+eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eogp_heads& k, const eogp_heads& v,
+                           const eogp_heads& out, const eogp_heads& dq, const eogp_heads& dk, const eogp_heads& dv,
+                           eogp_dtype t, eogp_dtype out_t, int64_t N, int64_t Tq, int64_t Tk, int64_t D, float scale,
+                           int causal, int64_t window, int64_t sinks, const int64_t* q_start, const uint8_t* q_mask,
+                           const uint8_t* k_mask, const float* lse, void* ws, hipStream_t s) {
+  if (N == 0) return EOGP_OK;
+  const int64_t Hq = q.heads, Hkv = k.heads, units = N * Hkv;
+  timing::Scope ts(EOGP_KT_ATTENTION, s);
+  return with_type(t, [&](auto el) {
+    using T = decltype(el);
+    BackArgs<T> a{};
+    auto in = [](const eogp_heads& x) {
+      return Heads<const T>{static_cast<const T*>(x.data), x.ld_example, x.ld_token, x.ld_head};
+    };
+    a.q = in(q);
+    a.k = in(k);
+    a.v = in(v);
+    a.dout = in(dout);
+    a.out = out.data;
+    a.out_n = out.ld_example;
+    a.out_t = out.ld_token;
+    a.out_h = out.ld_head;
+    a.out_f32 = out_t == EOGP_F32;
+    a.dq = heads_of<T>(dq);
+    a.dk = heads_of<T>(dk);
+    a.dv = heads_of<T>(dv);
+    a.sight = Sight{causal, (int)std::min<int64_t>(window, 1 << 30), (int)std::min<int64_t>(sinks, 1 << 30), (int)Tq, (int)Tk,
+                    q_start, q_mask, k_mask};
+    a.N = (int)N;
+    a.Hq = (int)Hq;
+    a.Hkv = (int)Hkv;
+    a.D = (int)D;
+    a.by_group = Divide(Hq / Hkv);
+    a.scale = scale;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.lse = lse;
+    a.splits = back_splits(N, Tq, Tk, Hq, Hkv);
+    a.key_tiles = (int)ceil_div(Tk, 32 * kBackWaves);
+    a.row_tiles = (int)ceil_div(Hq / Hkv * Tq, 32 * kBackWaves);
+    Carve w(ws, ~(size_t)0);
+    a.lse2 = w.take<float>(N * Tq * Hq);
+    a.delta = w.take<float>(N * Tq * Hq);
+    if (t == EOGP_F16) a.norms = w.take<uint32_t>(2 * units);
+    a.part = a.splits > 1 ? w.take<float>((size_t)a.splits * (units * Tk * 2 * D)) : nullptr;
+
+    int lanes = 1;
+    while (lanes * kPiece<T> < D) lanes *= 2;
+    const int64_t rows = N * Tq * Hq, keys = N * Tk * Hkv;
+    auto delta_blocks = [&](int64_t n) { return dim3((unsigned)std::min<int64_t>(ceil_div(n * lanes, 256), 16 * kCus)); };
+    if (t == EOGP_F16) {
+      hipLaunchKernelGGL(k_attend_zero, dim3((unsigned)std::min<int64_t>(ceil_div(2 * units, 256), 4 * kCus)), dim3(256), 0, s,
+                         a.norms, 2 * units);
+      EOGP_LAUNCH_CHECK("attention_backward (zero)");
+      if (keys > 0) {
+        hipLaunchKernelGGL(k_attend_delta<T>, delta_blocks(keys), dim3(256), 0, s, a, lanes, keys, 1);
+        EOGP_LAUNCH_CHECK("attention_backward (norms)");
+      }
+    }
+    if (rows > 0) {
+      hipLaunchKernelGGL(k_attend_delta<T>, delta_blocks(rows), dim3(256), 0, s, a, lanes, rows, 0);
+      EOGP_LAUNCH_CHECK("attention_backward (delta)");
+    }
+    auto go = [&](auto width) {
+      constexpr int DP = decltype(width)::value;
+      constexpr int lds = 4 * 32 * DP * (int)sizeof(T);
+      auto launch = [&](auto* kfn, int64_t blocks) {
+        if (lds > (48 << 10)) {
+          const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);
+          if (st != EOGP_OK) return st;
+        }
+        hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(64 * kBackWaves), lds, s, a);
+        EOGP_LAUNCH_CHECK("attention_backward");
+        return EOGP_OK;
+      };
+      if (keys > 0) {
+        const int64_t blocks = units * a.key_tiles * a.splits;
+        eogp_status st;
+        if constexpr (DP * sizeof(T) > 512) {            // both gradients of wide fp32 heads do not fit the registers
+          st = launch(k_attend_back_kv<T, DP, kBackWaves, 1>, blocks);
+          if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, kBackWaves, 2>, blocks);
+        } else {
+          st = launch(k_attend_back_kv<T, DP, kBackWaves, 3>, blocks);
+        }
+        if (st != EOGP_OK) return st;
+        if (a.part) {
+          hipLaunchKernelGGL(k_attend_back_join<T>, dim3((unsigned)std::min<int64_t>(ceil_div(keys * 2 * D, 256), 64 * kCus)),
+                             dim3(256), 0, s, a);
+          EOGP_LAUNCH_CHECK("attention_backward (join)");
+        }
+      }
+      return rows > 0 ? launch(k_attend_back_q<T, DP, kBackWaves>, units * a.row_tiles) : EOGP_OK;
+    };
+    using std::integral_constant;
+    return D <= 64    ? go(integral_constant<int, 64>{})
+           : D <= 128 ? go(integral_constant<int, 128>{})
+                      : go(integral_constant<int, 256>{});
+  });
+}
+
+}  // namespace eogp

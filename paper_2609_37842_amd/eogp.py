@@ -38,6 +38,11 @@ class PlanInfo(ctypes.Structure):
                 ("retained_flat", c_vp), ("retained_weight", c_vp)]
 
 
+class Heads(ctypes.Structure):
+    """A tensor of heads [N, T, heads, D] by its address and strides (eogp_heads)."""
+    _fields_ = [("data", c_vp), ("heads", c_i64), ("ld_example", c_i64), ("ld_token", c_i64), ("ld_head", c_i64)]
+
+
 _lib = None
 
 EXPORTED = (
@@ -56,6 +61,9 @@ EXPORTED = (
     "eogp_embed_tokens", "eogp_embed_backward_workspace_size", "eogp_embed_backward",
     "eogp_layer_norm", "eogp_layer_norm_backward_workspace_size", "eogp_layer_norm_backward",
     "eogp_softmax_xent", "eogp_sample_tokens",
+    "eogp_rotary_table", "eogp_rotate_heads", "eogp_rotate_heads_backward_workspace_size",
+    "eogp_rotate_heads_backward", "eogp_attention_workspace_size", "eogp_attention",
+    "eogp_attention_backward_workspace_size", "eogp_attention_backward",
     "eogp_timing_enable", "eogp_timing_read",
     "eogp_status_string", "eogp_last_error", "eogp_version",
 )
@@ -129,6 +137,20 @@ def load(path: str | None = None):
         "eogp_sample_tokens": (c_i32, [c_vp, c_i32, c_i64, c_i64, c_i64, c_vp, c_vp,
                                        ctypes.c_double, c_i64, ctypes.c_double, ctypes.c_double,
                                        c_vp, c_vp]),
+        "eogp_rotary_table": (c_i32, [c_i64, c_i64] + [ctypes.c_double] * 6 + [c_vp, c_vp]),
+        "eogp_rotate_heads": (c_i32, [c_vp, c_vp, c_i32, c_i64, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32, ctypes.c_float,
+                                      c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]),
+        "eogp_rotate_heads_backward_workspace_size": (c_sz, [c_i64] * 5 + [c_i32, c_i32, c_i64, c_i32]),
+        "eogp_rotate_heads_backward": (c_i32, [c_vp] * 4 + [c_i32, c_i64, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32,
+                                               ctypes.c_float, c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32, c_vp,
+                                               c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
+        "eogp_attention_workspace_size": (c_sz, [c_i64] * 6 + [c_i32]),
+        "eogp_attention": (c_i32, [c_vp] * 3 + [c_i32] + [c_i64] * 4 + [ctypes.c_float, c_i32, c_i64, c_i64, c_vp, c_vp,
+                                                                       c_vp, c_vp, c_i32, c_vp, c_vp, c_sz, c_vp]),
+        "eogp_attention_backward_workspace_size": (c_sz, [c_i64] * 6 + [c_i32]),
+        "eogp_attention_backward": (c_i32, [c_vp] * 4 + [c_i32] + [c_i64] * 4 +
+                                    [ctypes.c_float, c_i32, c_i64, c_i64, c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_vp,
+                                     c_vp, c_vp, c_vp, c_sz, c_vp]),
         "eogp_timing_enable": (c_i32, [c_i32]),
         "eogp_timing_read": (c_i32, [c_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(c_i64)]),
         "eogp_status_string": (ctypes.c_char_p, [c_i32]),
@@ -900,6 +922,251 @@ def eogp_sample_tokens(logits, uniforms=None, temperature=1.0, top_k=0, top_p=1.
     return out
 
 
+# ---------------------------------------------------------------------------
+# The middle of a block: rotary positions, norms of queries and keys, attention
+# ---------------------------------------------------------------------------
+NORMS = {"none": 0, "head": 1, "row": 2}
+
+
+def _heads_of(x, name):
+    """[N, T, heads, D] with unit stride in its last dimension, as the library takes it."""
+    if x.dim() != 4:
+        raise ValueError(f"{name} must be [N, T, heads, D]")
+    s = x.stride()
+    if s[3] != 1 and x.shape[3] > 1:
+        if x.numel():
+            raise ValueError(f"{name} must have unit stride within a head")
+        s = (0, 0, 0)
+    return Heads(x.data_ptr(), x.shape[2], s[0], s[1], s[2])
+
+
+def _heads_like(x, like, name):
+    if x.shape != like.shape or x.dtype != like.dtype:
+        raise ValueError(f"{name} must have the shape and type of its counterpart")
+    return _heads_of(x, name)
+
+
+def _norm_weights(norm, weight, x, name):
+    if weight is None:
+        return
+    if norm == 0:
+        raise ValueError(f"{name} without a norm")
+    _weight(weight, x.shape[3] if norm == 1 else x.shape[2] * x.shape[3], x, name)
+
+
+def _table_shape(table):
+    """(positions, width) of a rotary table, (0, 0) without one."""
+    if table is None:
+        return 0, 0
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32 [positions, width / 2, 2]")
+    return table.shape[0], 2 * table.shape[1]
+
+
+def eogp_rotary_table(positions, width, base=10000.0, factor=1.0, original=0, low=1.0, high=32.0, magnitude=1.0,
+                      out=None, device=None, stream=None):
+    """(cos, sin) of positions 0 .. positions - 1 times each pair's frequency, float32 [positions, width / 2, 2];
+    `factor`, `original`, `low` and `high` scale frequencies for long contexts; see eogp_rotary_table in eogp.h."""
+    L = load()
+    if positions < 0 or width < 2 or width % 2:
+        raise ValueError("a table needs positions >= 0 and an even width >= 2")
+    if out is None:
+        device = torch.device("cuda", _current_device()) if device is None else torch.device(device)
+        out = _empty((positions, width // 2, 2), torch.float32, device, stream)
+    _need_here(stream, out)
+    if out.dtype != torch.float32 or tuple(out.shape) != (positions, width // 2, 2) or not out.is_contiguous():
+        raise ValueError("out must be contiguous float32 [positions, width / 2, 2]")
+    _check(L.eogp_rotary_table(positions, width, float(base), float(factor), float(original), float(low), float(high),
+                               float(magnitude), _at(out), _stream_handle(stream, out.device)))
+    return out
+
+
+def eogp_rotate_heads(q, k=None, table=None, positions=None, norm="none", q_weight=None, k_weight=None, eps=1e-6,
+                      interleaved=False, token_mask=None, q_out=None, k_out=None, stream=None):
+    """(q_out, k_out) of queries [N, T, heads, D] and keys [N, T, key heads, D] or None: normed (norm "head", "row" or
+    "none") and turned by their positions; see eogp_rotate_heads in eogp.h."""
+    L = load()
+    _need_here(stream, q, k, table, positions, q_weight, k_weight, token_mask, q_out, k_out)
+    code = _model_dtype(q, "q")
+    qh = _heads_of(q, "q")
+    N, T, _, D = q.shape
+    if k is not None and (k.shape[:2] != q.shape[:2] or k.shape[3:] != q.shape[3:] or k.dtype != q.dtype):
+        raise ValueError("k must be [N, T, key heads, D] of q's type")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {', '.join(NORMS)}")
+    nc = NORMS[norm]
+    _norm_weights(nc, q_weight, q, "q_weight")
+    _norm_weights(nc, k_weight, q if k is None else k, "k_weight")
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise ValueError("q_weight and k_weight must have one type")
+    P, width = _table_shape(table)
+    _per_row(positions, (N, T), torch.int64, "positions")
+    _per_row(token_mask, (N, T), torch.uint8, "token_mask")
+    if q_out is None:
+        q_out = _empty(tuple(q.shape), q.dtype, q.device, stream)
+    oq, kh, ok = _heads_like(q_out, q, "q_out"), None, None
+    if k is not None:
+        kh = _heads_of(k, "k")
+        if k_out is None:
+            k_out = _empty(tuple(k.shape), k.dtype, k.device, stream)
+        ok = _heads_like(k_out, k, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    w = q_weight if q_weight is not None else k_weight
+    _check(L.eogp_rotate_heads(ctypes.byref(qh), kh and ctypes.byref(kh), code, N, T, D, nc, _at(q_weight), _at(k_weight),
+                               F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _at(table), P, width,
+                               1 if interleaved else 0, _at(positions), _at(token_mask), ctypes.byref(oq),
+                               ok and ctypes.byref(ok), _stream_handle(stream, q.device)))
+    return q_out, k_out
+
+
+def eogp_rotate_heads_backward_workspace_size(N, T, q_heads, k_heads, D, dtype, norm="none", width=0,
+                                              per_example=False) -> int:
+    return int(load().eogp_rotate_heads_backward_workspace_size(N, T, q_heads, k_heads, D, dtype, NORMS[norm], width,
+                                                                1 if per_example else 0))
+
+
+def eogp_rotate_heads_backward(dq, dk=None, q=None, k=None, table=None, positions=None, norm="none", q_weight=None,
+                               k_weight=None, eps=1e-6, interleaved=False, token_mask=None, per_example=False, dq_in=None,
+                               dk_in=None, dq_weight=None, dk_weight=None, ws=None, stream=None):
+    """(dq_in, dk_in, dq_weight, dk_weight): gradients at the inputs q, k (read only with a norm) of eogp_rotate_heads
+    from those of its outputs, and with a norm those of the weights, float32 [weight] or with per_example
+    [N, weight]; see eogp_rotate_heads_backward in eogp.h."""
+    L = load()
+    _need_here(stream, dq, dk, q, k, table, positions, q_weight, k_weight, token_mask, dq_in, dk_in, dq_weight, dk_weight, ws)
+    code = _model_dtype(dq, "dq")
+    N, T, Hq, D = dq.shape if dq.dim() == 4 else (0, 0, 0, 0)
+    gq = _heads_of(dq, "dq")
+    if dk is not None and (dk.shape[:2] != dq.shape[:2] or dk.shape[3:] != dq.shape[3:] or dk.dtype != dq.dtype):
+        raise ValueError("dk must be [N, T, key heads, D] of dq's type")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {', '.join(NORMS)}")
+    nc = NORMS[norm]
+    if nc and (q is None or (dk is not None and k is None)):
+        raise ValueError("a norm's backward pass reads the forward pass's inputs")
+    gk = None if dk is None else _heads_of(dk, "dk")
+    xq = _heads_like(q, dq, "q") if nc else None
+    xk = _heads_like(k, dk, "k") if nc and dk is not None else None
+    _norm_weights(nc, q_weight, dq, "q_weight")
+    _norm_weights(nc, k_weight, dq if dk is None else dk, "k_weight")
+    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        raise ValueError("q_weight and k_weight must have one type")
+    P, width = _table_shape(table)
+    _per_row(positions, (N, T), torch.int64, "positions")
+    _per_row(token_mask, (N, T), torch.uint8, "token_mask")
+    if dq_in is None:
+        dq_in = _empty(tuple(dq.shape), dq.dtype, dq.device, stream)
+    oq, ok = _heads_like(dq_in, dq, "dq_in"), None
+    if dk is not None:
+        if dk_in is None:
+            dk_in = _empty(tuple(dk.shape), dk.dtype, dk.device, stream)
+        ok = _heads_like(dk_in, dk, "dk_in")
+    elif dk_in is not None:
+        raise ValueError("dk_in without dk")
+    if nc:
+        lead = (N,) if per_example else ()
+        shape = lambda x: (*lead, D if nc == 1 else x.shape[2] * D)   # noqa: E731
+        if dq_weight is None:
+            dq_weight = _empty(shape(dq), torch.float32, dq.device, stream)
+        _per_row(dq_weight, shape(dq), torch.float32, "dq_weight")
+        if dk is not None:
+            if dk_weight is None:
+                dk_weight = _empty(shape(dk), torch.float32, dk.device, stream)
+            _per_row(dk_weight, shape(dk), torch.float32, "dk_weight")
+    elif dq_weight is not None or dk_weight is not None:
+        raise ValueError("weight gradients without a norm")
+    need = int(L.eogp_rotate_heads_backward_workspace_size(N, T, Hq, 0 if dk is None else dk.shape[2], D, code, nc, width,
+                                                           1 if per_example else 0)) if nc else 0
+    ws, wsb = _scratch(need, dq.device, ws, stream)
+    w = q_weight if q_weight is not None else k_weight
+    ref = lambda x: x and ctypes.byref(x)                              # noqa: E731
+    _check(L.eogp_rotate_heads_backward(ref(gq), ref(gk), ref(xq), ref(xk), code, N, T, D, nc, _at(q_weight),
+                                        _at(k_weight), F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _at(table),
+                                        P, width, 1 if interleaved else 0, _at(positions), _at(token_mask),
+                                        1 if per_example else 0, ref(oq), ref(ok), _at(dq_weight), _at(dk_weight), _at(ws),
+                                        wsb, _stream_handle(stream, dq.device)))
+    return dq_in, dk_in, dq_weight, dk_weight
+
+
+def _attention_shapes(q, k, v, q_start, q_mask, k_mask):
+    """Sizes (N, Tq, Tk, Hq, Hkv, D) of queries [N, Tq, Hq, D], keys and values [N, Tk, Hkv, D]."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q must be [N, Tq, heads, D], k and v [N, Tk, key heads, D]")
+    N, Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[1], k.shape[2]
+    if k.shape[0] != N or k.shape[3] != D or v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("k and v must be [N, Tk, key heads, D] of q's type")
+    _per_row(q_start, (N,), torch.int64, "q_start")
+    _per_row(q_mask, (N, Tq), torch.uint8, "q_mask")
+    _per_row(k_mask, (N, Tk), torch.uint8, "k_mask")
+    return N, Tq, Tk, Hq, Hkv, D
+
+
+def eogp_attention_workspace_size(N, Tq, Tk, q_heads, k_heads, D, dtype) -> int:
+    return int(load().eogp_attention_workspace_size(N, Tq, Tk, q_heads, k_heads, D, dtype))
+
+
+def eogp_attention(q, k, v, scale=None, causal=True, window=0, sinks=0, q_start=None, q_mask=None, k_mask=None,
+                   out=None, lse=None, stats=True, ws=None, stream=None):
+    """(out, lse): softmax attention of queries [N, Tq, heads, D] over keys and values [N, Tk, key heads, D], and the
+    rows' log-sum-exp, float32 [N, Tq, heads] (stats=False: left out, None). scale is D^-1/2 unless given; see
+    eogp_attention in eogp.h."""
+    L = load()
+    _need_here(stream, q, k, v, q_start, q_mask, k_mask, out, lse, ws)
+    code = _model_dtype(q, "q")
+    N, Tq, Tk, Hq, Hkv, D = _attention_shapes(q, k, v, q_start, q_mask, k_mask)
+    if out is None:
+        out = _empty((N, Tq, Hq, D), q.dtype, q.device, stream)
+    if out.shape != q.shape or out.dtype not in (q.dtype, torch.float32):
+        raise ValueError("out must be [N, Tq, heads, D] of q's type or float32")
+    if stats and lse is None:
+        lse = _empty((N, Tq, Hq), torch.float32, q.device, stream)
+    if not stats and lse is not None:
+        raise ValueError("lse without stats")
+    _per_row(lse, (N, Tq, Hq), torch.float32, "lse")
+    need = int(L.eogp_attention_workspace_size(N, Tq, Tk, Hq, Hkv, D, code))
+    ws, wsb = _scratch(need, q.device, ws, stream)
+    ref = ctypes.byref
+    _check(L.eogp_attention(ref(_heads_of(q, "q")), ref(_heads_of(k, "k")), ref(_heads_of(v, "v")), code, N, Tq, Tk, D,
+                            D ** -0.5 if scale is None and D else float(scale or 0), 1 if causal else 0, int(window),
+                            int(sinks), _at(q_start), _at(q_mask), _at(k_mask), ref(_heads_of(out, "out")),
+                            _DTYPE_CODE[out.dtype], _at(lse), _at(ws), wsb, _stream_handle(stream, q.device)))
+    return out, lse
+
+
+def eogp_attention_backward_workspace_size(N, Tq, Tk, q_heads, k_heads, D, dtype) -> int:
+    return int(load().eogp_attention_backward_workspace_size(N, Tq, Tk, q_heads, k_heads, D, dtype))
+
+
+def eogp_attention_backward(dout, q, k, v, out, lse, scale=None, causal=True, window=0, sinks=0, q_start=None,
+                            q_mask=None, k_mask=None, dq=None, dk=None, dv=None, ws=None, stream=None):
+    """(dq, dk, dv) from the gradient of eogp_attention's out, with its out and lse and the same other arguments; see
+    eogp_attention_backward in eogp.h."""
+    L = load()
+    _need_here(stream, dout, q, k, v, out, lse, q_start, q_mask, k_mask, dq, dk, dv, ws)
+    code = _model_dtype(q, "q")
+    N, Tq, Tk, Hq, Hkv, D = _attention_shapes(q, k, v, q_start, q_mask, k_mask)
+    if out.shape != q.shape or out.dtype not in (q.dtype, torch.float32):
+        raise ValueError("out must be [N, Tq, heads, D] of q's type or float32")
+    if lse is None:
+        raise ValueError("the backward pass reads the forward pass's lse")
+    _per_row(lse, (N, Tq, Hq), torch.float32, "lse")
+    dq = _empty(tuple(q.shape), q.dtype, q.device, stream) if dq is None else dq
+    dk = _empty(tuple(k.shape), k.dtype, k.device, stream) if dk is None else dk
+    dv = _empty(tuple(v.shape), v.dtype, v.device, stream) if dv is None else dv
+    need = int(L.eogp_attention_backward_workspace_size(N, Tq, Tk, Hq, Hkv, D, code))
+    ws, wsb = _scratch(need, q.device, ws, stream)
+    ref = ctypes.byref
+    _check(L.eogp_attention_backward(ref(_heads_like(dout, q, "dout")), ref(_heads_of(q, "q")), ref(_heads_of(k, "k")),
+                                     ref(_heads_of(v, "v")), code, N, Tq, Tk, D,
+                                     D ** -0.5 if scale is None and D else float(scale or 0), 1 if causal else 0,
+                                     int(window), int(sinks), _at(q_start), _at(q_mask), _at(k_mask),
+                                     ref(_heads_of(out, "out")), _DTYPE_CODE[out.dtype], _at(lse),
+                                     ref(_heads_like(dq, q, "dq")), ref(_heads_like(dk, k, "dk")),
+                                     ref(_heads_like(dv, v, "dv")), _at(ws), wsb, _stream_handle(stream, q.device)))
+    return dq, dk, dv
+
+
 def eogp_version() -> int:
     return int(load().eogp_version())
 
@@ -911,10 +1178,11 @@ KT_ROTATION_GEMM, KT_RETAINED, KT_PCA_GEMM, KT_SIGN_PACK = 0, 1, 2, 3
 KT_SCORE_PASS, KT_SCORE_MERGE, KT_SCORE_PREP, KT_COMPACTION = 4, 5, 6, 7
 KT_SRHT, KT_EKFAC, KT_PCA_FIT = 8, 9, 10
 KT_EMBED, KT_LAYER_NORM, KT_XENT, KT_SAMPLE = 11, 12, 13, 14
+KT_ROTARY, KT_ATTENTION = 15, 16
 KERNEL_CLASSES = {"rotation_gemm": 0, "retained": 1, "pca_gemm": 2, "sign_pack": 3,
                   "score_pass": 4, "score_merge": 5, "score_prep": 6, "compaction": 7,
                   "srht": 8, "ekfac": 9, "pca_fit": 10, "embed": 11, "layer_norm": 12,
-                  "xent": 13, "sample": 14}
+                  "xent": 13, "sample": 14, "rotary": 15, "attention": 16}
 
 
 def eogp_timing_enable(on: bool = True):

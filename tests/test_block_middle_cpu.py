@@ -1,0 +1,297 @@
+"""The operators in the middle of a block, without a GPU: the oracle's gradients against differences, the refusals of the
+C ABI and of the binding, workspace sizes, and where the calls run."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_middle as M
+from paper_2609_37842_amd import eogp as E
+
+FAKE = 0x1000
+
+
+def directional(f, x, d, h=1e-5):
+    return (f(x + h * d) - f(x - h * d)) / (2 * h)
+
+
+# ---- the oracle ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("norm", ["none", "head", "row"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotation_gradients_against_differences(norm, interleaved):
+    """Central differences in float64 at h = 1e-5: truncation h^2 and rounding 1e-16 / h of values of order 100."""
+    g = np.random.default_rng(1)
+    n, H, D = 6, 3, 10
+    x, dy, t = g.standard_normal((n, H, D)), g.standard_normal((n, H, D)), M.rotary_table(20, 6)
+    pos, mask = g.integers(0, 20, n), np.array([1, 1, 0, 1, 1, 0])
+    w = None if norm == "none" else g.standard_normal(D if norm == "head" else H * D)
+    at = lambda xx, ww: (M.rotate(xx, t, pos, norm, ww, 1e-6, interleaved, mask) * dy).sum()   # noqa: E731
+    dx, dw = M.rotate_backward(dy, x, t, pos, norm, w, 1e-6, interleaved, mask)
+    v = g.standard_normal(x.shape)
+    assert abs(directional(lambda q: at(q, w), x, v) - (dx * v).sum()) < 1e-7
+    assert np.all(dx[mask == 0] == 0)
+    if norm != "none":
+        u = g.standard_normal(w.shape)
+        assert abs(directional(lambda q: at(x, q), w, u) - (dw[0] * u).sum()) < 1e-7
+        assert np.allclose(M.rotate_backward(dy, x, t, pos, norm, w, 1e-6, interleaved, mask, groups=3)[1].sum(0), dw[0])
+
+
+def test_scores_depend_on_the_difference_of_positions():
+    g = np.random.default_rng(2)
+    q, k, t = g.standard_normal((1, 1, 8)), g.standard_normal((1, 1, 8)), M.rotary_table(50, 8)
+    for inter in (False, True):
+        at = lambda a, b: float((M.rotate(q, t, np.array([a]), interleaved=inter)   # noqa: E731
+                                 * M.rotate(k, t, np.array([b]), interleaved=inter)).sum())
+        assert abs(at(7, 3) - at(40, 36)) < 1e-12 and abs(at(7, 3) - at(7, 4)) > 1e-3
+
+
+def test_scaled_frequencies():
+    plain, all_of, parts = M.rotary_table(9, 16), M.rotary_table(9, 16, factor=4.0), M.rotary_table(9, 16, factor=4.0, original=4096)
+    assert np.allclose(plain[2], all_of[8])
+    assert np.array_equal(parts[:, 0], plain[:, 0])            # 652 turns over 4,096 positions
+    assert np.array_equal(parts[:, -1], all_of[:, -1])         # 0.2 turns
+
+
+@pytest.mark.parametrize("how", [dict(), dict(causal=False), dict(window=3, sinks=2), dict(causal=False, window=2, sinks=5)])
+def test_attention_gradients_against_differences(how):
+    g = np.random.default_rng(3)
+    N, Tq, Tk, Hq, Hkv, D = 2, 5, 7, 4, 2, 6
+    q, dout = g.standard_normal((N, Tq, Hq, D)), g.standard_normal((N, Tq, Hq, D))
+    k, v = g.standard_normal((N, Tk, Hkv, D)), g.standard_normal((N, Tk, Hkv, D))
+    how = dict(how, q_mask=g.integers(0, 2, (N, Tq)), k_mask=g.integers(0, 2, (N, Tk)))
+    grads = M.attention_backward(dout, q, k, v, 0.4, **how)
+    for i, x in enumerate((q, k, v)):
+        d = g.standard_normal(x.shape)
+        f = lambda y: (M.attention(*[y if j == i else (q, k, v)[j] for j in range(3)], 0.4, **how)[0] * dout).sum()  # noqa: E731
+        assert abs(directional(f, x, d) - (grads[i] * d).sum()) < 1e-7
+
+
+def test_sight_by_hand():
+    see = M.sight(0, 3, 6, window=2, sinks=1)
+    assert see.astype(int).tolist() == [[1, 0, 1, 1, 0, 0], [1, 0, 0, 1, 1, 0], [1, 0, 0, 0, 1, 1]]
+    see = M.sight(0, 2, 5, causal=False, window=2, sinks=4, q_start=[0])
+    assert see.astype(int).tolist() == [[1, 1, 1, 1, 0], [1, 1, 1, 1, 0]]
+    assert not M.sight(0, 2, 5, q_start=[-2]).any()
+
+
+# ---- refusals of the C ABI ---------------------------------------------------------------------------------------
+def heads(data=FAKE, heads=4, n=4096, t=512, h=64):
+    return E.Heads(data, heads, n, t, h)
+
+
+def call(name, args, **k):
+    """The C function on named arguments, some of them replaced; structures by address."""
+    use = dict(args, **k)
+    assert set(use) == set(args)
+    return getattr(E.load(), name)(*(ctypes.byref(x) if isinstance(x, E.Heads) else x for x in use.values()))
+
+
+TABLE = dict(P=8, width=16, base=1e4, factor=1.0, original=0.0, low=1.0, high=4.0, magnitude=1.0, table=FAKE, s=None)
+
+
+def test_table_refusals():
+    inf, nan = float("inf"), float("nan")
+    for bad in (dict(P=-1), dict(P=1 << 31), dict(width=0), dict(width=15), dict(width=1 << 26), dict(base=0.0), dict(base=-1.0),
+                dict(base=nan), dict(factor=0.0), dict(factor=inf), dict(original=-1.0), dict(high=1.0), dict(low=nan),
+                dict(magnitude=inf), dict(table=None), dict(table=FAKE + 2)):
+        assert call("eogp_rotary_table", TABLE, **bad) == -1, bad
+    assert call("eogp_rotary_table", TABLE, P=0, table=None) == 0
+
+
+ROTATE = dict(q=heads(), k=heads(heads=2), dt=1, N=3, T=8, D=64, norm=1, wq=FAKE, wk=None, wt=0, eps=1e-6, table=FAKE, P=8,
+              width=64, inter=0, pos=FAKE, mask=None, oq=heads(), ok=heads(heads=2), s=None)
+
+
+def test_rotate_refusals():
+    nan = float("nan")
+    for bad in (dict(q=None), dict(dt=7), dict(wt=9), dict(N=-1), dict(T=-1), dict(N=1 << 31), dict(N=1 << 16, T=1 << 15), dict(D=0),
+                dict(norm=3), dict(norm=0), dict(eps=-1.0), dict(eps=nan), dict(P=-1), dict(P=1 << 31), dict(width=63),
+                dict(width=66), dict(width=-2), dict(table=None), dict(table=FAKE + 1), dict(pos=FAKE + 4), dict(wq=FAKE + 1),
+                dict(q=heads(0)), dict(q=heads(FAKE + 1)), dict(q=heads(t=-1)), dict(q=heads(n=1 << 40)), dict(q=heads(heads=0)),
+                dict(k=heads(heads=3)), dict(oq=None), dict(ok=None), dict(oq=heads(heads=3)), dict(oq=heads(0)),
+                dict(oq=heads(t=32)), dict(oq=heads(h=0)), dict(oq=heads(n=512)), dict(oq=heads(h=32)), dict(k=None),
+                dict(q=heads(heads=-1))):
+        assert call("eogp_rotate_heads", ROTATE, **bad) == -1, bad
+    for bad in (dict(D=257, width=64), dict(wt=2), dict(norm=2, q=heads(heads=129), oq=heads(heads=129, n=1 << 20, t=1 << 16)),
+                dict(norm=2, D=4, width=4, q=heads(heads=513), oq=heads(heads=513, n=1 << 20, t=1 << 16))):
+        assert call("eogp_rotate_heads", ROTATE, **bad) == -2, bad
+    assert call("eogp_rotate_heads", ROTATE, N=0) == 0
+    assert call("eogp_rotate_heads", ROTATE, T=0, q=heads(0), k=heads(0, 2), oq=heads(0), ok=heads(0, 2)) == 0
+
+
+BACK = dict(dq=heads(), dk=heads(heads=2), q=heads(), k=heads(heads=2), dt=1, N=3, T=8, D=64, norm=1, wq=FAKE, wk=FAKE, wt=1,
+            eps=1e-6, table=FAKE, P=8, width=64, inter=0, pos=None, mask=FAKE, per=0, oq=heads(), ok=heads(heads=2), dwq=FAKE,
+            dwk=FAKE, ws=FAKE, wsb=1 << 30, s=None)
+
+
+def test_rotate_backward_refusals():
+    name = "eogp_rotate_heads_backward"
+    for bad in (dict(dq=None), dict(q=None), dict(k=None), dict(oq=None), dict(dk=None), dict(dwq=FAKE + 2), dict(ws=FAKE + 2),
+                dict(norm=0), dict(norm=0, wq=None, wk=None), dict(per=1, N=(1 << 21) + 1, T=0), dict(oq=heads(t=32))):
+        assert call(name, BACK, **bad) == -1, bad
+    assert call(name, BACK, ws=None) == -4 and call(name, BACK, wsb=64) == -4
+    assert call(name, BACK, N=0, per=1, ws=None, wsb=0) == 0
+    assert call(name, BACK, N=0, ws=None) == -4                # the batch's weight gradients are zeros then
+    assert call(name, BACK, N=0, norm=0, wq=None, wk=None, dwq=None, dwk=None, q=None, k=None, ws=None, wsb=0) == 0
+
+
+ATTEND = dict(q=heads(), k=heads(heads=2), v=heads(heads=2), dt=1, N=3, Tq=8, Tk=8, D=64, scale=0.1, causal=1, window=0, sinks=0,
+              start=FAKE, qm=FAKE, km=FAKE, out=heads(), ot=1, lse=FAKE, ws=FAKE, wsb=1 << 40, s=None)
+ATTEND_BACK = dict(dout=heads(), q=heads(), k=heads(heads=2), v=heads(heads=2), dt=1, N=3, Tq=8, Tk=8, D=64, scale=0.1, causal=1,
+                   window=0, sinks=0, start=FAKE, qm=FAKE, km=FAKE, out=heads(), ot=1, lse=FAKE, dq=heads(), dk=heads(heads=2),
+                   dv=heads(heads=2), ws=FAKE, wsb=1 << 40, s=None)
+
+
+@pytest.mark.parametrize("name,args", [("eogp_attention", ATTEND), ("eogp_attention_backward", ATTEND_BACK)])
+def test_attention_refusals(name, args):
+    inf, nan = float("inf"), float("nan")
+    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(dt=5), dict(ot=5), dict(N=-1), dict(Tq=-1), dict(Tk=-1),
+                dict(D=0), dict(N=1 << 20, Tq=1 << 10), dict(Tk=1 << 31), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan),
+                dict(scale=inf), dict(window=-1), dict(sinks=-1), dict(sinks=1), dict(k=heads(heads=3)), dict(v=heads(heads=4)),
+                dict(k=heads(heads=0), v=heads(heads=0)), dict(q=heads(0)), dict(k=heads(0, 2)), dict(v=heads(0, 2)),
+                dict(v=heads(FAKE + 1, 2)), dict(out=heads(FAKE + 1)), dict(start=FAKE + 4), dict(lse=FAKE + 2),
+                dict(ws=FAKE + 2)):
+        assert call(name, args, **bad) == -1, bad
+    for bad in (dict(D=7), dict(D=257), dict(ot=2)):
+        assert call(name, args, **bad) == -2, bad
+    assert call(name, args, N=0) == 0
+    if name == "eogp_attention":
+        assert call(name, args, Tq=0, q=heads(0), out=heads(0)) == 0
+        for bad in (dict(out=heads(t=128)), dict(out=heads(h=0)), dict(out=heads(n=0))):
+            assert call(name, args, **bad) == -1, bad
+        big = dict(Tq=1, Tk=100000, k=heads(heads=2, n=1 << 30), v=heads(heads=2, n=1 << 30))
+        assert call(name, args, ws=None, **big) == -4 and call(name, args, wsb=16, **big) == -4
+    else:
+        assert call(name, args, ws=None) == -4 and call(name, args, wsb=64) == -4 and call(name, args, lse=None) == -1
+        for bad in (dict(dq=None), dict(dk=None), dict(dv=None), dict(dout=None), dict(dq=heads(t=128)), dict(dk=heads(heads=2, h=0))):
+            assert call(name, args, **bad) == -1, bad
+
+
+# ---- workspaces ----------------------------------------------------------------------------------------------------
+def test_workspaces_of_the_largest_batch_serve_every_smaller_one():
+    """Sizes do not fall as examples, queries, heads or keys grow."""
+    g = np.random.default_rng(4)
+    for _ in range(400):
+        dt, D, Hkv, G = int(g.integers(3)), int(g.integers(8, 257)), int(g.integers(1, 9)), int(g.integers(1, 9))
+        N, Tq, Tk = (int(2 ** g.uniform(0, b)) for b in (6, 12, 17))
+        at = lambda f, n, a, b, m: f(n, a, b, Hkv * m, Hkv, D, dt)        # noqa: E731
+        for f in (E.eogp_attention_workspace_size, E.eogp_attention_backward_workspace_size):
+            full = at(f, N, Tq, Tk, G)
+            for _ in range(12):
+                n, a, b = (int(g.integers(0, x + 1)) for x in (N, Tq, Tk))
+                assert at(f, n, a, b, int(g.integers(1, G + 1))) <= full
+        norm, per, width = ["head", "row"][int(g.integers(2))], bool(g.integers(2)), 2 * int(g.integers(0, D // 2 + 1))
+        if norm == "row" and Hkv * G * D > 8192:
+            continue
+        size = lambda n, t: E.eogp_rotate_heads_backward_workspace_size(n, t, Hkv * G, Hkv, D, dt, norm, width, per)  # noqa: E731
+        full = size(N, Tq)
+        assert full > 0
+        for _ in range(12):
+            assert size(int(g.integers(0, N + 1)), int(g.integers(0, Tq + 1))) <= full
+
+
+def test_workspace_sizes_of_refused_calls_are_zero():
+    assert E.eogp_attention_workspace_size(1, 1, 100000, 3, 2, 64, 1) == 0
+    assert E.eogp_attention_backward_workspace_size(1, 8, 8, 2, 2, 300, 1) == 0
+    assert E.eogp_rotate_heads_backward_workspace_size(4, 8, 2, 2, 64, 1, "none") == 0
+    assert E.eogp_rotate_heads_backward_workspace_size(4, 8, 2, 2, 64, 1, "head", 3) == 0
+
+
+# ---- the binding ----------------------------------------------------------------------------------------------------
+@pytest.fixture
+def host_tensors(monkeypatch):
+    """Host tensors stand in for device ones, and nothing is launched."""
+    monkeypatch.setattr(E, "_need_here", lambda *a: None)
+    monkeypatch.setattr(E, "_stream_handle", lambda *a: None)
+    monkeypatch.setattr(E, "_check", lambda status: None)
+
+
+def test_binding_refusals(host_tensors):
+    q, k = torch.zeros(2, 4, 4, 16), torch.zeros(2, 4, 2, 16)
+    bad = lambda match: pytest.raises(ValueError, match=match)      # noqa: E731
+    with bad("unit stride"):
+        E.eogp_attention(torch.zeros(2, 4, 16, 4).transpose(2, 3), k, k)
+    with bad("key heads, D"):
+        E.eogp_attention(q, k, k[:, :, :1])
+    with bad("key heads, D"):
+        E.eogp_attention(q, k.half(), k.half())
+    with bad("float32, bfloat16"):
+        E.eogp_attention(q.double(), k.double(), k.double())
+    with bad("q_mask"):
+        E.eogp_attention(q, k, k, q_mask=torch.ones(2, 4))
+    with bad("k_mask"):
+        E.eogp_attention(q, k, k, k_mask=torch.ones(2, 3, dtype=torch.uint8))
+    with bad("q_start"):
+        E.eogp_attention(q, k, k, q_start=torch.zeros(2, dtype=torch.int32))
+    with bad("out must"):
+        E.eogp_attention(q, k, k, out=torch.empty(2, 4, 4, 16, dtype=torch.float16))
+    with bad("lse without stats"):
+        E.eogp_attention(q, k, k, lse=torch.empty(2, 4, 4), stats=False)
+    with bad("reads the forward pass's lse"):
+        E.eogp_attention_backward(q, q, k, k, q, None)
+    with bad("dout must"):
+        E.eogp_attention_backward(q.half(), q, k, k, q, torch.empty(2, 4, 4))
+    with bad("dk must"):
+        E.eogp_attention_backward(q, q, k, k, q, torch.empty(2, 4, 4), dk=q)
+    t = torch.zeros(8, 8, 2)
+    with bad("table must"):
+        E.eogp_rotate_heads(q, k, t[:, :, 0])
+    with bad("norm must"):
+        E.eogp_rotate_heads(q, k, t, norm="layer")
+    with bad("without a norm"):
+        E.eogp_rotate_heads(q, k, t, q_weight=torch.ones(16))
+    with bad("q_weight must"):
+        E.eogp_rotate_heads(q, k, t, norm="row", q_weight=torch.ones(16))
+    with bad("one type"):
+        E.eogp_rotate_heads(q.half(), k.half(), t, norm="head", q_weight=torch.ones(16), k_weight=torch.ones(16).half())
+    with bad("positions"):
+        E.eogp_rotate_heads(q, k, t, positions=torch.zeros(2, 4))
+    with bad("k must"):
+        E.eogp_rotate_heads(q, k[:, :2], t)
+    with bad("k_out without k"):
+        E.eogp_rotate_heads(q, None, t, k_out=k)
+    with bad("reads the forward pass's inputs"):
+        E.eogp_rotate_heads_backward(q, k, q, None, t, norm="head")
+    with bad("dq_weight must"):
+        E.eogp_rotate_heads_backward(q, k, q, k, t, norm="head", per_example=True, dq_weight=torch.empty(16))
+    with bad("weight gradients without a norm"):
+        E.eogp_rotate_heads_backward(q, k, table=t, dq_weight=torch.empty(16))
+    with bad("even width"):
+        E.eogp_rotary_table(4, 7, out=t)
+    with bad("out must"):
+        E.eogp_rotary_table(4, 8, out=t)
+
+
+class OnDevice:
+    """What the checks ask of a tensor (or stream) of device `index`, -1 for the host."""
+
+    def __init__(self, index):
+        self.index = self.device_index = index
+        self.is_cuda = index >= 0
+
+    def get_device(self):
+        return self.index
+
+
+CALLS = {
+    "table": lambda t, **k: E.eogp_rotary_table(4, 8, out=t[-1], **k),
+    "rotate": lambda t, **k: E.eogp_rotate_heads(t[0], t[1], **k),
+    "rotate_backward": lambda t, **k: E.eogp_rotate_heads_backward(t[0], t[1], **k),
+    "attention": lambda t, **k: E.eogp_attention(t[0], t[0], t[1], **k),
+    "attention_backward": lambda t, **k: E.eogp_attention_backward(t[0], t[0], t[0], t[0], t[0], t[1], **k),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_other_devices_are_refused(name, monkeypatch):
+    monkeypatch.setattr(E, "_current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device cuda:0, not cuda:1"):
+        CALLS[name]([OnDevice(0), OnDevice(1)])
+    with pytest.raises(ValueError, match="device tensors"):
+        CALLS[name]([OnDevice(0), OnDevice(-1)])
+    with pytest.raises(ValueError, match="stream must belong to the current device cuda:0, not cuda:1"):
+        CALLS[name]([OnDevice(0), OnDevice(0)], stream=OnDevice(1))
+    if name not in ("table", "rotate"):
+        with pytest.raises(ValueError, match="not cuda:1"):
+            CALLS[name]([OnDevice(0), OnDevice(0)], ws=OnDevice(1))

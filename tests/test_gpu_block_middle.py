@@ -1,0 +1,457 @@
+"""The operators in the middle of a block against float64, through the binding: every type, head widths, lengths and head
+counts on both sides of the kernels' tiles, layouts and rows at any element, masks that leave nothing, single tokens."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_middle as M
+from paper_2609_37842_amd import eogp as E
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+U = 2.0 ** -24
+# half a step of each type relative to the value, and half its subnormal step
+ULP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 2.0 ** -126, torch.bfloat16: 2.0 ** -126, torch.float16: 2.0 ** -25}
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+def gen(*key):
+    return np.random.default_rng(list(key))
+
+
+def host(t):
+    return t.detach().to(torch.float64).cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def dev(a, dtype=None):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+def rounded(a, dt):
+    """The values that the device gets."""
+    return torch.from_numpy(np.ascontiguousarray(a)).to(dt).double().numpy()
+
+
+def lay(a, dt, layout="split", shift=0):
+    """[N, T, H, D] on the device: contiguous, as [N, H, T, D], or with gaps between rows and `shift` elements in."""
+    x = torch.from_numpy(np.ascontiguousarray(a)).to(dt)
+    N, T, H, D = x.shape
+    if layout == "heads":
+        return x.transpose(1, 2).contiguous().to(DEV).transpose(1, 2)
+    if layout == "gaps":
+        ld = H * D + 3 + shift
+        buf = torch.full((N * (T * ld + 5) + shift + D,), float("nan"), dtype=dt, device=DEV)
+        view = torch.as_strided(buf, (N, T, H, D), (T * ld + 5, ld, D, 1), shift)
+        view.copy_(x)
+        return view
+    return x.to(DEV)
+
+
+def near(got, ref, tol, what):
+    """|got - ref| <= tol (fp32 arithmetic and inner roundings) + the rounding to got's type; NaN, inf where ref has them."""
+    g = host(got).reshape(ref.shape)
+    fine = np.isfinite(ref)
+    same = np.array_equal(np.isnan(g), np.isnan(ref)) and np.array_equal(g[np.isinf(ref)], ref[np.isinf(ref)])
+    assert same, f"{what}: infinities or NaN in other places, {int(np.isnan(g).sum())} NaN for {int(np.isnan(ref).sum())}"
+    bound = np.broadcast_to(tol + ULP[got.dtype] * 1.01 * np.abs(ref) + TINY[got.dtype], ref.shape)
+    with np.errstate(invalid="ignore"):
+        bad = ~(np.abs(g - ref) <= bound) & fine
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} beyond the bound, the first at {np.argwhere(bad)[0]}: " \
+        f"{g[bad][0]} for {ref[bad][0]} (+- {bound[bad][0]})"
+
+
+def masks(kind, N, T, g):
+    """Token masks [N, T]: none, all, prefixes, suffixes, scattered, or an example without a token."""
+    if kind == "all":
+        return None
+    j = np.arange(T)[None, :]
+    if kind == "prefix":
+        return (j < g.integers(0, T + 1, (N, 1))).astype(np.uint8)
+    if kind == "suffix":
+        return (j >= g.integers(0, T + 1, (N, 1))).astype(np.uint8)
+    m = (g.random((N, T)) < 0.6).astype(np.uint8)
+    if kind == "none":
+        m[0] = 0
+    return m
+
+
+# ---- rotary tables -----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("positions,width", [(1, 2), (3, 64), (257, 130), (33, 6)])
+@pytest.mark.parametrize("how", [dict(), dict(base=5e5, factor=8.0), dict(base=1e6, factor=40.0, original=2048, low=1.0, high=32.0,
+                                                                        magnitude=1.37)])
+def test_rotary_table(positions, width, how):
+    """Angles of fp64 (relative error below 2^-48 up to position 257), one rounding to fp32 of values up to magnitude."""
+    say(f"[rotary_table] {positions} x {width} {how}")
+    got = E.eogp_rotary_table(positions, width, **how)
+    ref = M.rotary_table(positions, width, **how)
+    near(got, ref, 2.0 ** -38, "table")
+
+
+def test_rotary_table_far_positions():
+    """Position 2^20 - 1 at frequency 1 turns 166,886 times: an fp32 angle would be off by 2^-5."""
+    say("[rotary_table] 2^20 x 2")
+    got = host(E.eogp_rotary_table(1 << 20, 2))[-1, 0]
+    assert np.all(np.abs(got - M.rotary_table(1 << 20, 2)[-1, 0]) <= 2.0 ** -24)
+
+
+# ---- norms and rotation of heads -----------------------------------------------------------------------------------
+ROTATE = [
+    # N, T, Hq, Hk, D, width, norm, interleaved, mask, layout, shift
+    (1, 1, 1, 1, 64, 64, "head", False, "all", "split", 0),
+    (2, 3, 4, 2, 128, 128, "head", False, "prefix", "split", 0),
+    (2, 5, 5, 1, 128, 64, "head", True, "some", "heads", 0),
+    (3, 7, 3, 3, 80, 40, "row", False, "suffix", "gaps", 1),
+    (2, 9, 12, 12, 64, 64, "none", True, "some", "gaps", 3),
+    (2, 33, 40, 8, 128, 128, "row", False, "none", "split", 0),
+    (1, 70, 7, 2, 33, 32, "head", True, "some", "gaps", 2),
+    (1, 70, 7, 2, 33, 14, "row", False, "some", "split", 0),
+    (2, 4, 3, 1, 256, 256, "head", False, "all", "split", 0),
+    (2, 4, 3, 1, 255, 248, "row", True, "all", "heads", 0),
+    (3, 2, 2, 0, 96, 96, "head", False, "prefix", "split", 0),
+    (2, 6, 3, 2, 7, 6, "head", False, "some", "split", 0),
+    (2, 6, 300, 2, 3, 2, "row", True, "some", "split", 0),
+    (2, 6, 2, 2, 64, 0, "head", False, "some", "split", 0),
+    (1, 5, 64, 64, 128, 128, "row", False, "some", "split", 0),
+    (1, 3, 744, 3, 11, 2, "row", False, "all", "split", 0),
+]
+
+
+def rotate_inputs(case, dt, g):
+    N, T, Hq, Hk, D, width, norm, inter, mk, layout, shift = case
+    mask = masks(mk, N, T, g)
+    table = E.eogp_rotary_table(50, width, magnitude=1.25) if width else None
+    pos = g.integers(0, 50, (N, T))
+    xs, ws = [], []
+    for H in (Hq, Hk):
+        x = rounded(g.standard_normal((N, T, H, D)) * np.exp(0.5 * g.standard_normal((H, D))) + 0.2, dt)
+        if mask is not None:
+            x[mask == 0] = np.nan
+        xs.append(x)
+        ws.append(None if norm == "none" else 1 + 0.3 * g.standard_normal(D if norm == "head" else H * D))
+    return mask, table, pos, xs, ws
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("case", ROTATE, ids=lambda c: "-".join(map(str, c)))
+def test_rotate_heads(case, dtype):
+    """The sum of squares runs in chains of at most 2 x 8 (row norm: 4 x 8) terms and 6 + 4 additions of lanes: 50
+    roundings, half of which reach rstd; products, the weight and the turn are 6 more of each pair's larger magnitude."""
+    dt = DT[dtype]
+    N, T, Hq, Hk, D, width, norm, inter, mk, layout, shift = case
+    say(f"[rotate_heads] {case} {dtype}")
+    g = gen(11, *(int(c) for c in case if not isinstance(c, (str, bool))))
+    mask, table, pos, xs, ws = rotate_inputs(case, dt, g)
+    wt = torch.float32 if shift else dt
+    ws = [None if w is None else rounded(w, wt) for w in ws]
+    ht = None if table is None else host(table)
+    xd = [lay(x, dt, layout, shift) for x in xs]
+    outs = [lay(np.full(x.shape, 7.0), dt, layout, shift) for x in xs]
+    if Hk == 0:
+        xd[1] = outs[1] = None
+    got = E.eogp_rotate_heads(xd[0], xd[1], table, dev(pos), norm, None if ws[0] is None else dev(ws[0], wt),
+                              None if ws[1] is None or Hk == 0 else dev(ws[1], wt), 1e-6, inter, dev(mask), outs[0], outs[1])
+    torch.cuda.synchronize()
+    for i, x in enumerate(xs):
+        if x.shape[2] == 0:
+            continue
+        flat = x.reshape(N * T, *x.shape[2:])
+        m = None if mask is None else mask.reshape(-1)
+        ref = M.rotate(flat, ht, pos.reshape(-1), norm, ws[i], 1e-6, inter, m)
+        size = M.rotate(flat, None, pos.reshape(-1), norm, ws[i], 1e-6, inter, m)
+        big = np.abs(size).max(2, keepdims=True) * 1.25 * 2            # of a head: both members of a pair
+        near(got[i].reshape(flat.shape), ref, 32 * U * big, "qk"[i])
+    # in place
+    again = [None if x is None else lay(xs[i], dt, layout, shift) for i, x in enumerate(xd)]
+    E.eogp_rotate_heads(again[0], again[1], table, dev(pos), norm, None if ws[0] is None else dev(ws[0], wt),
+                        None if ws[1] is None or Hk == 0 else dev(ws[1], wt), 1e-6, inter, dev(mask), again[0], again[1])
+    for a, b in zip(again, got):
+        assert a is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("per_example", [False, True])
+@pytest.mark.parametrize("case", ROTATE, ids=lambda c: "-".join(map(str, c)))
+def test_rotate_heads_backward(case, per_example, dtype):
+    """As above with two such sums: rstd's 32 roundings, the mean's of 60 of sum |t w xh|, 12 of the formula. Weight
+    gradients are sums over tokens and heads of products with 40 roundings each, in any order: n roundings of sum |t xh|."""
+    dt = DT[dtype]
+    N, T, Hq, Hk, D, width, norm, inter, mk, layout, shift = case
+    say(f"[rotate_heads_backward] {case} {dtype} per_example={per_example}")
+    g = gen(12, *(int(c) for c in case if not isinstance(c, (str, bool))))
+    mask, table, pos, xs, ws = rotate_inputs(case, dt, g)
+    ws = [None if w is None else rounded(w, dt) for w in ws]
+    ht = None if table is None else host(table)
+    dys = [rounded(g.standard_normal(x.shape), dt) for x in xs]
+    if mask is not None:
+        for d in dys:
+            d[mask == 0] = np.nan
+    xd, dd = [lay(x, dt, layout, shift) for x in xs], [lay(d, dt, layout) for d in dys]
+    if Hk == 0:
+        xd[1] = dd[1] = None
+    got = E.eogp_rotate_heads_backward(dd[0], dd[1], xd[0] if norm != "none" else None, xd[1] if norm != "none" else None, table,
+                                       dev(pos), norm, None if ws[0] is None else dev(ws[0], dt),
+                                       None if ws[1] is None or Hk == 0 else dev(ws[1], dt), 1e-6, inter, dev(mask), per_example)
+    torch.cuda.synchronize()
+    groups = N if per_example else 1
+    m = None if mask is None else mask.reshape(-1)
+    p = pos.reshape(-1)
+    for i, (x, dy) in enumerate(zip(xs, dys)):
+        H = x.shape[2]
+        if H == 0:
+            assert got[i] is None
+            continue
+        flat, dflat = x.reshape(N * T, H, D), dy.reshape(N * T, H, D)
+        ref, dw = M.rotate_backward(dflat, flat, ht, p, norm, ws[i], 1e-6, inter, m, groups)
+        live = np.ones(N * T, bool) if m is None else m != 0
+        t = np.zeros(dflat.shape)
+        t[live] = np.abs(M.turn(dflat[live], ht, p[live], inter, back=True))
+        pair = np.nan_to_num(np.abs(dflat)).max(2, keepdims=True) * 2.5    # bounds both members' products
+        if norm == "none":
+            near(got[i].reshape(flat.shape), ref, 4 * U * pair, "dx")
+            continue
+        xl = np.nan_to_num(flat)
+        r, gain, size = M._stats(xl, norm, ws[i], 1e-6)
+        axes = (2,) if norm == "head" else (1, 2)
+        xh, ga = np.abs(xl * r), np.abs(gain)
+        mean = ((t + pair) * ga * xh).sum(axes, keepdims=True) / size
+        tol = r * U * (60 * (t + pair) * ga + 150 * xh * mean)
+        near(got[i].reshape(flat.shape), ref, tol * live[:, None, None], "dx")
+        terms = ((t + pair) * xh * live[:, None, None]).reshape(groups, -1, H, D).sum(1)
+        terms = terms.sum(1) if norm == "head" else terms.reshape(groups, -1)
+        near(got[2 + i], dw.reshape(got[2 + i].shape), (N * T * H / groups + 60) * U * terms.reshape(got[2 + i].shape), "dw")
+
+
+def test_rotate_positions():
+    """Left out: a token's index in its example. Outside the table: NaN in turned elements alone; masked ones stay zero."""
+    say("[rotate_heads] positions")
+    q, t = torch.randn(2, 6, 3, 64, device=DEV), E.eogp_rotary_table(6, 32)
+    index = torch.arange(6, device=DEV).repeat(2, 1)
+    assert torch.equal(E.eogp_rotate_heads(q, None, t)[0], E.eogp_rotate_heads(q, None, t, index)[0])
+    index[0, 1], index[1, 2], index[1, 3] = 6, -1, 1 << 40
+    mask = torch.ones(2, 6, dtype=torch.uint8, device=DEV)
+    mask[1, 3] = 0
+    y = E.eogp_rotate_heads(q, None, t, index, token_mask=mask)[0]
+    assert y[0, 1, :, :32].isnan().all() and y[1, 2, :, :32].isnan().all() and (y[1, 3] == 0).all()
+    assert torch.equal(y[0, 1, :, 32:], q[0, 1, :, 32:]) and int(y.isnan().sum()) == 2 * 3 * 32
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+ATTEND = [
+    # N, Tq, Tk, Hq, Hkv, D, causal, window, sinks, start, q mask, k mask, layout, shift
+    (1, 1, 1, 1, 1, 64, True, 0, 0, None, "all", "all", "split", 0),
+    (2, 33, 33, 2, 2, 64, True, 0, 0, None, "prefix", "same", "split", 0),
+    (2, 64, 64, 4, 2, 128, True, 0, 0, None, "prefix", "same", "heads", 0),
+    (1, 129, 129, 5, 1, 128, True, 0, 0, None, "all", "all", "gaps", 1),
+    (2, 100, 100, 3, 3, 80, True, 17, 3, None, "suffix", "same", "split", 0),
+    (1, 257, 257, 2, 1, 33, True, 32, 0, None, "some", "same", "gaps", 3),
+    (2, 70, 70, 2, 2, 64, False, 0, 0, None, "some", "same", "split", 0),
+    (2, 150, 150, 2, 1, 64, False, 9, 40, None, "some", "same", "split", 0),
+    (1, 65, 65, 3, 1, 256, True, 0, 0, None, "prefix", "same", "split", 0),
+    (2, 40, 40, 2, 1, 200, True, 8, 1, None, "none", "same", "heads", 0),
+    (1, 40, 40, 2, 2, 8, True, 0, 0, None, "some", "same", "split", 0),
+    (3, 31, 95, 2, 2, 64, True, 0, 0, None, "all", "some", "split", 0),       # a chunk at the end of its keys
+    (4, 1, 300, 5, 1, 128, True, 0, 0, "cache", "all", "all", "split", 0),    # single tokens over a cache
+    (4, 1, 300, 8, 8, 64, True, 0, 0, "cache", "all", "all", "heads", 0),
+    (3, 3, 1000, 10, 2, 128, True, 100, 4, "cache", "all", "all", "split", 0),
+    (3, 20, 200, 6, 2, 96, True, 0, 0, "cache", "some", "all", "gaps", 5),
+    (2, 1, 5000, 2, 1, 256, True, 0, 0, "cache", "all", "some", "split", 0),
+    (3, 4, 50, 2, 1, 64, True, 0, 0, "wild", "all", "all", "split", 0),       # positions before the first and past the last key
+    (3, 90, 50, 2, 1, 64, True, 10, 3, "wild", "all", "some", "split", 0),
+    (3, 90, 50, 2, 1, 64, False, 10, 20, "wild", "all", "some", "split", 0),
+    (1, 60, 40, 2, 1, 64, True, 0, 0, None, "all", "all", "split", 0),        # more queries than keys: the first see nothing
+    (2, 5, 0, 2, 1, 64, True, 0, 0, None, "all", "all", "split", 0),
+    (2, 9, 9, 2, 1, 64, True, 1, 0, None, "all", "all", "split", 0),
+    (1, 300, 300, 8, 1, 64, True, 0, 0, None, "prefix", "same", "split", 0),
+    (1, 1, 9, 40, 1, 64, True, 0, 0, "cache", "all", "all", "split", 0),      # more rows of one token than a tile
+]
+
+
+def attend_inputs(case, dt, g):
+    N, Tq, Tk, Hq, Hkv, D, causal, window, sinks, start, qm, km, layout, shift = case
+    q = rounded(1.5 * g.standard_normal((N, Tq, Hq, D)), dt)
+    k, v = [rounded(g.standard_normal((N, Tk, Hkv, D)), dt) for _ in range(2)]
+    how = dict(causal=causal, window=window, sinks=sinks, q_start=None)
+    if start == "cache":
+        how["q_start"] = g.integers(0, Tk - Tq + 1, N)
+        for n, s in enumerate(how["q_start"]):
+            k[n, s + Tq:] = v[n, s + Tq:] = np.nan                  # never written
+    elif start == "wild":
+        how["q_start"] = np.array([-(1 << 62), 3, 1 << 62])
+    how["q_mask"] = masks(qm, N, Tq, g)
+    how["k_mask"] = how["q_mask"] if km == "same" else masks(km, N, Tk, g)
+    for x, m in ((q, how["q_mask"]), (k, how["k_mask"]), (v, how["k_mask"])):
+        if m is not None:
+            x[m == 0] = np.nan
+    return q, k, v, how
+
+
+def device_how(how):
+    masked = {x: dev(how[x], torch.uint8) for x in ("q_mask", "k_mask")}
+    return dict(how, **masked, q_start=dev(how["q_start"], torch.int64))
+
+
+def attend_bounds(q, k, v, scale, dt, how):
+    """Per output element: sum_j p |v| times the roundings of a weight, and of a row's log-sum-exp. A score of D products
+    is off by (D + 3) 2^-24 of scale sum |q k| (d below, at most of any key of the row), a weight relatively by 2 d + its
+    own arithmetic (2^-21: exponent product, exponential) + its rounding to a 16-bit type; sums run over at most Tk keys."""
+    N, Tq, Hq, D = q.shape
+    Tk = k.shape[1]
+    spread, rel = np.zeros(q.shape), np.zeros((N, Tq, Hq))
+    for n in range(N):
+        see = M.sight(n, Tq, Tk, **how)
+        rows, cols = see.any(1), see.any(0)
+        for h in range(Hq):
+            hk = h * k.shape[2] // Hq
+            p, _ = M.head_weights(q[n, :, h], k[n, :, hk], see, scale)
+            qa, ka = np.where(rows[:, None], np.abs(q[n, :, h]), 0.0), np.where(cols[:, None], np.abs(k[n, :, hk]), 0.0)
+            d = (D + 3) * U * scale * np.where(see, qa @ ka.T, 0.0).max(1, initial=0.0)
+            rel[n, :, h] = 2 * d + 2.0 ** -21 + Tk * U
+            spread[n, :, h] = p @ np.where(cols[:, None], np.abs(v[n, :, hk]), 0.0)
+    inner = 0.0 if dt == torch.float32 else ULP[dt]
+    return spread * (inner + 2 * rel[..., None]), rel
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(map(str, c)))
+def test_attention(case, dtype):
+    dt = DT[dtype]
+    N, Tq, Tk, Hq, Hkv, D, *_, layout, shift = case
+    say(f"[attention] {case} {dtype}")
+    q, k, v, how = attend_inputs(case, dt, gen(21, N, Tq, Tk, Hq, D))
+    scale = 1.3 * D ** -0.5
+    ref, rlse = M.attention(q, k, v, scale, **how)
+    tol, rel = attend_bounds(q, k, v, scale, dt, how)
+    qd, kd, vd = (lay(x, dt, layout, shift) for x in (q, k, v))
+    got, lse = E.eogp_attention(qd, kd, vd, scale, **device_how(how))
+    torch.cuda.synchronize()
+    near(got, ref, tol, "out")
+    # ln of the sum: its relative error, and one rounding of values up to |lse| and of the reference, two products
+    with np.errstate(invalid="ignore"):
+        near(lse, rlse, rel + 8 * U * (np.nan_to_num(np.abs(rlse), posinf=0) + 12), "lse")
+    # fp32 output into rows with gaps, a workspace of the caller's, no statistics: the same numbers before their rounding
+    buf = torch.full((N, Tq, Hq, D + 2), 7.0, device=DEV)
+    need = E.eogp_attention_workspace_size(N, Tq, Tk, Hq, Hkv, D, E._DTYPE_CODE[dt])
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    out32, none = E.eogp_attention(qd, kd, vd, scale, out=buf[..., 1:D + 1], stats=False, ws=ws, **device_how(how))
+    assert none is None and torch.all(buf[..., 0] == 7.0) and torch.all(buf[..., D + 1] == 7.0)
+    assert torch.equal(out32.to(dt), got)
+    assert torch.all(ws[need:] == 0xFF)
+
+
+def back_bounds(dout, q, k, v, scale, dt, how):
+    """A weight is off relatively by r (scores, log-sum-exp: as above, twice) and 2^-u of its rounding; dP by D 2^-24 of
+    sum |dout v|; delta by that and by out's own error e: sum |dout| e. So a score gradient P (dP - delta) is off by
+    P (|dP - delta| (r + 2 2^-u) + those), and fp16 ones by half a step of 2^-38 of the bound that scales them."""
+    N, Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[1], k.shape[2]
+    rout, _ = M.attention(q, k, v, scale, **how)
+    otol, rel = attend_bounds(q, k, v, scale, dt, how)
+    otol = otol + ULP[dt] * 1.01 * np.abs(rout)
+    tols = [np.zeros(x.shape) for x in (q, k, v)]
+    inner = 0.0 if dt == torch.float32 else ULP[dt]
+    for n in range(N):
+        see = M.sight(n, Tq, Tk, **how)
+        rows, cols = see.any(1)[:, None], see.any(0)[:, None]
+        for h in range(Hq):
+            hk = h * Hkv // Hq
+            p, _ = M.head_weights(q[n, :, h], k[n, :, hk], see, scale)
+            do, vh = np.where(rows, dout[n, :, h], 0.0), np.where(cols, v[n, :, hk], 0.0)
+            qa, ka = np.where(rows, np.abs(q[n, :, h]), 0.0), np.where(cols, np.abs(k[n, :, hk]), 0.0)
+            dp = do @ vh.T
+            gap = np.abs(dp - (p * dp).sum(1, keepdims=True))
+            r = 2 * rel[n, :, h][:, None]
+            wide = (D + 4) * U * (np.abs(do) @ np.abs(vh).T)
+            delta = (np.abs(do) * otol[n, :, h]).sum(1, keepdims=True) + (D + 4) * U * (np.abs(do) * np.abs(rout[n, :, h])).sum(1, keepdims=True)
+            e = p * (gap * (r + inner + 4 * U) + (1 + inner) * (wide + delta))
+            if dt == torch.float16:
+                e = e + see * 2.0 ** -38 * 2 * np.linalg.norm(do, axis=1).max(initial=0) * np.linalg.norm(vh, axis=1).max(initial=0)
+            chain = (Tk + Hq // Hkv * Tq + 8) * U
+            tols[0][n, :, h] = scale * ((e + chain * p * gap) @ ka)
+            tols[1][n, :, hk] += scale * ((e + chain * p * gap).T @ qa)
+            tols[2][n, :, hk] += (p * (r + inner + chain) + see * 2.0 ** -40).T @ np.abs(do)
+    return tols
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("case", [c for c in ATTEND if c[9] != "cache" or c[1] > 1], ids=lambda c: "-".join(map(str, c)))
+def test_attention_backward(case, dtype):
+    dt = DT[dtype]
+    N, Tq, Tk, Hq, Hkv, D, *_, layout, shift = case
+    say(f"[attention_backward] {case} {dtype}")
+    g = gen(22, N, Tq, Tk, Hq, D)
+    q, k, v, how = attend_inputs(case, dt, g)
+    scale = 1.3 * D ** -0.5
+    dout = rounded(0.01 * g.standard_normal(q.shape), dt)
+    if how["q_mask"] is not None:
+        dout[how["q_mask"] == 0] = np.nan
+    ref = M.attention_backward(dout, q, k, v, scale, **how)
+    tols = back_bounds(dout, q, k, v, scale, dt, how)
+    qd, kd, vd = (lay(x, dt, layout, shift) for x in (q, k, v))
+    hd = device_how(how)
+    out, lse = E.eogp_attention(qd, kd, vd, scale, **hd)
+    need = E.eogp_attention_backward_workspace_size(N, Tq, Tk, Hq, Hkv, D, E._DTYPE_CODE[dt])
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    dd = lay(dout, dt, "gaps", 1)
+    got = E.eogp_attention_backward(dd, qd, kd, vd, out, lse, scale, ws=ws, **hd)
+    torch.cuda.synchronize()
+    for x, y, t, name in zip(got, ref, tols, ("dq", "dk", "dv")):
+        near(x, y, t, name)
+    assert torch.all(ws[need:] == 0xFF)
+    again = E.eogp_attention_backward(dd, qd, kd, vd, out, lse, scale, ws=ws, **hd)
+    for x, y in zip(got, again):
+        assert torch.equal(x, y)
+
+
+def test_a_padded_batch_is_its_sequences():
+    """Every example of a padded batch alone, without mask: both are within the bounds of the same values."""
+    say("[attention] padded batch against single sequences")
+    N, T, H, D = 3, 96, 2, 64
+    torch.manual_seed(1)
+    q, k, v, do = (torch.randn(N, T, H, D, device=DEV) for _ in range(4))
+    lengths = [96, 41, 7]
+    mask = torch.zeros(N, T, dtype=torch.uint8, device=DEV)
+    for n, length in enumerate(lengths):
+        mask[n, :length] = 1
+        for x in (q, k, v, do):
+            x[n, length:] = float("nan")
+    out, lse = E.eogp_attention(q, k, v, q_mask=mask, k_mask=mask)
+    grads = E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask, k_mask=mask)
+    for n, length in enumerate(lengths):
+        one = [x[n:n + 1, :length] for x in (q, k, v, do)]
+        o, s = E.eogp_attention(*one[:3])
+        g = E.eogp_attention_backward(one[3], *one[:3], o, s)
+        h = [host(x) for x in one]
+        tol, rel = attend_bounds(*h[:3], D ** -0.5, torch.float32, {})
+        near(out[n:n + 1, :length], host(o), 2 * tol + U * np.abs(host(o)), "out")
+        near(lse[n:n + 1, :length], host(s), 2 * rel + 16 * U * (np.abs(host(s)) + 12), "lse")
+        for a, b, t in zip(grads, g, back_bounds(h[3], *h[:3], D ** -0.5, torch.float32, {})):
+            near(a[n:n + 1, :length], host(b), 2 * t + U * np.abs(host(b)), "gradients")
+            assert torch.all(a[n, length:] == 0)
+        assert torch.all(out[n, length:] == 0) and torch.all(lse[n, length:] == float("-inf"))
+
+
+def test_extreme_scores():
+    """Rows of one huge score, of scores that grow from tile to tile, of -inf and of equal lowest values."""
+    say("[attention] extreme scores")
+    D, T = 64, 200
+    k = torch.zeros(1, T, 1, D, device=DEV)
+    q = torch.zeros(1, 4, 1, D, device=DEV)
+    v = torch.randn(1, T, 1, D, device=DEV)
+    k[0, :, 0, 0] = torch.arange(T, device=DEV)                     # 100 per key in row 0
+    k[0, :, 0, 1] = float("-inf")
+    k[0, 150, 0, 1] = 1.0
+    q[0, 0, 0, 0], q[0, 2, 0, 2] = 100.0, 0.0
+    k[0, :, 0, 1] = torch.where(k[0, :, 0, 1] == 1.0, 1.0, -1e30)   # row 1: one key, the rest at 1e32 below
+    q[0, 1, 0, 1] = 100.0
+    k[0, :, 0, 3] = -3e37
+    q[0, 3, 0, 3] = 1.0                                             # row 3: all equal, near the lowest
+    out, lse = E.eogp_attention(q, k, v, scale=1.0, causal=False)
+    assert torch.equal(out[0, 0, 0], v[0, 199, 0]) and float(lse[0, 0, 0]) == 19900.0
+    assert torch.equal(out[0, 1, 0], v[0, 150, 0]) and float(lse[0, 1, 0]) == 100.0
+    mean = v[0, :, 0].double().mean(0)             # row 2: 200 equal weights, sums of 200 values below 4
+    assert (out[0, 2, 0].double() - mean).abs().max() < 300 * U * 4 and abs(float(lse[0, 2, 0]) - np.log(200)) < 1e-5
