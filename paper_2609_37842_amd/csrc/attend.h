@@ -57,7 +57,7 @@ __device__ __forceinline__ Span span_of(const Sight& s, int64_t p) {
   return v;
 }
 
-// (Without branches: what is tested is selected among values in matrix registers.)
+// (Without branches: what is tested is selected among values that matrix instructions made.)
 __device__ __forceinline__ bool sees(const Span& v, int j) { return ((j >= v.lo) & (j < v.hi)) | (j < v.sk); }
 
 // Division of numbers below 2^31 by one divisor.
@@ -79,6 +79,7 @@ struct Divide {
 struct Bounds {
   int lo_min, hi_max, sk_max;     // outside [lo_min, hi_max) and [0, sk_max) no row sees a key
   int lo_max, hi_min;             // in [lo_max, hi_min) every row sees every key
+  int first = 0;                  // no row sees a key before this one
 };
 
 __device__ __forceinline__ int wave_min_i(int v) {
@@ -201,70 +202,148 @@ struct RowPieces {
   }
 };
 
-// ROWS x DP elements on their way from memory to a tile, NT threads. `row_at(r)` gives row r's address
-// (always one that can be read), bit r of `live` whether it counts.
-template <typename T, int DP, int ROWS, int NT>
+// ROWS rows of a tensor's heads, `ld` elements apart, as a source of tiles.
+template <typename T>
+struct RowSource {
+  const T* base;                  // row 0
+  int64_t ld;
+  int rows;
+};
+
+// A buffer of `bytes` bytes for loads that take 0 past its end.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+
+// ROWS x DP elements on their way from memory to a tile, NT threads. FAST: rows of DP elements on 16-byte boundaries
+// that lie less than 2^31 bytes apart over a tile: addresses are one scalar per tile and one constant per thread.
+template <typename T, int DP, int ROWS, int NT, bool FAST>
 struct Stage {
   static constexpr int E = kPiece<T>, kPieces = DP / E, kROWB = DP * (int)sizeof(T);
   static constexpr int kEach = ROWS * kPieces / NT;
   static_assert(ROWS * kPieces % NT == 0, "whole rounds");
   AnyVec<T, E> x[kEach];
 
+  // Rows row0 .. of the source; those past its end are read as its last row or as zeros.
+  __device__ __forceinline__ void request(const RowSource<T>& s, int row0, int tid, int D) {
+    if constexpr (FAST) {
+      const int left = s.rows - row0, some = left < ROWS ? left : ROWS;
+      const auto r = buffer_of(s.base + (int64_t)row0 * s.ld, some > 0 ? (uint32_t)((some - 1) * s.ld + DP) * (uint32_t)sizeof(T) : 0u);
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int id = u * NT + tid;
+        const int at = (id / kPieces * (int)s.ld + id % kPieces * E) * (int)sizeof(T);
+        x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+      }
+    } else {
+      request_each(tid, D, [&](int r) { return s.base + (int64_t)(row0 + r < s.rows ? row0 + r : s.rows - 1) * s.ld; });
+    }
+  }
+  // `row_at(r)` gives row r's address (always one that can be read).
   template <typename F>
-  __device__ __forceinline__ void request(int tid, int D, F&& row_at) {
+  __device__ __forceinline__ void request_each(int tid, int D, F&& row_at) {
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
       const int id = u * NT + tid;
       x[u] = request_piece<T, E, false>(row_at(id / kPieces), (id % kPieces) * E, D);
     }
   }
+  // To a tile; zeros for rows whose bit of `live` is not set.
   __device__ __forceinline__ void store(int tid, int D, char* tile, uint64_t live) {
+    constexpr uint64_t kAll = ROWS == 64 ? ~0ull : (1ull << (ROWS & 63)) - 1;
+    if constexpr (!FAST) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) settle_piece<T, E, false>(x[u], (u * NT + tid) % kPieces * E, D);
+    }
+    if (live != kAll) {
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const uint4 w = __builtin_bit_cast(uint4, x[u]);
+        x[u] = __builtin_bit_cast(AnyVec<T, E>, (live >> ((u * NT + tid) / kPieces)) & 1 ? w : uint4{0, 0, 0, 0});
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kEach; ++u) {
-      const int id = u * NT + tid, row = id / kPieces, piece = id % kPieces;
-      settle_piece<T, E, false>(x[u], piece * E, D);
-      const uint4 w = __builtin_bit_cast(uint4, x[u]);
-      *reinterpret_cast<uint4*>(tile + tile_at<kROWB>(row, piece)) = (live >> row) & 1 ? w : uint4{0, 0, 0, 0};
+      const int id = u * NT + tid;
+      *reinterpret_cast<uint4*>(tile + tile_at<kROWB>(id / kPieces, id % kPieces)) = __builtin_bit_cast(uint4, x[u]);
     }
   }
 };
 
-// First and one past the last set byte of mask[lo .. hi), by a whole block of NT threads; {hi, hi} if none.
-// `slot` is LDS for two numbers per wave.
+// What a mask leaves of [lo, hi): first and one past the last set byte ({hi, hi} if none), and whether all between are.
+struct MaskRange {
+  int first, last;
+  bool solid;
+};
+
+// By a whole block of NT threads, 64 bytes a thread at a time; `slot` is LDS for three numbers per wave.
 template <int NT>
-__device__ __forceinline__ int2 set_range(const uint8_t* __restrict__ mask, int lo, int hi, int* slot) {
-  int last = lo, first = hi;
-  for (int64_t top = hi; top > lo; top -= NT * 16) {      // from the end: padding is skipped 16 bytes a thread
-    const int64_t from = top - 16 * ((int64_t)threadIdx.x + 1);
-    int mine = lo;
+__device__ __forceinline__ MaskRange mask_range(const uint8_t* __restrict__ mask, int lo, int hi, int (*slot)[3]) {
+  int first = hi, last = lo, count = 0;
+  for (int64_t at = lo; at < hi; at += NT * 64) {
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(1)));
+    words w[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t j = from + i;
-      if (j >= lo && mask[j]) mine = (int)j + 1;
+    for (int u = 0; u < 4; ++u) {
+      const int64_t from = at + (u * NT + (int)threadIdx.x) * 16;
+      w[u] = words{0, 0, 0, 0};
+      if (from + 16 <= hi) {
+        w[u] = *reinterpret_cast<const words*>(mask + from);
+      } else {
+        for (int i = 0; i < 16; ++i)
+          if (from + i < hi) w[u][i / 4] |= (uint32_t)mask[from + i] << (i % 4 * 8);
+      }
     }
-    mine = wave_max_i(mine);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    for (int w = 0; w < NT / 64; ++w) last = slot[w] > last ? slot[w] : last;
-    if (last > lo) break;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int from = (int)(at + (u * NT + (int)threadIdx.x) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // a bit per byte that is not 0
+        uint32_t z = w[u][i];
+        z = (((z & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | z) & 0x80808080u;
+        count += __builtin_popcount(z);
+        if (z) {
+          const int f = from + 4 * i + __builtin_ctz(z) / 8, l = from + 4 * i + 4 - __builtin_clz(z) / 8;
+          first = f < first ? f : first;
+          last = l > last ? l : last;
+        }
+      }
+    }
   }
-  for (int64_t at = lo; at < last; at += NT * 16) {
-    int mine = hi;
-#pragma unroll
-    for (int i = 15; i >= 0; --i) {
-      const int64_t j = at + 16 * (int64_t)threadIdx.x + i;
-      if (j < last && mask[j]) mine = (int)j;
-    }
-    mine = wave_min_i(mine);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    for (int w = 0; w < NT / 64; ++w) first = slot[w] < first ? slot[w] : first;
-    if (first < hi) break;
+  first = wave_min_i(first);
+  last = wave_max_i(last);
+  for (int m = 32; m; m >>= 1) count += __shfl_xor(count, m);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    slot[threadIdx.x >> 6][0] = first;
+    slot[threadIdx.x >> 6][1] = last;
+    slot[threadIdx.x >> 6][2] = count;
   }
   __syncthreads();
-  return last > lo ? int2{first, last} : int2{hi, hi};
+  count = 0;
+  for (int w = 0; w < NT / 64; ++w) {
+    first = slot[w][0] < first ? slot[w][0] : first;
+    last = slot[w][1] > last ? slot[w][1] : last;
+    count += slot[w][2];
+  }
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  count = __builtin_amdgcn_readfirstlane(count);
+  __syncthreads();
+  return count > 0 ? MaskRange{first, last, count == last - first} : MaskRange{hi, hi, true};
+}
+
+// Bits a .. b - 1 of 32.
+__device__ __forceinline__ uint32_t bits_between(int a, int b) {
+  a = a < 0 ? 0 : a;
+  b = b > 32 ? 32 : b;
+  return b > a ? (uint32_t)((1ull << b) - (1ull << a)) : 0u;
+}
+
+// Keys j0 .. j0 + 31 that a row sees, as bits.
+__device__ __forceinline__ uint32_t sight_bits(const Span& v, int j0) {
+  return bits_between(v.lo - j0, v.hi - j0) | bits_between(0, v.sk - j0);
 }
 
 // Tiles of KB keys that rows with bounds b have to look at: [0, head) and [from, from + count - head).

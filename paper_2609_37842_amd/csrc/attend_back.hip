@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
   __shared__ __align__(16) float row_f[2][2][RB];        // lse2, delta
   __shared__ __align__(16) int row_i[2][3][RB];          // spans
-  __shared__ int slot[NW];
+  __shared__ int slot[NW][3];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.Hq / a.Hkv;
   int b = blockIdx.x;
@@ -139,9 +139,9 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   const int any = __syncthreads_or(key_bits != 0);
   if (!any) i1 = i0;
   if (a.sight.q_mask && i0 < i1) {
-    const int2 r = set_range<NT>(a.sight.q_mask + (int64_t)n * a.sight.Tq, i0, i1, slot);
-    i0 = r.x;
-    i1 = r.y;
+    const MaskRange r = mask_range<NT>(a.sight.q_mask + (int64_t)n * a.sight.Tq, i0, i1, slot);
+    i0 = r.first;
+    i1 = r.last;
   }
   const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
   int t = (int)((int64_t)row_tiles * split / a.splits);
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>);
 
-  Stage<T, DP, RB, NT> qs, os;
+  Stage<T, DP, RB, NT, false> qs, os;
   float r_lse2 = 0.f, r_delta = 0.f;
   Span r_span{0, 0, 0};
   bool r_live = false;
@@ -173,8 +173,8 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
         return x.row(n, i, kvh * G + a.by_group.rest(row, i));
       };
     };
-    qs.request(threadIdx.x, a.D, at(a.q));
-    os.request(threadIdx.x, a.D, at(a.dout));
+    qs.request_each(threadIdx.x, a.D, at(a.q));
+    os.request_each(threadIdx.x, a.D, at(a.dout));
     const int row = r0 + l, rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
     const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + kvh * G + a.by_group.rest(rc, i);
     r_lse2 = row < rows_hi ? a.lse2[id] : INFINITY;
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   constexpr int NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [2][K, V]
-  __shared__ int slot[NW], all[3][NW];
+  __shared__ int slot[NW][3], all[3][NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.Hq / a.Hkv, rows = G * a.sight.Tq;
   const int unit = blockIdx.x % units, tile_row = a.row_tiles - 1 - blockIdx.x / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
@@ -339,10 +339,10 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
   if (kmask) {
     const int from = bd.sk_max > 0 ? 0 : bd.lo_min, to = max(bd.hi_max, bd.sk_max);
-    const int2 m = set_range<NT>(kmask, min(from, to), to, slot);
-    bd.lo_min = max(bd.lo_min, m.x);
-    bd.hi_max = min(bd.hi_max, m.y);
-    bd.sk_max = bd.sk_max > m.x ? min(bd.sk_max, m.y) : 0;
+    const MaskRange m = mask_range<NT>(kmask, min(from, to), to, slot);
+    bd.lo_min = max(bd.lo_min, m.first);
+    bd.hi_max = min(bd.hi_max, m.last);
+    bd.sk_max = bd.sk_max > m.first ? min(bd.sk_max, m.last) : 0;
   }
   const Tiles tiles = tiles_of(bd, KB);
 
@@ -355,16 +355,13 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
 
-  const T *kbase = a.k.row(n, 0, kvh), *vbase = a.v.row(n, 0, kvh);
-  Stage<T, DP, KB, NT> ks, vs;
+  const RowSource<T> ksrc{a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk}, vsrc{a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk};
+  Stage<T, DP, KB, NT, false> ks, vs;
   bool key_live = false;
   auto request = [&](int tile) {
     const int j0 = tile * KB;
-    auto at = [&](const T* base, int64_t ld) {
-      return [=](int row) { return base + (int64_t)min(j0 + row, a.sight.Tk - 1) * ld; };
-    };
-    ks.request(threadIdx.x, a.D, at(kbase, a.k.ld_t));
-    vs.request(threadIdx.x, a.D, at(vbase, a.v.ld_t));
+    ks.request(ksrc, j0, threadIdx.x, a.D);
+    vs.request(vsrc, j0, threadIdx.x, a.D);
     const int j = j0 + l;
     key_live = ((j >= bd.lo_min && j < bd.hi_max) || j < bd.sk_max) && (!kmask || kmask[j]);
   };
