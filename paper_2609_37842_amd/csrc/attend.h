@@ -75,22 +75,28 @@ struct Divide {
   __device__ __forceinline__ int rest(int n, int q) const { return n - q * (int)by; }
 };
 
-// The three numbers of every row of a set of rows, as bounds: where any row sees keys, and where all do.
+// Where any of a set of rows sees keys: none outside [lo, hi) and [0, sk), none before `first`.
 struct Bounds {
-  int lo_min, hi_max, sk_max;     // outside [lo_min, hi_max) and [0, sk_max) no row sees a key
-  int lo_max, hi_min;             // in [lo_max, hi_min) every row sees every key
-  int first = 0;                  // no row sees a key before this one
+  int lo, hi, sk, first;
 };
 
-__device__ __forceinline__ int wave_min_i(int v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) {
-    const int o = __shfl_xor(v, m);
-    v = o < v ? o : v;
-  }
-  return __builtin_amdgcn_readfirstlane(v);
+// Rows of a set that count, as bits of rows 0 .. 63 and 64 .. 127: none, or its first and last.
+struct LiveRows {
+  uint64_t low, high;
+  __device__ __forceinline__ bool none() const { return !(low | high); }
+  __device__ __forceinline__ int first() const { return low ? __builtin_ctzll(low) : 64 + __builtin_ctzll(high); }
+  __device__ __forceinline__ int last() const { return high ? 127 - __builtin_clzll(high) : 63 - __builtin_clzll(low); }
+};
+
+// Minimum and maximum over a wave, in every lane.
+__device__ __forceinline__ int wave_max_i(int v) {
+  v = (int)scan_steps((uint32_t)v, [](uint32_t x, auto step) {
+    const int y = (int)lane_before<decltype(step)::value>(x, x);
+    return (uint32_t)(y > (int)x ? y : (int)x);
+  });
+  return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ int wave_max_i(int v) { return -wave_min_i(-v); }
+__device__ __forceinline__ int wave_min_i(int v) { return -wave_max_i(-v); }
 
 // ---- tiles in LDS -------------------------------------------------------------------------------
 // Rows of ROWB bytes (a multiple of 128), 16-byte pieces exchanged within a row by its number, so that
@@ -184,30 +190,29 @@ __device__ __forceinline__ float half_max(float v) {
 }
 
 // A row of D elements as the pieces of a row operand, zero past the end and where the row does not count.
-template <typename T, int DP>
-struct RowPieces {
+template <typename T, int DP, bool EXACT = false>
+struct RowPieces {              // EXACT: D is DP
   static constexpr int kSteps = DP * (int)sizeof(T) / 32;
   Frag<T> f[kSteps];
-  __device__ __forceinline__ void load(const T* row, bool live, int D) {
-    const int h = (threadIdx.x >> 5) & 1;
-    AnyVec<T, kPiece<T>> x[kSteps];
+  __device__ __forceinline__ static int at(int s) { return (2 * s + (int)((threadIdx.x >> 5) & 1)) * kPiece<T>; }
+  __device__ __forceinline__ void request(const T* row, int D) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) x[s] = request_piece<T, kPiece<T>, false>(row, (2 * s + h) * kPiece<T>, D);
+    for (int s = 0; s < kSteps; ++s)
+      f[s] = __builtin_bit_cast(Frag<T>, __builtin_bit_cast(uint4, request_piece<T, kPiece<T>, false>(row, at(s), EXACT ? DP : D)));
+  }
+  __device__ __forceinline__ void settle(bool live, int D) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      settle_piece<T, kPiece<T>, false>(x[s], (2 * s + h) * kPiece<T>, D);
-      const uint4 w = __builtin_bit_cast(uint4, x[s]);
+      auto x = __builtin_bit_cast(AnyVec<T, kPiece<T>>, __builtin_bit_cast(uint4, f[s]));
+      if constexpr (!EXACT) settle_piece<T, kPiece<T>, false>(x, at(s), D);
+      const uint4 w = __builtin_bit_cast(uint4, x);
       f[s] = __builtin_bit_cast(Frag<T>, live ? w : uint4{0, 0, 0, 0});
     }
   }
-};
-
-// ROWS rows of a tensor's heads, `ld` elements apart, as a source of tiles.
-template <typename T>
-struct RowSource {
-  const T* base;                  // row 0
-  int64_t ld;
-  int rows;
+  __device__ __forceinline__ void load(const T* row, bool live, int D) {
+    request(row, D);
+    settle(live, D);
+  }
 };
 
 // A buffer of `bytes` bytes for loads that take 0 past its end.
@@ -215,8 +220,21 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, uint3
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
 }
 
-// ROWS x DP elements on their way from memory to a tile, NT threads. FAST: rows of DP elements on 16-byte boundaries
-// that lie less than 2^31 bytes apart over a tile: addresses are one scalar per tile and one constant per thread.
+// The tokens of one head as rows `ld` elements apart, a source of tiles.
+template <typename T>
+struct RowSource {
+  const T* base;                  // row 0
+  int64_t ld;
+  int rows;
+  __amdgpu_buffer_rsrc_t all;     // fast loads: the rows, less than 2^31 bytes
+
+  __device__ __forceinline__ RowSource(const T* b, int64_t stride, int n, int width, bool fast)
+      : base(b), ld(stride), rows(n),
+        all(buffer_of(b, fast && n > 0 ? (uint32_t)((n - 1) * stride + width) * (uint32_t)sizeof(T) : 0u)) {}
+};
+
+// ROWS x DP elements on their way from memory to a tile, NT threads. FAST: all rows of DP elements lie on 16-byte
+// boundaries within 2^31 bytes, so that an address is a number per tile plus one per thread.
 template <typename T, int DP, int ROWS, int NT, bool FAST>
 struct Stage {
   static constexpr int E = kPiece<T>, kPieces = DP / E, kROWB = DP * (int)sizeof(T);
@@ -227,13 +245,11 @@ struct Stage {
   // Rows row0 .. of the source; those past its end are read as its last row or as zeros.
   __device__ __forceinline__ void request(const RowSource<T>& s, int row0, int tid, int D) {
     if constexpr (FAST) {
-      const int left = s.rows - row0, some = left < ROWS ? left : ROWS;
-      const auto r = buffer_of(s.base + (int64_t)row0 * s.ld, some > 0 ? (uint32_t)((some - 1) * s.ld + DP) * (uint32_t)sizeof(T) : 0u);
+      const int tile = row0 * (int)s.ld * (int)sizeof(T);
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
-        const int id = u * NT + tid;
-        const int at = (id / kPieces * (int)s.ld + id % kPieces * E) * (int)sizeof(T);
-        x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+        const int id = u * NT + tid, at = (id / kPieces * (int)s.ld + id % kPieces * E) * (int)sizeof(T);
+        x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(s.all, at + tile, 0, 0));
       }
     } else {
       request_each(tid, D, [&](int r) { return s.base + (int64_t)(row0 + r < s.rows ? row0 + r : s.rows - 1) * s.ld; });
@@ -276,62 +292,49 @@ struct MaskRange {
   bool solid;
 };
 
-// By a whole block of NT threads, 64 bytes a thread at a time; `slot` is LDS for three numbers per wave.
-template <int NT>
-__device__ __forceinline__ MaskRange mask_range(const uint8_t* __restrict__ mask, int lo, int hi, int (*slot)[3]) {
+// By each wave for itself, 64 bytes a lane at a time; mask [rows].
+__device__ __forceinline__ MaskRange mask_range(const uint8_t* __restrict__ mask, int rows, int lo, int hi) {
   int first = hi, last = lo, count = 0;
-  for (int64_t at = lo; at < hi; at += NT * 64) {
+  for (int64_t at = lo; at < hi; at += 64 * 64) {
     typedef uint32_t words __attribute__((ext_vector_type(4), aligned(1)));
     words w[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int64_t from = at + (u * NT + (int)threadIdx.x) * 16;
-      w[u] = words{0, 0, 0, 0};
-      if (from + 16 <= hi) {
-        w[u] = *reinterpret_cast<const words*>(mask + from);
+      const int64_t from = at + (u * 64 + (int)(threadIdx.x & 63)) * 16;
+      if (rows >= 16) {
+        w[u] = *reinterpret_cast<const words*>(mask + (from + 16 <= rows ? from : rows - 16));
       } else {
-        for (int i = 0; i < 16; ++i)
-          if (from + i < hi) w[u][i / 4] |= (uint32_t)mask[from + i] << (i % 4 * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[u][i] = 0;
+        for (int i = 0; i < rows; ++i)
+          if (from + i < rows) w[u][i / 4] |= (uint32_t)mask[from + i] << (i % 4 * 8);
       }
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int from = (int)(at + (u * NT + (int)threadIdx.x) * 16);
+      const int64_t from = at + (u * 64 + (int)(threadIdx.x & 63)) * 16;
+      const int64_t begin = rows >= 16 && from + 16 > rows ? rows - 16 : from;     // of what was read
+      uint32_t set = 0;                                    // a bit per byte that is not 0
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // a bit per byte that is not 0
         uint32_t z = w[u][i];
         z = (((z & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | z) & 0x80808080u;
-        count += __builtin_popcount(z);
-        if (z) {
-          const int f = from + 4 * i + __builtin_ctz(z) / 8, l = from + 4 * i + 4 - __builtin_clz(z) / 8;
-          first = f < first ? f : first;
-          last = l > last ? l : last;
-        }
+        set |= ((z * 0x00204081u) >> 28) << (4 * i);
       }
+      // bytes of [from, hi) alone
+      const int skip = from - begin > 16 ? 16 : (int)(from - begin), keep = hi - begin > 16 ? 16 : hi < begin ? 0 : (int)(hi - begin);
+      set = set >> skip << skip & ((1u << keep) - 1u);
+      count += __builtin_popcount(set);
+      const int f = (int)begin + __builtin_ctz(set | 0x10000u), l = (int)begin + 32 - __builtin_clz(set | 1u);
+      first = set && f < first ? f : first;
+      last = set && l > last ? l : last;
     }
   }
   first = wave_min_i(first);
   last = wave_max_i(last);
-  for (int m = 32; m; m >>= 1) count += __shfl_xor(count, m);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    slot[threadIdx.x >> 6][0] = first;
-    slot[threadIdx.x >> 6][1] = last;
-    slot[threadIdx.x >> 6][2] = count;
-  }
-  __syncthreads();
-  count = 0;
-  for (int w = 0; w < NT / 64; ++w) {
-    first = slot[w][0] < first ? slot[w][0] : first;
-    last = slot[w][1] > last ? slot[w][1] : last;
-    count += slot[w][2];
-  }
-  first = __builtin_amdgcn_readfirstlane(first);
-  last = __builtin_amdgcn_readfirstlane(last);
-  count = __builtin_amdgcn_readfirstlane(count);
-  __syncthreads();
-  return count > 0 ? MaskRange{first, last, count == last - first} : MaskRange{hi, hi, true};
+  uint32_t total = wave_scan((uint32_t)count);
+  total = (uint32_t)__builtin_amdgcn_readlane((int)total, 63);
+  return total > 0 ? MaskRange{first, last, (int)total == last - first} : MaskRange{hi, hi, true};
 }
 
 // Bits a .. b - 1 of 32.
@@ -346,18 +349,62 @@ __device__ __forceinline__ uint32_t sight_bits(const Span& v, int j0) {
   return bits_between(v.lo - j0, v.hi - j0) | bits_between(0, v.sk - j0);
 }
 
+// Bounds of the keys that rows at positions `first` to `last` see (their numbers grow with the position), no further
+// than the first and last key that the mask leaves; no mask any more where it leaves all between.
+__device__ __forceinline__ Bounds bounds_of(const Sight& s, int64_t first, int64_t last, const MaskRange& m, const uint8_t*& kmask) {
+  const Span f = span_of(s, first), l = span_of(s, last);
+  Bounds b{f.lo, l.hi, l.sk, 0};
+  if (!kmask) return b;
+  b.lo = max(b.lo, m.first);
+  b.hi = min(b.hi, m.last);
+  b.sk = b.sk > m.first ? min(b.sk, m.last) : 0;
+  b.first = m.first;
+  if (m.solid) kmask = nullptr;
+  return b;
+}
+
+// The mask's range for rows at those positions: of all keys where a wave reads them at once (which need not wait for the
+// rows' own masks), else of the keys that the rows see.
+constexpr int kMaskAtOnce = 4096;
+__device__ __forceinline__ MaskRange range_of(const Sight& s, const uint8_t* kmask, int64_t first, int64_t last) {
+  const Span f = span_of(s, first), l = span_of(s, last);
+  const int to = max(l.hi, l.sk);
+  return mask_range(kmask, s.Tk, l.sk > 0 ? 0 : min(f.lo, to), to);
+}
+
+// Keys of a tile that any row of the block sees, as bits, with the mask's byte of the lane's key (1 without a mask).
+struct KeyMask {
+  const uint8_t* bytes;           // without a mask, any that can be read: byte 0 is, and does not matter
+  int index;                      // all bits set, or none without a mask
+  int last;
+  __device__ __forceinline__ KeyMask(const uint8_t* mask, const void* other, int Tk)
+      : bytes(mask ? mask : static_cast<const uint8_t*>(other)), index(mask ? -1 : 0), last(Tk - 1) {}
+  __device__ __forceinline__ uint8_t request(int j) const { return bytes[min(j, last) & index]; }
+  __device__ __forceinline__ uint32_t bits(const Bounds& b, int j0, uint8_t byte) const {
+    const uint32_t seen = (bits_between(b.lo - j0, b.hi - j0) | bits_between(0, b.sk - j0)) & ~bits_between(0, b.first - j0);
+    return seen & ((uint32_t)__ballot(byte != 0) | ~(uint32_t)index);
+  }
+};
+
+// Scores that their row does not see become -inf.
+__device__ __forceinline__ void hide(f32x16& s, const Span& span, uint32_t bits, int j0) {
+  const uint32_t seen = (bits & sight_bits(span, j0)) >> (4 * ((threadIdx.x >> 5) & 1));
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e / 4) + e % 4)) & 1 ? s[e] : -INFINITY;
+}
+
 // Tiles of KB keys that rows with bounds b have to look at: [0, head) and [from, from + count - head).
 struct Tiles {
   int head, from, count;
-  __device__ __forceinline__ int at(int i) const { return i < head ? i : from + i - head; }
+  __device__ __forceinline__ int at(int i) const { return i + (i < head ? 0 : from - head); }
 };
 
 __device__ __forceinline__ Tiles tiles_of(const Bounds& b, int kb) {
   Tiles t;
-  const int sk = (b.sk_max + kb - 1) / kb;
-  const int end = (b.hi_max + kb - 1) / kb;
-  t.from = b.lo_min < b.hi_max ? b.lo_min / kb : end;
-  const int tail = b.lo_min < b.hi_max ? end - t.from : 0;
+  const int sk = (b.sk + kb - 1) / kb;
+  const int end = (b.hi + kb - 1) / kb;
+  t.from = b.lo < b.hi ? b.lo / kb : end;
+  const int tail = b.lo < b.hi ? end - t.from : 0;
   if (tail == 0) t.from = sk;
   t.head = sk < t.from ? sk : t.from;
   int more = 0;

@@ -16,6 +16,7 @@ struct AttendArgs {
   Sight sight;
   int N, Hq, Hkv, D;
   Divide by_group;                // query heads of a key head
+  Divide by_splits, by_units, by_heads;   // splits; key heads of all examples, of one
   float scale_log2;               // scale log2(e): weights are powers of two of scores times it
   float* lse;                     // [N, Tq, Hq] or NULL
   int row_tiles, splits;
@@ -30,64 +31,31 @@ template <typename T> constexpr float kLift = 0.f;
 template <> constexpr float kLift<_Float16> = 7.f;
 constexpr float kLowest = -1e30f;   // reference of a row that has seen no key (finite: differences stay numbers)
 
-// What a lane knows of its rows. Rows of a head group: query i of head kvh G + g is row i G + g of key head kvh.
-template <typename T, int QG>
-struct Rows {
-  int i[QG], h[QG];               // query and head of the lane's row in each group of 32
-  bool live[QG];
-  Span span[QG];
-  Bounds b;                       // of the wave's rows
-
-  __device__ __forceinline__ void place(const AttendArgs<T>& a, int n, int kvh, int first, int rows, int64_t start) {
-    const int G = a.by_group.by;
-    b = Bounds{a.sight.Tk, 0, 0, 0, a.sight.Tk};
+// Elements c .. c + 3 of a row of D (EXACT: D is a multiple of 4), by plain stores: the lines are filled by the two
+// halves of the wave, one after the other.
+template <typename T, bool EXACT>
+__device__ __forceinline__ void put4(T* row, int c, int D, const float (&v)[4]) {
+  if (EXACT || c + 4 <= D) {
+    AnyVec<T, 4> x;
 #pragma unroll
-    for (int qg = 0; qg < QG; ++qg) {
-      const int r = first + qg * 32 + (int)(threadIdx.x & 31), rc = r < rows ? r : rows - 1;
-      i[qg] = a.by_group.quotient(rc);
-      h[qg] = kvh * G + a.by_group.rest(rc, i[qg]);
-      live[qg] = r < rows && (!a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i[qg]]);
-      span[qg] = live[qg] ? span_of(a.sight, start + i[qg]) : Span{0, 0, 0};
-      if (live[qg]) {
-        const bool some = span[qg].hi > span[qg].lo;
-        b.lo_min = min(b.lo_min, some ? span[qg].lo : a.sight.Tk);
-        b.hi_max = max(b.hi_max, some ? span[qg].hi : 0);
-        b.sk_max = max(b.sk_max, span[qg].sk);
-        b.lo_max = max(b.lo_max, span[qg].lo);
-        b.hi_min = min(b.hi_min, span[qg].hi);
-      }
-    }
-    b.lo_max = wave_max_i(b.lo_max);
-    b.hi_min = wave_min_i(b.hi_min);
-    b.lo_min = wave_min_i(b.lo_min);
-    b.hi_max = wave_max_i(b.hi_max);
-    b.sk_max = wave_max_i(b.sk_max);
+    for (int e = 0; e < 4; ++e) x[e] = (T)v[e];
+    *reinterpret_cast<AnyVec<T, 4>*>(row + c) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < D) row[c + e] = (T)v[e];
   }
-};
-
-// Bounds no further than the first and last key that the mask leaves, by the whole block; no mask any more where it
-// leaves all between.
-template <int NT>
-__device__ __forceinline__ void clip_bounds(Bounds& b, const uint8_t*& kmask, int (*slot)[3]) {
-  if (!kmask) return;
-  const int from = b.sk_max > 0 ? 0 : b.lo_min, to = max(b.hi_max, b.sk_max);
-  const MaskRange r = mask_range<NT>(kmask, min(from, to), to, slot);
-  b.lo_min = max(b.lo_min, r.first);
-  b.hi_max = min(b.hi_max, r.last);
-  b.sk_max = b.sk_max > r.first ? min(b.sk_max, r.last) : 0;
-  b.first = r.first;
-  if (r.solid) kmask = nullptr;
 }
 
 // A row group's results: to the output, or unnormalised with their reference and sum to a worker's part.
-template <typename T, int DP>
+template <typename T, int DP, bool EXACT>
 __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* acc, float ref, float sum, int n, int r, int i,
                                          int hq, bool live, int64_t part_row) {
-  const int h = (threadIdx.x >> 5) & 1;
+  const int h = (threadIdx.x >> 5) & 1, D = EXACT ? DP : a.D;
   const float total = half_sum(sum);
   if (r < 0) return;
   if (a.part) {                                          // joined by k_attend_join
-    float* to = a.part + part_row * (a.D + 2);
+    float* to = a.part + part_row * (D + 2);
     if (h == 0) {
       to[0] = ref;
       to[1] = total;
@@ -97,7 +65,7 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float v[4] = {acc[dt][4 * g], acc[dt][4 * g + 1], acc[dt][4 * g + 2], acc[dt][4 * g + 3]};
-        store_piece<float, 4>(to + 2, dt * 32 + 8 * g + 4 * h, a.D, v);
+        put4<float, EXACT>(to + 2, dt * 32 + 8 * g + 4 * h, D, v);
       }
     return;
   }
@@ -116,26 +84,31 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = some ? acc[dt][4 * g + e] * inv : 0.f;
       if (a.out_f32)
-        store_piece<float, 4>(static_cast<float*>(a.out) + at, c, a.D, v);
+        put4<float, EXACT>(static_cast<float*>(a.out) + at, c, D, v);
       else
-        store_piece<T, 4>(static_cast<T*>(a.out) + at, c, a.D, v);
+        put4<T, EXACT>(static_cast<T*>(a.out) + at, c, D, v);
     }
 }
 
-// Keys of a tile that any row of the block sees, as bits, with the mask's byte of the lane's key (1 without a mask).
-__device__ __forceinline__ uint32_t tile_bits(const Bounds& b, int j0, uint8_t mask) {
-  const uint32_t seen = (bits_between(b.lo_min - j0, b.hi_max - j0) | bits_between(0, b.sk_max - j0)) & ~bits_between(0, b.first - j0);
-  return seen & (uint32_t)__ballot(mask != 0);
-}
-__device__ __forceinline__ uint8_t mask_of(const uint8_t* kmask, int j, int Tk) {
-  return kmask ? kmask[j < Tk ? j : Tk - 1] : 1;
-}
-
-// Scores that their row does not see become -inf.
-__device__ __forceinline__ void hide(f32x16& s, const Span& span, uint32_t bits, int j0) {
-  const uint32_t seen = (bits & sight_bits(span, j0)) >> (4 * ((threadIdx.x >> 5) & 1));
+// The order of a step's instructions: operands are read kAhead products ahead, and each product is followed by its
+// share of the vector instructions.
+template <typename T, int SCORES, int VALUES, int QG>
+__device__ __forceinline__ void interleave() {
+  if constexpr (sizeof(T) == 2) {
+    constexpr int kMfma = 8, kValu = 2, kRead = 0x100, kTrans = 0x400;
+    constexpr int kAhead = 4;
+    constexpr int kValuEach = 48 * QG / (SCORES + VALUES) + 1, kTransEach = (16 * QG + SCORES + VALUES - 1) / (SCORES + VALUES);
+    __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e / 4) + e % 4)) & 1 ? s[e] : -INFINITY;
+    for (int i = 0; i < SCORES + VALUES; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, QG, 0);
+      const int ahead = i + kAhead;
+      if (ahead < SCORES) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+      else if (ahead < SCORES + VALUES) __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kValu, kValuEach, 0);
+      __builtin_amdgcn_sched_group_barrier(kTrans, kTransEach, 0);
+    }
+  }
 }
 
 // Four waves side by side over rows (QG groups of 32 each) share tiles of 32 keys. A step works on three tiles at
@@ -148,36 +121,77 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
   constexpr int NWR = 4, NT = 256, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB;
   constexpr int kRows = 32 * QG * NWR, kDt = DP / 32, kSteps = kROWB / 32, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [2] K, [2] V
-  __shared__ int slot[NWR][3], all[3][NWR];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31;
   const int tid = threadIdx.x;
   const int rows = a.by_group.by * a.sight.Tq, units = a.N * a.Hkv;
   // heavier row tiles (later positions) first
-  int b = blockIdx.x;
-  const int split = b % a.splits;
-  b /= a.splits;
-  const int unit = b % units, tile_row = a.row_tiles - 1 - b / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
+  const int b = a.by_splits.quotient(blockIdx.x), split = a.by_splits.rest(blockIdx.x, b);
+  const int turn = a.by_units.quotient(b), unit = a.by_units.rest(b, turn), tile_row = a.row_tiles - 1 - turn;
+  const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
-  const int first = tile_row * kRows + wid * QG * 32;
-  Rows<T, QG> row;
-  row.place(a, n, kvh, first, rows, start);
-  Bounds bd = row.b;
-  if (lane == 0) {
-    all[0][wid] = bd.lo_min;
-    all[1][wid] = bd.hi_max;
-    all[2][wid] = bd.sk_max;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NWR; ++w) {
-    bd.lo_min = min(bd.lo_min, all[0][w]);
-    bd.hi_max = max(bd.hi_max, all[1][w]);
-    bd.sk_max = max(bd.sk_max, all[2][w]);
-  }
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
-  clip_bounds<NT>(bd, kmask, slot);
+  const uint8_t* qmask = a.sight.q_mask ? a.sight.q_mask + (int64_t)n * a.sight.Tq : nullptr;
+
+  // Row r of a key head is query r / G of query head kvh G + r mod G. Rows of the block that count, in halves of at most
+  // 128; this wave's; and the lane's own.
+  const int r0 = tile_row * kRows, first = r0 + wid * QG * 32;
+  auto counts = [&](int r) { return r < rows && (!qmask || qmask[a.by_group.quotient(r)]); };
+  LiveRows block[QG];
+#pragma unroll
+  for (int u = 0; u < QG; ++u) {
+    block[u].low = __ballot(counts(r0 + u * 128 + lane));
+    block[u].high = __ballot(counts(r0 + u * 128 + 64 + lane));
+  }
+  int row_i[QG], row_h[QG];
+  RowPieces<T, DP, FAST> q[QG];
+#pragma unroll
+  for (int qg = 0; qg < QG; ++qg) {
+    const int r = first + qg * 32 + l, rc = r < rows ? r : rows - 1;
+    row_i[qg] = a.by_group.quotient(rc);
+    row_h[qg] = kvh * (int)a.by_group.by + a.by_group.rest(rc, row_i[qg]);
+    q[qg].request(a.q.row(n, row_i[qg], row_h[qg]), a.D);
+  }
+  MaskRange range{0, 0, true};
+  const bool at_once = a.sight.Tk <= kMaskAtOnce;
+  if (kmask && at_once) range = mask_range(kmask, a.sight.Tk, 0, a.sight.Tk);
+  bool any = false;
+  int block_first = 0, block_last = 0;
+#pragma unroll
+  for (int u = 0; u < QG; ++u)
+    if (!block[u].none()) {
+      if (!any) block_first = u * 128 + block[u].first();
+      block_last = u * 128 + block[u].last();
+      any = true;
+    }
+  auto position = [&](int r) { return start + a.by_group.quotient(r0 + r); };
+  Bounds bd{0, 0, 0, 0};
+  if (any) {
+    if (kmask && !at_once) range = range_of(a.sight, kmask, position(block_first), position(block_last));
+    bd = bounds_of(a.sight, position(block_first), position(block_last), range, kmask);
+  }
+  // the lane's spans, and the keys that all rows of the wave see
+  bool live[QG];
+  Span span[QG];
+  int lo_max = 0, hi_min = a.sight.Tk;
+#pragma unroll
+  for (int qg = 0; qg < QG; ++qg) {
+    const int at = (wid * QG + qg) * 32;
+    const LiveRows& of = block[QG == 1 ? 0 : at / 128];
+    const uint32_t mine = (uint32_t)((at % 128 < 64 ? of.low : of.high) >> (at % 64));
+    live[qg] = (mine >> l) & 1;
+    span[qg] = live[qg] ? span_of(a.sight, start + row_i[qg]) : Span{0, 0, 0};
+    if (mine) {
+      lo_max = max(lo_max, span_of(a.sight, position(at + 31 - __builtin_clz(mine))).lo);
+      hi_min = min(hi_min, span_of(a.sight, position(at + __builtin_ctz(mine))).hi);
+    }
+    q[qg].settle(live[qg], a.D);
+  }
   const Tiles tiles = tiles_of(bd, KB);
-  const int t0 = (int)((int64_t)tiles.count * split / a.splits), t1 = (int)((int64_t)tiles.count * (split + 1) / a.splits);
+  int t0 = 0, t1 = tiles.count;
+  if (a.splits > 1) {
+    t0 = (int)((int64_t)tiles.count * split / a.splits);
+    t1 = (int)((int64_t)tiles.count * (split + 1) / a.splits);
+  }
 
   f32x16 acc[QG][kDt];
   float ref[QG], sum[QG];
@@ -189,21 +203,18 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
     for (int dt = 0; dt < kDt; ++dt) acc[qg][dt] = zeros16();
   }
   if (t0 < t1) {
-    RowPieces<T, DP> q[QG];
-#pragma unroll
-    for (int qg = 0; qg < QG; ++qg) q[qg].load(a.q.row(n, row.i[qg], row.h[qg]), row.live[qg], a.D);
-    const RowSource<T> ksrc{a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk}, vsrc{a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk};
+    const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
     char *kt = lds, *vt = lds + 2 * kTile;
     Stage<T, DP, KB, NT, FAST> ks, vs;
-    auto mask_at = [&](int t) { return mask_of(kmask, tiles.at(t) * KB + l, a.sight.Tk); };
-    auto bits_at = [&](int t, uint8_t mask) { return t < t1 ? tile_bits(bd, tiles.at(t) * KB, mask) : 0; };
-    uint32_t bits = bits_at(t0, mask_at(t0)), bits_next = bits_at(t0 + 1, mask_at(t0 + 1));   // of the step's tile and the one after it
+    const KeyMask km(kmask, ksrc.base, a.sight.Tk);
+    auto bits_at = [&](int t, uint8_t byte) { return t < t1 ? km.bits(bd, tiles.at(t) * KB, byte) : 0; };
+    // bits of the step's tile and the one after it
+    const uint8_t byte0 = km.request(tiles.at(t0) * KB + l), byte1 = km.request(tiles.at(t0 + 1) * KB + l);
     ks.request(ksrc, tiles.at(t0) * KB, tid, a.D);
+    vs.request(ksrc, tiles.at(t0 + 1) * KB, tid, a.D);
+    uint32_t bits = bits_at(t0, byte0), bits_next = bits_at(t0 + 1, byte1);
     ks.store(tid, a.D, kt, bits);
-    if (t0 + 1 < t1) {
-      ks.request(ksrc, tiles.at(t0 + 1) * KB, tid, a.D);
-      ks.store(tid, a.D, kt + kTile, bits_next);
-    }
+    vs.store(tid, a.D, kt + kTile, bits_next);
     // the first step's product with the tile before: weights 0 of values 0
     for (int c = tid * 16; c < kTile; c += NT * 16) *reinterpret_cast<uint4*>(vt + kTile + c) = uint4{0, 0, 0, 0};
     f32x16 s[2][QG];
@@ -229,14 +240,13 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
       constexpr int PAR = decltype(parity)::value;
       __syncthreads();
       const char *kn = kt + (1 - PAR) * kTile, *vl = vt + (1 - PAR) * kTile;
-      const bool more = t + 2 < t1;
-      if (more) ks.request(ksrc, tiles.at(t + 2) * KB, tid, a.D);
+      ks.request(ksrc, tiles.at(t + 2) * KB, tid, a.D);   // (behind the last tile: not used)
       vs.request(vsrc, tiles.at(t) * KB, tid, a.D);
-      const uint8_t mask_after = mask_at(t + 2);
+      const uint8_t byte_after = km.request(tiles.at(t + 2) * KB + l);
       const int j0 = tiles.at(t) * KB;
-      if (!(bits == 0xFFFFFFFFu && j0 >= row.b.lo_max && j0 + KB <= row.b.hi_min)) {
+      if (!(bits == 0xFFFFFFFFu && j0 >= lo_max && j0 + KB <= hi_min)) {
 #pragma unroll
-        for (int qg = 0; qg < QG; ++qg) hide(s[PAR][qg], row.span[qg], bits, j0);
+        for (int qg = 0; qg < QG; ++qg) hide(s[PAR][qg], span[qg], bits, j0);
       }
       float next[QG], by_sum[QG];
       bool moved = false;
@@ -277,6 +287,14 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
           for (int qg = 0; qg < QG; ++qg) mma(acc[qg][dt], vf, p[1 - PAR][qg][k]);
         }
+      // (made here, and not where the next step uses them)
+#pragma unroll
+      for (int qg = 0; qg < QG; ++qg) {
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) asm volatile("" : "+v"(p[PAR][qg][k]));
+        asm volatile("" : "+v"(by_sum[qg]));
+      }
+      interleave<T, kSteps, kDt * kKs, QG>();
       if (__ballot(moved)) {
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {
@@ -291,8 +309,8 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
       }
 #pragma unroll
       for (int qg = 0; qg < QG; ++qg) sum[qg] += by_sum[qg];
-      const uint32_t bits_after = bits_at(t + 2, mask_after);
-      if (more) ks.store(tid, a.D, kt + PAR * kTile, bits_after);
+      const uint32_t bits_after = bits_at(t + 2, byte_after);
+      ks.store(tid, a.D, kt + PAR * kTile, bits_after);
       vs.store(tid, a.D, vt + PAR * kTile, bits);
       bits = bits_next;
       bits_next = bits_after;
@@ -326,51 +344,65 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
   for (int qg = 0; qg < QG; ++qg) {
     const int r = first + qg * 32 + l;
-    put_rows<T, DP>(a, acc[qg], ref[qg], sum[qg], n, r < rows ? r : -1, row.i[qg], row.h[qg], row.live[qg],
-                    ((int64_t)split * units + unit) * rows + r);
+    put_rows<T, DP, FAST>(a, acc[qg], ref[qg], sum[qg], n, r < rows ? r : -1, row_i[qg], row_h[qg], live[qg],
+                          ((int64_t)split * units + unit) * rows + r);
   }
 }
 
 // At most 32 rows a key head: single tokens, short chunks. The waves of a block take different keys, as splits do, so
 // that a cache is read by many at once; each has tiles of its own and waits for nobody.
-template <typename T, int DP, int NWK>
+template <typename T, int DP, int NWK, bool FAST>
 __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) {
-  constexpr int NT = 64 * NWK, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB;
+  constexpr int KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB;
   constexpr int kDt = DP / 32, kSteps = kROWB / 32, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [NWK] K, V
-  __shared__ int slot[NWK][3];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31;
   const int rows = a.by_group.by * a.sight.Tq, units = a.N * a.Hkv;
-  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, n = unit / a.Hkv, kvh = unit % a.Hkv;
-  Rows<T, 1> row;
-  row.place(a, n, kvh, 0, rows, a.sight.start(n));
-  Bounds bd = row.b;
+  const int unit = a.by_splits.quotient(blockIdx.x), split = a.by_splits.rest(blockIdx.x, unit);
+  const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
+  const int64_t start = a.sight.start(n);
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
-  clip_bounds<NT>(bd, kmask, slot);
+  const int rc = l < rows ? l : rows - 1, row_i = a.by_group.quotient(rc);
+  const int row_h = kvh * (int)a.by_group.by + a.by_group.rest(rc, row_i);
+  RowPieces<T, DP, FAST> q;
+  q.request(a.q.row(n, row_i, row_h), a.D);
+  const bool live = l < rows && (!a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + row_i]);
+  const uint32_t mine = (uint32_t)__ballot(live);
+  const Span span = live ? span_of(a.sight, start + row_i) : Span{0, 0, 0};
+  Bounds bd{0, 0, 0, 0};
+  int lo_max = 0, hi_min = a.sight.Tk;
+  if (mine) {
+    const int64_t p0 = start + a.by_group.quotient(__builtin_ctz(mine)), p1 = start + a.by_group.quotient(31 - __builtin_clz(mine));
+    MaskRange range{0, 0, true};
+    if (kmask) range = range_of(a.sight, kmask, p0, p1);
+    bd = bounds_of(a.sight, p0, p1, range, kmask);
+    lo_max = span_of(a.sight, p1).lo;
+    hi_min = span_of(a.sight, p0).hi;
+  }
+  q.settle(live, a.D);
   const Tiles tiles = tiles_of(bd, KB);
   const int workers = a.splits * NWK, me = split * NWK + wid;
   int t = (int)((int64_t)tiles.count * me / workers);
   const int t_end = (int)((int64_t)tiles.count * (me + 1) / workers);
 
-  RowPieces<T, DP> q;
-  q.load(a.q.row(n, row.i[0], row.h[0]), row.live[0], a.D);
   f32x16 acc[kDt];
   float ref = kLowest, sum = 0.f;
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt) acc[dt] = zeros16();
-  const RowSource<T> ksrc{a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk}, vsrc{a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk};
-  Stage<T, DP, KB, 64, false> ks, vs;
-  uint8_t mask = 0;
+  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
+  Stage<T, DP, KB, 64, FAST> ks, vs;
+  const KeyMask km(kmask, ksrc.base, a.sight.Tk);
+  uint8_t byte = 0;
   auto request = [&](int tile) {
     ks.request(ksrc, tile * KB, lane, a.D);
     vs.request(vsrc, tile * KB, lane, a.D);
-    mask = mask_of(kmask, tile * KB + l, a.sight.Tk);
+    byte = km.request(tile * KB + l);
   };
   char *kt = lds + wid * 2 * kTile, *vt = kt + kTile;
   if (t < t_end) request(tiles.at(t));
   for (; t < t_end; ++t) {
     const int j0 = tiles.at(t) * KB;
-    const uint32_t bits = tile_bits(bd, j0, mask);
+    const uint32_t bits = km.bits(bd, j0, byte);
     wave_lds_order();
     ks.store(lane, a.D, kt, bits);
     vs.store(lane, a.D, vt, bits);
@@ -380,7 +412,7 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
     f32x16 s[1] = {zeros16()};
 #pragma unroll
     for (int st = 0; st < kSteps; ++st) mma(s[0], row_frag<T, kROWB>(kt, l, st), q.f[st]);
-    if (!(bits == 0xFFFFFFFFu && j0 >= row.b.lo_max && j0 + KB <= row.b.hi_min)) hide(s[0], row.span[0], bits, j0);
+    if (!(bits == 0xFFFFFFFFu && j0 >= lo_max && j0 + KB <= hi_min)) hide(s[0], span, bits, j0);
     float most = s[0][0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) most = fmaxf(most, s[0][e]);
@@ -408,7 +440,7 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
 #pragma unroll
       for (int k = 0; k < kKs; ++k) mma(acc[dt], col_frag<T, kROWB>(vt, 0, k, dt), p[k]);
   }
-  put_rows<T, DP>(a, acc, ref, sum, n, l < rows ? l : -1, row.i[0], row.h[0], row.live[0], ((int64_t)me * units + unit) * rows + l);
+  put_rows<T, DP, FAST>(a, acc, ref, sum, n, l < rows ? l : -1, row_i, row_h, live, ((int64_t)me * units + unit) * rows + l);
 }
 
 // A wave joins the workers' parts of one row: references, sums and unnormalised outputs, in their order.
@@ -494,10 +526,10 @@ eogp_status launch(K* kfn, const A& a, int64_t blocks, int threads, int lds, hip
   return EOGP_OK;
 }
 
-// Rows of exactly the built width on 16-byte boundaries, a tile of which spans less than 2^31 bytes.
-bool fast_rows(const eogp_heads& x, int64_t D, int size) {
+// Rows of exactly the built width on 16-byte boundaries, all of a head within 2^31 bytes.
+bool fast_rows(const eogp_heads& x, int64_t rows, int64_t D, int size) {
   return D == padded(D) && (uintptr_t)x.data % 16 == 0 && x.ld_example * size % 16 == 0 && x.ld_token * size % 16 == 0 &&
-         x.ld_head * size % 16 == 0 && x.ld_token * size * 32 < ((int64_t)1 << 31);
+         x.ld_head * size % 16 == 0 && x.ld_token * size < ((int64_t)1 << 31) / (rows + 64);
 }
 
 }  // namespace
@@ -541,6 +573,9 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
     a.Hkv = (int)k.heads;
     a.D = (int)D;
     a.by_group = Divide(q.heads / k.heads);
+    a.by_splits = Divide(p.splits);
+    a.by_units = Divide(N * k.heads);
+    a.by_heads = Divide(k.heads);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.lse = lse;
     a.row_tiles = p.row_tiles;
@@ -550,9 +585,11 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
     auto go = [&](auto width) {
       constexpr int DP = decltype(width)::value, size = (int)sizeof(T);
       constexpr int NWK = waves_of_keys(DP, size);
-      if (p.few) return launch(k_attend_few<T, DP, NWK>, a, blocks, 64 * NWK, NWK * 2 * 32 * DP * size, s);
+      const bool fast = fast_rows(k, Tk, D, size) && fast_rows(v, Tk, D, size);
+      if (p.few)
+        return fast ? launch(k_attend_few<T, DP, NWK, true>, a, blocks, 64 * NWK, NWK * 2 * 32 * DP * size, s)
+                    : launch(k_attend_few<T, DP, NWK, false>, a, blocks, 64 * NWK, NWK * 2 * 32 * DP * size, s);
       constexpr int lds = 4 * 32 * DP * size;
-      const bool fast = fast_rows(k, D, size) && fast_rows(v, D, size);
       if constexpr (row_groups(DP, size) == 2) {
         if (p.wide)
           return fast ? launch(k_attend<T, DP, 2, true>, a, blocks, 256, lds, s)

@@ -116,7 +116,6 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
   __shared__ __align__(16) float row_f[2][2][RB];        // lse2, delta
   __shared__ __align__(16) int row_i[2][3][RB];          // spans
-  __shared__ int slot[NW][3];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.Hq / a.Hkv;
   int b = blockIdx.x;
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   const int any = __syncthreads_or(key_bits != 0);
   if (!any) i1 = i0;
   if (a.sight.q_mask && i0 < i1) {
-    const MaskRange r = mask_range<NT>(a.sight.q_mask + (int64_t)n * a.sight.Tq, i0, i1, slot);
+    const MaskRange r = mask_range(a.sight.q_mask + (int64_t)n * a.sight.Tq, a.sight.Tq, i0, i1);
     i0 = r.first;
     i1 = r.last;
   }
@@ -307,7 +306,8 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   constexpr int NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [2][K, V]
-  __shared__ int slot[NW][3], all[3][NW];
+  static_assert(NW == 4, "128 rows a block");
+  __shared__ uint32_t all[NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.Hq / a.Hkv, rows = G * a.sight.Tq;
   const int unit = blockIdx.x % units, tile_row = a.row_tiles - 1 - blockIdx.x / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
@@ -318,31 +318,24 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   const float lse2 = r < rows ? a.lse2[id] : INFINITY, delta = a.delta[id];
   const bool live = lse2 != INFINITY;
   const Span span = live ? span_of(a.sight, start + i) : Span{0, 0, 0};
-  Bounds bd;
-  bd.lo_min = wave_min_i(span.hi > span.lo ? span.lo : a.sight.Tk);
-  bd.hi_max = wave_max_i(span.hi > span.lo ? span.hi : 0);
-  bd.sk_max = wave_max_i(span.sk);
-  bd.lo_max = wave_max_i(span.lo);
-  bd.hi_min = wave_min_i(live ? span.hi : a.sight.Tk);
-  if (lane == 0) {
-    all[0][wid] = bd.lo_min;
-    all[1][wid] = bd.hi_max;
-    all[2][wid] = bd.sk_max;
-  }
+  // keys that any row of the block sees, and those that every row of the wave does
+  const uint32_t mine = (uint32_t)__ballot(live);
+  if (lane == 0) all[wid] = mine;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    bd.lo_min = min(bd.lo_min, all[0][w]);
-    bd.hi_max = max(bd.hi_max, all[1][w]);
-    bd.sk_max = max(bd.sk_max, all[2][w]);
-  }
+  LiveRows block{all[0] | (uint64_t)all[1] << 32, all[2] | (uint64_t)all[3] << 32};
+  auto position = [&](int at) { return start + a.by_group.quotient(tile_row * kRows + at); };
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
-  if (kmask) {
-    const int from = bd.sk_max > 0 ? 0 : bd.lo_min, to = max(bd.hi_max, bd.sk_max);
-    const MaskRange m = mask_range<NT>(kmask, min(from, to), to, slot);
-    bd.lo_min = max(bd.lo_min, m.first);
-    bd.hi_max = min(bd.hi_max, m.last);
-    bd.sk_max = bd.sk_max > m.first ? min(bd.sk_max, m.last) : 0;
+  Bounds bd{0, 0, 0, 0};
+  int lo_max = 0, hi_min = a.sight.Tk;
+  if (!block.none()) {
+    const int64_t p0 = position(block.first()), p1 = position(block.last());
+    MaskRange range{0, 0, true};
+    if (kmask) range = range_of(a.sight, kmask, p0, p1);
+    bd = bounds_of(a.sight, p0, p1, range, kmask);
+  }
+  if (mine) {
+    lo_max = span_of(a.sight, position(wid * 32 + 31 - __builtin_clz(mine))).lo;
+    hi_min = span_of(a.sight, position(wid * 32 + __builtin_ctz(mine))).hi;
   }
   const Tiles tiles = tiles_of(bd, KB);
 
@@ -355,21 +348,21 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
 
-  const RowSource<T> ksrc{a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk}, vsrc{a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk};
+  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, false), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, false);
   Stage<T, DP, KB, NT, false> ks, vs;
-  bool key_live = false;
+  const KeyMask km(kmask, ksrc.base, a.sight.Tk);
+  uint8_t byte = 0;
   auto request = [&](int tile) {
     const int j0 = tile * KB;
     ks.request(ksrc, j0, threadIdx.x, a.D);
     vs.request(vsrc, j0, threadIdx.x, a.D);
-    const int j = j0 + l;
-    key_live = ((j >= bd.lo_min && j < bd.hi_max) || j < bd.sk_max) && (!kmask || kmask[j]);
+    byte = km.request(j0 + l);
   };
   if (tiles.count > 0) request(tiles.at(0));
   for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= 1) {
     char *kt = lds + turn * 2 * kTile, *vt = kt + kTile;
-    const uint64_t bits = __ballot(key_live) & 0xFFFFFFFFull;
     const int j0 = tiles.at(t) * KB;
+    const uint64_t bits = km.bits(bd, j0, byte);
     ks.store(threadIdx.x, a.D, kt, bits);
     vs.store(threadIdx.x, a.D, vt, bits);
     __syncthreads();
@@ -381,7 +374,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
       mma(s, row_frag<T, kROWB>(kt, l, k), q.f[k]);
       mma(dp, row_frag<T, kROWB>(vt, l, k), o.f[k]);
     }
-    const bool full = bits == 0xFFFFFFFFull && j0 >= bd.lo_max && j0 + KB <= bd.hi_min;
+    const bool full = bits == 0xFFFFFFFFull && j0 >= lo_max && j0 + KB <= hi_min;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref));
