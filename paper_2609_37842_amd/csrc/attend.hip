@@ -20,7 +20,7 @@ struct AttendArgs {
   float scale_log2;               // scale log2(e): weights are powers of two of scores times it
   float* lse;                     // [N, Tq, Hq] or NULL
   int row_tiles, splits;
-  float* part;                    // splits > 1 or several waves of keys: [workers][rows of all][D + 2]
+  float *part, *part_stats;       // splits > 1: [splits][rows of all][D] unnormalised outputs, [..][2] references and sums
 };
 
 // Weights are 2^(score - reference); the reference follows a row's maximum only when that has grown by 2^kLag,
@@ -55,17 +55,17 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
   const float total = half_sum(sum);
   if (r < 0) return;
   if (a.part) {                                          // joined by k_attend_join
-    float* to = a.part + part_row * (D + 2);
+    float* to = a.part + part_row * D;
     if (h == 0) {
-      to[0] = ref;
-      to[1] = total;
+      a.part_stats[2 * part_row] = ref;
+      a.part_stats[2 * part_row + 1] = total;
     }
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float v[4] = {acc[dt][4 * g], acc[dt][4 * g + 1], acc[dt][4 * g + 2], acc[dt][4 * g + 3]};
-        put4<float, EXACT>(to + 2, dt * 32 + 8 * g + 4 * h, D, v);
+        put4<float, EXACT>(to, dt * 32 + 8 * g + 4 * h, D, v);
       }
     return;
   }
@@ -440,42 +440,109 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
 #pragma unroll
       for (int k = 0; k < kKs; ++k) mma(acc[dt], col_frag<T, kROWB>(vt, 0, k, dt), p[k]);
   }
-  put_rows<T, DP, FAST>(a, acc, ref, sum, n, l < rows ? l : -1, row_i, row_h, live, ((int64_t)me * units + unit) * rows + l);
+  // the waves' outputs to LDS (each over its own tiles, 16-byte pieces exchanged by row), and joined there
+  constexpr int kPieces4 = DP / 4;
+  static_assert(32 * DP * 4 <= 2 * kTile || sizeof(T) == 4, "a wave's output fits its tiles");
+  __shared__ float stats[2][NWK][32];
+  const float total = half_sum(sum);
+  auto at = [&](int w, int r, int piece) {
+    return reinterpret_cast<f32x4*>(lds + w * 2 * kTile + (r * kPieces4 + (piece ^ (r & (kPieces4 - 1 < 31 ? kPieces4 - 1 : 31)))) * 16);
+  };
+  wave_lds_order();
+  if (l < rows) {
+    if (lane < 32) {
+      stats[0][wid][l] = ref;
+      stats[1][wid][l] = total;
+    }
+#pragma unroll
+    for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *at(wid, l, dt * 8 + 2 * g + (lane >> 5)) = f32x4{acc[dt][4 * g], acc[dt][4 * g + 1], acc[dt][4 * g + 2], acc[dt][4 * g + 3]};
+  }
+  __syncthreads();
+  const int D = FAST ? DP : a.D;
+  for (int e = threadIdx.x; e < rows * kPieces4; e += 64 * NWK) {
+    const int r = e / kPieces4, c = e % kPieces4 * 4;
+    float most = kLowest, all = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NWK; ++w) most = fmaxf(most, stats[0][w][r]);
+#pragma unroll
+    for (int w = 0; w < NWK; ++w) {
+      const float by = __builtin_amdgcn_exp2f(stats[0][w][r] - most);
+      const f32x4 x = *at(w, r, e % kPieces4);
+      all += by * stats[1][w][r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += by * x[i];
+    }
+    if (c >= D) continue;
+    if (a.part) {
+      const int64_t row = ((int64_t)split * units + unit) * rows + r;
+      if (c == 0) {
+        a.part_stats[2 * row] = most;
+        a.part_stats[2 * row + 1] = all;
+      }
+      put4<float, FAST>(a.part + row * D, c, D, v);
+      continue;
+    }
+    const int i = a.by_group.quotient(r), hq = kvh * (int)a.by_group.by + a.by_group.rest(r, i);
+    const bool some = ((mine >> r) & 1) && all != 0.f;
+    const float inv = some ? 1.f / all : 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = some ? v[k] * inv : 0.f;
+    if (a.lse && c == 0)
+      a.lse[((int64_t)n * a.sight.Tq + i) * a.Hq + hq] = some ? (most + __builtin_amdgcn_logf(all)) * 0.6931471805599453f : -INFINITY;
+    const int64_t to = n * a.out_n + i * a.out_t + hq * a.out_h;
+    if (a.out_f32)
+      put4<float, FAST>(static_cast<float*>(a.out) + to, c, D, v);
+    else
+      put4<T, FAST>(static_cast<T*>(a.out) + to, c, D, v);
+  }
 }
 
-// A wave joins the workers' parts of one row: references, sums and unnormalised outputs, in their order.
+// A block joins the splits' parts of one row: references, sums and unnormalised outputs, each wave those of every fourth
+// split in order, and the waves' in theirs.
 template <typename T>
-__global__ __launch_bounds__(256) void k_attend_join(const AttendArgs<T> a, int workers) {
-  const int G = a.Hq / a.Hkv, rows = G * a.sight.Tq, units = a.N * a.Hkv, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(256) void k_attend_join(const AttendArgs<T> a) {
+  __shared__ float slot[4], sums[4], parts[4][256];
+  const int rows = a.by_group.by * a.sight.Tq, units = a.N * a.Hkv, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int64_t all = (int64_t)units * rows;
-  for (int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); id < all; id += (int64_t)gridDim.x * 4) {
-    const int unit = (int)(id / rows), r = (int)(id % rows), n = unit / a.Hkv, i = r / G, hq = unit % a.Hkv * G + r % G;
-    const bool live = !a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i];
-    const float* from = a.part + id * (a.D + 2);
-    const int64_t step = all * (a.D + 2);
-    float ref = kLowest;
-    for (int w = lane; w < workers; w += 64) ref = fmaxf(ref, from[w * step]);
+  for (int64_t id = blockIdx.x; id < all; id += gridDim.x) {
+    const int unit = (int)(id / rows), r = (int)(id % rows), n = unit / a.Hkv, i = a.by_group.quotient(r);
+    const int hq = unit % a.Hkv * (int)a.by_group.by + a.by_group.rest(r, i);
+    float ref = (int)threadIdx.x < a.splits ? a.part_stats[2 * ((int64_t)threadIdx.x * all + id)] : kLowest;
     ref = wave_max(ref);
+    __syncthreads();
+    if (lane == 0) slot[wid] = ref;
+    __syncthreads();
+    ref = fmaxf(fmaxf(slot[0], slot[1]), fmaxf(slot[2], slot[3]));
     float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};      // elements lane, lane + 64, ...
-    for (int w = 0; w < workers; ++w) {
-      const float by = __builtin_amdgcn_exp2f(from[w * step] - ref);
-      total += by * from[w * step + 1];
+#pragma unroll 4
+    for (int w = wid; w < a.splits; w += 4) {
+      const int64_t row = (int64_t)w * all + id;
+      const float by = __builtin_amdgcn_exp2f(a.part_stats[2 * row] - ref);
+      total += by * a.part_stats[2 * row + 1];
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < a.D) v[c] += by * from[w * step + 2 + lane + 64 * c];
+        if (64 * c < a.D) v[c] += by * a.part[row * a.D + min(lane + 64 * c, a.D - 1)];
     }
-    const bool some = live && total != 0.f;
-    const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (lane + 64 * c < a.D) {
-        const float o = some ? v[c] / total : 0.f;
-        if (a.out_f32)
-          static_cast<float*>(a.out)[at + lane + 64 * c] = o;
-        else
-          static_cast<T*>(a.out)[at + lane + 64 * c] = (T)o;
-      }
-    if (a.lse && lane == 0)
+    for (int c = 0; c < 4; ++c) parts[wid][lane + 64 * c] = v[c];
+    if (lane == 0) sums[wid] = total;
+    __syncthreads();
+    total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    const bool live = !a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i];
+    const bool some = live && total != 0.f;
+    const int c = threadIdx.x;
+    if (c < a.D) {
+      const float o = some ? ((parts[0][c] + parts[1][c]) + (parts[2][c] + parts[3][c])) / total : 0.f;
+      const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h + c;
+      if (a.out_f32)
+        static_cast<float*>(a.out)[at] = o;
+      else
+        static_cast<T*>(a.out)[at] = (T)o;
+    }
+    if (a.lse && threadIdx.x == 0)
       a.lse[((int64_t)n * a.sight.Tq + i) * a.Hq + hq] =
           some ? (ref + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
   }
@@ -491,11 +558,10 @@ constexpr int waves_of_keys(int dp, int size) { return dp * size > 512 ? 2 : 4; 
 struct Plan {
   bool few, wide;                 // one tile of rows a key head; two groups of rows a wave
   int waves_of_keys, row_tiles, splits;
-  int workers() const { return splits * waves_of_keys; }
 };
 
 constexpr int kFewRows = 32;
-constexpr int kMaxWorkers = 256;
+constexpr int kMaxSplits = 256;
 constexpr int64_t kWantBlocks = 4 * kCus;      // of a launch that splits keys
 
 Plan plan_of(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D, int64_t window,
@@ -511,7 +577,7 @@ Plan plan_of(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_
   const int64_t keys = window > 0 ? std::min(Tk, window + sinks + Tq) : Tk;
   const int64_t most = std::max<int64_t>(1, keys / (2 * 32 * p.waves_of_keys));
   const int64_t blocks = std::max<int64_t>(1, units * p.row_tiles);
-  p.splits = (int)std::min(std::min<int64_t>(most, kMaxWorkers / p.waves_of_keys), std::max<int64_t>(1, kWantBlocks / blocks));
+  p.splits = (int)std::min(std::min<int64_t>(most, kMaxSplits), std::max<int64_t>(1, kWantBlocks / blocks));
   return p;
 }
 
@@ -534,18 +600,13 @@ bool fast_rows(const eogp_heads& x, int64_t rows, int64_t D, int size) {
 
 }  // namespace
 
-// Bytes for the parts of any call of up to N examples, Tq queries and Tk keys: no launch that splits keys has more than
-// kWantBlocks blocks, unless one worker a row tile is more, and no more workers than the longest keys give. (Fewer
-// queries may be the few of a block whose waves take different keys: then every wave writes a part.)
+// Bytes for the parts of any call of up to N examples, Tq queries and Tk keys: a launch that splits keys has at most
+// kWantBlocks blocks, of at most 32 rows where a key head has no more and 128 else, and at most kMaxSplits splits.
 size_t attention_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
-  if (N == 0 || Tq == 0) return 0;
-  const int waves = waves_of_keys(padded(D), t == EOGP_F32 ? 4 : 2);
-  const int64_t rows = Hq / Hkv * Tq, units = N * Hkv;
-  // rows of the parts: (blocks at most) x rows a block x waves
-  const int64_t few = std::min<int64_t>(units * std::min<int64_t>(rows, kFewRows) * kMaxWorkers,
-                                        std::max(kWantBlocks, units) * std::min<int64_t>(rows, kFewRows) * waves);
-  const int64_t many = rows <= kFewRows || ceil_div(Tk, 64) < 2 ? 0 : kWantBlocks * 128;
-  return align256((size_t)std::max(few, many) * (D + 2) * sizeof(float));
+  if (N == 0 || Tq == 0 || Tk < 128) return 0;
+  const int64_t rows = Hq / Hkv * Tq, all = N * Hkv * rows;
+  const int64_t most = kWantBlocks * (rows <= kFewRows ? rows : 128);
+  return align256((size_t)std::min(all * kMaxSplits, most) * (D + 2) * sizeof(float));
 }
 
 eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads& v, const eogp_heads& out,
@@ -557,7 +618,7 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
   timing::Scope ts(EOGP_KT_ATTENTION, s);
   return with_type(t, [&](auto el) {
     using T = decltype(el);
-    AttendArgs<T> a;
+    AttendArgs<T> a{};
     a.q = Heads<const T>{static_cast<const T*>(q.data), q.ld_example, q.ld_token, q.ld_head};
     a.k = Heads<const T>{static_cast<const T*>(k.data), k.ld_example, k.ld_token, k.ld_head};
     a.v = Heads<const T>{static_cast<const T*>(v.data), v.ld_example, v.ld_token, v.ld_head};
@@ -580,7 +641,10 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
     a.lse = lse;
     a.row_tiles = p.row_tiles;
     a.splits = p.splits;
-    a.part = p.workers() > 1 ? static_cast<float*>(ws) : nullptr;
+    if (p.splits > 1) {
+      a.part = static_cast<float*>(ws);
+      a.part_stats = a.part + p.splits * (N * Tq * q.heads) * D;
+    }
     const int64_t blocks = N * k.heads * p.row_tiles * p.splits;
     auto go = [&](auto width) {
       constexpr int DP = decltype(width)::value, size = (int)sizeof(T);
@@ -603,9 +667,7 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
                            : D <= 128 ? go(integral_constant<int, 128>{})
                                       : go(integral_constant<int, 256>{});
     if (st != EOGP_OK || !a.part) return st;
-    const int64_t rows = N * Tq * q.heads;
-    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows, 4), 1 << 20)), dim3(256), 0, s, a,
-                       p.workers());
+    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)std::min<int64_t>(N * Tq * q.heads, 1 << 20)), dim3(256), 0, s, a);
     EOGP_LAUNCH_CHECK("attention (join)");
     return EOGP_OK;
   });
