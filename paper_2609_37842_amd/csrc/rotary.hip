@@ -11,21 +11,30 @@ namespace {
 // table[p][i] = magnitude (cos, sin)(p f_i), f_i = base^(-2i/width) (g_i + (1 - g_i) / factor), where g_i
 // runs from 0 to 1 as the pair's turns over the original length run from low to high (0 without one).
 // A far position times a frequency is many turns: frequencies, angles, cosines and sines are fp64, rounded
-// once. Each thread has one frequency and every 8th position of its block's.
-__global__ __launch_bounds__(256) void k_rotary_table(int64_t positions, int pairs, double log2_step, double inv_factor,
+// once. A thread has one frequency and K positions 8 apart: the sine and cosine of the first are computed,
+// those of the others follow by K - 1 turns of 8 f (a product of complex numbers, 2^-52 of error each).
+__global__ __launch_bounds__(256) void k_rotary_table(int64_t positions, int pairs, int K, double log2_step, double inv_factor,
                                                       double turns, double low, double inv_range, double magnitude,
                                                       float* __restrict__ table) {
   const int i = blockIdx.y * 32 + (threadIdx.x & 31);
-  if (i >= pairs) return;
+  int64_t p = (int64_t)blockIdx.x * 8 * K + (threadIdx.x >> 5);
+  if (i >= pairs || p >= positions) return;
   double f = exp2((double)i * log2_step);
   double stay = 0.0;
   if (turns > 0.0) stay = fmin(fmax((f * turns - low) * inv_range, 0.0), 1.0);
   f *= stay + (1.0 - stay) * inv_factor;
-  for (int64_t p = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); p < positions; p += (int64_t)gridDim.x * 8) {
-    double s, c;
-    sincos((double)p * f, &s, &c);
+  double s, c, ds = 0.0, dc = 1.0;
+  sincos((double)p * f, &s, &c);
+  s *= magnitude;
+  c *= magnitude;
+  if (K > 1) sincos(8.0 * f, &ds, &dc);
+  for (int k = 0; k < K && p < positions; ++k, p += 8) {
     typedef float f32x2 __attribute__((ext_vector_type(2), aligned(4)));
-    *reinterpret_cast<f32x2*>(table + (p * pairs + i) * 2) = f32x2{(float)(c * magnitude), (float)(s * magnitude)};
+    const f32x2 v{(float)c, (float)s};
+    __builtin_nontemporal_store(v, reinterpret_cast<f32x2*>(table + (p * pairs + i) * 2));
+    const double t = c * dc - s * ds;
+    s = s * dc + c * ds;
+    c = t;
   }
 }
 
@@ -46,28 +55,32 @@ struct RotateArgs {
   int64_t positions;              // rows of the table
   const int64_t* at;              // position of each token, or NULL: its index in the example
   const uint8_t* mask;
-  int64_t T_, tokens;             // tokens of an example, of a group (one example, or all)
+  int tokens;                     // of a group (one example, or all)
+  Divide by_length;               // tokens of an example
   int shift;                      // 2^shift lanes hold a head
-  int chunks[2];                  // waves (row norm: blocks) that share a token's heads, of queries and keys
-  int splits;                     // workers that share a group's tokens
-  int64_t groups;
+  int chunks[2];                  // workers that share a token's heads, of queries and keys
+  int splits;                     // blocks that share a group's tokens, for each chunk
   float* part;                    // backward: [groups][splits][chunks][part_ld] sums, or NULL
   int64_t part_ld;
 };
 
+// How a head lies in the lanes: any widths; or all pieces whole, with a pair's members in halves, or side by side.
+enum Layout { kAny = 0, kHalves = 1, kPairs = 2 };
+
 // What a lane has of a head: E pairs of the turned part (both members), or 2 E elements of the rest.
-template <typename T>
+template <typename T, int LAYOUT>
 struct Slot {
   static constexpr int E = kPiece<T>;
   int ca, cb, end_a, end_b;       // first elements of its two pieces, and where these have to end
-  bool turned, together;          // a pair's members alternate in memory
+  bool turned;
+  bool pairs;                     // a pair's members alternate in memory
   bool any;
 
   __device__ __forceinline__ void place(int slot, int D, int width, int interleaved) {
     const int half = width >> 1, turning = (half + E - 1) / E;
     turned = slot < turning;
-    together = turned && interleaved;
-    if (turned && !interleaved) {
+    pairs = turned && (LAYOUT == kAny ? interleaved != 0 : LAYOUT == kPairs);
+    if (turned && !pairs) {
       ca = slot * E;
       cb = half + ca;
       end_a = half;
@@ -78,15 +91,22 @@ struct Slot {
       end_a = end_b = turned ? width : D;
     }
     any = ca < end_a;
+    if (!any) ca = cb = 0;
   }
+  // The place in a head of element e of a and of b.
+  __device__ __forceinline__ int at_a(int e) const { return pairs ? ca + 2 * e : ca + e; }
+  __device__ __forceinline__ int at_b(int e) const { return pairs ? ca + 2 * e + 1 : cb + e; }
 };
 
-template <typename T>
+template <typename T, int LAYOUT>
 struct Raw {
-  AnyVec<T, kPiece<T>> a, b;
-  __device__ __forceinline__ void request(const Slot<T>& s, const T* row, int D) {
-    constexpr int E = kPiece<T>;
-    if (D >= E) {
+  static constexpr int E = kPiece<T>;
+  AnyVec<T, E> a, b;
+  __device__ __forceinline__ void request(const Slot<T, LAYOUT>& s, const T* row, int D) {
+    if constexpr (LAYOUT != kAny) {
+      a = *reinterpret_cast<const AnyVec<T, E>*>(row + s.ca);
+      b = *reinterpret_cast<const AnyVec<T, E>*>(row + s.cb);
+    } else if (D >= E) {
       a = request_piece<T, E, false>(row, s.ca, D);
       b = request_piece<T, E, false>(row, s.cb, D);
     } else {
@@ -97,39 +117,57 @@ struct Raw {
 };
 
 // A slot's elements as fp32, zero past its end: pair members in a and b, or its first and second piece.
-template <typename T>
+template <typename T, int LAYOUT>
 struct Values {
   static constexpr int E = kPiece<T>;
   float a[E], b[E];
 
-  __device__ __forceinline__ void take(const Slot<T>& s, Raw<T> r, int D) {
-    if (D >= E) {
-      settle_piece<T, E, false>(r.a, s.ca, D);
-      settle_piece<T, E, false>(r.b, s.cb, D);
+  __device__ __forceinline__ void take(const Slot<T, LAYOUT>& s, Raw<T, LAYOUT> r, int D) {
+    if constexpr (LAYOUT == kAny) {
+      if (D >= E) {
+        settle_piece<T, E, false>(r.a, s.ca, D);
+        settle_piece<T, E, false>(r.b, s.cb, D);
+      }
     }
     float u[E], v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      u[e] = s.ca + e < s.end_a ? (float)r.a[e] : 0.f;
-      v[e] = s.cb + e < s.end_b ? (float)r.b[e] : 0.f;
+      u[e] = (float)r.a[e];
+      v[e] = (float)r.b[e];
+      if constexpr (LAYOUT == kAny) {
+        u[e] = s.ca + e < s.end_a ? u[e] : 0.f;
+        v[e] = s.cb + e < s.end_b ? v[e] : 0.f;
+      }
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const float even = e < E / 2 ? u[2 * e % E] : v[2 * e % E], odd = e < E / 2 ? u[(2 * e + 1) % E] : v[(2 * e + 1) % E];
-      a[e] = s.together ? even : u[e];
-      b[e] = s.together ? odd : v[e];
+      a[e] = LAYOUT == kHalves ? u[e] : s.pairs ? even : u[e];
+      b[e] = LAYOUT == kHalves ? v[e] : s.pairs ? odd : v[e];
     }
   }
-  __device__ __forceinline__ void put(const Slot<T>& s, T* row) const {
+  __device__ __forceinline__ void put(const Slot<T, LAYOUT>& s, T* row) const {
+    AnyVec<T, E> x, y;
     float u[E], v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const float fu = e % 2 ? b[e / 2] : a[e / 2], fv = e % 2 ? b[E / 2 + e / 2] : a[E / 2 + e / 2];
-      u[e] = s.together ? fu : a[e];
-      v[e] = s.together ? fv : b[e];
+      u[e] = LAYOUT == kHalves ? a[e] : s.pairs ? fu : a[e];
+      v[e] = LAYOUT == kHalves ? b[e] : s.pairs ? fv : b[e];
+      x[e] = (T)u[e];
+      y[e] = (T)v[e];
     }
-    store_piece<T, E>(row, s.ca, s.end_a, u);
-    store_piece<T, E>(row, s.cb, s.end_b, v);
+    if constexpr (LAYOUT != kAny) {
+      *reinterpret_cast<AnyVec<T, E>*>(row + s.ca) = x;
+      *reinterpret_cast<AnyVec<T, E>*>(row + s.cb) = y;
+    } else {
+      store_piece<T, E>(row, s.ca, s.end_a, u);
+      store_piece<T, E>(row, s.cb, s.end_b, v);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[e] = b[e] = 0.f;
   }
   __device__ __forceinline__ float square() const {
     float s = 0.f;
@@ -141,84 +179,89 @@ struct Values {
 
 // Cosines and sines of a slot's pairs: 1 and 0 for the part that is not turned, NaN for a position that
 // the table does not have.
-template <typename T>
+template <typename T, int LAYOUT>
 struct Turn {
   static constexpr int E = kPiece<T>;
-  float c[E], s[E];
-  __device__ __forceinline__ void load(const Slot<T>& slot, const float* table, int64_t positions, int64_t p, int width,
-                                       float sign) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      c[e] = 1.f;
-      s[e] = 0.f;
-    }
+  AnyVec<float, 4> x[E / 2];
+  bool known;
+  __device__ __forceinline__ void request(const Slot<T, LAYOUT>& slot, const float* table, int64_t positions, int64_t p, int width) {
+    known = p >= 0 && p < positions;
     if (!slot.turned) return;
-    const bool known = p >= 0 && p < positions;
     const float* row = table + (known ? p : 0) * width;
-    const int first = slot.together ? slot.ca : 2 * slot.ca;
+    const int first = slot.pairs ? slot.ca : 2 * slot.ca;
+    if (positions == 0) return;
 #pragma unroll
     for (int u = 0; u < E / 2; ++u) {
-      const AnyVec<float, 4> x = fetch_piece<float, 4>(row, first + 4 * u, width, 0.f);
-      c[2 * u] = known ? x[0] : NAN;
-      s[2 * u] = known ? x[1] * sign : NAN;
-      c[2 * u + 1] = known ? x[2] : NAN;
-      s[2 * u + 1] = known ? x[3] * sign : NAN;
+      if constexpr (LAYOUT != kAny)
+        x[u] = *reinterpret_cast<const AnyVec<float, 4>*>(row + first + 4 * u);
+      else
+        x[u] = fetch_piece<float, 4>(row, first + 4 * u, width, 0.f);
     }
   }
-  __device__ __forceinline__ void apply(Values<T>& v) const {
+  __device__ __forceinline__ void apply(const Slot<T, LAYOUT>& slot, float sign, Values<T, LAYOUT>& v) const {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
+      const float c = !slot.turned ? 1.f : known ? x[e / 2][2 * (e % 2)] : NAN;
+      const float s = !slot.turned ? 0.f : known ? x[e / 2][2 * (e % 2) + 1] * sign : NAN;
       const float a = v.a[e], b = v.b[e];
-      v.a[e] = a * c[e] - b * s[e];
-      v.b[e] = a * s[e] + b * c[e];
+      v.a[e] = a * c - b * s;
+      v.b[e] = a * s + b * c;
     }
   }
 };
 
 // Tokens first, first + step, ... below n of a group, masks and positions of 64 at once.
 struct TokenQueue {
-  int64_t first, step, n, base, length;
+  int first, step, n, base;
   const uint8_t* mask;
   const int64_t* at;
+  const Divide& by_length;
   uint64_t left = 0;
   int lane_mask = 0;
   int64_t lane_at = 0;
   int64_t position;               // of the token that next returned
+  int example, index;
   bool live;
 
-  __device__ __forceinline__ TokenQueue(const uint8_t* m, const int64_t* a, int64_t f, int64_t st, int64_t rows, int64_t b,
-                                        int64_t len)
-      : first(f - 64 * st), step(st), n(rows), base(b), length(len), mask(m), at(a) {}
+  __device__ __forceinline__ TokenQueue(const uint8_t* m, const int64_t* a, int f, int st, int rows, int b, const Divide& len)
+      : first(f - 64 * st), step(st), n(rows), base(b), mask(m), at(a), by_length(len) {}
 
-  __device__ __forceinline__ int64_t next() {
+  // False at the end.
+  __device__ __forceinline__ bool next() {
     if (!left) {
       first += 64 * step;
-      if (first >= n) return -1;
-      const int64_t mine = first + (threadIdx.x & 63) * step;
+      if (first >= n) return false;
+      const int64_t mine = first + (int64_t)(threadIdx.x & 63) * step;
       const bool in = mine < n;
       left = __ballot(in);
       lane_mask = in && (!mask || mask[base + mine] != 0);
-      lane_at = !in ? 0 : at ? at[base + mine] : (base + mine) % length;
+      lane_at = in && at ? at[base + mine] : 0;
     }
-    const int k = __builtin_ctzll(left);
+    const int k = __builtin_ctzll(left), token = base + first + k * step;
     left &= left - 1;
     live = __builtin_amdgcn_readlane(lane_mask, k);
-    position = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(lane_at >> 32), k) << 32 |
-                         (uint32_t)__builtin_amdgcn_readlane((int)lane_at, k));
-    return base + first + k * step;
+    example = by_length.quotient(token);
+    index = by_length.rest(token, example);
+    position = at ? (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(lane_at >> 32), k) << 32 |
+                              (uint32_t)__builtin_amdgcn_readlane((int)lane_at, k))
+                  : index;
+    return true;
   }
 };
 
+// Sum over the 2^shift lanes that hold a head.
 __device__ __forceinline__ float lanes_sum(float v, int shift) {
   for (int m = 1; m < 1 << shift; m <<= 1) v += __shfl_xor(v, m);
   return v;
 }
 
-// Sums of two values over the threads of a block; `slot` is LDS for two floats a wave, another one for the next sums.
+// Sums of two values over the threads of a block (of one wave: over it); `slot` is LDS for two floats a wave, another
+// one for the next sums.
 template <int NT>
-__device__ __forceinline__ float2 block_sums(float u, float v, float2* slot) {
+__device__ __forceinline__ float2 row_sums(float u, float v, float2* slot) {
   u = wave_sum(u);
   v = wave_sum(v);
+  if constexpr (NT == 64) return float2{u, v};
   if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = float2{u, v};
   __syncthreads();
   float2 s = slot[0];
@@ -230,238 +273,267 @@ __device__ __forceinline__ float2 block_sums(float u, float v, float2* slot) {
   return s;
 }
 
-template <typename T>
-__device__ __forceinline__ void load_weights(const RotateArgs<T>& a, const Slot<T>& s, int tensor, int64_t from, Values<T>& w) {
-  constexpr int E = kPiece<T>;
-  const void* p = a.weight[tensor];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int ia = s.together ? s.ca + 2 * e : s.ca + e, ib = s.together ? s.ca + 2 * e + 1 : s.cb + e;
-    w.a[e] = p && ia < s.end_a ? load_any(p, a.wt, from + ia) : 1.f;
-    w.b[e] = p && ib < s.end_b ? load_any(p, a.wt, from + ib) : 1.f;
-  }
-}
+// Who works on what: a worker of NW threads (a wave, or a block for long rows) has the heads of one chunk of a token at a
+// time, R to a lane; the workers of a block take different tokens of the same group and chunk.
+template <typename T, int NORM, int NW, int R, int LAYOUT>
+struct Share {
+  static constexpr int E = kPiece<T>, NT = NW == 64 ? 256 : NW, kWorkers = NT / NW;
+  int place, tensor, H, head0, step, group, first_token, token_step, worker;
+  Slot<T, LAYOUT> slot;
 
-// y = R_p (x rstd w): each head is read once and written once. A wave holds 64 >> shift heads of a token at a
-// time (row norm: a block of four waves the whole row), R of them after one another, and requests the next
-// token's while it works; a token's cosines and sines are read once per wave.
-template <typename T, int NORM, int NT, int R>
-__global__ __launch_bounds__(NT) void k_rotate(const RotateArgs<T> a) {
-  constexpr bool kRow = NORM == kNormRow;
-  __shared__ float2 sums[2][kRow ? NT / 64 : 1];
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int place = kRow ? (int)threadIdx.x : lane, width_of = kRow ? NT : 64;    // among the threads that share a token
-  const int chunks = a.chunks[0] + a.chunks[1];
-  const int64_t worker = kRow ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wid;
-  if (worker >= (int64_t)chunks * a.splits) return;
-  const int chunk = (int)(worker % chunks);
-  const int64_t split = worker / chunks;
-  const int tensor = chunk >= a.chunks[0], H = a.heads[tensor];
-  const int head0 = (chunk - (tensor ? a.chunks[0] : 0)) * R * (width_of >> a.shift) + (place >> a.shift);
-  Slot<T> slot;
-  slot.place(place & ((1 << a.shift) - 1), a.D, a.width, a.interleaved);
-  TokenQueue queue(a.mask, a.at, split, a.splits, a.tokens, 0, a.T_);
-  const int step = width_of >> a.shift;
-  Raw<T> raw[R];
-  auto request = [&](int64_t token) {
-    const T* base = a.in[tensor].row(token / a.T_, token % a.T_, 0);
+  __device__ __forceinline__ Share(const RotateArgs<T>& a) {
+    const int chunks = a.chunks[0] + a.chunks[1], b = blockIdx.x;
+    const int chunk = b % chunks, split = b / chunks % a.splits;
+    group = b / chunks / a.splits;
+    worker = NW == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    place = NW == 64 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+    tensor = chunk >= a.chunks[0];
+    H = a.heads[tensor];
+    step = NW >> a.shift;
+    head0 = (chunk - (tensor ? a.chunks[0] : 0)) * R * step + (place >> a.shift);
+    slot.place(place & ((1 << a.shift) - 1), a.D, a.width, a.interleaved);
+    first_token = split * kWorkers + worker;
+    token_step = a.splits * kWorkers;
+  }
+  __device__ __forceinline__ int head(int r) const { return head0 + r * step; }
+  __device__ __forceinline__ bool has(int r) const { return slot.any && head(r) < H; }
+};
+
+// The weights in LDS as the lanes of a worker use them: 2 E a lane and head that it holds (for the norm of each head, 2 E),
+// in 16-byte pieces, lanes side by side.
+template <typename T, int NORM, int NW, int R, int LAYOUT>
+struct Weights {
+  static constexpr int E = kPiece<T>, kSets = NORM == kNormRow ? R : 1, kQuads = E / 2;
+  float* lds;
+
+  __device__ __forceinline__ void stage(const RotateArgs<T>& a, const Share<T, NORM, NW, R, LAYOUT>& s) {
+    if (s.worker == 0) {
+      const void* w = a.weight[s.tensor];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int head = head0 + r * step;
-      raw[r].request(slot, base + (int64_t)(head < H ? head : 0) * a.in[tensor].ld_h, a.D);
+      for (int r = 0; r < kSets; ++r)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int64_t from = NORM == kNormRow ? (int64_t)s.head(r) * a.D : 0;
+          const bool in = NORM == kNormRow ? s.has(r) : s.slot.any;
+          const int ia = s.slot.at_a(e), ib = s.slot.at_b(e);
+          put(s, r, e, w && in && ia < s.slot.end_a ? load_any(w, a.wt, from + ia) : in ? 1.f : 0.f);
+          put(s, r, E + e, w && in && ib < s.slot.end_b ? load_any(w, a.wt, from + ib) : in ? 1.f : 0.f);
+        }
     }
-  };
-  int turn_no = 0;
-  int64_t token = queue.next();
-  if (token >= 0 && queue.live) request(token);
-  while (token >= 0) {
-    const bool live = queue.live;
-    T* out = a.out[tensor].row(token / a.T_, token % a.T_, 0);
-    Values<T> v[R];
-    if (live) {
-      Turn<T> turn;
-      turn.load(slot, a.table, a.positions, queue.position, a.width, a.sin_sign);
+    __syncthreads();
+  }
+  __device__ __forceinline__ void put(const Share<T, NORM, NW, R, LAYOUT>& s, int r, int e, float v) {
+    lds[((r * kQuads + e / 4) * NW + s.place) * 4 + e % 4] = v;
+  }
+  __device__ __forceinline__ void load(const Share<T, NORM, NW, R, LAYOUT>& s, int r, Values<T, LAYOUT>& w) const {
+    const int set = NORM == kNormRow ? r : 0;
 #pragma unroll
-      for (int r = 0; r < R; ++r) v[r].take(slot, raw[r], a.D);
-      token = queue.next();
-      if (token >= 0 && queue.live) request(token);
+    for (int q = 0; q < kQuads; ++q) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lds + ((set * kQuads + q) * NW + s.place) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) (4 * q + i < E ? w.a[(4 * q + i) % E] : w.b[(4 * q + i) % E]) = x[i];
+    }
+  }
+};
+
+constexpr int weight_floats(int norm, int nw, int r, int e) { return norm == kNormNone ? 4 : (norm == kNormRow ? r : 1) * 2 * e * nw; }
+
+// y = R_p (x rstd w): each head is read once and written once, its next token's requested before this one is worked on; a
+// token's cosines and sines are read once per worker.
+template <typename T, int NORM, int NW, int R, int LAYOUT>
+__global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate(const RotateArgs<T> a) {
+  constexpr bool kRow = NORM == kNormRow;
+  constexpr int E = kPiece<T>;
+  __shared__ float2 sums[2][kRow && NW > 64 ? NW / 64 : 1];
+  __shared__ __align__(16) float staged[weight_floats(NORM, NW, R, E)];
+  const Share<T, NORM, NW, R, LAYOUT> share(a);
+  TokenQueue queue(a.mask, a.at, share.first_token, share.token_step, a.tokens, 0, a.by_length);
+  Raw<T, LAYOUT> raw[R];
+  Turn<T, LAYOUT> turn, turn_next;
+  int n = 0, t = 0;
+  bool live = false;
+  auto request = [&]() {
+    n = queue.example;
+    t = queue.index;
+    live = queue.live;
+    if (!live) return;
+    turn_next.request(share.slot, a.table, a.positions, queue.position, a.width);
+    const T* base = a.in[share.tensor].row(n, t, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r].request(share.slot, base + (share.has(r) ? share.head(r) : 0) * a.in[share.tensor].ld_h, a.D);
+  };
+  bool more = queue.next();
+  if (more) request();
+  Weights<T, NORM, NW, R, LAYOUT> weights{staged};
+  if constexpr (NORM != kNormNone) weights.stage(a, share);
+  int turn_no = 0;
+  while (more) {
+    T* out = a.out[share.tensor].row(n, t, 0);
+    Values<T, LAYOUT> v[R];
+    const bool now = live;
+    if (now) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) v[r].take(share.slot, raw[r], a.D);
+      turn = turn_next;
+    }
+    more = queue.next();
+    if (more) request();
+    if (now) {
       if constexpr (NORM != kNormNone) {
-        float row = 0.f;
+        float part[R], row = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const int head = head0 + r * step;
-          float s = slot.any && head < H ? v[r].square() : 0.f;
-          if constexpr (kRow) {
-            row += s;
-          } else {
-            s = lanes_sum(s, a.shift);
-            const float rstd = 1.f / sqrtf(s / (float)a.D + a.eps);
-            Values<T> w;
-            load_weights<T>(a, slot, tensor, 0, w);
-#pragma unroll
-            for (int e = 0; e < kPiece<T>; ++e) {
-              v[r].a[e] *= rstd * w.a[e];
-              v[r].b[e] *= rstd * w.b[e];
-            }
-          }
+          part[r] = share.has(r) ? v[r].square() : 0.f;
+          row += part[r];
         }
         if constexpr (kRow) {
-          row = block_sums<NT>(row, 0.f, sums[turn_no]).x;
+          row = row_sums<NW>(row, 0.f, sums[turn_no]).x;
           turn_no ^= 1;
-          const float rstd = 1.f / sqrtf(row / (float)((int64_t)H * a.D) + a.eps);
+        }
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const int head = head0 + r * step;
-            if (head >= H) continue;
-            Values<T> w;
-            load_weights<T>(a, slot, tensor, (int64_t)head * a.D, w);
+        for (int r = 0; r < R; ++r) {
+          const float s = kRow ? row / (float)(share.H * a.D) : lanes_sum(part[r], a.shift) / (float)a.D;
+          const float rstd = 1.f / sqrtf(s + a.eps);
+          Values<T, LAYOUT> w;
+          weights.load(share, r, w);
 #pragma unroll
-            for (int e = 0; e < kPiece<T>; ++e) {
-              v[r].a[e] *= rstd * w.a[e];
-              v[r].b[e] *= rstd * w.b[e];
-            }
+          for (int e = 0; e < E; ++e) {
+            v[r].a[e] *= rstd * w.a[e];
+            v[r].b[e] *= rstd * w.b[e];
           }
         }
       }
 #pragma unroll
-      for (int r = 0; r < R; ++r) turn.apply(v[r]);
+      for (int r = 0; r < R; ++r) turn.apply(share.slot, a.sin_sign, v[r]);
     } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < kPiece<T>; ++e) v[r].a[e] = v[r].b[e] = 0.f;
-      token = queue.next();
-      if (token >= 0 && queue.live) request(token);
+      for (int r = 0; r < R; ++r) v[r].clear();
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int head = head0 + r * step;
-      if (slot.any && head < H) v[r].put(slot, out + (int64_t)head * a.out[tensor].ld_h);
-    }
+    for (int r = 0; r < R; ++r)
+      if (share.has(r)) v[r].put(share.slot, out + share.head(r) * a.out[share.tensor].ld_h);
   }
 }
 
-// With t = R_p^T dy, xh = x rstd: dx = rstd (t w - xh mean(t w xh)), and sums of t xh over the worker's tokens (and
+// With t = R_p^T dy, xh = x rstd: dx = rstd (t w - xh mean(t w xh)), and sums of t xh over the block's tokens (and
 // heads, where each has its own norm), which k_rotate_fold adds up in order.
-template <typename T, int NORM, int NT, int R>
-__global__ __launch_bounds__(NT) void k_rotate_back(const RotateArgs<T> a) {
+template <typename T, int NORM, int NW, int R, int LAYOUT>
+__global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate_back(const RotateArgs<T> a) {
   constexpr bool kRow = NORM == kNormRow;
-  constexpr int E = kPiece<T>;
-  __shared__ float2 sums[2][kRow ? NT / 64 : 1];
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int place = kRow ? (int)threadIdx.x : lane, width_of = kRow ? NT : 64;
-  const int chunks = a.chunks[0] + a.chunks[1];
-  const int64_t worker = kRow ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wid;
-  if (worker >= (int64_t)chunks * a.splits * a.groups) return;
-  const int chunk = (int)(worker % chunks);
-  const int64_t split = worker / chunks % a.splits, group = worker / chunks / a.splits;
-  const int tensor = chunk >= a.chunks[0], H = a.heads[tensor];
-  const int step = width_of >> a.shift;
-  const int head0 = (chunk - (tensor ? a.chunks[0] : 0)) * R * step + (place >> a.shift);
-  Slot<T> slot;
-  slot.place(place & ((1 << a.shift) - 1), a.D, a.width, a.interleaved);
-  TokenQueue queue(a.mask, a.at, split, a.splits, a.tokens, group * a.tokens, a.T_);
-  Raw<T> rx[R], rg[R];
-  auto request = [&](int64_t token) {
-    const T* base = a.in[tensor].row(token / a.T_, token % a.T_, 0);
-    const T* grad = a.grad[tensor].row(token / a.T_, token % a.T_, 0);
+  constexpr int E = kPiece<T>, kSets = kRow ? R : 1, NT = NW == 64 ? 256 : NW;
+  __shared__ float2 sums[2][kRow && NW > 64 ? NW / 64 : 1];
+  constexpr int kWeights = weight_floats(NORM, NW, R, E), kFold = NW == 64 ? 4 * kSets * 2 * E * 64 : 4;
+  __shared__ __align__(16) float staged[kWeights > kFold ? kWeights : kFold];
+  const Share<T, NORM, NW, R, LAYOUT> share(a);
+  TokenQueue queue(a.mask, a.at, share.first_token, share.token_step, a.tokens, share.group * a.tokens, a.by_length);
+  Raw<T, LAYOUT> rx[R], rg[R];
+  Turn<T, LAYOUT> turn, turn_next;
+  int n = 0, t = 0;
+  bool live = false;
+  auto request = [&]() {
+    n = queue.example;
+    t = queue.index;
+    live = queue.live;
+    if (!live) return;
+    turn_next.request(share.slot, a.table, a.positions, queue.position, a.width);
+    const T *base = a.in[share.tensor].row(n, t, 0), *grad = a.grad[share.tensor].row(n, t, 0);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int head = head0 + r * step, from = head < H ? head : 0;
-      rx[r].request(slot, base + (int64_t)from * a.in[tensor].ld_h, a.D);
-      rg[r].request(slot, grad + (int64_t)from * a.grad[tensor].ld_h, a.D);
+      const int from = share.has(r) ? share.head(r) : 0;
+      rx[r].request(share.slot, base + from * a.in[share.tensor].ld_h, a.D);
+      rg[r].request(share.slot, grad + from * a.grad[share.tensor].ld_h, a.D);
     }
   };
-  Values<T> dw[kRow ? R : 1];
+  bool more = queue.next();
+  if (more) request();
+  Weights<T, NORM, NW, R, LAYOUT> weights{staged};
+  weights.stage(a, share);
+  Values<T, LAYOUT> dw[kSets];
 #pragma unroll
-  for (int r = 0; r < (kRow ? R : 1); ++r)
-#pragma unroll
-    for (int e = 0; e < E; ++e) dw[r].a[e] = dw[r].b[e] = 0.f;
+  for (int r = 0; r < kSets; ++r) dw[r].clear();
   int turn_no = 0;
-  int64_t token = queue.next();
-  if (token >= 0 && queue.live) request(token);
-  while (token >= 0) {
-    const bool live = queue.live;
-    T* out = a.out[tensor].row(token / a.T_, token % a.T_, 0);
-    Values<T> x[R], t[R];
-    if (live) {
-      Turn<T> turn;
-      turn.load(slot, a.table, a.positions, queue.position, a.width, -a.sin_sign);
+  while (more) {
+    T* out = a.out[share.tensor].row(n, t, 0);
+    Values<T, LAYOUT> x[R], g[R];
+    const bool now = live;
+    if (now) {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        x[r].take(slot, rx[r], a.D);
-        t[r].take(slot, rg[r], a.D);
-        turn.apply(t[r]);
+        x[r].take(share.slot, rx[r], a.D);
+        g[r].take(share.slot, rg[r], a.D);
       }
-      token = queue.next();
-      if (token >= 0 && queue.live) request(token);
-      float row = 0.f, dot = 0.f;
-      Values<T> w[kRow ? R : 1];
-      if constexpr (!kRow) load_weights<T>(a, slot, tensor, 0, w[0]);
+      turn = turn_next;
+    }
+    more = queue.next();
+    if (more) request();
+    if (now) {
+      float square[R], dot[R], row = 0.f, row_dot = 0.f;
+      Values<T, LAYOUT> w;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const int head = head0 + r * step;
-        const bool in = slot.any && head < H;
-        Values<T>& wr = w[kRow ? r : 0];
-        if constexpr (kRow) load_weights<T>(a, slot, tensor, (int64_t)(head < H ? head : 0) * a.D, wr);
-        float s = in ? x[r].square() : 0.f, d = 0.f;
+        turn.apply(share.slot, -a.sin_sign, g[r]);
+        weights.load(share, r, w);
+        square[r] = x[r].square();
+        dot[r] = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) d += t[r].a[e] * wr.a[e] * x[r].a[e] + t[r].b[e] * wr.b[e] * x[r].b[e];
-        d = in ? d : 0.f;
-        if constexpr (kRow) {
-          row += s;
-          dot += d;
-        } else {
-          s = lanes_sum(s, a.shift);
-          d = lanes_sum(d, a.shift);
-          const float rstd = 1.f / sqrtf(s / (float)a.D + a.eps), m = d * rstd / (float)a.D;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float ha = x[r].a[e] * rstd, hb = x[r].b[e] * rstd;
-            if (in) {
-              dw[0].a[e] += t[r].a[e] * ha;
-              dw[0].b[e] += t[r].b[e] * hb;
-            }
-            x[r].a[e] = rstd * (t[r].a[e] * wr.a[e] - ha * m);
-            x[r].b[e] = rstd * (t[r].b[e] * wr.b[e] - hb * m);
-          }
-        }
+        for (int e = 0; e < E; ++e) dot[r] += g[r].a[e] * w.a[e] * x[r].a[e] + g[r].b[e] * w.b[e] * x[r].b[e];
+        square[r] = share.has(r) ? square[r] : 0.f;
+        dot[r] = share.has(r) ? dot[r] : 0.f;
+        row += square[r];
+        row_dot += dot[r];
       }
       if constexpr (kRow) {
-        const float n = (float)((int64_t)H * a.D);
-        const float2 both = block_sums<NT>(row, dot, sums[turn_no]);
+        const float2 both = row_sums<NW>(row, row_dot, sums[turn_no]);
         turn_no ^= 1;
-        const float rstd = 1.f / sqrtf(both.x / n + a.eps), m = both.y * rstd / n;
+        row = both.x;
+        row_dot = both.y;
+      }
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R; ++r) {
+        const float count = (float)(kRow ? share.H * a.D : a.D);
+        const float s = kRow ? row : lanes_sum(square[r], a.shift), d = kRow ? row_dot : lanes_sum(dot[r], a.shift);
+        const float rstd = 1.f / sqrtf(s / count + a.eps), m = d * rstd / count;
+        const bool in = share.has(r);
+        if constexpr (R > 1 || kRow) weights.load(share, r, w);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float ha = x[r].a[e] * rstd, hb = x[r].b[e] * rstd;
-            dw[r].a[e] += t[r].a[e] * ha;
-            dw[r].b[e] += t[r].b[e] * hb;
-            x[r].a[e] = rstd * (t[r].a[e] * w[r].a[e] - ha * m);
-            x[r].b[e] = rstd * (t[r].b[e] * w[r].b[e] - hb * m);
-          }
+        for (int e = 0; e < E; ++e) {
+          const float ha = x[r].a[e] * rstd, hb = x[r].b[e] * rstd;
+          dw[kRow ? r : 0].a[e] += in ? g[r].a[e] * ha : 0.f;
+          dw[kRow ? r : 0].b[e] += in ? g[r].b[e] * hb : 0.f;
+          x[r].a[e] = rstd * (g[r].a[e] * w.a[e] - ha * m);
+          x[r].b[e] = rstd * (g[r].b[e] * w.b[e] - hb * m);
+        }
       }
     } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[r].a[e] = x[r].b[e] = 0.f;
-      token = queue.next();
-      if (token >= 0 && queue.live) request(token);
+      for (int r = 0; r < R; ++r) x[r].clear();
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int head = head0 + r * step;
-      if (slot.any && head < H) x[r].put(slot, out + (int64_t)head * a.out[tensor].ld_h);
-    }
+    for (int r = 0; r < R; ++r)
+      if (share.has(r)) x[r].put(share.slot, out + share.head(r) * a.out[share.tensor].ld_h);
   }
   if (!a.part) return;
-  float* part = a.part + worker * a.part_ld;
+  if constexpr (NW == 64) {                    // the block's four waves, in their order
+    __syncthreads();
 #pragma unroll
-  for (int r = 0; r < (kRow ? R : 1); ++r) {
-    const int head = head0 + r * step;
+    for (int r = 0; r < kSets; ++r)
+#pragma unroll
+      for (int e = 0; e < 2 * E; ++e)
+        staged[((share.worker * kSets + r) * 2 * E + e) * 64 + share.place] = e < E ? dw[r].a[e % E] : dw[r].b[e % E];
+    __syncthreads();
+    if (share.worker > 0) return;
+#pragma unroll
+    for (int r = 0; r < kSets; ++r)
+#pragma unroll
+      for (int e = 0; e < 2 * E; ++e) {
+        float& v = e < E ? dw[r].a[e % E] : dw[r].b[e % E];
+#pragma unroll
+        for (int wv = 1; wv < 4; ++wv) v += staged[((wv * kSets + r) * 2 * E + e) * 64 + share.place];
+      }
+  }
+  float* part = a.part + (int64_t)blockIdx.x * a.part_ld;
+#pragma unroll
+  for (int r = 0; r < kSets; ++r) {
     if constexpr (!kRow) {                     // the wave's heads
       for (int m = 1 << a.shift; m < 64; m <<= 1)
 #pragma unroll
@@ -470,35 +542,50 @@ __global__ __launch_bounds__(NT) void k_rotate_back(const RotateArgs<T> a) {
           dw[0].b[e] += __shfl_xor(dw[0].b[e], m);
         }
     }
-    if (!slot.any || (kRow ? head >= H : (place >> a.shift) != 0)) continue;
-    float* to = part + (kRow ? (int64_t)head * a.D : 0);
+    if (kRow ? !share.has(r) : !share.slot.any || (share.place >> a.shift) != 0) continue;
+    float* to = part + (kRow ? (int64_t)share.head(r) * a.D : 0);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int ia = slot.together ? slot.ca + 2 * e : slot.ca + e, ib = slot.together ? slot.ca + 2 * e + 1 : slot.cb + e;
-      if (ia < slot.end_a) to[ia] = dw[r].a[e];
-      if (ib < slot.end_b) to[ib] = dw[r].b[e];
+      const int ia = share.slot.at_a(e), ib = share.slot.at_b(e);
+      if (ia < share.slot.end_a) to[ia] = dw[r].a[e];
+      if (ib < share.slot.end_b) to[ib] = dw[r].b[e];
     }
   }
 }
 
-// Sums of the workers' parts, in a fixed order: 32 columns x 8 slices of the workers per block.
-__global__ __launch_bounds__(256) void k_rotate_fold(const float* __restrict__ part, int64_t part_ld, int64_t groups,
-                                                     int splits, int chunks, int first, int count, int64_t n,
-                                                     float* __restrict__ out) {
-  __shared__ float sum[8][33];
-  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  const int64_t col_blocks = (n + 31) / 32;
-  for (int64_t unit = blockIdx.x; unit < groups * col_blocks; unit += gridDim.x) {
-    const int64_t group = unit / col_blocks, c = unit % col_blocks * 32 + col;
+// Sums of the blocks' parts, in a fixed order: 32 columns x 32 slices of the parts per block, eight requests of a thread
+// at a time. Columns run over both tensors' weights.
+__global__ __launch_bounds__(1024) void k_rotate_fold(const float* __restrict__ part, int64_t part_ld, int64_t groups, int splits,
+                                                      int chunks_q, int chunks_k, int nq, int nk, float* __restrict__ dq,
+                                                      float* __restrict__ dk) {
+  __shared__ float sum[32][33];
+  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, chunks = chunks_q + chunks_k;
+  const int64_t blocks_q = (nq + 31) / 32, blocks = blocks_q + (nk + 31) / 32;
+  for (int64_t unit = blockIdx.x; unit < groups * blocks; unit += gridDim.x) {
+    const int64_t group = unit / blocks, b = unit % blocks;
+    const bool of_k = b >= blocks_q;
+    const int c = (int)(of_k ? b - blocks_q : b) * 32 + col, n = of_k ? nk : nq, count = of_k ? chunks_k : chunks_q;
+    const float* from = part + (group * splits * chunks + (of_k ? chunks_q : 0)) * part_ld + c;
+    float* out = of_k ? dk : dq;
     float s = 0.f;
-    if (c < n)
-      for (int64_t j = slice; j < (int64_t)splits * count; j += 8)
-        s += part[((group * splits + j / count) * chunks + first + j % count) * part_ld + c];
+    if (c < n && out) {
+      const int all = splits * count;
+      for (int j = slice; j < all; j += 8 * 32) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = j + k * 32;
+          v[k] = at < all ? from[((int64_t)(at / count) * chunks + at % count) * part_ld] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[k];
+      }
+    }
     sum[slice][col] = s;
     __syncthreads();
-    if (slice == 0 && c < n) {
+    if (slice == 0 && c < n && out) {
 #pragma unroll
-      for (int k = 1; k < 8; ++k) s += sum[k][col];
+      for (int k = 1; k < 32; ++k) s += sum[k][col];
       out[group * n + c] = s;
     }
     __syncthreads();
@@ -507,44 +594,49 @@ __global__ __launch_bounds__(256) void k_rotate_fold(const float* __restrict__ p
 
 // How a token's heads and a group's tokens are shared out.
 struct RotatePlan {
-  int shift, threads, reps, chunks[2];
+  int shift, worker, reps, chunks[2], layout;  // lanes of a head, threads of a worker, heads of a lane
   int64_t splits, part_ld;
 };
 
-constexpr int64_t kRotateWorkers = 8192;       // waves that are there at once, about
+constexpr int64_t kRotateBlocks = 8 * kCus;    // that are there at once, about (of 256 threads)
 
-RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_t width, int64_t groups, int64_t tokens,
-                       bool back) {
+RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_t width, int interleaved, int64_t groups,
+                       int64_t tokens) {
   RotatePlan p;
   const int E = t == EOGP_F32 ? 4 : 8;
   const int64_t slots = ceil_div(width / 2, E) + ceil_div(D - width, 2 * E);
   p.shift = 0;
   while ((1 << p.shift) < slots) ++p.shift;
-  const int at_once = 64 >> p.shift;           // heads of a wave
+  const bool whole = width / 2 % E == 0 && (D - width) % (2 * E) == 0;
+  p.layout = !whole ? kAny : interleaved ? kPairs : kHalves;
   const int heads[2] = {Hq, Hk};
-  p.threads = 256;
   if (norm == kNormRow) {
+    // a wave has the row while four heads a lane hold it: no barrier per token
     const int64_t lanes = (int64_t)std::max(Hq, Hk) << p.shift;
-    if (lanes > 512) p.threads = 1024;
+    p.worker = lanes <= 256 ? 64 : lanes <= 512 ? 256 : 1024;
     p.reps = 1;
-    while (p.reps * p.threads < lanes) p.reps *= 2;
+    while (p.reps * p.worker < lanes) p.reps *= 2;
     for (int i = 0; i < 2; ++i) p.chunks[i] = heads[i] > 0;
     p.part_ld = std::max(Hq, Hk) * D;
   } else {
-    // more heads a wave only where there are waves enough without
-    p.reps = groups * tokens * ceil_div(Hq + Hk, at_once) >= 4 * kRotateWorkers ? 2 : 1;
+    // two heads a lane where there are tokens enough for all waves
+    const int at_once = 64 >> p.shift;
+    p.worker = 64;
+    p.reps = groups * tokens * ceil_div(Hq + Hk, at_once) >= 16 * kRotateBlocks ? 2 : 1;
     for (int i = 0; i < 2; ++i) p.chunks[i] = (int)ceil_div(heads[i], at_once * p.reps);
     p.part_ld = D;
   }
-  const int64_t want = norm == kNormRow ? kRotateWorkers * 64 / p.threads : back ? kRotateWorkers / 2 : kRotateWorkers;
-  p.splits = std::min(std::max<int64_t>(1, tokens), std::max<int64_t>(1, want / std::max<int64_t>(1, groups * (p.chunks[0] + p.chunks[1]))));
+  const int64_t per_block = p.worker == 64 ? 4 : 1, want = p.worker == 1024 ? kRotateBlocks / 4 : kRotateBlocks;
+  p.splits = std::min(std::max<int64_t>(1, ceil_div(tokens, per_block)),
+                      std::max<int64_t>(1, want / std::max<int64_t>(1, groups * (p.chunks[0] + p.chunks[1]))));
   return p;
 }
 
 template <typename T>
 RotateArgs<T> rotate_args(const eogp_heads* in, const eogp_heads* grad, const eogp_heads* out, int64_t D, const void* qw,
                           const void* kw, eogp_dtype wt, float eps, const float* table, int64_t positions, int64_t width,
-                          int interleaved, const int64_t* at, const uint8_t* mask, int64_t T_, const RotatePlan& p) {
+                          int interleaved, const int64_t* at, const uint8_t* mask, int64_t T_, int64_t tokens,
+                          const RotatePlan& p) {
   RotateArgs<T> a{};
   for (int i = 0; i < 2; ++i) {
     if (in) a.in[i] = Heads<const T>{static_cast<const T*>(in[i].data), in[i].ld_example, in[i].ld_token, in[i].ld_head};
@@ -565,31 +657,44 @@ RotateArgs<T> rotate_args(const eogp_heads* in, const eogp_heads* grad, const eo
   a.positions = positions;
   a.at = at;
   a.mask = mask;
-  a.T_ = T_;
+  a.tokens = (int)tokens;
+  a.by_length = Divide(std::max<int64_t>(1, T_));
   a.shift = p.shift;
   a.splits = (int)p.splits;
   a.part_ld = p.part_ld;
-  a.groups = 1;
   return a;
 }
 
-// Threads of a block and heads that a lane holds. (fp32 rows of up to 8,192 elements in heads of 8 or more take up to
-// 4,096 lanes, 16-bit ones 2,048.)
+// f(threads of a worker, heads of a lane, layout). (fp32 rows of up to 8,192 elements in heads of 8 or more take up to
+// 4,096 lanes, 16-bit ones 2,048; layouts of whole pieces up to 1,024 and 2,048, and of 2,048 elements in all others.)
 template <typename T, int NORM, typename F>
 eogp_status with_shape(const RotatePlan& p, F&& f) {
   using std::integral_constant;
-  using N256 = integral_constant<int, 256>;
-  using N1024 = integral_constant<int, 1024>;
-  using One = integral_constant<int, 1>;
-  using Two = integral_constant<int, 2>;
-  if (p.threads == 256) return p.reps == 1 ? f(N256{}, One{}) : f(N256{}, Two{});
-  if constexpr (NORM == kNormRow) {
-    if (p.reps == 1) return f(N1024{}, One{});
-    if constexpr (sizeof(T) == 4)
-      if (p.reps > 2) return f(N1024{}, integral_constant<int, 4>{});
-    return f(N1024{}, Two{});
-  }
-  return EOGP_ERR_UNSUPPORTED;
+  auto go = [&](auto layout) {
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    using Four = integral_constant<int, 4>;
+    using W64 = integral_constant<int, 64>;
+    using W256 = integral_constant<int, 256>;
+    using W1024 = integral_constant<int, 1024>;
+    if (p.worker == 64) {
+      if (p.reps == 1) return f(W64{}, One{}, layout);
+      if constexpr (NORM == kNormRow)
+        if (p.reps == 4) return f(W64{}, Four{}, layout);
+      return f(W64{}, Two{}, layout);
+    }
+    if constexpr (NORM == kNormRow) {
+      if (p.worker == 256) return f(W256{}, Two{}, layout);
+      if (p.reps == 1) return f(W1024{}, One{}, layout);
+      if constexpr (sizeof(T) == 4)
+        if (p.reps > 2) return f(W1024{}, Four{}, layout);
+      return f(W1024{}, Two{}, layout);
+    }
+    return EOGP_ERR_UNSUPPORTED;
+  };
+  if (p.layout == kHalves) return go(integral_constant<int, kHalves>{});
+  if (p.layout == kPairs) return go(integral_constant<int, kPairs>{});
+  return go(integral_constant<int, kAny>{});
 }
 
 template <typename F>
@@ -600,17 +705,22 @@ eogp_status with_norm(int norm, F&& f) {
   return f(integral_constant<int, kNormNone>{});
 }
 
-unsigned rotate_blocks(int norm, int64_t workers) { return (unsigned)(norm == kNormRow ? workers : ceil_div(workers, 4)); }
-
 }  // namespace
+
+// Elements of a row that one norm takes.
+int64_t rotate_max_row(int64_t D) { return D < 8 ? 2048 : 8192; }
 
 eogp_status rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
                          double high, double magnitude, float* table, hipStream_t s) {
   if (positions == 0) return EOGP_OK;
   timing::Scope ts(EOGP_KT_ROTARY, s);
-  const int pairs = (int)(width / 2);
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(positions, 8), 2048), (unsigned)ceil_div(pairs, 32));
-  hipLaunchKernelGGL(k_rotary_table, grid, dim3(256), 0, s, positions, pairs, -2.0 / (double)width * std::log2(base),
+  const int64_t pairs = width / 2, columns = ceil_div(pairs, 32);
+  // as many positions a thread as leave the chip full of threads
+  int64_t K = 1;
+  while (K < 32 && ceil_div(positions, 16 * K) * columns >= 8 * kCus) K *= 2;
+  while (ceil_div(positions, 8 * K) > (1 << 23)) K *= 2;
+  const dim3 grid((unsigned)ceil_div(positions, 8 * K), (unsigned)columns);
+  hipLaunchKernelGGL(k_rotary_table, grid, dim3(256), 0, s, positions, (int)pairs, (int)K, -2.0 / (double)width * std::log2(base),
                      1.0 / factor, original / (2.0 * M_PI), low, 1.0 / (high - low), magnitude, table);
   EOGP_LAUNCH_CHECK("rotary_table");
   return EOGP_OK;
@@ -621,18 +731,18 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
                          int interleaved, bool back, const int64_t* at, const uint8_t* mask, int64_t N, int64_t T_,
                          int64_t D, hipStream_t s) {
   if (N * T_ == 0) return EOGP_OK;
-  const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, 1, N * T_, false);
+  const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, 1, N * T_);
   timing::Scope ts(EOGP_KT_ROTARY, s);
   return with_type(t, [&](auto el) {
     using T = decltype(el);
-    RotateArgs<T> a = rotate_args<T>(in, nullptr, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_, p);
-    a.tokens = N * T_;
+    RotateArgs<T> a = rotate_args<T>(in, nullptr, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_,
+                                     N * T_, p);
     a.sin_sign = back ? -1.f : 1.f;
     return with_norm(norm, [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
-      return with_shape<T, NORM>(p, [&](auto nt, auto reps) {
-        hipLaunchKernelGGL((k_rotate<T, NORM, decltype(nt)::value, decltype(reps)::value>),
-                           dim3(rotate_blocks(norm, p.splits * (p.chunks[0] + p.chunks[1]))), dim3(p.threads), 0, s, a);
+      return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {
+        hipLaunchKernelGGL((k_rotate<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>),
+                           dim3((unsigned)(p.splits * (p.chunks[0] + p.chunks[1]))), dim3(std::max(256, p.worker)), 0, s, a);
         EOGP_LAUNCH_CHECK("rotate_heads");
         return EOGP_OK;
       });
@@ -640,15 +750,12 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
   });
 }
 
-// Elements of a row that one norm takes.
-int64_t rotate_max_row(int64_t D) { return D < 8 ? 2048 : 8192; }
-
 size_t rotate_back_ws(eogp_dtype t, int norm, int64_t Hq, int64_t Hk, int64_t D, int64_t width, int64_t groups, int64_t tokens) {
-  // the workers of any call of up to `groups` groups of up to `tokens` tokens, with one head a lane
-  const RotatePlan p = rotate_plan(t, norm, (int)Hq, (int)Hk, D, width, 1, 1, true);
+  // the blocks of any call of up to `groups` groups of up to `tokens` tokens, with one head a lane
+  const RotatePlan p = rotate_plan(t, norm, (int)Hq, (int)Hk, D, width, 0, 1, 1);
   const int64_t chunks = p.chunks[0] + p.chunks[1];
-  const int64_t workers = std::min(groups * tokens * chunks, std::max(kRotateWorkers / 2, groups * chunks));
-  return align256((size_t)std::max<int64_t>(workers, groups * chunks) * p.part_ld * sizeof(float));
+  const int64_t blocks = std::min(groups * std::max<int64_t>(1, tokens) * chunks, std::max(kRotateBlocks, groups * chunks));
+  return align256((size_t)blocks * p.part_ld * sizeof(float));
 }
 
 eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, const eogp_heads* out, eogp_dtype t, int norm,
@@ -658,22 +765,20 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
                               hipStream_t s) {
   const int64_t groups = per_example ? N : 1, tokens = per_example ? T_ : N * T_;
   if (groups == 0) return EOGP_OK;
-  const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, groups, tokens, true);
-  const int chunks = p.chunks[0] + p.chunks[1];
-  const int64_t workers = groups * p.splits * chunks;
+  const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, groups, tokens);
   float* part = dqw || dkw ? static_cast<float*>(ws) : nullptr;
   timing::Scope ts(EOGP_KT_ROTARY, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
-    RotateArgs<T> a = rotate_args<T>(in, grad, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_, p);
-    a.tokens = tokens;
-    a.groups = groups;
+    RotateArgs<T> a = rotate_args<T>(in, grad, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_,
+                                     tokens, p);
     a.part = part;
     auto go = [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
-      return with_shape<T, NORM>(p, [&](auto nt, auto reps) {
-        hipLaunchKernelGGL((k_rotate_back<T, NORM, decltype(nt)::value, decltype(reps)::value>),
-                           dim3(rotate_blocks(norm, workers)), dim3(p.threads), 0, s, a);
+      return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {
+        hipLaunchKernelGGL((k_rotate_back<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>),
+                           dim3((unsigned)(groups * p.splits * (p.chunks[0] + p.chunks[1]))), dim3(std::max(256, p.worker)), 0,
+                           s, a);
         EOGP_LAUNCH_CHECK("rotate_heads_backward");
         return EOGP_OK;
       });
@@ -681,15 +786,12 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
     using std::integral_constant;
     return norm == kNormRow ? go(integral_constant<int, kNormRow>{}) : go(integral_constant<int, kNormHead>{});
   });
-  if (st != EOGP_OK) return st;
-  float* outs[2] = {dqw, dkw};
-  for (int i = 0; i < 2; ++i) {
-    if (!outs[i] || !p.chunks[i]) continue;
-    const int64_t n = norm == kNormRow ? out[i].heads * D : D;
-    hipLaunchKernelGGL(k_rotate_fold, dim3((unsigned)std::min<int64_t>(groups * ceil_div(n, 32), 1 << 20)), dim3(256), 0, s,
-                       part, p.part_ld, groups, (int)p.splits, chunks, i ? p.chunks[0] : 0, p.chunks[i], n, outs[i]);
-    EOGP_LAUNCH_CHECK("rotate_heads_backward (fold)");
-  }
+  if (st != EOGP_OK || !part) return st;
+  const int64_t nq = norm == kNormRow ? out[0].heads * D : D, nk = p.chunks[1] ? (norm == kNormRow ? out[1].heads * D : D) : 0;
+  hipLaunchKernelGGL(k_rotate_fold, dim3((unsigned)std::min<int64_t>(groups * (ceil_div(nq, 32) + ceil_div(nk, 32)), 1 << 20)),
+                     dim3(1024), 0, s, part, p.part_ld, groups, (int)p.splits, p.chunks[0], p.chunks[1], (int)nq, (int)nk, dqw,
+                     dkw);
+  EOGP_LAUNCH_CHECK("rotate_heads_backward (fold)");
   return EOGP_OK;
 }
 
