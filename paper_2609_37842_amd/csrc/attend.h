@@ -255,6 +255,15 @@ struct Stage {
       request_each(tid, D, [&](int r) { return s.base + (int64_t)(row0 + r < s.rows ? row0 + r : s.rows - 1) * s.ld; });
     }
   }
+  // `offset(r)` gives row r's first byte in a buffer that holds all (FAST).
+  template <typename F>
+  __device__ __forceinline__ void request_from(__amdgpu_buffer_rsrc_t all, int tid, F&& offset) {
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int id = u * NT + tid;
+      x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(all, offset(id / kPieces) + id % kPieces * 16, 0, 0));
+    }
+  }
   // `row_at(r)` gives row r's address (always one that can be read).
   template <typename F>
   __device__ __forceinline__ void request_each(int tid, int D, F&& row_at) {
@@ -393,6 +402,22 @@ __device__ __forceinline__ void hide(f32x16& s, const Span& span, uint32_t bits,
   for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e / 4) + e % 4)) & 1 ? s[e] : -INFINITY;
 }
 
+// Elements c .. c + 3 of a row of D (EXACT: D is a multiple of 4), by plain stores: the lines are filled by the two
+// halves of the wave, one after the other.
+template <typename T, bool EXACT>
+__device__ __forceinline__ void put4(T* row, int c, int D, const float (&v)[4]) {
+  if (EXACT || c + 4 <= D) {
+    AnyVec<T, 4> x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (T)v[e];
+    *reinterpret_cast<AnyVec<T, 4>*>(row + c) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < D) row[c + e] = (T)v[e];
+  }
+}
+
 // Tiles of KB keys that rows with bounds b have to look at: [0, head) and [from, from + count - head).
 struct Tiles {
   int head, from, count;
@@ -411,6 +436,14 @@ __device__ __forceinline__ Tiles tiles_of(const Bounds& b, int kb) {
   if (tail && sk > end) more = sk - end;                  // sinks beyond the window's end (not causal)
   t.count = t.head + tail + more;
   return t;
+}
+
+// Head widths that the kernels are built for.
+inline constexpr int padded(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+// Rows of exactly the built width on 16-byte boundaries, all heads of an example within 2^31 bytes.
+inline bool fast_rows(const eogp_heads& x, int64_t rows, int64_t D, int size) {
+  return D == padded(D) && (uintptr_t)x.data % 16 == 0 && x.ld_example * size % 16 == 0 && x.ld_token * size % 16 == 0 &&
+         x.ld_head * size % 16 == 0 && (rows + 64) * x.ld_token < ((int64_t)1 << 30) / size && x.heads * x.ld_head < ((int64_t)1 << 30) / size;
 }
 
 }  // namespace eogp

@@ -31,22 +31,6 @@ template <typename T> constexpr float kLift = 0.f;
 template <> constexpr float kLift<_Float16> = 7.f;
 constexpr float kLowest = -1e30f;   // reference of a row that has seen no key (finite: differences stay numbers)
 
-// Elements c .. c + 3 of a row of D (EXACT: D is a multiple of 4), by plain stores: the lines are filled by the two
-// halves of the wave, one after the other.
-template <typename T, bool EXACT>
-__device__ __forceinline__ void put4(T* row, int c, int D, const float (&v)[4]) {
-  if (EXACT || c + 4 <= D) {
-    AnyVec<T, 4> x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = (T)v[e];
-    *reinterpret_cast<AnyVec<T, 4>*>(row + c) = x;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < D) row[c + e] = (T)v[e];
-  }
-}
-
 // A row group's results: to the output, or unnormalised with their reference and sum to a worker's part.
 template <typename T, int DP, bool EXACT>
 __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* acc, float ref, float sum, int n, int r, int i,
@@ -548,8 +532,6 @@ __global__ __launch_bounds__(256) void k_attend_join(const AttendArgs<T> a) {
   }
 }
 
-// Head widths that the kernels are built for.
-constexpr int padded(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 // Groups of 32 rows of a wave: as many as the registers hold.
 constexpr int row_groups(int dp, int size) { return dp * size <= 128 ? 2 : 1; }
 // Waves of a block that takes different keys, by the LDS of their tiles.
@@ -590,12 +572,6 @@ eogp_status launch(K* kfn, const A& a, int64_t blocks, int threads, int lds, hip
   hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(threads), lds, s, a);
   EOGP_LAUNCH_CHECK("attention");
   return EOGP_OK;
-}
-
-// Rows of exactly the built width on 16-byte boundaries, all of a head within 2^31 bytes.
-bool fast_rows(const eogp_heads& x, int64_t rows, int64_t D, int size) {
-  return D == padded(D) && (uintptr_t)x.data % 16 == 0 && x.ld_example * size % 16 == 0 && x.ld_token * size % 16 == 0 &&
-         x.ld_head * size % 16 == 0 && x.ld_token * size < ((int64_t)1 << 31) / (rows + 64);
 }
 
 }  // namespace

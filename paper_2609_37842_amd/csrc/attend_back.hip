@@ -17,6 +17,7 @@ struct BackArgs {
   Sight sight;
   int N, Hq, Hkv, D;
   Divide by_group;                // query heads of a key head
+  Divide by_splits, by_units, by_heads;   // splits; key heads of all examples, of one
   float scale, scale_log2;
   const float* lse;               // [N, Tq, Hq]
   float *lse2, *delta;            // [N, Tq, Hq]: log-sum-exp in powers of two (+inf: the row counts for nothing), dout . out
@@ -40,6 +41,9 @@ __device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit) {
   const int e = 14 - (ilogbf(bound) + 1);
   return e < -100 ? -100 : e > 100 ? 100 : e;
 }
+
+// Waves of a SIMD, by the bytes of a row: so that registers are taken from one file without copies.
+constexpr int back_waves(int row_bytes, int most) { return row_bytes <= most ? 2 : 1; }
 
 __device__ __forceinline__ float sum_of(float v, int lanes) {
   for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor(v, m);
@@ -108,48 +112,49 @@ __global__ __launch_bounds__(256) void k_attend_delta(const BackArgs<T> a, int l
 // Gradients of keys and values: a wave has 32 keys, their rows of K and V and both gradients in registers; the
 // block's waves share tiles of 32 rows of queries and output gradients, over all query heads of the key head.
 // PARTS: 1 gradients of V, 2 of K, 3 both.
-template <typename T, int DP, int NW, int PARTS>
-__global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a) {
-  constexpr int NT = 64 * NW, kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+template <typename T, int DP, int PARTS, bool FAST>
+__global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 128 : 256)) void k_attend_back_kv(const BackArgs<T> a) {
+  constexpr int NW = 4, NT = 64 * NW, kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kKs = 32 / (2 * kPiece<T>);
   constexpr bool kV = PARTS & 1, kK = PARTS & 2;
   extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
-  __shared__ __align__(16) float row_f[2][2][RB];        // lse2, delta
-  __shared__ __align__(16) int row_i[2][3][RB];          // spans
+  __shared__ __align__(16) float row_f[2][2][RB];        // log-sum-exps and deltas of the rows of a tile
+  __shared__ __align__(16) uint32_t seen[NW][RB];        // a wave's keys that each row sees
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
-  const int units = a.N * a.Hkv, G = a.Hq / a.Hkv;
-  int b = blockIdx.x;
-  const int split = b % a.splits;
-  b /= a.splits;
-  const int unit = b % units, tile_key = b / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
+  const int units = a.N * a.Hkv, G = a.by_group.by;
+  const int b = a.by_splits.quotient(blockIdx.x), split = a.by_splits.rest(blockIdx.x, b);
+  const int tile_key = a.by_units.quotient(b), unit = a.by_units.rest(b, tile_key);
+  const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   const int k0 = tile_key * 32 * NW, j0 = k0 + wid * 32, j = j0 + l;
   const int k1 = min(k0 + 32 * NW, a.sight.Tk);
   const bool key_live = j < a.sight.Tk && (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
-  const uint32_t key_bits = (uint32_t)__ballot(key_live);
+  RowPieces<T, DP, FAST> kf, vf;
+  const int jc = min(j, a.sight.Tk - 1);
+  kf.request(a.k.row(n, jc, kvh), a.D);
+  if constexpr (kK) vf.request(a.v.row(n, jc, kvh), a.D);
 
   // queries that can see one of the block's keys
   constexpr int64_t kFar = (int64_t)1 << 40;
   const int64_t st = start < -kFar ? -kFar : start > kFar ? kFar : start;
   const bool sink = k0 < a.sight.sinks;
-  int64_t i_lo = a.sight.causal ? k0 - st : a.sight.window && !sink ? k0 - a.sight.window + 1 - st : 0;
-  int64_t i_hi = a.sight.window && !sink ? (int64_t)k1 - 1 + a.sight.window - st : a.sight.Tq;
+  const int64_t i_lo = a.sight.causal ? k0 - st : a.sight.window && !sink ? k0 - a.sight.window + 1 - st : 0;
+  const int64_t i_hi = a.sight.window && !sink ? (int64_t)k1 - 1 + a.sight.window - st : a.sight.Tq;
   int i0 = clamp_key(i_lo, a.sight.Tq), i1 = clamp_key(i_hi, a.sight.Tq);
-  const int any = __syncthreads_or(key_bits != 0);
-  if (!any) i1 = i0;
   if (a.sight.q_mask && i0 < i1) {
     const MaskRange r = mask_range(a.sight.q_mask + (int64_t)n * a.sight.Tq, a.sight.Tq, i0, i1);
     i0 = r.first;
     i1 = r.last;
   }
-  const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
-  int t = (int)((int64_t)row_tiles * split / a.splits);
-  const int t_end = (int)((int64_t)row_tiles * (split + 1) / a.splits);
-
-  RowPieces<T, DP> kf, vf;
-  const int jc = min(j, a.sight.Tk - 1);
-  kf.load(a.k.row(n, jc, kvh), key_live, a.D);
-  if constexpr (kK) vf.load(a.v.row(n, jc, kvh), key_live, a.D);
+  const int some_keys = __syncthreads_or(key_live);
+  const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = some_keys && i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
+  int t = 0, t_end = row_tiles;
+  if (a.splits > 1) {
+    t = (int)((int64_t)row_tiles * split / a.splits);
+    t_end = (int)((int64_t)row_tiles * (split + 1) / a.splits);
+  }
+  kf.settle(key_live, a.D);
+  if constexpr (kK) vf.settle(key_live, a.D);
   f32x16 dv[kV ? kDt : 1], dk[kK ? kDt : 1];
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt) {
@@ -159,49 +164,66 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>);
 
-  Stage<T, DP, RB, NT, false> qs, os;
+  // the first query head of the key head as rows: row r is query r / G of head r mod G
+  const T *qbase = a.q.row(n, 0, kvh * G), *obase = a.dout.row(n, 0, kvh * G);
+  const auto qall = buffer_of(qbase, 0x7FFFFFFFu), oall = buffer_of(obase, 0x7FFFFFFFu);
+  const int64_t id0 = (int64_t)n * a.sight.Tq * a.Hq + kvh * G;
+  Stage<T, DP, RB, NT, FAST> qs, os;
   float r_lse2 = 0.f, r_delta = 0.f;
-  Span r_span{0, 0, 0};
   bool r_live = false;
   auto request = [&](int tile) {
     const int r0 = rows_lo + tile * RB;
-    auto at = [&](const Heads<const T>& x) {
-      return [=](int r) {
-        const int row = min(r0 + r, rows_hi - 1);
-        const int i = a.by_group.quotient(row);
-        return x.row(n, i, kvh * G + a.by_group.rest(row, i));
+    if constexpr (FAST) {
+      auto at = [&](const Heads<const T>& x) {
+        return [&, x](int r) {
+          const int row = min(r0 + r, rows_hi - 1), i = a.by_group.quotient(row);
+          return (i * (int)x.ld_t + a.by_group.rest(row, i) * (int)x.ld_h) * (int)sizeof(T);
+        };
       };
-    };
-    qs.request_each(threadIdx.x, a.D, at(a.q));
-    os.request_each(threadIdx.x, a.D, at(a.dout));
+      qs.request_from(qall, threadIdx.x, at(a.q));
+      os.request_from(oall, threadIdx.x, at(a.dout));
+    } else {
+      auto at = [&](const T* base, const Heads<const T>& x) {
+        return [&, base](int r) {
+          const int row = min(r0 + r, rows_hi - 1), i = a.by_group.quotient(row);
+          return base + i * x.ld_t + a.by_group.rest(row, i) * x.ld_h;
+        };
+      };
+      qs.request_each(threadIdx.x, a.D, at(qbase, a.q));
+      os.request_each(threadIdx.x, a.D, at(obase, a.dout));
+    }
     const int row = r0 + l, rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
-    const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + kvh * G + a.by_group.rest(rc, i);
-    r_lse2 = row < rows_hi ? a.lse2[id] : INFINITY;
+    const int64_t id = id0 + (int64_t)i * a.Hq + a.by_group.rest(rc, i);
+    r_lse2 = a.lse2[id];
     r_delta = a.delta[id];
-    r_live = r_lse2 != INFINITY;
-    r_span = span_of(a.sight, start + i);
+    r_live = row < rows_hi;
   };
   if (t < t_end) request(t);
   for (int turn = 0; t < t_end; ++t, turn ^= 1) {
     char *qt = lds + turn * 2 * kTile, *ot = qt + kTile;
-    const uint64_t live = __ballot(r_live) & 0xFFFFFFFFull;
     const int r0 = rows_lo + t * RB;
+    r_lse2 = r_live ? r_lse2 : INFINITY;
+    const uint64_t live = __ballot(r_lse2 != INFINITY) & 0xFFFFFFFFull;
     qs.store(threadIdx.x, a.D, qt, live);
     os.store(threadIdx.x, a.D, ot, live);
     if (threadIdx.x < RB) {
       row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
       row_f[turn][1][l] = r_delta;
-      row_i[turn][0][l] = r_span.lo;
-      row_i[turn][1][l] = r_span.hi;
-      row_i[turn][2][l] = r_span.sk;
     }
     __syncthreads();
     if (t + 1 < t_end) request(t + 1);
-    if (live == 0 || key_bits == 0) continue;
+    if (live == 0) continue;
     const int last = min(r0 + RB, rows_hi) - 1;
-    const bool full = key_bits == 0xFFFFFFFFu && j0 >= span_of(a.sight, start + a.by_group.quotient(last)).lo &&
+    const bool full = j0 >= span_of(a.sight, start + a.by_group.quotient(last)).lo &&
                       j0 + 32 <= span_of(a.sight, start + a.by_group.quotient(r0)).hi;
-
+    uint32_t mine = 0xFFFFFFFFu;
+    if (!full) {
+      mine = sight_bits(span_of(a.sight, start + a.by_group.quotient(min(r0 + l, rows_hi - 1))), j0);
+      if (__ballot(mine != 0) == 0) continue;            // (none of the wave's keys)
+      wave_lds_order();
+      seen[wid][l] = mine;
+      wave_lds_order();
+    }
     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
@@ -217,15 +239,13 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
     if (!full) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const i32x4 lo = *reinterpret_cast<const i32x4*>(&row_i[turn][0][8 * g + 4 * h]);
-        const i32x4 hi = *reinterpret_cast<const i32x4*>(&row_i[turn][1][8 * g + 4 * h]);
-        const i32x4 sk = *reinterpret_cast<const i32x4*>(&row_i[turn][2][8 * g + 4 * h]);
+        const i32x4 w = *reinterpret_cast<const i32x4*>(&seen[wid][8 * g + 4 * h]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           // (dP as well: a key that the row does not see may hold anything)
-          const bool seen = key_live & sees(Span{lo[i], hi[i], sk[i]}, j);
-          s[4 * g + i] = seen ? s[4 * g + i] : 0.f;
-          dp[4 * g + i] = seen ? dp[4 * g + i] : 0.f;
+          const bool sees_it = ((uint32_t)w[i] >> l) & 1;
+          s[4 * g + i] = sees_it ? s[4 * g + i] : 0.f;
+          dp[4 * g + i] = sees_it ? dp[4 * g + i] : 0.f;
         }
       }
     }
@@ -261,6 +281,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
 
   if (j >= a.sight.Tk) return;
   const float by_v = exp2f(-kLiftBack<T>), by_k = a.scale * exp2f(-(float)lift);
+  const int D = FAST ? DP : a.D;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     if (!(which ? kK : kV)) continue;
@@ -276,12 +297,12 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_kv(const BackArgs<T> a)
           if constexpr (PARTS == 1) v[i] = dv[dt][4 * g + i] * by_v;
           else if constexpr (PARTS == 2) v[i] = dk[dt][4 * g + i] * by_k;
           else v[i] = which ? dk[dt][4 * g + i] * by_k : dv[dt][4 * g + i] * by_v;
-          if (!key_live) v[i] = 0.f;
+          v[i] = key_live ? v[i] : 0.f;
         }
         if (a.part)
-          store_piece<float, 4>(a.part + ((((int64_t)split * units + unit) * a.sight.Tk + j) * 2 + which) * a.D, c, a.D, v);
+          put4<float, FAST>(a.part + ((((int64_t)split * units + unit) * a.sight.Tk + j) * 2 + which) * D, c, D, v);
         else
-          store_piece<T, 4>(to.row(n, j, kvh), c, a.D, v);
+          put4<T, FAST>(to.row(n, j, kvh), c, D, v);
       }
   }
 }
@@ -301,19 +322,23 @@ __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
 
 // Gradients of queries: a wave has 32 rows of queries, output gradients and the result in registers; the block's
 // waves share tiles of keys and values.
-template <typename T, int DP, int NW>
-__global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) {
-  constexpr int NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+template <typename T, int DP, bool FAST>
+__global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
+  constexpr int NW = 4, NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [2][K, V]
   static_assert(NW == 4, "128 rows a block");
   __shared__ uint32_t all[NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
-  const int units = a.N * a.Hkv, G = a.Hq / a.Hkv, rows = G * a.sight.Tq;
-  const int unit = blockIdx.x % units, tile_row = a.row_tiles - 1 - blockIdx.x / units, n = unit / a.Hkv, kvh = unit % a.Hkv;
+  const int G = a.by_group.by, rows = G * a.sight.Tq;
+  const int from_end = a.by_units.quotient(blockIdx.x), unit = a.by_units.rest(blockIdx.x, from_end);
+  const int tile_row = a.row_tiles - 1 - from_end, n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   const int r = tile_row * kRows + wid * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
             hq = kvh * G + a.by_group.rest(rc, i);
+  RowPieces<T, DP, FAST> q, o;
+  q.request(a.q.row(n, i, hq), a.D);
+  o.request(a.dout.row(n, i, hq), a.D);
   const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + hq;
   const float lse2 = r < rows ? a.lse2[id] : INFINITY, delta = a.delta[id];
   const bool live = lse2 != INFINITY;
@@ -339,17 +364,16 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
   }
   const Tiles tiles = tiles_of(bd, KB);
 
-  RowPieces<T, DP> q, o;
-  q.load(a.q.row(n, i, hq), live, a.D);
-  o.load(a.dout.row(n, i, hq), live, a.D);
+  q.settle(live, a.D);
+  o.settle(live, a.D);
   f32x16 dq[kDt];
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt) dq[dt] = zeros16();
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
 
-  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, false), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, false);
-  Stage<T, DP, KB, NT, false> ks, vs;
+  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
+  Stage<T, DP, KB, NT, FAST> ks, vs;
   const KeyMask km(kmask, ksrc.base, a.sight.Tk);
   uint8_t byte = 0;
   auto request = [&](int tile) {
@@ -375,14 +399,10 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
       mma(dp, row_frag<T, kROWB>(vt, l, k), o.f[k]);
     }
     const bool full = bits == 0xFFFFFFFFull && j0 >= lo_max && j0 + KB <= hi_min;
+    if (!full) hide(s, span, (uint32_t)bits, j0);        // (weights 0)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref));
-      if (!full) {
-        const int at = 8 * (e / 4) + 4 * h + e % 4;
-        p = ((bool)((bits >> at) & 1) & sees(span, j0 + at)) ? p : 0.f;
-      }
-      float d = p * (dp[e] - delta);
+      float d = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref)) * (dp[e] - delta);
       if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
       s[e] = d;
     }
@@ -404,7 +424,7 @@ __global__ __launch_bounds__(64 * NW) void k_attend_back_q(const BackArgs<T> a) 
       float v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = live ? dq[dt][4 * g + e] * by : 0.f;
-      store_piece<T, 4>(to, dt * 32 + 8 * g + 4 * h, a.D, v);
+      put4<T, FAST>(to, dt * 32 + 8 * g + 4 * h, FAST ? DP : a.D, v);
     }
 }
 
@@ -463,10 +483,13 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     a.Hkv = (int)Hkv;
     a.D = (int)D;
     a.by_group = Divide(Hq / Hkv);
+    a.by_units = Divide(units);
+    a.by_heads = Divide(Hkv);
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.lse = lse;
     a.splits = back_splits(N, Tq, Tk, Hq, Hkv);
+    a.by_splits = Divide(a.splits);
     a.key_tiles = (int)ceil_div(Tk, 32 * kBackWaves);
     a.row_tiles = (int)ceil_div(Hq / Hkv * Tq, 32 * kBackWaves);
     Carve w(ws, ~(size_t)0);
@@ -492,8 +515,11 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
       hipLaunchKernelGGL(k_attend_delta<T>, delta_blocks(rows), dim3(256), 0, s, a, lanes, rows, 0);
       EOGP_LAUNCH_CHECK("attention_backward (delta)");
     }
-    auto go = [&](auto width) {
+    const int size = (int)sizeof(T);
+    const bool fast = fast_rows(q, Tq, D, size) && fast_rows(dout, Tq, D, size) && fast_rows(k, Tk, D, size) && fast_rows(v, Tk, D, size);
+    auto go = [&](auto width, auto exact) {
       constexpr int DP = decltype(width)::value;
+      constexpr bool FAST = decltype(exact)::value;
       constexpr int lds = 4 * 32 * DP * (int)sizeof(T);
       auto launch = [&](auto* kfn, int64_t blocks) {
         if (lds > (48 << 10)) {
@@ -507,11 +533,11 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
       if (keys > 0) {
         const int64_t blocks = units * a.key_tiles * a.splits;
         eogp_status st;
-        if constexpr (DP * sizeof(T) > 512) {            // both gradients of wide fp32 heads do not fit the registers
-          st = launch(k_attend_back_kv<T, DP, kBackWaves, 1>, blocks);
-          if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, kBackWaves, 2>, blocks);
+        if constexpr (DP * sizeof(T) > 128) {            // both gradients of wide heads do not fit the registers
+          st = launch(k_attend_back_kv<T, DP, 1, FAST>, blocks);
+          if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, 2, FAST>, blocks);
         } else {
-          st = launch(k_attend_back_kv<T, DP, kBackWaves, 3>, blocks);
+          st = launch(k_attend_back_kv<T, DP, 3, FAST>, blocks);
         }
         if (st != EOGP_OK) return st;
         if (a.part) {
@@ -520,12 +546,15 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
           EOGP_LAUNCH_CHECK("attention_backward (join)");
         }
       }
-      return rows > 0 ? launch(k_attend_back_q<T, DP, kBackWaves>, units * a.row_tiles) : EOGP_OK;
+      return rows > 0 ? launch(k_attend_back_q<T, DP, FAST>, units * a.row_tiles) : EOGP_OK;
     };
-    using std::integral_constant;
-    return D <= 64    ? go(integral_constant<int, 64>{})
-           : D <= 128 ? go(integral_constant<int, 128>{})
-                      : go(integral_constant<int, 256>{});
+    auto with = [&](auto exact) {
+      using std::integral_constant;
+      return D <= 64    ? go(integral_constant<int, 64>{}, exact)
+             : D <= 128 ? go(integral_constant<int, 128>{}, exact)
+                        : go(integral_constant<int, 256>{}, exact);
+    };
+    return fast ? with(std::true_type{}) : with(std::false_type{});
   });
 }
 
