@@ -255,14 +255,9 @@ struct Stage {
       request_each(tid, D, [&](int r) { return s.base + (int64_t)(row0 + r < s.rows ? row0 + r : s.rows - 1) * s.ld; });
     }
   }
-  // `offset(r)` gives row r's first byte in a buffer that holds all (FAST).
-  template <typename F>
-  __device__ __forceinline__ void request_from(__amdgpu_buffer_rsrc_t all, int tid, F&& offset) {
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int id = u * NT + tid;
-      x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(all, offset(id / kPieces) + id % kPieces * 16, 0, 0));
-    }
+  // The thread's piece u at a byte of a buffer (FAST).
+  __device__ __forceinline__ void request_one(int u, __amdgpu_buffer_rsrc_t all, int at) {
+    x[u] = __builtin_bit_cast(AnyVec<T, E>, __builtin_amdgcn_raw_buffer_load_b128(all, at, 0, 0));
   }
   // `row_at(r)` gives row r's address (always one that can be read).
   template <typename F>

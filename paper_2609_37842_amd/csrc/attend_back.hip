@@ -164,24 +164,54 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
   const int lift = lift_of(a, unit);
   const float ds_by = exp2f((float)lift - kLiftBack<T>);
 
+  // Rows of the block from which on, and up to which, each sees all of the wave's keys (the sinks' share aside), and
+  // those outside which none sees any.
+  auto row_of = [&](int64_t p) { return (int)min(max(p - st, (int64_t)0), (int64_t)a.sight.Tq) * G; };
+  const int64_t w = a.sight.window;
+  const int full_lo = a.sight.causal ? row_of((int64_t)j0 + 31) : w ? row_of((int64_t)j0 + 32 - w) : 0;
+  const int full_hi = w ? row_of((int64_t)j0 + w) : rows_hi;
+  const bool wave_sink = j0 < a.sight.sinks;
+  const int some_lo = a.sight.causal ? row_of(j0) : w && !wave_sink ? row_of((int64_t)j0 - w + 1) : 0;
+  const int some_hi = w && !wave_sink ? row_of((int64_t)j0 + 31 + w) : rows_hi;
+
   // the first query head of the key head as rows: row r is query r / G of head r mod G
   const T *qbase = a.q.row(n, 0, kvh * G), *obase = a.dout.row(n, 0, kvh * G);
-  const auto qall = buffer_of(qbase, 0x7FFFFFFFu), oall = buffer_of(obase, 0x7FFFFFFFu);
+  auto span_bytes = [&](const Heads<const T>& x) {
+    return (uint32_t)((a.sight.Tq - 1) * (int)x.ld_t + (G - 1) * (int)x.ld_h + DP) * (uint32_t)sizeof(T);
+  };
+  const auto qall = buffer_of(qbase, FAST ? span_bytes(a.q) : 0u), oall = buffer_of(obase, FAST ? span_bytes(a.dout) : 0u);
   const int64_t id0 = (int64_t)n * a.sight.Tq * a.Hq + kvh * G;
   Stage<T, DP, RB, NT, FAST> qs, os;
+  constexpr int kEach = Stage<T, DP, RB, NT, FAST>::kEach, kPieces = DP / kPiece<T>;
+  // What the thread asks for next: its rows' heads and first bytes (FAST), and the lane's row.
+  int walk_g[kEach], walk_q[kEach], walk_o[kEach];
+  const int step_i = a.by_group.quotient(RB), step_g = a.by_group.rest(RB, step_i);
+  const int q_t = (int)a.q.ld_t * (int)sizeof(T), q_h = (int)a.q.ld_h * (int)sizeof(T);
+  const int o_t = (int)a.dout.ld_t * (int)sizeof(T), o_h = (int)a.dout.ld_h * (int)sizeof(T);
+  if constexpr (FAST) {
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int at = u * NT + (int)threadIdx.x, row = rows_lo + t * RB + at / kPieces, i = a.by_group.quotient(row);
+      walk_g[u] = a.by_group.rest(row, i);
+      walk_q[u] = i * q_t + walk_g[u] * q_h + at % kPieces * 16;
+      walk_o[u] = i * o_t + walk_g[u] * o_h + at % kPieces * 16;
+    }
+  }
   float r_lse2 = 0.f, r_delta = 0.f;
   bool r_live = false;
   auto request = [&](int tile) {
     const int r0 = rows_lo + tile * RB;
     if constexpr (FAST) {
-      auto at = [&](const Heads<const T>& x) {
-        return [&, x](int r) {
-          const int row = min(r0 + r, rows_hi - 1), i = a.by_group.quotient(row);
-          return (i * (int)x.ld_t + a.by_group.rest(row, i) * (int)x.ld_h) * (int)sizeof(T);
-        };
-      };
-      qs.request_from(qall, threadIdx.x, at(a.q));
-      os.request_from(oall, threadIdx.x, at(a.dout));
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        qs.request_one(u, qall, walk_q[u]);
+        os.request_one(u, oall, walk_o[u]);
+        walk_g[u] += step_g;
+        const bool over = walk_g[u] >= G;
+        walk_g[u] -= over ? G : 0;
+        walk_q[u] += step_i * q_t + step_g * q_h + (over ? q_t - G * q_h : 0);
+        walk_o[u] += step_i * o_t + step_g * o_h + (over ? o_t - G * o_h : 0);
+      }
     } else {
       auto at = [&](const T* base, const Heads<const T>& x) {
         return [&, base](int r) {
@@ -195,7 +225,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
     const int row = r0 + l, rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
     const int64_t id = id0 + (int64_t)i * a.Hq + a.by_group.rest(rc, i);
     r_lse2 = a.lse2[id];
-    r_delta = a.delta[id];
+    if constexpr (kK) r_delta = a.delta[id];
     r_live = row < rows_hi;
   };
   if (t < t_end) request(t);
@@ -208,22 +238,18 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
     os.store(threadIdx.x, a.D, ot, live);
     if (threadIdx.x < RB) {
       row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
-      row_f[turn][1][l] = r_delta;
+      if constexpr (kK) row_f[turn][1][l] = r_delta;
     }
     __syncthreads();
     if (t + 1 < t_end) request(t + 1);
-    if (live == 0) continue;
-    const int last = min(r0 + RB, rows_hi) - 1;
-    const bool full = j0 >= span_of(a.sight, start + a.by_group.quotient(last)).lo &&
-                      j0 + 32 <= span_of(a.sight, start + a.by_group.quotient(r0)).hi;
-    uint32_t mine = 0xFFFFFFFFu;
-    if (!full) {
-      mine = sight_bits(span_of(a.sight, start + a.by_group.quotient(min(r0 + l, rows_hi - 1))), j0);
-      if (__ballot(mine != 0) == 0) continue;            // (none of the wave's keys)
+    const bool full = r0 >= full_lo && r0 + RB <= full_hi;
+    const bool some = live != 0 && r0 + RB > some_lo && r0 < some_hi;
+    if (some && !full) {
       wave_lds_order();
-      seen[wid][l] = mine;
+      seen[wid][l] = sight_bits(span_of(a.sight, start + a.by_group.quotient(min(r0 + l, rows_hi - 1))), j0);
       wave_lds_order();
     }
+    if (some) {
     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
@@ -276,6 +302,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
       for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
         for (int k = 0; k < kKs; ++k) mma(dk[dt], col_frag<T, kROWB>(qt, 0, k, dt), p[k]);
+    }
     }
   }
 
