@@ -189,6 +189,22 @@ __device__ __forceinline__ float half_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// A piece that request_piece took at c of a row of d elements: zero past the row's end, by selects alone (once: what is
+// there already would be moved again).
+template <typename T>
+__device__ __forceinline__ uint4 settled(uint4 x, int c, int d) {
+  constexpr int E = kPiece<T>;
+  const uint32_t down = (uint32_t)(c + E > d ? c + E - d : 0) * (uint32_t)sizeof(T);
+  x = down & 8 ? uint4{x.z, x.w, 0, 0} : x;
+  x = down & 4 ? uint4{x.y, x.z, x.w, 0} : x;
+  if constexpr (sizeof(T) == 2) {
+    const uint4 y{__builtin_amdgcn_alignbit(x.y, x.x, 16), __builtin_amdgcn_alignbit(x.z, x.y, 16),
+                  __builtin_amdgcn_alignbit(x.w, x.z, 16), x.w >> 16};
+    x = down & 2 ? y : x;
+  }
+  return down >= 16 ? uint4{0, 0, 0, 0} : x;
+}
+
 // A row of D elements as the pieces of a row operand, zero past the end and where the row does not count.
 template <typename T, int DP, bool EXACT = false>
 struct RowPieces {              // EXACT: D is DP
@@ -203,9 +219,8 @@ struct RowPieces {              // EXACT: D is DP
   __device__ __forceinline__ void settle(bool live, int D) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      auto x = __builtin_bit_cast(AnyVec<T, kPiece<T>>, __builtin_bit_cast(uint4, f[s]));
-      if constexpr (!EXACT) settle_piece<T, kPiece<T>, false>(x, at(s), D);
-      const uint4 w = __builtin_bit_cast(uint4, x);
+      uint4 w = __builtin_bit_cast(uint4, f[s]);
+      if constexpr (!EXACT) w = settled<T>(w, at(s), D);
       f[s] = __builtin_bit_cast(Frag<T>, live ? w : uint4{0, 0, 0, 0});
     }
   }
@@ -273,7 +288,8 @@ struct Stage {
     constexpr uint64_t kAll = ROWS == 64 ? ~0ull : (1ull << (ROWS & 63)) - 1;
     if constexpr (!FAST) {
 #pragma unroll
-      for (int u = 0; u < kEach; ++u) settle_piece<T, E, false>(x[u], (u * NT + tid) % kPieces * E, D);
+      for (int u = 0; u < kEach; ++u)
+        x[u] = __builtin_bit_cast(AnyVec<T, E>, settled<T>(__builtin_bit_cast(uint4, x[u]), (u * NT + tid) % kPieces * E, D));
     }
     if (live != kAll) {
 #pragma unroll

@@ -33,10 +33,11 @@ template <> constexpr float kLiftBack<_Float16> = 15.f;
 // fp16 score gradients P (dP - delta) are small where many keys share a row, and lie below fp16's normal range where
 // the output gradients are small as well. They are held times 2^e, e from |dP - delta| <= 2 max |dout row| max |v row|
 // of the key head's rows, so that none passes 2^14.
+// (The gradients of queries take each row's own norm.)
 template <typename T>
-__device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit) {
-  if constexpr (sizeof(T) == 4 || kLiftBack<T> == 0.f) return 0;
-  const float bound = 2.f * sqrtf(__uint_as_float(a.norms[2 * unit])) * sqrtf(__uint_as_float(a.norms[2 * unit + 1]));
+__device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit, float dout_square) {
+  if constexpr (kLiftBack<T> == 0.f) return 0;
+  const float bound = 2.f * sqrtf(dout_square) * sqrtf(__uint_as_float(a.norms[2 * unit + 1]));
   if (!(bound > 0.f) || isinf(bound)) return 0;
   const int e = 14 - (ilogbf(bound) + 1);
   return e < -100 ? -100 : e > 100 ? 100 : e;
@@ -54,58 +55,26 @@ __global__ __launch_bounds__(256) void k_attend_zero(uint32_t* p, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
-// delta = dout . out of each row, its log-sum-exp in powers of two, and (fp16) the largest norms of rows of dout,
-// then of v. A row takes `lanes` lanes, 16 bytes each.
+// fp16: the largest norms of rows of v. A row takes `lanes` lanes, 16 bytes each.
 template <typename T>
-__global__ __launch_bounds__(256) void k_attend_delta(const BackArgs<T> a, int lanes, int64_t rows, int of_v) {
+__global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int lanes, int64_t rows) {
   constexpr int E = kPiece<T>;
   const int lane = threadIdx.x & 63, per = 64 / lanes, c = (lane % lanes) * E;
-  const int H = of_v ? a.Hkv : a.Hq, Tn = of_v ? a.sight.Tk : a.sight.Tq;
   for (int64_t id0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * per; id0 < rows; id0 += (int64_t)gridDim.x * 4 * per) {
-    const int64_t id = id0 + lane / lanes;
-    const bool in = id < rows;
-    const int64_t rc = in ? id : rows - 1;
-    const int hq = (int)(rc % H);
-    const int64_t i = rc / H % Tn, n = rc / H / Tn;
-    const uint8_t* mask = of_v ? a.sight.k_mask : a.sight.q_mask;
-    bool live = in && (!mask || mask[n * Tn + i]);
-    float dot = 0.f, square = 0.f;
-    if (of_v) {
-      if (live) {
-        float x[E];
-        load_piece<T, E>(a.v.row(n, i, hq), c, a.D, 0.f, x);
+    const int64_t id = id0 + lane / lanes, rc = id < rows ? id : rows - 1;
+    const int h = (int)(rc % a.Hkv);
+    const int64_t j = rc / a.Hkv % a.sight.Tk, n = rc / a.Hkv / a.sight.Tk;
+    const bool live = id < rows && (!a.sight.k_mask || a.sight.k_mask[n * a.sight.Tk + j]);
+    float square = 0.f;
+    if (live) {
+      float x[E];
+      load_piece<T, E>(a.v.row(n, j, h), c, a.D, 0.f, x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) square += x[e] * x[e];
-      }
-    } else {
-      const float s = in ? a.lse[id] : 0.f;
-      live = live && s != -INFINITY;
-      if (live) {
-        float x[E], y[E];
-        load_piece<T, E>(a.dout.row(n, i, hq), c, a.D, 0.f, x);
-        const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h;
-        if (a.out_f32)
-          load_piece<float, E>(static_cast<const float*>(a.out) + at, c, a.D, 0.f, y);
-        else
-          load_piece<T, E>(static_cast<const T*>(a.out) + at, c, a.D, 0.f, y);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          dot += x[e] * y[e];
-          square += x[e] * x[e];
-        }
-      }
-      dot = sum_of(dot, lanes);
-      if (in && lane % lanes == 0) {
-        a.delta[id] = live ? dot : 0.f;
-        a.lse2[id] = live ? s * 1.4426950408889634f : INFINITY;
-      }
+      for (int e = 0; e < E; ++e) square += x[e] * x[e];
     }
-    if constexpr (kLiftBack<T> != 0.f) {
-      square = sum_of(square, lanes);
-      const int unit = (int)(n * a.Hkv) + hq / (H / a.Hkv);
-      // (the largest of a set does not depend on the order; a key that no query sees only makes the bound larger)
-      if (live && lane % lanes == 0) atomicMax(a.norms + 2 * unit + of_v, __float_as_uint(square == square ? square : 0.f));
-    }
+    square = sum_of(square, lanes);
+    // (the largest of a set does not depend on the order; a key that no query sees only makes the bound larger)
+    if (live && lane % lanes == 0) atomicMax(a.norms + 2 * (n * a.Hkv + h) + 1, __float_as_uint(square == square ? square : 0.f));
   }
 }
 
@@ -123,10 +92,12 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.by_group.by;
   const int b = a.by_splits.quotient(blockIdx.x), split = a.by_splits.rest(blockIdx.x, b);
+  // tiles of the first keys, which most queries see, first
   const int tile_key = a.by_units.quotient(b), unit = a.by_units.rest(b, tile_key);
   const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
-  const int k0 = tile_key * 32 * NW, j0 = k0 + wid * 32, j = j0 + l;
+  // (the last keys of a causal tile have fewer queries: blocks of a CU, 256 apart, have them in opposite waves)
+  const int k0 = tile_key * 32 * NW, j0 = k0 + ((blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid) * 32, j = j0 + l;
   const int k1 = min(k0 + 32 * NW, a.sight.Tk);
   const bool key_live = j < a.sight.Tk && (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
   RowPieces<T, DP, FAST> kf, vf;
@@ -161,7 +132,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
     if constexpr (kV) dv[dt] = zeros16();
     if constexpr (kK) dk[dt] = zeros16();
   }
-  const int lift = lift_of(a, unit);
+  const int lift = kLiftBack<T> == 0.f ? 0 : lift_of(a, unit, __uint_as_float(a.norms[2 * unit]));
   const float ds_by = exp2f((float)lift - kLiftBack<T>);
 
   // Rows of the block from which on, and up to which, each sees all of the wave's keys (the sinks' share aside), and
@@ -348,36 +319,76 @@ __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
 }
 
 // Gradients of queries: a wave has 32 rows of queries, output gradients and the result in registers; the block's
-// waves share tiles of keys and values.
+// waves share tiles of keys and values. Before that each row's delta = dout . out is formed, and its log-sum-exp in powers
+// of two, which the other kernels read (+inf: the row counts for nothing).
 template <typename T, int DP, bool FAST>
 __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
   constexpr int NW = 4, NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
   extern __shared__ __align__(16) char lds[];            // [2][K, V]
-  static_assert(NW == 4, "128 rows a block");
   __shared__ uint32_t all[NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int G = a.by_group.by, rows = G * a.sight.Tq;
   const int from_end = a.by_units.quotient(blockIdx.x), unit = a.by_units.rest(blockIdx.x, from_end);
   const int tile_row = a.row_tiles - 1 - from_end, n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
-  const int r = tile_row * kRows + wid * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
+  // (The first rows of a causal tile have fewer keys: blocks of a CU, 256 apart, have them in opposite waves.)
+  const int group = (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid;
+  const int r = tile_row * kRows + group * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
             hq = kvh * G + a.by_group.rest(rc, i);
   RowPieces<T, DP, FAST> q, o;
   q.request(a.q.row(n, i, hq), a.D);
   o.request(a.dout.row(n, i, hq), a.D);
   const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + hq;
-  const float lse2 = r < rows ? a.lse2[id] : INFINITY, delta = a.delta[id];
-  const bool live = lse2 != INFINITY;
-  const Span span = live ? span_of(a.sight, start + i) : Span{0, 0, 0};
-  // keys that any row of the block sees, and those that every row of the wave does
+  const float lse = r < rows && (!a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i]) ? a.lse[id] : -INFINITY;
+  const bool live = lse != -INFINITY;
+  const float lse2 = live ? lse * 1.4426950408889634f : INFINITY;
   const uint32_t mine = (uint32_t)__ballot(live);
-  if (lane == 0) all[wid] = mine;
+  if (lane == 0) all[group] = mine;
+  q.settle(live, a.D);
+  o.settle(live, a.D);
+  float delta = 0.f, square = 0.f;
+  {
+    const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h;
+    const int D = FAST ? DP : a.D;
+    if (a.out_f32) {
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        float y[kPiece<T>];
+        load_piece<float, kPiece<T>>(static_cast<const float*>(a.out) + at, RowPieces<T, DP, FAST>::at(st), D, 0.f, y);
+#pragma unroll
+        for (int e = 0; e < kPiece<T>; ++e) delta += (float)o.f[st][e] * y[e];
+      }
+    } else {
+      RowPieces<T, DP, FAST> y;
+      y.load(static_cast<const T*>(a.out) + at, live, a.D);
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+        for (int e = 0; e < kPiece<T>; ++e) delta += (float)o.f[st][e] * (float)y.f[st][e];
+    }
+    delta = half_sum(delta);                             // (0 where the row does not count: dout is)
+    if (r < rows && h == 0) {
+      a.lse2[id] = lse2;
+      a.delta[id] = delta;
+    }
+    if constexpr (kLiftBack<T> != 0.f) {
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+        for (int e = 0; e < kPiece<T>; ++e) square += (float)o.f[st][e] * (float)o.f[st][e];
+      square = half_sum(square);
+      // (the largest of a set does not depend on the order)
+      if (live && h == 0) atomicMax(a.norms + 2 * unit, __float_as_uint(square == square ? square : 0.f));
+    }
+  }
+  // keys that any row of the block sees, those that any of the wave does, and those that every row of it does
   __syncthreads();
   LiveRows block{all[0] | (uint64_t)all[1] << 32, all[2] | (uint64_t)all[3] << 32};
   auto position = [&](int at) { return start + a.by_group.quotient(tile_row * kRows + at); };
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
   Bounds bd{0, 0, 0, 0};
+  Span some{0, 0, 0};
   int lo_max = 0, hi_min = a.sight.Tk;
   if (!block.none()) {
     const int64_t p0 = position(block.first()), p1 = position(block.last());
@@ -386,17 +397,19 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
     bd = bounds_of(a.sight, p0, p1, range, kmask);
   }
   if (mine) {
-    lo_max = span_of(a.sight, position(wid * 32 + 31 - __builtin_clz(mine))).lo;
-    hi_min = span_of(a.sight, position(wid * 32 + __builtin_ctz(mine))).hi;
+    const Span f = span_of(a.sight, position(group * 32 + __builtin_ctz(mine)));
+    const Span e = span_of(a.sight, position(group * 32 + 31 - __builtin_clz(mine)));
+    some = Span{f.lo, e.hi, e.sk};
+    lo_max = e.lo;
+    hi_min = f.hi;
   }
+  const Span span = live ? span_of(a.sight, start + i) : Span{0, 0, 0};
   const Tiles tiles = tiles_of(bd, KB);
 
-  q.settle(live, a.D);
-  o.settle(live, a.D);
   f32x16 dq[kDt];
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt) dq[dt] = zeros16();
-  const int lift = lift_of(a, unit);
+  const int lift = kLiftBack<T> == 0.f ? 0 : lift_of(a, unit, square);
   const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
 
   const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
@@ -418,28 +431,29 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
     vs.store(threadIdx.x, a.D, vt, bits);
     __syncthreads();
     if (t + 1 < tiles.count) request(tiles.at(t + 1));
-    if (bits == 0) continue;
-    f32x16 s = zeros16(), dp = zeros16();
+    if (bits != 0 && ((j0 < some.hi && j0 + KB > some.lo) || j0 < some.sk)) {
+      f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      mma(s, row_frag<T, kROWB>(kt, l, k), q.f[k]);
-      mma(dp, row_frag<T, kROWB>(vt, l, k), o.f[k]);
+      for (int k = 0; k < kSteps; ++k) {
+        mma(s, row_frag<T, kROWB>(kt, l, k), q.f[k]);
+        mma(dp, row_frag<T, kROWB>(vt, l, k), o.f[k]);
+      }
+      const bool full = bits == 0xFFFFFFFFull && j0 >= lo_max && j0 + KB <= hi_min;
+      if (!full) hide(s, span, (uint32_t)bits, j0);      // (weights 0)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float d = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref)) * (dp[e] - delta);
+        if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
+        s[e] = d;
+      }
+      Frag<T> ds[kKs];
+#pragma unroll
+      for (int k = 0; k < kKs; ++k) ds[k] = acc_frag<T>(s, k);
+#pragma unroll
+      for (int dt = 0; dt < kDt; ++dt)
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) mma(dq[dt], col_frag<T, kROWB>(kt, 0, k, dt), ds[k]);
     }
-    const bool full = bits == 0xFFFFFFFFull && j0 >= lo_max && j0 + KB <= hi_min;
-    if (!full) hide(s, span, (uint32_t)bits, j0);        // (weights 0)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float d = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref)) * (dp[e] - delta);
-      if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
-      s[e] = d;
-    }
-    Frag<T> ds[kKs];
-#pragma unroll
-    for (int k = 0; k < kKs; ++k) ds[k] = acc_frag<T>(s, k);
-#pragma unroll
-    for (int dt = 0; dt < kDt; ++dt)
-#pragma unroll
-      for (int k = 0; k < kKs; ++k) mma(dq[dt], col_frag<T, kROWB>(kt, 0, k, dt), ds[k]);
   }
   if (r >= rows) return;
   const float by = a.scale * exp2f(-(float)lift);
@@ -456,9 +470,9 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
 }
 
 constexpr int kBackWaves = 4;
-constexpr int64_t kSplitBlocks = 4 * kCus;
+constexpr int64_t kSplitBlocks = 4 * kCus;     // twice as many as are there at once: the first have more to do
 
-// Workers that share a key tile's rows: as many as fill the chip a few times over, none with fewer than 8 tiles.
+// Workers that share a key tile's rows, none with fewer than 8 tiles.
 int back_splits(int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv) {
   const int64_t blocks = N * Hkv * ceil_div(Tk, 32 * kBackWaves), tiles = ceil_div(Hq / Hkv * Tq, 32);
   return (int)std::min<int64_t>(std::max<int64_t>(1, tiles / 8), std::max<int64_t>(1, kSplitBlocks / std::max<int64_t>(1, blocks)));
@@ -525,22 +539,18 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     if (t == EOGP_F16) a.norms = w.take<uint32_t>(2 * units);
     a.part = a.splits > 1 ? w.take<float>((size_t)a.splits * (units * Tk * 2 * D)) : nullptr;
 
-    int lanes = 1;
-    while (lanes * kPiece<T> < D) lanes *= 2;
     const int64_t rows = N * Tq * Hq, keys = N * Tk * Hkv;
-    auto delta_blocks = [&](int64_t n) { return dim3((unsigned)std::min<int64_t>(ceil_div(n * lanes, 256), 16 * kCus)); };
     if (t == EOGP_F16) {
+      int lanes = 1;
+      while (lanes * kPiece<T> < D) lanes *= 2;
       hipLaunchKernelGGL(k_attend_zero, dim3((unsigned)std::min<int64_t>(ceil_div(2 * units, 256), 4 * kCus)), dim3(256), 0, s,
                          a.norms, 2 * units);
       EOGP_LAUNCH_CHECK("attention_backward (zero)");
       if (keys > 0) {
-        hipLaunchKernelGGL(k_attend_delta<T>, delta_blocks(keys), dim3(256), 0, s, a, lanes, keys, 1);
+        hipLaunchKernelGGL(k_attend_norms<T>, dim3((unsigned)std::min<int64_t>(ceil_div(keys * lanes, 256), 16 * kCus)), dim3(256),
+                           0, s, a, lanes, keys);
         EOGP_LAUNCH_CHECK("attention_backward (norms)");
       }
-    }
-    if (rows > 0) {
-      hipLaunchKernelGGL(k_attend_delta<T>, delta_blocks(rows), dim3(256), 0, s, a, lanes, rows, 0);
-      EOGP_LAUNCH_CHECK("attention_backward (delta)");
     }
     const int size = (int)sizeof(T);
     const bool fast = fast_rows(q, Tq, D, size) && fast_rows(dout, Tq, D, size) && fast_rows(k, Tk, D, size) && fast_rows(v, Tk, D, size);
@@ -557,9 +567,10 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
         EOGP_LAUNCH_CHECK("attention_backward");
         return EOGP_OK;
       };
-      if (keys > 0) {
+      eogp_status st = EOGP_OK;
+      if (rows > 0) st = launch(k_attend_back_q<T, DP, FAST>, units * a.row_tiles);
+      if (st == EOGP_OK && keys > 0) {
         const int64_t blocks = units * a.key_tiles * a.splits;
-        eogp_status st;
         if constexpr (DP * sizeof(T) > 128) {            // both gradients of wide heads do not fit the registers
           st = launch(k_attend_back_kv<T, DP, 1, FAST>, blocks);
           if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, 2, FAST>, blocks);
@@ -573,7 +584,7 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
           EOGP_LAUNCH_CHECK("attention_backward (join)");
         }
       }
-      return rows > 0 ? launch(k_attend_back_q<T, DP, FAST>, units * a.row_tiles) : EOGP_OK;
+      return st;
     };
     auto with = [&](auto exact) {
       using std::integral_constant;
