@@ -43,6 +43,11 @@ __device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit, float dou
   return e < -100 ? -100 : e > 100 ? 100 : e;
 }
 
+// Waves that share tiles. fp32 products are bound by the matrix units alone: there each wave has tiles of its own and waits
+// for no other, so that short and ragged sequences leave no wave idle at another's pace; 16-bit ones would be bound by the
+// tiles' way to LDS.
+constexpr int back_share(int size, int dp) { return size == 4 && dp <= 128 ? 2 : 4; }
+
 // Waves of a SIMD, by the bytes of a row: so that registers are taken from one file without copies.
 constexpr int back_waves(int row_bytes, int most) { return row_bytes <= most ? 2 : 1; }
 
@@ -82,11 +87,13 @@ __global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int l
 // block's waves share tiles of 32 rows of queries and output gradients, over all query heads of the key head.
 // PARTS: 1 gradients of V, 2 of K, 3 both.
 template <typename T, int DP, int PARTS, bool FAST>
-__global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 128 : 256)) void k_attend_back_kv(const BackArgs<T> a) {
-  constexpr int NW = 4, NT = 64 * NW, kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+__global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), PARTS == 3 ? 128 : 256)) void k_attend_back_kv(
+    const BackArgs<T> a) {
+  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, kFlip = NW > 1;   // (a wave of its own tiles is in order with itself)
+  constexpr int kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kKs = 32 / (2 * kPiece<T>);
   constexpr bool kV = PARTS & 1, kK = PARTS & 2;
-  extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
+  extern __shared__ __align__(16) char lds[];            // [1 + kFlip][Q, dO]
   __shared__ __align__(16) float row_f[2][2][RB];        // log-sum-exps and deltas of the rows of a tile
   __shared__ __align__(16) uint32_t seen[NW][RB];        // a wave's keys that each row sees
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
@@ -97,7 +104,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
   const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   // (the last keys of a causal tile have fewer queries: blocks of a CU, 256 apart, have them in opposite waves)
-  const int k0 = tile_key * 32 * NW, j0 = k0 + ((blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid) * 32, j = j0 + l;
+  const int k0 = tile_key * 32 * NW, j0 = k0 + (NW > 1 && (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid) * 32, j = j0 + l;
   const int k1 = min(k0 + 32 * NW, a.sight.Tk);
   const bool key_live = j < a.sight.Tk && (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
   RowPieces<T, DP, FAST> kf, vf;
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
     i0 = r.first;
     i1 = r.last;
   }
-  const int some_keys = __syncthreads_or(key_live);
+  const int some_keys = (NW > 1 ? __syncthreads_or(key_live) : __ballot(key_live) != 0);
   const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = some_keys && i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
   int t = 0, t_end = row_tiles;
   if (a.splits > 1) {
@@ -200,18 +207,22 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), PARTS == 3 ? 1
     r_live = row < rows_hi;
   };
   if (t < t_end) request(t);
-  for (int turn = 0; t < t_end; ++t, turn ^= 1) {
+  for (int turn = 0; t < t_end; ++t, turn ^= kFlip) {
     char *qt = lds + turn * 2 * kTile, *ot = qt + kTile;
     const int r0 = rows_lo + t * RB;
     r_lse2 = r_live ? r_lse2 : INFINITY;
     const uint64_t live = __ballot(r_lse2 != INFINITY) & 0xFFFFFFFFull;
+    if constexpr (NW == 1) wave_lds_order();
     qs.store(threadIdx.x, a.D, qt, live);
     os.store(threadIdx.x, a.D, ot, live);
     if (threadIdx.x < RB) {
       row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
       if constexpr (kK) row_f[turn][1][l] = r_delta;
     }
-    __syncthreads();
+    if constexpr (NW > 1)
+      __syncthreads();
+    else
+      wave_lds_order();
     if (t + 1 < t_end) request(t + 1);
     const bool full = r0 >= full_lo && r0 + RB <= full_hi;
     const bool some = live != 0 && r0 + RB > some_lo && r0 < some_hi;
@@ -322,10 +333,11 @@ __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
 // waves share tiles of keys and values. Before that each row's delta = dout . out is formed, and its log-sum-exp in powers
 // of two, which the other kernels read (+inf: the row counts for nothing).
 template <typename T, int DP, bool FAST>
-__global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
-  constexpr int NW = 4, NT = 64 * NW, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
+__global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
+  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, KB = 32, kFlip = NW > 1;
+  constexpr int kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
-  extern __shared__ __align__(16) char lds[];            // [2][K, V]
+  extern __shared__ __align__(16) char lds[];            // [1 + kFlip][K, V]
   __shared__ uint32_t all[NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int G = a.by_group.by, rows = G * a.sight.Tq;
@@ -333,7 +345,7 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
   const int tile_row = a.row_tiles - 1 - from_end, n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   // (The first rows of a causal tile have fewer keys: blocks of a CU, 256 apart, have them in opposite waves.)
-  const int group = (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid;
+  const int group = NW > 1 && (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid;
   const int r = tile_row * kRows + group * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
             hq = kvh * G + a.by_group.rest(rc, i);
   RowPieces<T, DP, FAST> q, o;
@@ -384,7 +396,9 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
   }
   // keys that any row of the block sees, those that any of the wave does, and those that every row of it does
   __syncthreads();
-  LiveRows block{all[0] | (uint64_t)all[1] << 32, all[2] | (uint64_t)all[3] << 32};
+  LiveRows block{mine, 0};
+  if constexpr (NW > 1) block.low = all[0] | (uint64_t)all[1] << 32;
+  if constexpr (NW > 2) block.high = all[NW - 2] | (uint64_t)all[NW - 1] << 32;
   auto position = [&](int at) { return start + a.by_group.quotient(tile_row * kRows + at); };
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
   Bounds bd{0, 0, 0, 0};
@@ -423,13 +437,17 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
     byte = km.request(j0 + l);
   };
   if (tiles.count > 0) request(tiles.at(0));
-  for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= 1) {
+  for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= kFlip) {
     char *kt = lds + turn * 2 * kTile, *vt = kt + kTile;
     const int j0 = tiles.at(t) * KB;
     const uint64_t bits = km.bits(bd, j0, byte);
+    if constexpr (NW == 1) wave_lds_order();
     ks.store(threadIdx.x, a.D, kt, bits);
     vs.store(threadIdx.x, a.D, vt, bits);
-    __syncthreads();
+    if constexpr (NW > 1)
+      __syncthreads();
+    else
+      wave_lds_order();
     if (t + 1 < tiles.count) request(tiles.at(t + 1));
     if (bits != 0 && ((j0 < some.hi && j0 + KB > some.lo) || j0 < some.sk)) {
       f32x16 s = zeros16(), dp = zeros16();
@@ -469,25 +487,24 @@ __global__ __launch_bounds__(256, back_waves(DP * (int)sizeof(T), 256)) void k_a
     }
 }
 
-constexpr int kBackWaves = 4;
 constexpr int64_t kSplitBlocks = 4 * kCus;     // twice as many as are there at once: the first have more to do
 
 // Workers that share a key tile's rows, none with fewer than 8 tiles.
-int back_splits(int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv) {
-  const int64_t blocks = N * Hkv * ceil_div(Tk, 32 * kBackWaves), tiles = ceil_div(Hq / Hkv * Tq, 32);
-  return (int)std::min<int64_t>(std::max<int64_t>(1, tiles / 8), std::max<int64_t>(1, kSplitBlocks / std::max<int64_t>(1, blocks)));
+int back_splits(int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int share) {
+  const int64_t blocks = N * Hkv * ceil_div(Tk, 32 * share), tiles = ceil_div(Hq / Hkv * Tq, 32);
+  return (int)std::min<int64_t>(std::max<int64_t>(1, tiles / 8), std::max<int64_t>(1, kSplitBlocks * 4 / share / std::max<int64_t>(1, blocks)));
 }
 
 }  // namespace
 
 // Bytes for any call of up to N examples, Tq queries and Tk keys: launches with several workers a key tile have at most
-// kSplitBlocks blocks, and a worker has no fewer than 8 tiles of 32 rows.
+// kSplitBlocks blocks of 128 keys (or four times as many of 32), and a worker has no fewer than 8 tiles of 32 rows.
 size_t attention_back_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
   size_t bytes = 2 * align256((size_t)(N * Tq * Hq) * sizeof(float)) + 256;
   if (t == EOGP_F16) bytes += align256((size_t)(2 * N * Hkv) * sizeof(float));
   const int64_t most = ceil_div(Hq / Hkv * Tq, 32) / 8;
   if (most > 1)
-    bytes += align256((size_t)std::min(most * (N * Hkv * Tk), kSplitBlocks * 32 * kBackWaves) * (2 * D) * sizeof(float));
+    bytes += align256((size_t)std::min(most * (N * Hkv * Tk), kSplitBlocks * 128) * (2 * D) * sizeof(float));
   return bytes;
 }
 
@@ -529,10 +546,11 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.lse = lse;
-    a.splits = back_splits(N, Tq, Tk, Hq, Hkv);
+    const int share = back_share((int)sizeof(T), padded(D));
+    a.splits = back_splits(N, Tq, Tk, Hq, Hkv, share);
     a.by_splits = Divide(a.splits);
-    a.key_tiles = (int)ceil_div(Tk, 32 * kBackWaves);
-    a.row_tiles = (int)ceil_div(Hq / Hkv * Tq, 32 * kBackWaves);
+    a.key_tiles = (int)ceil_div(Tk, 32 * share);
+    a.row_tiles = (int)ceil_div(Hq / Hkv * Tq, 32 * share);
     Carve w(ws, ~(size_t)0);
     a.lse2 = w.take<float>(N * Tq * Hq);
     a.delta = w.take<float>(N * Tq * Hq);
@@ -557,13 +575,13 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     auto go = [&](auto width, auto exact) {
       constexpr int DP = decltype(width)::value;
       constexpr bool FAST = decltype(exact)::value;
-      constexpr int lds = 4 * 32 * DP * (int)sizeof(T);
+      constexpr int lds = (back_share((int)sizeof(T), DP) > 1 ? 4 : 2) * 32 * DP * (int)sizeof(T);
       auto launch = [&](auto* kfn, int64_t blocks) {
         if (lds > (48 << 10)) {
           const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);
           if (st != EOGP_OK) return st;
         }
-        hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(64 * kBackWaves), lds, s, a);
+        hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(64 * back_share((int)sizeof(T), DP)), lds, s, a);
         EOGP_LAUNCH_CHECK("attention_backward");
         return EOGP_OK;
       };
