@@ -544,7 +544,9 @@ struct Plan {
 
 constexpr int kFewRows = 32;
 constexpr int kMaxSplits = 256;
-constexpr int64_t kWantBlocks = 4 * kCus;      // of a launch that splits keys
+// Blocks that a launch which splits keys goes up to: of rows, what is there at once (2 x 2,048 tokens of 16 x 128 bf16, not
+// causal, 512 blocks: 97 us, in two splits with the join 217); of few rows, four times as many as CUs.
+constexpr int64_t kWantBlocks = 2 * kCus, kWantFew = 4 * kCus;
 
 Plan plan_of(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D, int64_t window,
              int64_t sinks) {
@@ -557,9 +559,10 @@ Plan plan_of(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_
   p.waves_of_keys = p.few ? waves_of_keys(padded(D), size) : 1;
   p.row_tiles = (int)(p.few ? 1 : ceil_div(rows, p.wide ? 256 : 128));
   const int64_t keys = window > 0 ? std::min(Tk, window + sinks + Tq) : Tk;
-  const int64_t most = std::max<int64_t>(1, keys / (2 * 32 * p.waves_of_keys));
+  const int64_t want = p.few ? kWantFew : kWantBlocks, least = p.few ? 64 * p.waves_of_keys : 256;   // keys of a split
+  const int64_t most = std::max<int64_t>(1, keys / least);
   const int64_t blocks = std::max<int64_t>(1, units * p.row_tiles);
-  p.splits = (int)std::min(std::min<int64_t>(most, kMaxSplits), std::max<int64_t>(1, kWantBlocks / blocks));
+  p.splits = (int)std::min(std::min<int64_t>(most, kMaxSplits), std::max<int64_t>(1, want / blocks));
   return p;
 }
 
@@ -577,11 +580,11 @@ eogp_status launch(K* kfn, const A& a, int64_t blocks, int threads, int lds, hip
 }  // namespace
 
 // Bytes for the parts of any call of up to N examples, Tq queries and Tk keys: a launch that splits keys has at most
-// kWantBlocks blocks, of at most 32 rows where a key head has no more and 128 else, and at most kMaxSplits splits.
+// kWantFew blocks of at most 32 rows or kWantBlocks of 128, and at most kMaxSplits splits.
 size_t attention_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
-  if (N == 0 || Tq == 0 || Tk < 128) return 0;
+  if (N == 0 || Tq == 0 || Tk < 256) return 0;
   const int64_t rows = Hq / Hkv * Tq, all = N * Hkv * rows;
-  const int64_t most = kWantBlocks * (rows <= kFewRows ? rows : 128);
+  const int64_t most = std::max(kWantFew * std::min<int64_t>(rows, kFewRows), rows <= kFewRows ? 0 : kWantBlocks * 128);
   return align256((size_t)std::min(all * kMaxSplits, most) * (D + 2) * sizeof(float));
 }
 
