@@ -930,9 +930,9 @@ NORMS = {"none": 0, "head": 1, "row": 2}
 
 def _heads_of(x, name):
     """[N, T, heads, D] with unit stride in its last dimension, as the library takes it."""
-    if x.dim() != 4:
-        raise ValueError(f"{name} must be [N, T, heads, D]")
     s = x.stride()
+    if len(s) != 4:
+        raise ValueError(f"{name} must be [N, T, heads, D]")
     if s[3] != 1 and x.shape[3] > 1:
         if x.numel():
             raise ValueError(f"{name} must have unit stride within a head")
@@ -940,18 +940,19 @@ def _heads_of(x, name):
     return Heads(x.data_ptr(), x.shape[2], s[0], s[1], s[2])
 
 
-def _heads_like(x, like, name):
-    if x.shape != like.shape or x.dtype != like.dtype:
+def _heads_like(x, like, shape, name):
+    """The same of a tensor with the shape and type of `like`."""
+    if x is not like and (x.shape != shape or x.dtype != like.dtype):
         raise ValueError(f"{name} must have the shape and type of its counterpart")
     return _heads_of(x, name)
 
 
-def _norm_weights(norm, weight, x, name):
+def _norm_weights(norm, weight, x, shape, name):
     if weight is None:
         return
     if norm == 0:
         raise ValueError(f"{name} without a norm")
-    _weight(weight, x.shape[3] if norm == 1 else x.shape[2] * x.shape[3], x, name)
+    _weight(weight, shape[3] if norm == 1 else shape[2] * shape[3], x, name)
 
 
 def _table_shape(table):
@@ -988,30 +989,33 @@ def eogp_rotate_heads(q, k=None, table=None, positions=None, norm="none", q_weig
     L = load()
     _need_here(stream, q, k, table, positions, q_weight, k_weight, token_mask, q_out, k_out)
     code = _model_dtype(q, "q")
-    qh = _heads_of(q, "q")
-    N, T, _, D = q.shape
-    if k is not None and (k.shape[:2] != q.shape[:2] or k.shape[3:] != q.shape[3:] or k.dtype != q.dtype):
-        raise ValueError("k must be [N, T, key heads, D] of q's type")
+    qh, kh, ok = _heads_of(q, "q"), None, None
+    shape = q.shape
+    N, T, _, D = shape
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {', '.join(NORMS)}")
     nc = NORMS[norm]
-    _norm_weights(nc, q_weight, q, "q_weight")
-    _norm_weights(nc, k_weight, q if k is None else k, "k_weight")
-    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
-        raise ValueError("q_weight and k_weight must have one type")
+    _norm_weights(nc, q_weight, q, shape, "q_weight")
     P, width = _table_shape(table)
-    _per_row(positions, (N, T), torch.int64, "positions")
-    _per_row(token_mask, (N, T), torch.uint8, "token_mask")
+    lead = (N, T)
+    _per_row(positions, lead, torch.int64, "positions")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
     if q_out is None:
-        q_out = _empty(tuple(q.shape), q.dtype, q.device, stream)
-    oq, kh, ok = _heads_like(q_out, q, "q_out"), None, None
+        q_out = _empty(tuple(shape), q.dtype, q.device, stream)
+    oq = _heads_like(q_out, q, shape, "q_out")
     if k is not None:
+        ks = k.shape
+        if len(ks) != 4 or ks[0] != N or ks[1] != T or ks[3] != D or k.dtype != q.dtype:
+            raise ValueError("k must be [N, T, key heads, D] of q's type")
         kh = _heads_of(k, "k")
+        _norm_weights(nc, k_weight, k, ks, "k_weight")
+        if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+            raise ValueError("q_weight and k_weight must have one type")
         if k_out is None:
-            k_out = _empty(tuple(k.shape), k.dtype, k.device, stream)
-        ok = _heads_like(k_out, k, "k_out")
-    elif k_out is not None:
-        raise ValueError("k_out without k")
+            k_out = _empty(tuple(ks), k.dtype, k.device, stream)
+        ok = _heads_like(k_out, k, ks, "k_out")
+    elif k_out is not None or k_weight is not None:
+        raise ValueError(f"{'k_weight' if k_out is None else 'k_out'} without k")
     w = q_weight if q_weight is not None else k_weight
     _check(L.eogp_rotate_heads(ctypes.byref(qh), kh and ctypes.byref(kh), code, N, T, D, nc, _at(q_weight), _at(k_weight),
                                F32 if w is None else _DTYPE_CODE[w.dtype], float(eps), _at(table), P, width,
@@ -1035,44 +1039,50 @@ def eogp_rotate_heads_backward(dq, dk=None, q=None, k=None, table=None, position
     L = load()
     _need_here(stream, dq, dk, q, k, table, positions, q_weight, k_weight, token_mask, dq_in, dk_in, dq_weight, dk_weight, ws)
     code = _model_dtype(dq, "dq")
-    N, T, Hq, D = dq.shape if dq.dim() == 4 else (0, 0, 0, 0)
-    gq = _heads_of(dq, "dq")
-    if dk is not None and (dk.shape[:2] != dq.shape[:2] or dk.shape[3:] != dq.shape[3:] or dk.dtype != dq.dtype):
-        raise ValueError("dk must be [N, T, key heads, D] of dq's type")
+    gq, gk, xq, xk, ok = _heads_of(dq, "dq"), None, None, None, None
+    shape = dq.shape
+    N, T, Hq, D = shape
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {', '.join(NORMS)}")
     nc = NORMS[norm]
-    if nc and (q is None or (dk is not None and k is None)):
-        raise ValueError("a norm's backward pass reads the forward pass's inputs")
-    gk = None if dk is None else _heads_of(dk, "dk")
-    xq = _heads_like(q, dq, "q") if nc else None
-    xk = _heads_like(k, dk, "k") if nc and dk is not None else None
-    _norm_weights(nc, q_weight, dq, "q_weight")
-    _norm_weights(nc, k_weight, dq if dk is None else dk, "k_weight")
-    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
-        raise ValueError("q_weight and k_weight must have one type")
+    if nc:
+        if q is None or (dk is not None and k is None):
+            raise ValueError("a norm's backward pass reads the forward pass's inputs")
+        xq = _heads_like(q, dq, shape, "q")
+    _norm_weights(nc, q_weight, dq, shape, "q_weight")
     P, width = _table_shape(table)
-    _per_row(positions, (N, T), torch.int64, "positions")
-    _per_row(token_mask, (N, T), torch.uint8, "token_mask")
+    lead = (N, T)
+    _per_row(positions, lead, torch.int64, "positions")
+    _per_row(token_mask, lead, torch.uint8, "token_mask")
     if dq_in is None:
-        dq_in = _empty(tuple(dq.shape), dq.dtype, dq.device, stream)
-    oq, ok = _heads_like(dq_in, dq, "dq_in"), None
+        dq_in = _empty(tuple(shape), dq.dtype, dq.device, stream)
+    oq = _heads_like(dq_in, dq, shape, "dq_in")
     if dk is not None:
+        ks = dk.shape
+        if len(ks) != 4 or ks[0] != N or ks[1] != T or ks[3] != D or dk.dtype != dq.dtype:
+            raise ValueError("dk must be [N, T, key heads, D] of dq's type")
+        gk = _heads_of(dk, "dk")
+        if nc:
+            xk = _heads_like(k, dk, ks, "k")
+        _norm_weights(nc, k_weight, dk, ks, "k_weight")
+        if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+            raise ValueError("q_weight and k_weight must have one type")
         if dk_in is None:
-            dk_in = _empty(tuple(dk.shape), dk.dtype, dk.device, stream)
-        ok = _heads_like(dk_in, dk, "dk_in")
-    elif dk_in is not None:
-        raise ValueError("dk_in without dk")
+            dk_in = _empty(tuple(ks), dk.dtype, dk.device, stream)
+        ok = _heads_like(dk_in, dk, ks, "dk_in")
+    elif dk_in is not None or dk_weight is not None or k_weight is not None:
+        raise ValueError("dk_in, dk_weight and k_weight need dk")
     if nc:
         lead = (N,) if per_example else ()
-        shape = lambda x: (*lead, D if nc == 1 else x.shape[2] * D)   # noqa: E731
+        size = (*lead, D if nc == 1 else Hq * D)
         if dq_weight is None:
-            dq_weight = _empty(shape(dq), torch.float32, dq.device, stream)
-        _per_row(dq_weight, shape(dq), torch.float32, "dq_weight")
+            dq_weight = _empty(size, torch.float32, dq.device, stream)
+        _per_row(dq_weight, size, torch.float32, "dq_weight")
         if dk is not None:
+            size = (*lead, D if nc == 1 else ks[2] * D)
             if dk_weight is None:
-                dk_weight = _empty(shape(dk), torch.float32, dk.device, stream)
-            _per_row(dk_weight, shape(dk), torch.float32, "dk_weight")
+                dk_weight = _empty(size, torch.float32, dk.device, stream)
+            _per_row(dk_weight, size, torch.float32, "dk_weight")
     elif dq_weight is not None or dk_weight is not None:
         raise ValueError("weight gradients without a norm")
     need = int(L.eogp_rotate_heads_backward_workspace_size(N, T, Hq, 0 if dk is None else dk.shape[2], D, code, nc, width,
@@ -1090,11 +1100,12 @@ def eogp_rotate_heads_backward(dq, dk=None, q=None, k=None, table=None, position
 
 def _attention_shapes(q, k, v, q_start, q_mask, k_mask):
     """Sizes (N, Tq, Tk, Hq, Hkv, D) of queries [N, Tq, Hq, D], keys and values [N, Tk, Hkv, D]."""
-    if q.dim() != 4 or k.dim() != 4:
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or len(ks) != 4:
         raise ValueError("q must be [N, Tq, heads, D], k and v [N, Tk, key heads, D]")
-    N, Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[1], k.shape[2]
-    if k.shape[0] != N or k.shape[3] != D or v.shape != k.shape or k.dtype != q.dtype or v.dtype != q.dtype:
+    N, Tq, Hq, D = qs
+    _, Tk, Hkv, _ = ks
+    if ks[0] != N or ks[3] != D or v.shape != ks or k.dtype != q.dtype or v.dtype != q.dtype:
         raise ValueError("k and v must be [N, Tk, key heads, D] of q's type")
     _per_row(q_start, (N,), torch.int64, "q_start")
     _per_row(q_mask, (N, Tq), torch.uint8, "q_mask")
@@ -1157,13 +1168,13 @@ def eogp_attention_backward(dout, q, k, v, out, lse, scale=None, causal=True, wi
     need = int(L.eogp_attention_backward_workspace_size(N, Tq, Tk, Hq, Hkv, D, code))
     ws, wsb = _scratch(need, q.device, ws, stream)
     ref = ctypes.byref
-    _check(L.eogp_attention_backward(ref(_heads_like(dout, q, "dout")), ref(_heads_of(q, "q")), ref(_heads_of(k, "k")),
+    _check(L.eogp_attention_backward(ref(_heads_like(dout, q, q.shape, "dout")), ref(_heads_of(q, "q")), ref(_heads_of(k, "k")),
                                      ref(_heads_of(v, "v")), code, N, Tq, Tk, D,
                                      D ** -0.5 if scale is None and D else float(scale or 0), 1 if causal else 0,
                                      int(window), int(sinks), _at(q_start), _at(q_mask), _at(k_mask),
                                      ref(_heads_of(out, "out")), _DTYPE_CODE[out.dtype], _at(lse),
-                                     ref(_heads_like(dq, q, "dq")), ref(_heads_like(dk, k, "dk")),
-                                     ref(_heads_like(dv, v, "dv")), _at(ws), wsb, _stream_handle(stream, q.device)))
+                                     ref(_heads_like(dq, q, q.shape, "dq")), ref(_heads_like(dk, k, k.shape, "dk")),
+                                     ref(_heads_like(dv, v, k.shape, "dv")), _at(ws), wsb, _stream_handle(stream, q.device)))
     return dq, dk, dv
 
 
