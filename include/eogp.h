@@ -577,7 +577,7 @@ typedef struct {
  * divided, and those between are interpolated:
  *   g_i = clamp((original base^(-2 i / width) / 2 pi - low) / (high - low), 0, 1).
  *   table   [positions, width / 2, 2] fp32. Angles are fp64.
- * Errors: EOGP_ERR_INVALID for an odd or non-positive width, positions outside [0, 2^31),
+ * Errors: EOGP_ERR_INVALID for an odd width or one outside [2, 65536], positions outside [0, 2^31),
  * base <= 0, factor <= 0, original < 0, high <= low, values that are not finite, or NULL. */
 eogp_status eogp_rotary_table(int64_t positions, int64_t width, double base, double factor,
                               double original, double low, double high, double magnitude, float* table,
@@ -648,7 +648,8 @@ eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* d
  *             or keys.
  * 16-bit weights enter the product with v rounded to `dtype` (their sum is that of the unrounded ones, fp32); fp32 runs
  * in fp32 throughout. Errors: EOGP_ERR_INVALID for bad sizes (need key heads that divide the query heads; N * Tq * heads
- * and N * Tk * key heads below 2^31), scale <= 0, window or sinks < 0, sinks without a window, NULL pointers;
+ * and N * Tk * key heads below 2^29, N * heads up to 2^22), scale <= 0, window or sinks outside [0, 2^30), sinks without a
+ * window, NULL pointers;
  * EOGP_ERR_UNSUPPORTED for D < 8 or D > 256 or another output type; EOGP_ERR_WORKSPACE if ws is too small. */
 size_t eogp_attention_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads, int64_t D,
                                      eogp_dtype dtype);
@@ -664,6 +665,7 @@ eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_
  *   d_out, dq, dk, dv  of `dtype`, shaped as out, q, k, v; the gradients overlap nothing else.
  *   out, lse           of the forward pass (out of `dtype` or fp32), from the same arguments.
  *   ws                 eogp_attention_backward_workspace_size bytes, no fewer for more examples, queries, heads or keys.
+ * An output gradient that is not finite may reach every key and query of its example.
  * Sums run in a fixed order. 16-bit weights and score gradients are rounded to `dtype` once, before the products that
  * take them. Errors as for eogp_attention. */
 size_t eogp_attention_backward_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,

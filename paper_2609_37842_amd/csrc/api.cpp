@@ -870,8 +870,8 @@ eogp_status check_rotate(const char* op, eogp_dtype dtype, int64_t N, int64_t T,
 eogp_status eogp_rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
                               double high, double magnitude, float* table, void* stream) {
   const char* op = "rotary_table";
-  if (positions < 0 || positions >= kMaxFlat || width < 2 || width % 2 || width >= kMaxFlat / 64)
-    return fail(EOGP_ERR_INVALID, "rotary_table: need 0 <= positions < 2^31 and an even width >= 2");
+  if (positions < 0 || positions >= kMaxFlat || width < 2 || width % 2 || width > 65536)
+    return fail(EOGP_ERR_INVALID, "rotary_table: need 0 <= positions < 2^31 and an even width of 2 to 65536");
   for (double v : {base, factor, original, low, high, magnitude})
     if (!std::isfinite(v)) return fail(EOGP_ERR_INVALID, "rotary_table: values must be finite");
   if (!(base > 0.0) || !(factor > 0.0) || original < 0.0 || !(high > low))
@@ -965,9 +965,12 @@ eogp_status check_attention(const char* op, int64_t Hq, int64_t Hkv, eogp_dtype 
   EOGP_CHECK(check_batch(op, N, Tq, Hq));
   EOGP_CHECK(check_batch(op, N, Tk, Hkv));
   EOGP_CHECK(check_batch(op, N, 1, Hq));
+  // rows of tiles and key heads as blocks of one launch
+  if (N * std::max(Tq * Hq, Tk * Hkv) >= ((int64_t)1 << 29) || N * Hq > ((int64_t)1 << 22))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": examples x tokens x heads must be < 2^29, examples x heads <= 2^22");
   if (!(scale > 0.f) || std::isinf(scale)) return fail(EOGP_ERR_INVALID, std::string(op) + ": scale must be > 0");
-  if (window < 0 || sinks < 0 || (sinks > 0 && window == 0))
-    return fail(EOGP_ERR_INVALID, std::string(op) + ": need window >= 0, and sinks >= 0 with a window only");
+  if (window < 0 || sinks < 0 || window >= ((int64_t)1 << 30) || sinks >= ((int64_t)1 << 30) || (sinks > 0 && window == 0))
+    return fail(EOGP_ERR_INVALID, std::string(op) + ": need window and sinks in [0, 2^30), and sinks with a window only");
   return EOGP_OK;
 }
 }  // namespace

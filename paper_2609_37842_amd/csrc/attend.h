@@ -326,7 +326,8 @@ __device__ __forceinline__ MaskRange mask_range(const uint8_t* __restrict__ mask
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[u][i] = 0;
-        for (int i = 0; i < rows; ++i)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
           if (from + i < rows) w[u][i / 4] |= (uint32_t)mask[from + i] << (i % 4 * 8);
       }
     }

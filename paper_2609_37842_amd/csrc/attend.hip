@@ -74,27 +74,6 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
     }
 }
 
-// The order of a step's instructions: operands are read kAhead products ahead, and each product is followed by its
-// share of the vector instructions.
-template <typename T, int SCORES, int VALUES, int QG>
-__device__ __forceinline__ void interleave() {
-  if constexpr (sizeof(T) == 2) {
-    constexpr int kMfma = 8, kValu = 2, kRead = 0x100, kTrans = 0x400;
-    constexpr int kAhead = 4;
-    constexpr int kValuEach = 48 * QG / (SCORES + VALUES) + 1, kTransEach = (16 * QG + SCORES + VALUES - 1) / (SCORES + VALUES);
-    __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
-#pragma unroll
-    for (int i = 0; i < SCORES + VALUES; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kMfma, QG, 0);
-      const int ahead = i + kAhead;
-      if (ahead < SCORES) __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-      else if (ahead < SCORES + VALUES) __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(kValu, kValuEach, 0);
-      __builtin_amdgcn_sched_group_barrier(kTrans, kTransEach, 0);
-    }
-  }
-}
-
 // Four waves side by side over rows (QG groups of 32 each) share tiles of 32 keys. A step works on three tiles at
 // once, which depend on nothing of each other: the products of the next tile's scores, the weights of this one and the
 // product of the last one's weights with V, so that the vector units make exponentials while the matrix units multiply.
@@ -271,14 +250,6 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
           for (int qg = 0; qg < QG; ++qg) mma(acc[qg][dt], vf, p[1 - PAR][qg][k]);
         }
-      // (made here, and not where the next step uses them)
-#pragma unroll
-      for (int qg = 0; qg < QG; ++qg) {
-#pragma unroll
-        for (int k = 0; k < kKs; ++k) asm volatile("" : "+v"(p[PAR][qg][k]));
-        asm volatile("" : "+v"(by_sum[qg]));
-      }
-      interleave<T, kSteps, kDt * kKs, QG>();
       if (__ballot(moved)) {
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {

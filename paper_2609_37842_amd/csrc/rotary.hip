@@ -599,6 +599,7 @@ struct RotatePlan {
 };
 
 constexpr int64_t kRotateBlocks = 8 * kCus;    // that are there at once, about (of 256 threads)
+constexpr int64_t kMostLaunched = 1 << 21;     // blocks of a launch (of up to 1,024 threads)
 
 RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_t width, int interleaved, int64_t groups,
                        int64_t tokens) {
@@ -732,6 +733,7 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
                          int64_t D, hipStream_t s) {
   if (N * T_ == 0) return EOGP_OK;
   const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, 1, N * T_);
+  if (p.splits * (p.chunks[0] + p.chunks[1]) > kMostLaunched) return fail(EOGP_ERR_INVALID, "rotate_heads: too many heads for one call");
   timing::Scope ts(EOGP_KT_ROTARY, s);
   return with_type(t, [&](auto el) {
     using T = decltype(el);
@@ -767,6 +769,8 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
   if (groups == 0) return EOGP_OK;
   const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, groups, tokens);
   float* part = dqw || dkw ? static_cast<float*>(ws) : nullptr;
+  if (groups * p.splits * (p.chunks[0] + p.chunks[1]) > kMostLaunched)
+    return fail(EOGP_ERR_INVALID, "rotate_heads_backward: too many examples and heads for one call");
   timing::Scope ts(EOGP_KT_ROTARY, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);

@@ -92,7 +92,7 @@ TABLE = dict(P=8, width=16, base=1e4, factor=1.0, original=0.0, low=1.0, high=4.
 
 def test_table_refusals():
     inf, nan = float("inf"), float("nan")
-    for bad in (dict(P=-1), dict(P=1 << 31), dict(width=0), dict(width=15), dict(width=1 << 26), dict(base=0.0), dict(base=-1.0),
+    for bad in (dict(P=-1), dict(P=1 << 31), dict(width=0), dict(width=15), dict(width=65538), dict(base=0.0), dict(base=-1.0),
                 dict(base=nan), dict(factor=0.0), dict(factor=inf), dict(original=-1.0), dict(high=1.0), dict(low=nan),
                 dict(magnitude=inf), dict(table=None), dict(table=FAKE + 2)):
         assert call("eogp_rotary_table", TABLE, **bad) == -1, bad
@@ -148,7 +148,8 @@ def test_attention_refusals(name, args):
     inf, nan = float("inf"), float("nan")
     for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(dt=5), dict(ot=5), dict(N=-1), dict(Tq=-1), dict(Tk=-1),
                 dict(D=0), dict(N=1 << 20, Tq=1 << 10), dict(Tk=1 << 31), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan),
-                dict(scale=inf), dict(window=-1), dict(sinks=-1), dict(sinks=1), dict(k=heads(heads=3)), dict(v=heads(heads=4)),
+                dict(scale=inf), dict(window=-1), dict(sinks=-1), dict(sinks=1), dict(window=1 << 30), dict(window=4, sinks=1 << 30),
+                dict(N=1 << 21), dict(N=1 << 17, Tq=1 << 10), dict(N=1 << 10, Tk=1 << 18), dict(k=heads(heads=3)), dict(v=heads(heads=4)),
                 dict(k=heads(heads=0), v=heads(heads=0)), dict(q=heads(0)), dict(k=heads(0, 2)), dict(v=heads(0, 2)),
                 dict(v=heads(FAKE + 1, 2)), dict(out=heads(FAKE + 1)), dict(start=FAKE + 4), dict(lse=FAKE + 2),
                 dict(ws=FAKE + 2)):
