@@ -48,6 +48,12 @@ __device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit, float dou
 // tiles' way to LDS.
 constexpr int back_share(int size, int dp) { return size == 4 && dp <= 128 ? 2 : 4; }
 
+// Whether one kernel makes the gradients of keys and values. Together they take seven products where two kernels take eight
+// (scores are made again), apart they leave two waves a SIMD: 16-bit heads of 128 are faster apart (2 x 2,048 tokens of
+// 40 / 8 x 128 bf16, whole backward pass: 386 us, together 418), fp32 heads of 64, bound by the products, together (32 x 512
+// tokens of 12 x 64: 359 us, apart 399); wider ones do not fit the registers together.
+constexpr bool kv_together(int size, int dp) { return dp <= 64; }
+
 // Waves of a SIMD, by the bytes of a row: so that registers are taken from one file without copies.
 constexpr int back_waves(int row_bytes, int most) { return row_bytes <= most ? 2 : 1; }
 
@@ -589,7 +595,7 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
       if (rows > 0) st = launch(k_attend_back_q<T, DP, FAST>, units * a.row_tiles);
       if (st == EOGP_OK && keys > 0) {
         const int64_t blocks = units * a.key_tiles * a.splits;
-        if constexpr (DP * sizeof(T) > 128) {            // both gradients of wide heads do not fit the registers
+        if constexpr (!kv_together((int)sizeof(T), DP)) {
           st = launch(k_attend_back_kv<T, DP, 1, FAST>, blocks);
           if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, 2, FAST>, blocks);
         } else {
