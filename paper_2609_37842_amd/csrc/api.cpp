@@ -968,7 +968,7 @@ eogp_status check_attention(const char* op, int64_t Hq, int64_t Hkv, eogp_dtype 
   // rows of tiles and key heads as blocks of one launch
   if (N * std::max(Tq * Hq, Tk * Hkv) >= ((int64_t)1 << 29) || N * Hq > ((int64_t)1 << 22))
     return fail(EOGP_ERR_INVALID, std::string(op) + ": examples x tokens x heads must be < 2^29, examples x heads <= 2^22");
-  if (!(scale > 0.f) || std::isinf(scale)) return fail(EOGP_ERR_INVALID, std::string(op) + ": scale must be > 0");
+  if (!(scale > 0.f) || std::isinf(2.f * scale)) return fail(EOGP_ERR_INVALID, std::string(op) + ": scale must be > 0, and below 2^127");
   if (window < 0 || sinks < 0 || window >= ((int64_t)1 << 30) || sinks >= ((int64_t)1 << 30) || (sinks > 0 && window == 0))
     return fail(EOGP_ERR_INVALID, std::string(op) + ": need window and sinks in [0, 2^30), and sinks with a window only");
   return EOGP_OK;

@@ -36,7 +36,12 @@ struct Sight {
   const int64_t* q_start;         // position of an example's first query, or NULL: Tk - Tq
   const uint8_t *q_mask, *k_mask;
 
-  __device__ __forceinline__ int64_t start(int64_t n) const { return q_start ? q_start[n] : (int64_t)Tk - Tq; }
+  // (Positions further than 2^40 see what those see: no sum of a position leaves 64 bits.)
+  __device__ __forceinline__ int64_t start(int64_t n) const {
+    constexpr int64_t kFar = (int64_t)1 << 40;
+    const int64_t p = q_start ? q_start[n] : (int64_t)Tk - Tq;
+    return p < -kFar ? -kFar : p > kFar ? kFar : p;
+  }
 };
 
 // Keys [lo, hi) and [0, sk) of a query at position p.
@@ -47,18 +52,12 @@ struct Span {
 __device__ __forceinline__ int clamp_key(int64_t j, int most) { return (int)(j < 0 ? 0 : j > most ? most : j); }
 
 __device__ __forceinline__ Span span_of(const Sight& s, int64_t p) {
-  // far positions see what positions 2^40 see: no sum below leaves 64 bits
-  constexpr int64_t kFar = (int64_t)1 << 40;
-  p = p < -kFar ? -kFar : p > kFar ? kFar : p;
   Span v;
   v.hi = clamp_key(s.causal ? p + 1 : s.window ? p + s.window : s.Tk, s.Tk);
   v.lo = s.window ? clamp_key(p - s.window + 1, v.hi) : 0;
   v.sk = clamp_key(s.causal ? p + 1 : s.Tk, s.sinks < s.Tk ? s.sinks : s.Tk);
   return v;
 }
-
-// (Without branches: what is tested is selected among values that matrix instructions made.)
-__device__ __forceinline__ bool sees(const Span& v, int j) { return ((j >= v.lo) & (j < v.hi)) | (j < v.sk); }
 
 // Division of numbers below 2^31 by one divisor.
 struct Divide {
@@ -116,9 +115,6 @@ __device__ __forceinline__ int tile_at(int row, int piece) {
 // ---- operands -----------------------------------------------------------------------------------
 template <typename T>
 using Frag = AlignedVec<T, kPiece<T>>;
-
-template <typename T>
-struct MmaStep;                   // inner indices of one operand pair
 
 __device__ __forceinline__ void mma(f32x16& c, const Frag<__bf16>& a, const Frag<__bf16>& b) {
   c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);

@@ -16,7 +16,7 @@ struct AttendArgs {
   Sight sight;
   int N, Hq, Hkv, D;
   Divide by_group;                // query heads of a key head
-  Divide by_splits, by_units, by_heads;   // splits; key heads of all examples, of one
+  Divide by_splits, by_units, by_heads, by_rows;   // splits; key heads of all examples, of one; rows of a key head
   float scale_log2;               // scale log2(e): weights are powers of two of scores times it
   float* lse;                     // [N, Tq, Hq] or NULL
   int row_tiles, splits;
@@ -29,7 +29,11 @@ struct AttendArgs {
 constexpr float kLag = 8.f;
 template <typename T> constexpr float kLift = 0.f;
 template <> constexpr float kLift<_Float16> = 7.f;
-constexpr float kLowest = -1e30f;   // reference of a row that has seen no key (finite: differences stay numbers)
+constexpr int kMaxSplits = 256;     // workers that share a row tile's keys
+// Workers whose parts a wave a row joins; of more, a block a row. (bf16, 128 queries of 32 / 8 x 128 over 16,384 keys, 16
+// splits: 60 us, by blocks 73; 33 queries of 8 x 128 over 32,768 keys, 64 splits: by blocks 31 us, by waves 37.)
+constexpr int kFewSplits = 16;
+constexpr float kLowest = -3.4028234e38f;   // reference of a row that has seen no key (finite: its difference to itself is 0)
 
 // A row group's results: to the output, or unnormalised with their reference and sum to a worker's part.
 template <typename T, int DP, bool EXACT>
@@ -79,6 +83,11 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
 // product of the last one's weights with V, so that the vector units make exponentials while the matrix units multiply.
 // (A step's weights may move a row's reference: the output takes its factor at the step's end, when the last tile's
 // product, made with the old one, is in.)
+// Bound by the vector units' maxima, exponentials and roundings beside the matrix units: bf16 heads of 128, causal, 8 x 1,024
+// to 2,048 tokens of 16 heads 148 us (81 GFLOP, 548 TFLOP/s; vector units busy 0.37 of the SIMDs' time, matrix 0.28, and
+// few blocks: 1.7 waves a SIMD), 2 x 8,192 tokens and more 900 TFLOP/s; heads of 64 880, of 256 (one wave a SIMD) 417; fp32
+// 116 to 129 of the 154 that a large matrix product reaches. With the three steps of one tile after another the first took
+// 381 us; with three tiles at once but masks and rows' bounds read one after another before the first tile, 226.
 template <typename T, int DP, int QG, bool FAST>
 __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void k_attend(const AttendArgs<T> a) {
   constexpr int NWR = 4, NT = 256, KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB;
@@ -305,7 +314,11 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
 }
 
 // At most 32 rows a key head: single tokens, short chunks. The waves of a block take different keys, as splits do, so
-// that a cache is read by many at once; each has tiles of its own and waits for nobody.
+// that a cache is read by many at once; each has tiles of its own and waits for nobody: one tile is on its way while one is
+// multiplied. Bound by the cache's bytes: fp16, one token over 131,072 keys of 16 x 128, 1.07 GB, 200 us and the join 5
+// (5.3 TB/s; matrix units busy 0.08 of the SIMDs' time, one wave a SIMD); bf16, 16 tokens of 40 / 8 x 128 over 512 to 4,096
+// keys, 152 MB, 34 us and the join 5, where the longest sequence's blocks are a third of the time. With every wave's
+// part joined behind the kernel (four times as many) the first took 493 us in all.
 template <typename T, int DP, int NWK, bool FAST>
 __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) {
   constexpr int KB = 32, kROWB = DP * (int)sizeof(T), kTile = KB * kROWB;
@@ -455,51 +468,126 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
   }
 }
 
-// A block joins the splits' parts of one row: references, sums and unnormalised outputs, each wave those of every fourth
-// split in order, and the waves' in theirs.
+// Where row `id` of all key heads' rows lies.
+struct JoinRow {
+  int n, i, hq;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_attend_join(const AttendArgs<T> a) {
-  __shared__ float slot[4], sums[4], parts[4][256];
-  const int rows = a.by_group.by * a.sight.Tq, units = a.N * a.Hkv, lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int64_t all = (int64_t)units * rows;
-  for (int64_t id = blockIdx.x; id < all; id += gridDim.x) {
-    const int unit = (int)(id / rows), r = (int)(id % rows), n = unit / a.Hkv, i = a.by_group.quotient(r);
-    const int hq = unit % a.Hkv * (int)a.by_group.by + a.by_group.rest(r, i);
-    float ref = (int)threadIdx.x < a.splits ? a.part_stats[2 * ((int64_t)threadIdx.x * all + id)] : kLowest;
-    ref = wave_max(ref);
-    __syncthreads();
-    if (lane == 0) slot[wid] = ref;
-    __syncthreads();
-    ref = fmaxf(fmaxf(slot[0], slot[1]), fmaxf(slot[2], slot[3]));
-    float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};      // elements lane, lane + 64, ...
-#pragma unroll 4
-    for (int w = wid; w < a.splits; w += 4) {
-      const int64_t row = (int64_t)w * all + id;
-      const float by = __builtin_amdgcn_exp2f(a.part_stats[2 * row] - ref);
-      total += by * a.part_stats[2 * row + 1];
+__device__ __forceinline__ JoinRow join_row(const AttendArgs<T>& a, int id) {
+  const int unit = a.by_rows.quotient(id), r = a.by_rows.rest(id, unit), n = a.by_heads.quotient(unit);
+  const int i = a.by_group.quotient(r);
+  return JoinRow{n, i, a.by_heads.rest(unit, n) * (int)a.by_group.by + a.by_group.rest(r, i)};
+}
+template <typename T>
+__device__ __forceinline__ bool counts(const AttendArgs<T>& a, const JoinRow& to, float total) {
+  return total != 0.f && (!a.sight.q_mask || a.sight.q_mask[(int64_t)to.n * a.sight.Tq + to.i]);
+}
+template <typename T>
+__device__ __forceinline__ void put_joined(const AttendArgs<T>& a, const JoinRow& to, int c, float v) {
+  const int64_t at = to.n * a.out_n + to.i * a.out_t + to.hq * a.out_h + c;
+  if (a.out_f32)
+    static_cast<float*>(a.out)[at] = v;
+  else
+    static_cast<T*>(a.out)[at] = (T)v;
+}
+template <typename T>
+__device__ __forceinline__ void put_lse(const AttendArgs<T>& a, const JoinRow& to, bool some, float ref, float total) {
+  if (a.lse)
+    a.lse[((int64_t)to.n * a.sight.Tq + to.i) * a.Hq + to.hq] =
+        some ? (ref + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+// The splits' parts of a row joined: references, sums and unnormalised outputs, in the order of the splits. Bound by the
+// reading of the parts. Few splits: a wave takes a row, D / 64 columns a lane, and asks for four splits' at once.
+template <typename T, int COLS>
+__global__ __launch_bounds__(256) void k_attend_join_few(const AttendArgs<T> a) {
+  const int all = a.N * a.Hkv * (int)a.by_rows.by, lane = threadIdx.x & 63;
+  const int64_t step = (int64_t)all * a.D;
+  for (int id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); id < all; id += gridDim.x * 4) {
+    const float* from = a.part + (int64_t)id * a.D;
+    const int64_t at = 2 * ((int64_t)min(lane, a.splits - 1) * all + id);   // a lane has a split's weight
+    const float ref = a.part_stats[at], sum = a.part_stats[at + 1], most = wave_max(ref);
+    const float by = lane < a.splits ? __builtin_amdgcn_exp2f(ref - most) : 0.f, total = wave_sum(by * sum);
+    float v[COLS / 64];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (64 * c < a.D) v[c] += by * a.part[row * a.D + min(lane + 64 * c, a.D - 1)];
-    }
+    for (int k = 0; k < COLS / 64; ++k) v[k] = 0.f;
+    for (int w0 = 0; w0 < a.splits; w0 += 4) {
+      float x[4][COLS / 64];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) parts[wid][lane + 64 * c] = v[c];
-    if (lane == 0) sums[wid] = total;
-    __syncthreads();
-    total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    const bool live = !a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i];
-    const bool some = live && total != 0.f;
-    const int c = threadIdx.x;
-    if (c < a.D) {
-      const float o = some ? ((parts[0][c] + parts[1][c]) + (parts[2][c] + parts[3][c])) / total : 0.f;
-      const int64_t at = n * a.out_n + i * a.out_t + hq * a.out_h + c;
-      if (a.out_f32)
-        static_cast<float*>(a.out)[at] = o;
-      else
-        static_cast<T*>(a.out)[at] = (T)o;
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int k = 0; k < COLS / 64; ++k) x[w][k] = from[min(w0 + w, a.splits - 1) * step + min(lane + 64 * k, a.D - 1)];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float of = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), min(w0 + w, 63)));
+#pragma unroll
+        for (int k = 0; k < COLS / 64; ++k) v[k] += w0 + w < a.splits ? of * x[w][k] : 0.f;
+      }
     }
-    if (a.lse && threadIdx.x == 0)
-      a.lse[((int64_t)n * a.sight.Tq + i) * a.Hq + hq] =
-          some ? (ref + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+    const JoinRow to = join_row(a, id);
+    const bool some = counts(a, to, total);
+#pragma unroll
+    for (int k = 0; k < COLS / 64; ++k)
+      if (lane + 64 * k < a.D) put_joined(a, to, lane + 64 * k, some ? v[k] / total : 0.f);
+    if (lane == 0) put_lse(a, to, some, most, total);
+  }
+}
+
+// Many splits: a block takes a row, COLS columns a slice of its threads, each slice every SLICES-th split in order, four
+// requests of a thread at a time; the slices' sums in their order.
+template <typename T, int COLS>
+__global__ __launch_bounds__(1024) void k_attend_join(const AttendArgs<T> a) {
+  constexpr int SLICES = 1024 / COLS;
+  __shared__ float weight[kMaxSplits], parts[SLICES][COLS], both[2];
+  const int all = a.N * a.Hkv * (int)a.by_rows.by;
+  const int col = threadIdx.x % COLS, slice = threadIdx.x / COLS;
+  for (int id = blockIdx.x; id < all; id += gridDim.x) {
+    __syncthreads();
+    if (threadIdx.x < 64) {                              // the first wave: weights of the splits, and the row's sum
+      const int lane = threadIdx.x;
+      float ref[kMaxSplits / 64], sum[kMaxSplits / 64], most = kLowest, total = 0.f;
+#pragma unroll
+      for (int k = 0; k < kMaxSplits / 64; ++k) {
+        const int w = min(lane + 64 * k, a.splits - 1);
+        ref[k] = a.part_stats[2 * ((int64_t)w * all + id)];
+        sum[k] = lane + 64 * k < a.splits ? a.part_stats[2 * ((int64_t)w * all + id) + 1] : 0.f;
+        most = fmaxf(most, ref[k]);
+      }
+      most = wave_max(most);
+#pragma unroll
+      for (int k = 0; k < kMaxSplits / 64; ++k) {
+        const float by = __builtin_amdgcn_exp2f(ref[k] - most);
+        weight[lane + 64 * k] = by;
+        total += by * sum[k];
+      }
+      total = wave_sum(total);
+      if (lane == 0) {
+        both[0] = most;
+        both[1] = total;
+      }
+    }
+    __syncthreads();
+    float v = 0.f;
+    const float* from = a.part + (int64_t)id * a.D + min(col, a.D - 1);
+    const int64_t step = (int64_t)all * a.D;
+    for (int w = slice; w < a.splits; w += 4 * SLICES) {
+      float x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = from[min(w + k * SLICES, a.splits - 1) * step];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v += w + k * SLICES < a.splits ? x[k] * weight[min(w + k * SLICES, a.splits - 1)] : 0.f;
+    }
+    parts[slice][col] = v;
+    __syncthreads();
+    const float total = both[1];
+    const JoinRow to = join_row(a, id);
+    const bool some = counts(a, to, total);
+    if (slice == 0 && col < a.D) {
+#pragma unroll
+      for (int k = 1; k < SLICES; ++k) v += parts[k][col];
+      put_joined(a, to, col, some ? v / total : 0.f);
+    }
+    if (threadIdx.x == 0) put_lse(a, to, some, both[0], total);
   }
 }
 
@@ -514,9 +602,9 @@ struct Plan {
 };
 
 constexpr int kFewRows = 32;
-constexpr int kMaxSplits = 256;
 // Blocks that a launch which splits keys goes up to: of rows, what is there at once (2 x 2,048 tokens of 16 x 128 bf16, not
-// causal, 512 blocks: 97 us, in two splits with the join 217); of few rows, four times as many as CUs.
+// causal, 512 blocks: 97 us, in two splits 217 when the join took 100; 1,024 x 8,192 tokens, 128 blocks of rows: 102 us in
+// four splits, 122 in two); of few rows, four times as many as CUs.
 constexpr int64_t kWantBlocks = 2 * kCus, kWantFew = 4 * kCus;
 
 Plan plan_of(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D, int64_t window,
@@ -587,6 +675,7 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
     a.by_splits = Divide(p.splits);
     a.by_units = Divide(N * k.heads);
     a.by_heads = Divide(k.heads);
+    a.by_rows = Divide(q.heads / k.heads * Tq);
     a.scale_log2 = scale * 1.4426950408889634f;
     a.lse = lse;
     a.row_tiles = p.row_tiles;
@@ -617,7 +706,20 @@ eogp_status attention(const eogp_heads& q, const eogp_heads& k, const eogp_heads
                            : D <= 128 ? go(integral_constant<int, 128>{})
                                       : go(integral_constant<int, 256>{});
     if (st != EOGP_OK || !a.part) return st;
-    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)std::min<int64_t>(N * Tq * q.heads, 1 << 20)), dim3(256), 0, s, a);
+    const int64_t rows = N * Tq * q.heads;
+    auto join = [&](auto width) {
+      constexpr int DP = decltype(width)::value;
+      if (p.splits <= kFewSplits)
+        hipLaunchKernelGGL((k_attend_join_few<T, DP>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_attend_join<T, DP>), dim3((unsigned)rows), dim3(1024), 0, s, a);
+    };
+    if (D <= 64)
+      join(integral_constant<int, 64>{});
+    else if (D <= 128)
+      join(integral_constant<int, 128>{});
+    else
+      join(integral_constant<int, 256>{});
     EOGP_LAUNCH_CHECK("attention (join)");
     return EOGP_OK;
   });

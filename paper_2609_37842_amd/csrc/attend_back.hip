@@ -43,8 +43,8 @@ __device__ __forceinline__ int lift_of(const BackArgs<T>& a, int unit, float dou
   return e < -100 ? -100 : e > 100 ? 100 : e;
 }
 
-// Waves that share tiles. fp32 products are bound by the matrix units alone: there each wave has tiles of its own and waits
-// for no other, so that short and ragged sequences leave no wave idle at another's pace; 16-bit ones would be bound by the
+// Waves that share tiles. fp32 products are bound by the matrix units alone: there two waves share theirs, so that short and
+// ragged sequences leave fewer idle at another's pace (rows of more than 512 bytes aside); 16-bit ones would be bound by the
 // tiles' way to LDS.
 constexpr int back_share(int size, int dp) { return size == 4 && dp <= 128 ? 2 : 4; }
 
@@ -91,15 +91,18 @@ __global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int l
 
 // Gradients of keys and values: a wave has 32 keys, their rows of K and V and both gradients in registers; the
 // block's waves share tiles of 32 rows of queries and output gradients, over all query heads of the key head.
-// PARTS: 1 gradients of V, 2 of K, 3 both.
+// PARTS: 1 gradients of V, 2 of K, 3 both. Bound by the products at one or two waves a SIMD (registers) and the latency of a
+// tile's scores, which the next product waits for: fp32, 32 x 64 to 512 tokens of 12 x 64, both 235 us under a profiler (matrix
+// units busy 0.35 of the SIMDs' time); bf16, 2 x 1,024 to 2,048 of 40 / 8 x 128, V 97 us (0.24, vector units 0.33), K 122
+// (0.30, 0.34).
 template <typename T, int DP, int PARTS, bool FAST>
 __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), PARTS == 3 ? 128 : 256)) void k_attend_back_kv(
     const BackArgs<T> a) {
-  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, kFlip = NW > 1;   // (a wave of its own tiles is in order with itself)
+  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW;
   constexpr int kROWB = DP * (int)sizeof(T), RB = 32, kTile = RB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kKs = 32 / (2 * kPiece<T>);
   constexpr bool kV = PARTS & 1, kK = PARTS & 2;
-  extern __shared__ __align__(16) char lds[];            // [1 + kFlip][Q, dO]
+  extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
   __shared__ __align__(16) float row_f[2][2][RB];        // log-sum-exps and deltas of the rows of a tile
   __shared__ __align__(16) uint32_t seen[NW][RB];        // a wave's keys that each row sees
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   const int n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   // (the last keys of a causal tile have fewer queries: blocks of a CU, 256 apart, have them in opposite waves)
-  const int k0 = tile_key * 32 * NW, j0 = k0 + (NW > 1 && (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid) * 32, j = j0 + l;
+  const int k0 = tile_key * 32 * NW, j0 = k0 + ((blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid) * 32, j = j0 + l;
   const int k1 = min(k0 + 32 * NW, a.sight.Tk);
   const bool key_live = j < a.sight.Tk && (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
   RowPieces<T, DP, FAST> kf, vf;
@@ -119,18 +122,16 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   if constexpr (kK) vf.request(a.v.row(n, jc, kvh), a.D);
 
   // queries that can see one of the block's keys
-  constexpr int64_t kFar = (int64_t)1 << 40;
-  const int64_t st = start < -kFar ? -kFar : start > kFar ? kFar : start;
   const bool sink = k0 < a.sight.sinks;
-  const int64_t i_lo = a.sight.causal ? k0 - st : a.sight.window && !sink ? k0 - a.sight.window + 1 - st : 0;
-  const int64_t i_hi = a.sight.window && !sink ? (int64_t)k1 - 1 + a.sight.window - st : a.sight.Tq;
+  const int64_t i_lo = a.sight.causal ? k0 - start : a.sight.window && !sink ? k0 - a.sight.window + 1 - start : 0;
+  const int64_t i_hi = a.sight.window && !sink ? (int64_t)k1 - 1 + a.sight.window - start : a.sight.Tq;
   int i0 = clamp_key(i_lo, a.sight.Tq), i1 = clamp_key(i_hi, a.sight.Tq);
   if (a.sight.q_mask && i0 < i1) {
     const MaskRange r = mask_range(a.sight.q_mask + (int64_t)n * a.sight.Tq, a.sight.Tq, i0, i1);
     i0 = r.first;
     i1 = r.last;
   }
-  const int some_keys = (NW > 1 ? __syncthreads_or(key_live) : __ballot(key_live) != 0);
+  const int some_keys = __syncthreads_or(key_live);
   const int rows_lo = i0 * G, rows_hi = i1 * G, row_tiles = some_keys && i1 > i0 ? (rows_hi - rows_lo + RB - 1) / RB : 0;
   int t = 0, t_end = row_tiles;
   if (a.splits > 1) {
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
 
   // Rows of the block from which on, and up to which, each sees all of the wave's keys (the sinks' share aside), and
   // those outside which none sees any.
-  auto row_of = [&](int64_t p) { return (int)min(max(p - st, (int64_t)0), (int64_t)a.sight.Tq) * G; };
+  auto row_of = [&](int64_t p) { return (int)min(max(p - start, (int64_t)0), (int64_t)a.sight.Tq) * G; };
   const int64_t w = a.sight.window;
   const int full_lo = a.sight.causal ? row_of((int64_t)j0 + 31) : w ? row_of((int64_t)j0 + 32 - w) : 0;
   const int full_hi = w ? row_of((int64_t)j0 + w) : rows_hi;
@@ -213,22 +214,18 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
     r_live = row < rows_hi;
   };
   if (t < t_end) request(t);
-  for (int turn = 0; t < t_end; ++t, turn ^= kFlip) {
+  for (int turn = 0; t < t_end; ++t, turn ^= 1) {
     char *qt = lds + turn * 2 * kTile, *ot = qt + kTile;
     const int r0 = rows_lo + t * RB;
     r_lse2 = r_live ? r_lse2 : INFINITY;
     const uint64_t live = __ballot(r_lse2 != INFINITY) & 0xFFFFFFFFull;
-    if constexpr (NW == 1) wave_lds_order();
     qs.store(threadIdx.x, a.D, qt, live);
     os.store(threadIdx.x, a.D, ot, live);
     if (threadIdx.x < RB) {
       row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
       if constexpr (kK) row_f[turn][1][l] = r_delta;
     }
-    if constexpr (NW > 1)
-      __syncthreads();
-    else
-      wave_lds_order();
+    __syncthreads();
     if (t + 1 < t_end) request(t + 1);
     const bool full = r0 >= full_lo && r0 + RB <= full_hi;
     const bool some = live != 0 && r0 + RB > some_lo && r0 < some_hi;
@@ -322,7 +319,8 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   }
 }
 
-// Sums of the splits' parts in their order, one element of both gradients per thread.
+// Sums of the splits' parts in their order, one element of both gradients per thread. Bound by reading the parts: bf16, 2 x
+// 2,048 keys of 8 x 128, 16 splits, 134 MB of parts: 42 us (3.2 TB/s; a wave a row, with fewer divisions, the same).
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
   const int64_t units = (int64_t)a.N * a.Hkv, all = units * a.sight.Tk * 2 * a.D;
@@ -337,13 +335,14 @@ __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
 
 // Gradients of queries: a wave has 32 rows of queries, output gradients and the result in registers; the block's
 // waves share tiles of keys and values. Before that each row's delta = dout . out is formed, and its log-sum-exp in powers
-// of two, which the other kernels read (+inf: the row counts for nothing).
+// of two, which the other kernels read (+inf: the row counts for nothing). Bound as k_attend_back_kv is: the fp32 batch
+// there 158 us (matrix units busy 0.39), the bf16 one 151 (0.29, vector units 0.31).
 template <typename T, int DP, bool FAST>
 __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
-  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, KB = 32, kFlip = NW > 1;
+  constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, KB = 32;
   constexpr int kROWB = DP * (int)sizeof(T), kTile = KB * kROWB, kDt = DP / 32, kSteps = kROWB / 32;
   constexpr int kRows = 32 * NW, kKs = 32 / (2 * kPiece<T>);
-  extern __shared__ __align__(16) char lds[];            // [1 + kFlip][K, V]
+  extern __shared__ __align__(16) char lds[];            // [2][K, V]
   __shared__ uint32_t all[NW];
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int G = a.by_group.by, rows = G * a.sight.Tq;
@@ -351,7 +350,7 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   const int tile_row = a.row_tiles - 1 - from_end, n = a.by_heads.quotient(unit), kvh = a.by_heads.rest(unit, n);
   const int64_t start = a.sight.start(n);
   // (The first rows of a causal tile have fewer keys: blocks of a CU, 256 apart, have them in opposite waves.)
-  const int group = NW > 1 && (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid;
+  const int group = (blockIdx.x >> 8) & 1 ? NW - 1 - wid : wid;
   const int r = tile_row * kRows + group * 32 + l, rc = min(r, rows - 1), i = a.by_group.quotient(rc),
             hq = kvh * G + a.by_group.rest(rc, i);
   RowPieces<T, DP, FAST> q, o;
@@ -385,7 +384,8 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
 #pragma unroll
         for (int e = 0; e < kPiece<T>; ++e) delta += (float)o.f[st][e] * (float)y.f[st][e];
     }
-    delta = half_sum(delta);                             // (0 where the row does not count: dout is)
+    delta = half_sum(delta);
+    delta = live ? delta : 0.f;                          // (whatever the output holds there)
     if (r < rows && h == 0) {
       a.lse2[id] = lse2;
       a.delta[id] = delta;
@@ -402,9 +402,8 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   }
   // keys that any row of the block sees, those that any of the wave does, and those that every row of it does
   __syncthreads();
-  LiveRows block{mine, 0};
-  if constexpr (NW > 1) block.low = all[0] | (uint64_t)all[1] << 32;
-  if constexpr (NW > 2) block.high = all[NW - 2] | (uint64_t)all[NW - 1] << 32;
+  LiveRows block{all[0] | (uint64_t)all[1] << 32, 0};
+  if constexpr (NW > 2) block.high = all[2] | (uint64_t)all[3] << 32;
   auto position = [&](int at) { return start + a.by_group.quotient(tile_row * kRows + at); };
   const uint8_t* kmask = a.sight.k_mask ? a.sight.k_mask + (int64_t)n * a.sight.Tk : nullptr;
   Bounds bd{0, 0, 0, 0};
@@ -443,17 +442,13 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
     byte = km.request(j0 + l);
   };
   if (tiles.count > 0) request(tiles.at(0));
-  for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= kFlip) {
+  for (int t = 0, turn = 0; t < tiles.count; ++t, turn ^= 1) {
     char *kt = lds + turn * 2 * kTile, *vt = kt + kTile;
     const int j0 = tiles.at(t) * KB;
     const uint64_t bits = km.bits(bd, j0, byte);
-    if constexpr (NW == 1) wave_lds_order();
     ks.store(threadIdx.x, a.D, kt, bits);
     vs.store(threadIdx.x, a.D, vt, bits);
-    if constexpr (NW > 1)
-      __syncthreads();
-    else
-      wave_lds_order();
+    __syncthreads();
     if (t + 1 < tiles.count) request(tiles.at(t + 1));
     if (bits != 0 && ((j0 < some.hi && j0 + KB > some.lo) || j0 < some.sk)) {
       f32x16 s = zeros16(), dp = zeros16();
@@ -581,7 +576,7 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     auto go = [&](auto width, auto exact) {
       constexpr int DP = decltype(width)::value;
       constexpr bool FAST = decltype(exact)::value;
-      constexpr int lds = (back_share((int)sizeof(T), DP) > 1 ? 4 : 2) * 32 * DP * (int)sizeof(T);
+      constexpr int lds = 4 * 32 * DP * (int)sizeof(T);
       auto launch = [&](auto* kfn, int64_t blocks) {
         if (lds > (48 << 10)) {
           const eogp_status st = ensure_dynamic_lds(reinterpret_cast<const void*>(kfn), lds);

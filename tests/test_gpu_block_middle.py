@@ -459,3 +459,36 @@ def test_extreme_scores():
         assert abs(float(lse[0, row, 0]) - score) <= 5 * U * score
     mean = v[0, :, 0].double().mean(0)             # row 2: 200 equal weights, sums of 200 values below 4
     assert (out[0, 2, 0].double() - mean).abs().max() < 300 * U * 4 and abs(float(lse[0, 2, 0]) - np.log(200)) < 1e-5
+
+
+@pytest.mark.parametrize("Tq", [1, 40])
+@pytest.mark.parametrize("Tk", [1, 4096])
+def test_scores_far_below_zero(Tq, Tk):
+    """All scores -2^119 (products exact): the weights are equal, the sums of up to 4,096 of them and of products with values
+    below 8 exact to 2^-24 of each partial sum; split keys are joined with the same reference."""
+    say(f"[attention] scores of -2^119, {Tq} queries, {Tk} keys")
+    torch.manual_seed(2)
+    q = torch.full((1, Tq, 2, 8), 2.0 ** 58, device=DEV)
+    k = torch.full((1, Tk, 2, 8), -2.0 ** 58, device=DEV)
+    v = torch.randn(1, Tk, 2, 8, device=DEV).clamp(-8, 8)
+    out, lse = E.eogp_attention(q, k, v, scale=1.0, causal=False)
+    near(out, np.broadcast_to(host(v).mean(1, keepdims=True), out.shape), (Tk + 4) * U * 8, "out")
+    near(lse, np.full(lse.shape, -2.0 ** 119), 4 * U * 2.0 ** 119, "lse")
+
+
+def test_masked_outputs_are_not_read():
+    """The backward pass of a padded batch, whatever `out` (fp32) and lse hold at masked queries."""
+    say("[attention] backward pass, outputs of masked queries")
+    torch.manual_seed(3)
+    N, T, H, D = 2, 70, 2, 64
+    for dt in DT.values():
+        q, k, v, do = (torch.randn(N, T, H, D, device=DEV).to(dt) for _ in range(4))
+        mask = torch.ones(N, T, dtype=torch.uint8, device=DEV)
+        mask[1, 9:] = 0
+        out = torch.empty(N, T, H, D, device=DEV)
+        _, lse = E.eogp_attention(q, k, v, out=out, q_mask=mask)
+        clean = E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask)
+        for x in (out, lse, do, q):
+            x[1, 9:] = float("nan")
+        for a, b in zip(clean, E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask)):
+            assert torch.equal(a, b) and bool(a.isfinite().all())
