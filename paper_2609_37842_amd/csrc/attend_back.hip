@@ -319,17 +319,36 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   }
 }
 
-// Sums of the splits' parts in their order, one element of both gradients per thread. Bound by reading the parts: bf16, 2 x
-// 2,048 keys of 8 x 128, 16 splits, 134 MB of parts: 42 us (3.2 TB/s; a wave a row, with fewer divisions, the same).
-template <typename T>
+// Sums of the splits' parts in their order, V elements of a gradient per thread (4 where D allows), four splits' asked for at
+// once. Bound by reading the parts: bf16, 2 x 2,048 keys of 8 x 128, 4 splits, 134 MB: 24 us (6.4 TB/s; an element a thread,
+// with 64-bit divisions, 42).
+template <typename T, int V>
 __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
-  const int64_t units = (int64_t)a.N * a.Hkv, all = units * a.sight.Tk * 2 * a.D;
-  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
-    float v = 0.f;
-    for (int s = 0; s < a.splits; ++s) v += a.part[s * all + id];
-    const int c = (int)(id % a.D), which = (int)(id / a.D % 2);
-    const int64_t row = id / a.D / 2, j = row % a.sight.Tk, unit = row / a.sight.Tk;
-    (which ? a.dk : a.dv).row(unit / a.Hkv, j, unit % a.Hkv)[c] = (T)v;
+  using Piece = std::conditional_t<V == 4, AnyVec<float, 4>, float>;
+  // (the parts of a launch are at most kSplitBlocks blocks of 128 keys: numbers of 32 bits)
+  const uint32_t units = a.N * a.Hkv, wide = a.D / V, all = units * a.sight.Tk * 2 * wide;
+  for (uint32_t id = blockIdx.x * 256 + threadIdx.x; id < all; id += gridDim.x * 256) {
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+      Piece x[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        x[s] = *reinterpret_cast<const Piece*>(a.part + ((int64_t)min(s0 + s, a.splits - 1) * all + id) * V);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += s0 + s < a.splits ? reinterpret_cast<const float*>(&x[s])[e] : 0.f;
+    }
+    const uint32_t row = id / wide, c = (id - row * wide) * V, which = row & 1, key = row >> 1;
+    const uint32_t unit = key / (uint32_t)a.sight.Tk, j = key - unit * a.sight.Tk, n = unit / (uint32_t)a.Hkv;
+    T* to = (which ? a.dk : a.dv).row(n, j, unit - n * a.Hkv) + c;
+    if constexpr (V == 4) {
+      put4<T, true>(to, 0, 4, v);
+    } else {
+      to[0] = (T)v[0];
+    }
   }
 }
 
@@ -598,8 +617,11 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
         }
         if (st != EOGP_OK) return st;
         if (a.part) {
-          hipLaunchKernelGGL(k_attend_back_join<T>, dim3((unsigned)std::min<int64_t>(ceil_div(keys * 2 * D, 256), 64 * kCus)),
-                             dim3(256), 0, s, a);
+          const dim3 grid((unsigned)std::min<int64_t>(ceil_div(keys * 2 * D / (D % 4 ? 1 : 4), 256), 32 * kCus));
+          if (D % 4 == 0)
+            hipLaunchKernelGGL((k_attend_back_join<T, 4>), grid, dim3(256), 0, s, a);
+          else
+            hipLaunchKernelGGL((k_attend_back_join<T, 1>), grid, dim3(256), 0, s, a);
           EOGP_LAUNCH_CHECK("attention_backward (join)");
         }
       }
