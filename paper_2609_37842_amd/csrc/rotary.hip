@@ -419,9 +419,10 @@ __global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate(const RotateArgs
 }
 
 // With t = R_p^T dy, xh = x rstd: dx = rstd (t w - xh mean(t w xh)), and sums of t xh over the block's tokens (and
-// heads, where each has its own norm), which k_rotate_fold adds up in order. Bound by the latency of one token's sums at 215
-// registers (1.8 waves a SIMD; vector units busy 0.51): bf16, 4 x 1,024 to 2,048 tokens of 40 + 8 heads of 128, 252 MB: 79 us
-// (3.2 TB/s) and the fold 5; 187 in all with weights in registers and each piece tested against its head's end.
+// heads, where each has its own norm), which k_rotate_fold adds up in order. Bound by the latency of one token's sums at 2.4
+// waves a SIMD (registers; vector units busy 0.49): bf16, 4 x 1,024 to 2,048 tokens of 40 + 8 heads of 128, 252 MB: 64 us (3.9
+// TB/s) and the fold 5. With two heads a lane 79 us (1.8 waves); 187 in all with weights in registers and each piece tested
+// against its head's end.
 template <typename T, int NORM, int NW, int R, int LAYOUT>
 __global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate_back(const RotateArgs<T> a) {
   constexpr bool kRow = NORM == kNormRow;
@@ -625,10 +626,14 @@ RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_
     for (int i = 0; i < 2; ++i) p.chunks[i] = heads[i] > 0;
     p.part_ld = std::max(Hq, Hk) * D;
   } else {
-    // two heads a lane where there are tokens enough for all waves
+    // Two heads a lane where there are tokens enough for all waves, so that cosines and weights are read once for both; not
+    // for 16-bit heads with a norm, whose registers then leave too few waves. Two and one, bf16: 32,768 tokens of 64 x 128
+    // without a norm 217 and 231 us, 8,192 of 48 38 and 35, with a norm of each 42 and 36, its gradient 96 and 79; fp32, the
+    // same: 420 and 452, 77 and 78, 80 and 83, 133 and 130.
     const int at_once = 64 >> p.shift;
+    const int64_t waves = groups * tokens * ceil_div(Hq + Hk, at_once);
     p.worker = 64;
-    p.reps = groups * tokens * ceil_div(Hq + Hk, at_once) >= 16 * kRotateBlocks ? 2 : 1;
+    p.reps = (E == 4 ? waves >= 16 * kRotateBlocks : norm == kNormNone && waves >= 64 * kRotateBlocks) ? 2 : 1;
     for (int i = 0; i < 2; ++i) p.chunks[i] = (int)ceil_div(heads[i], at_once * p.reps);
     p.part_ld = D;
   }
@@ -684,10 +689,12 @@ eogp_status with_shape(const RotatePlan& p, F&& f) {
     using W256 = integral_constant<int, 256>;
     using W1024 = integral_constant<int, 1024>;
     if (p.worker == 64) {
-      if (p.reps == 1) return f(W64{}, One{}, layout);
+      if constexpr (NORM != kNormHead || sizeof(T) == 4)
+        if (p.reps == 1) return f(W64{}, One{}, layout);
       if constexpr (NORM == kNormRow)
         if (p.reps == 4) return f(W64{}, Four{}, layout);
-      return f(W64{}, Two{}, layout);
+      if constexpr (NORM != kNormHead || sizeof(T) == 4) return f(W64{}, Two{}, layout);
+      return f(W64{}, One{}, layout);
     }
     if constexpr (NORM == kNormRow) {
       if (p.worker == 256) return f(W256{}, Two{}, layout);
