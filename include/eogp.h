@@ -648,8 +648,8 @@ eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* d
  *             or keys.
  * 16-bit weights enter the product with v rounded to `dtype` (their sum is that of the unrounded ones, fp32); fp32 runs
  * in fp32 throughout. Errors: EOGP_ERR_INVALID for bad sizes (need key heads that divide the query heads; N * Tq * heads
- * and N * Tk * key heads below 2^29, N * heads up to 2^22), scale <= 0, window or sinks outside [0, 2^30), sinks without a
- * window, NULL pointers;
+ * and N * Tk * key heads below 2^29, N * heads up to 2^22), a scale <= 0 or of 2^127 and more, window or sinks outside
+ * [0, 2^30), sinks without a window, NULL pointers;
  * EOGP_ERR_UNSUPPORTED for D < 8 or D > 256 or another output type; EOGP_ERR_WORKSPACE if ws is too small. */
 size_t eogp_attention_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads, int64_t D,
                                      eogp_dtype dtype);

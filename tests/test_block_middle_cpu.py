@@ -144,6 +144,13 @@ ATTEND_BACK = dict(dout=heads(), q=heads(), k=heads(heads=2), v=heads(heads=2), 
 
 
 @pytest.mark.parametrize("name,args", [("eogp_attention", ATTEND), ("eogp_attention_backward", ATTEND_BACK)])
+def test_scales_beyond_their_exponent_are_refused(name, args):
+    """Scores are taken in powers of two: scale log2(e) has to be finite in fp32."""
+    for bad in (2.0 ** 127, 3e38):
+        assert call(name, args, scale=bad) == -1, bad
+
+
+@pytest.mark.parametrize("name,args", [("eogp_attention", ATTEND), ("eogp_attention_backward", ATTEND_BACK)])
 def test_attention_refusals(name, args):
     inf, nan = float("inf"), float("nan")
     for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(dt=5), dict(ot=5), dict(N=-1), dict(Tq=-1), dict(Tk=-1),
