@@ -646,6 +646,8 @@ eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* d
  *   lse       [N, Tq, heads of q] fp32: ln sum_j exp(scale q . k), for the backward pass, or NULL.
  *   ws        eogp_attention_workspace_size bytes (0: none; NULL then), no fewer for more examples, queries, query heads
  *             or keys.
+ * Scores are fp32 sums of products, of any finite size up to 2^126 in magnitude: an error of theirs is the relative error of
+ * a weight, so scores beyond 2^20 tell keys apart only where they differ by more than their own roundings.
  * 16-bit weights enter the product with v rounded to `dtype` (their sum is that of the unrounded ones, fp32); fp32 runs
  * in fp32 throughout. Errors: EOGP_ERR_INVALID for bad sizes (need key heads that divide the query heads; N * Tq * heads
  * and N * Tk * key heads below 2^29, N * heads up to 2^22), a scale <= 0 or of 2^127 and more, window or sinks outside

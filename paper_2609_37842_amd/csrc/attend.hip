@@ -29,11 +29,25 @@ struct AttendArgs {
 constexpr float kLag = 8.f;
 template <typename T> constexpr float kLift = 0.f;
 template <> constexpr float kLift<_Float16> = 7.f;
+// Exponents are scale_log2 score - reference in one rounding. The reference is a rounded product itself, so the largest
+// weight of a row is 2 to the power of that rounding: with a reference of 2^20 and more (half a step: 2^-5) in any row of the
+// wave, scores are rounded as the reference is before it is taken off, and the largest weight is what it is meant to be at any
+// size. (Scores that far below a smaller reference have weights of 0 either way. References change with `moved` alone.)
+constexpr float kFar = 1048576.f, kLowest = -3.4028234e38f;   // kLowest: a row that has seen no key (finite: kLowest - kLowest is 0)
+__device__ __forceinline__ bool is_far(float ref) { return fabsf(ref) >= kFar && ref != kLowest; }
+// A product as it is rounded, whatever takes it. (The compiler makes one rounding of a product and a difference.)
+__device__ __forceinline__ float rounded(float x) {
+  asm("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ void round_scores(f32x16& s, float by) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) s[e] = rounded(s[e] * by);
+}
 constexpr int kMaxSplits = 256;     // workers that share a row tile's keys
 // Workers whose parts a wave a row joins; of more, a block a row. (bf16, 128 queries of 32 / 8 x 128 over 16,384 keys, 16
 // splits: 60 us, by blocks 73; 33 queries of 8 x 128 over 32,768 keys, 64 splits: by blocks 31 us, by waves 37.)
 constexpr int kFewSplits = 16;
-constexpr float kLowest = -3.4028234e38f;   // reference of a row that has seen no key (finite: its difference to itself is 0)
 
 // A row group's results: to the output, or unnormalised with their reference and sum to a worker's part.
 template <typename T, int DP, bool EXACT>
@@ -191,6 +205,7 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
     for (int c = tid * 16; c < kTile; c += NT * 16) *reinterpret_cast<uint4*>(vt + kTile + c) = uint4{0, 0, 0, 0};
     f32x16 s[2][QG];
     Frag<T> p[2][QG][kKs];
+    bool far = false;
 #pragma unroll
     for (int qg = 0; qg < QG; ++qg)
 #pragma unroll
@@ -216,6 +231,18 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
       vs.request(vsrc, tiles.at(t) * KB, tid, a.D);
       const uint8_t byte_after = km.request(tiles.at(t + 2) * KB + l);
       const int j0 = tiles.at(t) * KB;
+      // (One row group: before the maxima, the other order is 1% slower; two: behind the branch, 3% faster, without spills.)
+      auto products = [&]() {
+#pragma unroll
+        for (int qg = 0; qg < QG; ++qg) s[1 - PAR][qg] = zeros16();
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          const Frag<T> kf = row_frag<T, kROWB>(kn, l, st);
+#pragma unroll
+          for (int qg = 0; qg < QG; ++qg) mma(s[1 - PAR][qg], kf, q[qg].f[st]);
+        }
+      };
+      if constexpr (QG == 1) products();
       if (!(bits == 0xFFFFFFFFu && j0 >= lo_max && j0 + KB <= hi_min)) {
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) hide(s[PAR][qg], span[qg], bits, j0);
@@ -224,27 +251,34 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
       bool moved = false;
 #pragma unroll
       for (int qg = 0; qg < QG; ++qg) {
-        s[1 - PAR][qg] = zeros16();
         float most = s[PAR][qg][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = fmaxf(most, s[PAR][qg][e]);
-        most = half_max(most) * a.scale_log2;
-        const bool up = most > ref[qg] + (kLag + kLift<T>);
+        most = rounded(half_max(most) * a.scale_log2);
+        const bool up = most - ref[qg] > kLag + kLift<T>;   // (a sum with a large reference would round)
         next[qg] = up ? most - kLift<T> : ref[qg];
         moved |= up;
       }
+      const bool any_moved = __ballot(moved) != 0;
+      float per_score = a.scale_log2;
+      if (__builtin_expect(any_moved || far, 0)) {
+        bool some = false;
 #pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const Frag<T> kf = row_frag<T, kROWB>(kn, l, st);
+        for (int qg = 0; qg < QG; ++qg) some |= is_far(next[qg]);
+        far = __ballot(some) != 0;
+        if (far) {
+          per_score = 1.f;
 #pragma unroll
-        for (int qg = 0; qg < QG; ++qg) mma(s[1 - PAR][qg], kf, q[qg].f[st]);
+          for (int qg = 0; qg < QG; ++qg) round_scores(s[PAR][qg], a.scale_log2);
+        }
       }
+      if constexpr (QG == 2) products();
 #pragma unroll
       for (int qg = 0; qg < QG; ++qg) {
         by_sum[qg] = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[PAR][qg][e], a.scale_log2, -next[qg]));
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[PAR][qg][e], per_score, -next[qg]));
           s[PAR][qg][e] = w;
           by_sum[qg] += w;
         }
@@ -259,7 +293,7 @@ __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void 
 #pragma unroll
           for (int qg = 0; qg < QG; ++qg) mma(acc[qg][dt], vf, p[1 - PAR][qg][k]);
         }
-      if (__ballot(moved)) {
+      if (any_moved) {
 #pragma unroll
         for (int qg = 0; qg < QG; ++qg) {
           const float by = __builtin_amdgcn_exp2f(ref[qg] - next[qg]);
@@ -367,6 +401,7 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
     byte = km.request(tile * KB + l);
   };
   char *kt = lds + wid * 2 * kTile, *vt = kt + kTile;
+  bool far = false;
   if (t < t_end) request(tiles.at(t));
   for (; t < t_end; ++t) {
     const int j0 = tiles.at(t) * KB;
@@ -384,20 +419,26 @@ __global__ __launch_bounds__(64 * NWK) void k_attend_few(const AttendArgs<T> a) 
     float most = s[0][0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) most = fmaxf(most, s[0][e]);
-    most = half_max(most) * a.scale_log2;
-    if (__ballot(most > ref + (kLag + kLift<T>))) {
+    most = rounded(half_max(most) * a.scale_log2);
+    if (__ballot(most - ref > kLag + kLift<T>)) {
       const float next = fmaxf(ref, most - kLift<T>), by = __builtin_amdgcn_exp2f(ref - next);
       ref = next;
+      far = __ballot(is_far(ref)) != 0;
       sum *= by;
 #pragma unroll
       for (int dt = 0; dt < kDt; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[dt][e] *= by;
     }
+    float per_score = a.scale_log2;
+    if (far) {
+      per_score = 1.f;
+      round_scores(s[0], a.scale_log2);
+    }
     Frag<T> p[kKs];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], a.scale_log2, -ref));
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], per_score, -ref));
       s[0][e] = w;
       sum += w;
     }

@@ -1,0 +1,87 @@
+"""The operators in the middle of a block at the ends of their types: scores of any finite size, infinities in places that
+count for nothing, the most examples and heads of a call."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_block_middle as B
+from oracle import block_middle as M
+from paper_2609_37842_amd import eogp as E
+
+pytestmark = pytest.mark.gpu
+DEV, DT, U, ULP = B.DEV, B.DT, B.U, B.ULP
+say, gen, host, dev, near = B.say, B.gen, B.host, B.dev, B.near
+
+# (q, k) with one element each, whose product is exact in fp32 and no power of two: a few bits of mantissa
+SCORES = {
+    "f32": [(76800.0, 65280.0), (76800.0, -65280.0), (150 * 2.0 ** 14, 255 * 2.0 ** 14), (150 * 2.0 ** 53, -255 * 2.0 ** 55), (19.0, 2.625e5), (150.0, -2.5625)],
+    "bf16": [(76800.0, 65280.0), (76800.0, -65280.0), (150 * 2.0 ** 14, 255 * 2.0 ** 14), (150 * 2.0 ** 53, -255 * 2.0 ** 55), (19.0, 2.621e5)],
+    "f16": [(19200.0, 16320.0), (19200.0, -16320.0), (38400.0, 65280.0), (1104.0, 9056.0), (1104.0, -9056.0)],
+}
+
+
+def large_scores(a, b, dt, N, Tq, Tk, H, D, g):
+    """q, k and v: every third key has the score a b with all queries, the others are further down by at least 2^-9 of it.
+    Queries of every second head have scores of 1 and less instead."""
+    q, k = np.zeros((N, Tq, H, D)), np.zeros((N, Tk, H, D))
+    q[..., 1] = a
+    low = b - np.abs(b) * np.exp2(-g.integers(0, 8, (N, Tk, H)))
+    k[..., 1] = np.where(np.arange(Tk)[None, :, None] % 3 == 0, b, low)
+    q[:, :, 1::2, 1] = 0.0
+    q[:, :, 1::2, 0] = 0.5
+    k[..., 0] = g.integers(-8, 9, (N, Tk, H)) / 8.0
+    return B.rounded(q, dt), B.rounded(k, dt), B.rounded(g.standard_normal((N, Tk, H, D)), dt)
+
+
+def exact_bounds(q, k, v, scale, dt, how):
+    """As attend_bounds, for scores that no rounding of a product or a sum touches: a weight is off by that of the score in
+    powers of two, which all weights of its row share, and by its exponential's 2^-21; sums of at most Tk keys."""
+    spread, rel = np.zeros(q.shape), np.full(q.shape[:3], 2.0 ** -21 + k.shape[1] * U)
+    for n in range(q.shape[0]):
+        see = M.sight(n, q.shape[1], k.shape[1], **how)
+        cols = see.any(0)[:, None]
+        for h in range(q.shape[2]):
+            hk = h * k.shape[2] // q.shape[2]
+            p, _ = M.head_weights(q[n, :, h], k[n, :, hk], see, scale)
+            spread[n, :, h] = p @ np.where(cols, np.abs(v[n, :, hk]), 0.0)
+    return spread * ((0.0 if dt == torch.float32 else ULP[dt]) + 2 * rel[..., None]), rel
+
+
+@pytest.mark.parametrize("dtype,score", [(d, s) for d in DT for s in SCORES[d]])
+@pytest.mark.parametrize("Tq", [1, 40])
+@pytest.mark.parametrize("Tk", [1, 100, 4200])
+def test_large_scores(dtype, score, Tq, Tk):
+    """Weights of scores between 2^8 and 2^123 of either sign, few and many queries, keys in one piece and split. The
+    log-sum-exp is that of the score, rounded in powers of two and back: 4 roundings."""
+    dt = DT[dtype]
+    say(f"[attention] scores {score} {dtype}, {Tq} queries, {Tk} keys")
+    q, k, v = large_scores(*score, dt, 1, Tq, Tk, 3, 8, gen(31, Tq, Tk))
+    how = dict(causal=False)
+    ref, rlse = M.attention(q, k, v, 0.5, **how)
+    tol, rel = exact_bounds(q, k, v, 0.5, dt, how)
+    out, lse = E.eogp_attention(dev(q, dt), dev(k, dt), dev(v, dt), 0.5, **how)
+    near(out, ref, tol, "out")
+    near(lse, rlse, rel + 4 * U * (np.abs(rlse) + 12), "lse")
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("Tq", [1, 40])
+def test_scores_of_minus_infinity(dtype, Tq):
+    """Keys whose score is -inf have no weight; the lowest finite ones of a row that has no others have equal weights."""
+    dt = DT[dtype]
+    say(f"[attention] scores of -inf, {dtype}, {Tq} queries")
+    g = gen(33, Tq)
+    T, D, low = 200, 64, {"f32": -3e37, "bf16": -3e37, "f16": -6e4}[dtype]
+    q, k, v = (B.rounded(x, dt) for x in (np.abs(g.standard_normal((1, Tq, 2, D))), g.standard_normal((1, T, 2, D)),
+                                          g.standard_normal((1, T, 2, D))))
+    k[0, ::3, 0, 0] = -np.inf
+    q[0, :, 1], k[0, :, 1] = 0.0, 0.0
+    q[0, :, 1, 3], k[0, :, 1, 3] = 1.0, B.rounded(np.array(low), dt)
+    out, lse = E.eogp_attention(dev(q, dt), dev(k, dt), dev(v, dt), 0.75, causal=False)
+    keep = np.arange(T) % 3 != 0
+    for h, some in ((0, keep), (1, np.ones(T, bool))):
+        one = [x[:, :, h:h + 1] if x is q else x[:, some, h:h + 1] for x in (q, k, v)]
+        ref, rlse = M.attention(*one, 0.75, causal=False)
+        tol, rel = (B.attend_bounds if h == 0 else exact_bounds)(*one, 0.75, dt, dict(causal=False))
+        near(out[:, :, h:h + 1], ref, tol, "out")
+        near(lse[:, :, h:h + 1], rlse, rel + 4 * U * (np.abs(rlse) + 12), "lse")
