@@ -668,6 +668,8 @@ eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_
  *   out, lse           of the forward pass (out of `dtype` or fp32), from the same arguments.
  *   ws                 eogp_attention_backward_workspace_size bytes, no fewer for more examples, queries, heads or keys.
  * An output gradient that is not finite may reach every key and query of its example.
+ * Weights are made from lse, to 2^-22 |lse| of their size while that is below 710; rows beyond have theirs summed anew, so
+ * that they add up to 1 for scores of any size.
  * Sums run in a fixed order. 16-bit weights and score gradients are rounded to `dtype` once, before the products that
  * take them. Errors as for eogp_attention. */
 size_t eogp_attention_backward_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,

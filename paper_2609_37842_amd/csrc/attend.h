@@ -403,6 +403,16 @@ struct KeyMask {
   }
 };
 
+// Scores and references in powers of two from which on their own roundings count (half a step of 2^20 is 2^-5).
+constexpr float kFar = 1048576.f;
+constexpr float kLowest = -3.4028234e38f;   // reference of a row that has seen no key (finite: its difference to itself is 0)
+
+// A product as it is rounded, whatever takes it. (The compiler makes one rounding of a product and a difference.)
+__device__ __forceinline__ float rounded(float x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
 // Scores that their row does not see become -inf.
 __device__ __forceinline__ void hide(f32x16& s, const Span& span, uint32_t bits, int j0) {
   const uint32_t seen = (bits & sight_bits(span, j0)) >> (4 * ((threadIdx.x >> 5) & 1));

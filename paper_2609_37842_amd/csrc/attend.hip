@@ -33,13 +33,7 @@ template <> constexpr float kLift<_Float16> = 7.f;
 // weight of a row is 2 to the power of that rounding: with a reference of 2^20 and more (half a step: 2^-5) in any row of the
 // wave, scores are rounded as the reference is before it is taken off, and the largest weight is what it is meant to be at any
 // size. (Scores that far below a smaller reference have weights of 0 either way. References change with `moved` alone.)
-constexpr float kFar = 1048576.f, kLowest = -3.4028234e38f;   // kLowest: a row that has seen no key (finite: kLowest - kLowest is 0)
 __device__ __forceinline__ bool is_far(float ref) { return fabsf(ref) >= kFar && ref != kLowest; }
-// A product as it is rounded, whatever takes it. (The compiler makes one rounding of a product and a difference.)
-__device__ __forceinline__ float rounded(float x) {
-  asm("" : "+v"(x));
-  return x;
-}
 __device__ __forceinline__ void round_scores(f32x16& s, float by) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) s[e] = rounded(s[e] * by);

@@ -20,7 +20,8 @@ struct BackArgs {
   Divide by_splits, by_units, by_heads;   // splits; key heads of all examples, of one
   float scale, scale_log2;
   const float* lse;               // [N, Tq, Hq]
-  float *lse2, *delta;            // [N, Tq, Hq]: log-sum-exp in powers of two (+inf: the row counts for nothing), dout . out
+  // [N, Tq, Hq]: a weight is 2^(score - lse2 - low) (lse2 +inf: the row counts for nothing); dout . out
+  float *lse2, *low, *delta;
   uint32_t* norms;                // fp16: [N Hkv][2] largest squared norms of a row of dout and of v, as bits
   int row_tiles, key_tiles, splits;
   float* part;                    // splits > 1: [splits][N Hkv][Tk][2][D]
@@ -29,6 +30,15 @@ struct BackArgs {
 // Weights times 2^kLiftBack: fp16 holds small ones as precisely as large ones. (Weights are at most 1.)
 template <typename T> constexpr float kLiftBack = 0.f;
 template <> constexpr float kLiftBack<_Float16> = 15.f;
+
+// A log-sum-exp in fp32 holds a row's weights to 2^-22 of its size: below 2^10 (in powers of two) to 2^-12. Rows beyond have
+// their scores' largest and the sum of the weights beside it made anew, lse2 and low, so that their weights add up to 1
+// whatever the size. (lse2 is at most 29 below the log-sum-exp that made a row one of them.)
+constexpr float kFarLse = 1024.f, kFarTile = 512.f;
+__device__ __forceinline__ bool is_far(float lse2, float from) { return fabsf(lse2) >= from && fabsf(lse2) < INFINITY; }
+__device__ __forceinline__ float far_score(float s, float scale_log2, float lse2) {
+  return fabsf(lse2) < kFar ? __builtin_fmaf(s, scale_log2, -lse2) : rounded(s * scale_log2) - lse2;
+}
 
 // fp16 score gradients P (dP - delta) are small where many keys share a row, and lie below fp16's normal range where
 // the output gradients are small as well. They are held times 2^e, e from |dP - delta| <= 2 max |dout row| max |v row|
@@ -103,7 +113,7 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   constexpr int kKs = 32 / (2 * kPiece<T>);
   constexpr bool kV = PARTS & 1, kK = PARTS & 2;
   extern __shared__ __align__(16) char lds[];            // [2][Q, dO]
-  __shared__ __align__(16) float row_f[2][2][RB];        // log-sum-exps and deltas of the rows of a tile
+  __shared__ __align__(16) float row_f[2][3][RB];        // rows of a tile: log-sum-exps and deltas; far ones' `low`
   __shared__ __align__(16) uint32_t seen[NW][RB];        // a wave's keys that each row sees
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int units = a.N * a.Hkv, G = a.by_group.by;
@@ -182,6 +192,10 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
       walk_o[u] = i * o_t + walk_g[u] * o_h + at % kPieces * 16;
     }
   }
+  auto id_of = [&](int row) {
+    const int rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
+    return id0 + (int64_t)i * a.Hq + a.by_group.rest(rc, i);
+  };
   float r_lse2 = 0.f, r_delta = 0.f;
   bool r_live = false;
   auto request = [&](int tile) {
@@ -207,8 +221,8 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
       qs.request_each(threadIdx.x, a.D, at(qbase, a.q));
       os.request_each(threadIdx.x, a.D, at(obase, a.dout));
     }
-    const int row = r0 + l, rc = min(row, rows_hi - 1), i = a.by_group.quotient(rc);
-    const int64_t id = id0 + (int64_t)i * a.Hq + a.by_group.rest(rc, i);
+    const int row = r0 + l;
+    const int64_t id = id_of(row);
     r_lse2 = a.lse2[id];
     if constexpr (kK) r_delta = a.delta[id];
     r_live = row < rows_hi;
@@ -221,8 +235,10 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
     const uint64_t live = __ballot(r_lse2 != INFINITY) & 0xFFFFFFFFull;
     qs.store(threadIdx.x, a.D, qt, live);
     os.store(threadIdx.x, a.D, ot, live);
+    const bool far = __ballot(is_far(r_lse2, kFarTile)) != 0;
     if (threadIdx.x < RB) {
-      row_f[turn][0][l] = r_lse2 - kLiftBack<T>;
+      row_f[turn][0][l] = far ? r_lse2 : r_lse2 - kLiftBack<T>;
+      if (__builtin_expect(far, 0)) row_f[turn][2][l] = a.low[id_of(r0 + l)] - kLiftBack<T>;
       if constexpr (kK) row_f[turn][1][l] = r_delta;
     }
     __syncthreads();
@@ -241,11 +257,19 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
       mma(s, row_frag<T, kROWB>(qt, l, k), kf.f[k]);
       if constexpr (kK) mma(dp, row_frag<T, kROWB>(ot, l, k), vf.f[k]);
     }
+    if (__builtin_expect(far, 0)) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&row_f[turn][0][8 * g + 4 * h]);
+      for (int e = 0; e < 16; ++e) {
+        const int at = 8 * (e / 4) + 4 * h + e % 4;
+        s[e] = __builtin_amdgcn_exp2f(far_score(s[e], a.scale_log2, row_f[turn][0][at]) - row_f[turn][2][at]);
+      }
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + i], a.scale_log2, -lse2[i]));
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&row_f[turn][0][8 * g + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * g + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + i], a.scale_log2, -lse2[i]));
+      }
     }
     if (!full) {
 #pragma unroll
@@ -378,7 +402,7 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   const int64_t id = ((int64_t)n * a.sight.Tq + i) * a.Hq + hq;
   const float lse = r < rows && (!a.sight.q_mask || a.sight.q_mask[(int64_t)n * a.sight.Tq + i]) ? a.lse[id] : -INFINITY;
   const bool live = lse != -INFINITY;
-  const float lse2 = live ? lse * 1.4426950408889634f : INFINITY;
+  float lse2 = live ? lse * 1.4426950408889634f : INFINITY, low = 0.f;
   const uint32_t mine = (uint32_t)__ballot(live);
   if (lane == 0) all[group] = mine;
   q.settle(live, a.D);
@@ -405,10 +429,6 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
     }
     delta = half_sum(delta);
     delta = live ? delta : 0.f;                          // (whatever the output holds there)
-    if (r < rows && h == 0) {
-      a.lse2[id] = lse2;
-      a.delta[id] = delta;
-    }
     if constexpr (kLiftBack<T> != 0.f) {
 #pragma unroll
       for (int st = 0; st < kSteps; ++st)
@@ -420,7 +440,8 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
     }
   }
   // keys that any row of the block sees, those that any of the wave does, and those that every row of it does
-  __syncthreads();
+  const bool far_row = is_far(lse2, kFarLse);
+  const int far_block = __syncthreads_or(far_row);
   LiveRows block{all[0] | (uint64_t)all[1] << 32, 0};
   if constexpr (NW > 2) block.high = all[2] | (uint64_t)all[3] << 32;
   auto position = [&](int at) { return start + a.by_group.quotient(tile_row * kRows + at); };
@@ -444,15 +465,51 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
   const Span span = live ? span_of(a.sight, start + i) : Span{0, 0, 0};
   const Tiles tiles = tiles_of(bd, KB);
 
+  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
+  Stage<T, DP, KB, NT, FAST> ks, vs;
+  const KeyMask km(kmask, ksrc.base, a.sight.Tk);
+  if (far_block) {                                       // the far rows' largest scores, and their weights' sums
+    float most = kLowest, total = 0.f;
+    for (int t = 0; t < tiles.count; ++t) {
+      const int j0 = tiles.at(t) * KB;
+      ks.request(ksrc, j0, threadIdx.x, a.D);
+      const uint32_t bits = km.bits(bd, j0, km.request(j0 + l));
+      __syncthreads();
+      ks.store(threadIdx.x, a.D, lds, bits);
+      __syncthreads();
+      f32x16 s = zeros16();
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) mma(s, row_frag<T, kROWB>(lds, l, k), q.f[k]);
+      hide(s, span, bits, j0);
+      float top = s[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+      const float next = fmaxf(most, rounded(half_max(top) * a.scale_log2));
+      total *= __builtin_amdgcn_exp2f(most - next);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) total += __builtin_amdgcn_exp2f(far_score(s[e], a.scale_log2, next));
+      most = next;
+    }
+    total = half_sum(total);
+    if (far_row) {
+      lse2 = most;
+      low = __builtin_amdgcn_logf(total);
+    }
+    __syncthreads();
+  }
+  if (r < rows && h == 0) {
+    a.lse2[id] = lse2;
+    a.low[id] = low;
+    a.delta[id] = delta;
+  }
+
   f32x16 dq[kDt];
 #pragma unroll
   for (int dt = 0; dt < kDt; ++dt) dq[dt] = zeros16();
   const int lift = kLiftBack<T> == 0.f ? 0 : lift_of(a, unit, square);
-  const float ds_by = exp2f((float)lift - kLiftBack<T>), ref = lse2 - kLiftBack<T>;
-
-  const RowSource<T> ksrc(a.k.row(n, 0, kvh), a.k.ld_t, a.sight.Tk, DP, FAST), vsrc(a.v.row(n, 0, kvh), a.v.ld_t, a.sight.Tk, DP, FAST);
-  Stage<T, DP, KB, NT, FAST> ks, vs;
-  const KeyMask km(kmask, ksrc.base, a.sight.Tk);
+  const bool far = __ballot(far_row) != 0;
+  const float ref = (far ? low : lse2) - kLiftBack<T>;
+  const float ds_by = exp2f((float)lift - kLiftBack<T>);
   uint8_t byte = 0;
   auto request = [&](int tile) {
     const int j0 = tile * KB;
@@ -478,9 +535,16 @@ __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP 
       }
       const bool full = bits == 0xFFFFFFFFull && j0 >= lo_max && j0 + KB <= hi_min;
       if (!full) hide(s, span, (uint32_t)bits, j0);      // (weights 0)
+      if (__builtin_expect(far, 0)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = far_score(s[e], a.scale_log2, lse2) - ref;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_fmaf(s[e], a.scale_log2, -ref);
+      }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float d = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -ref)) * (dp[e] - delta);
+        float d = __builtin_amdgcn_exp2f(s[e]) * (dp[e] - delta);
         if constexpr (kLiftBack<T> != 0.f) d *= ds_by;
         s[e] = d;
       }
@@ -520,7 +584,7 @@ int back_splits(int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int 
 // Bytes for any call of up to N examples, Tq queries and Tk keys: launches with several workers a key tile have at most
 // kSplitBlocks blocks of 128 keys (or four times as many of 32), and a worker has no fewer than 8 tiles of 32 rows.
 size_t attention_back_ws(eogp_dtype t, int64_t N, int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hkv, int64_t D) {
-  size_t bytes = 2 * align256((size_t)(N * Tq * Hq) * sizeof(float)) + 256;
+  size_t bytes = 3 * align256((size_t)(N * Tq * Hq) * sizeof(float)) + 256;
   if (t == EOGP_F16) bytes += align256((size_t)(2 * N * Hkv) * sizeof(float));
   const int64_t most = ceil_div(Hq / Hkv * Tq, 32) / 8;
   if (most > 1)
@@ -573,6 +637,7 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
     a.row_tiles = (int)ceil_div(Hq / Hkv * Tq, 32 * share);
     Carve w(ws, ~(size_t)0);
     a.lse2 = w.take<float>(N * Tq * Hq);
+    a.low = w.take<float>(N * Tq * Hq);
     a.delta = w.take<float>(N * Tq * Hq);
     if (t == EOGP_F16) a.norms = w.take<uint32_t>(2 * units);
     a.part = a.splits > 1 ? w.take<float>((size_t)a.splits * (units * Tk * 2 * D)) : nullptr;

@@ -85,3 +85,33 @@ def test_scores_of_minus_infinity(dtype, Tq):
         tol, rel = (B.attend_bounds if h == 0 else exact_bounds)(*one, 0.75, dt, dict(causal=False))
         near(out[:, :, h:h + 1], ref, tol, "out")
         near(lse[:, :, h:h + 1], rlse, rel + 4 * U * (np.abs(rlse) + 12), "lse")
+
+
+def gradient_bounds(q, k, v, scale, dt, how):
+    """exact_bounds, and what the backward pass reads: the log-sum-exp is (reference + log2 of the sum) ln 2 in fp32, taken back
+    to powers of two: roundings of the sum, both products and both constants, 5 half steps of its size in a weight's exponent.
+    From 2^10 in powers of two on (710 in natural units) weights no longer depend on it."""
+    tol, rel = exact_bounds(q, k, v, scale, dt, how)
+    lse = np.nan_to_num(np.abs(M.attention(q, k, v, scale, **how)[1]), posinf=0.0)
+    return tol, rel + 5 * U * np.minimum(lse, 710.0)
+
+
+@pytest.mark.parametrize("dtype,score", [(d, s) for d in DT for s in SCORES[d] if abs(s[0] * s[1]) < 2.0 ** 60])
+@pytest.mark.parametrize("Tq,Tk", [(1, 1), (1, 100), (40, 40), (70, 600)])
+@pytest.mark.parametrize("one", [False, True])
+def test_gradients_at_large_scores(dtype, score, Tq, Tk, one, monkeypatch):
+    """The same scores in the backward pass, where queries see all keys or one: a log-sum-exp in fp32 does not hold what these
+    weights are, sums of which are 1 all the same."""
+    dt = DT[dtype]
+    say(f"[attention_backward] scores {score} {dtype}, {Tq} queries, {Tk} keys, one={one}")
+    g = gen(32, Tq, Tk)
+    q, k, v = large_scores(*score, dt, 2, Tq, Tk, 3, 8, g)
+    dout = B.rounded(0.01 * g.standard_normal(q.shape), dt)
+    how = dict(causal=one, window=1 if one else 0)
+    qd, kd, vd, dd = (dev(x, dt) for x in (q, k, v, dout))
+    out, lse = E.eogp_attention(qd, kd, vd, 0.5, **how)
+    got = E.eogp_attention_backward(dd, qd, kd, vd, out, lse, 0.5, **how)
+    monkeypatch.setattr(B, "attend_bounds", gradient_bounds)
+    ref = M.attention_backward(dout, q, k, v, 0.5, **how)
+    for x, y, t, name in zip(got, ref, B.back_bounds(dout, q, k, v, 0.5, dt, how), ("dq", "dk", "dv")):
+        near(x, y, t, name)
