@@ -178,8 +178,7 @@ struct Values {
   }
 };
 
-// Cosines and sines of a slot's pairs: 1 and 0 for the part that is not turned, NaN for a position that
-// the table does not have.
+// Cosines and sines of a slot's pairs, NaN for a position that the table does not have.
 template <typename T, int LAYOUT>
 struct Turn {
   static constexpr int E = kPiece<T>;
@@ -199,14 +198,14 @@ struct Turn {
         x[u] = fetch_piece<float, 4>(row, first + 4 * u, width, 0.f);
     }
   }
+  // (Selects, no product with 1 and 0: elements behind the turned part pass whatever their neighbours hold.)
   __device__ __forceinline__ void apply(const Slot<T, LAYOUT>& slot, float sign, Values<T, LAYOUT>& v) const {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float c = !slot.turned ? 1.f : known ? x[e / 2][2 * (e % 2)] : NAN;
-      const float s = !slot.turned ? 0.f : known ? x[e / 2][2 * (e % 2) + 1] * sign : NAN;
+      const float c = known ? x[e / 2][2 * (e % 2)] : NAN, s = known ? x[e / 2][2 * (e % 2) + 1] * sign : NAN;
       const float a = v.a[e], b = v.b[e];
-      v.a[e] = a * c - b * s;
-      v.b[e] = a * s + b * c;
+      v.a[e] = slot.turned ? a * c - b * s : a;
+      v.b[e] = slot.turned ? a * s + b * c : b;
     }
   }
 };

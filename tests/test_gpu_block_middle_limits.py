@@ -115,3 +115,24 @@ def test_gradients_at_large_scores(dtype, score, Tq, Tk, one, monkeypatch):
     ref = M.attention_backward(dout, q, k, v, 0.5, **how)
     for x, y, t, name in zip(got, ref, B.back_bounds(dout, q, k, v, 0.5, dt, how), ("dq", "dk", "dv")):
         near(x, y, t, name)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("D,width,interleaved", [(64, 32, False), (64, 32, True), (33, 14, False), (64, 0, False), (7, 2, True)])
+def test_elements_that_pass(dtype, D, width, interleaved):
+    """Elements behind the turned part come out as they are, whatever any of them holds, in both directions."""
+    say(f"[rotate_heads] infinities behind {width} of {D} elements, {dtype}")
+    dt = DT[dtype]
+    torch.manual_seed(6)
+    q, k = (torch.randn(2, 5, h, D, device=DEV).to(dt) for h in (3, 1))
+    for x in (q, k):
+        rest = x[..., width:].reshape(-1)
+        rest[::5], rest[1::7], rest[2::11], rest[3::13] = float("inf"), float("-inf"), float("nan"), -0.0
+        x[..., width:] = rest.view(x[..., width:].shape)
+    table = E.eogp_rotary_table(5, width) if width else None
+    for got in (E.eogp_rotate_heads(q, k, table, interleaved=interleaved),
+                E.eogp_rotate_heads_backward(q, k, table=table, interleaved=interleaved)[:2]):
+        for x, y in zip((q, k), got):
+            assert torch.equal(torch.nan_to_num(x[..., width:], nan=7.0), torch.nan_to_num(y[..., width:], nan=7.0))
+            assert torch.equal(x[..., width:].isnan(), y[..., width:].isnan())
+            assert bool(y[..., :width].isfinite().all())
