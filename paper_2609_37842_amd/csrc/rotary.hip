@@ -4,6 +4,7 @@
 
 #include "attend.h"
 #include "timing.h"
+#include "token_walk.h"
 
 namespace eogp {
 namespace {
@@ -212,7 +213,8 @@ struct Turn {
 
 // Tokens first, first + step, ... below n of a group, masks and positions of 64 at once.
 struct TokenQueue {
-  int first, step, n, base;
+  TokenWalk walk;
+  int base;
   const uint8_t* mask;
   const int64_t* at;
   const Divide& by_length;
@@ -224,20 +226,20 @@ struct TokenQueue {
   bool live;
 
   __device__ __forceinline__ TokenQueue(const uint8_t* m, const int64_t* a, int f, int st, int rows, int b, const Divide& len)
-      : first(f - 64 * st), step(st), n(rows), base(b), mask(m), at(a), by_length(len) {}
+      : walk(f, st, rows), base(b), mask(m), at(a), by_length(len) {}
 
   // False at the end.
   __device__ __forceinline__ bool next() {
     if (!left) {
-      first += 64 * step;
-      if (first >= n) return false;
-      const int64_t mine = first + (int64_t)(threadIdx.x & 63) * step;
-      const bool in = mine < n;
+      if (!walk.next()) return false;
+      const int lane = threadIdx.x & 63;
+      const bool in = walk.has(lane);
+      const int64_t mine = base + walk.at(lane);
       left = __ballot(in);
-      lane_mask = in && (!mask || mask[base + mine] != 0);
-      lane_at = in && at ? at[base + mine] : 0;
+      lane_mask = in && (!mask || mask[mine] != 0);
+      lane_at = in && at ? at[mine] : 0;
     }
-    const int k = __builtin_ctzll(left), token = base + first + k * step;
+    const int k = __builtin_ctzll(left), token = base + (int)walk.at(k);
     left &= left - 1;
     live = __builtin_amdgcn_readlane(lane_mask, k);
     example = by_length.quotient(token);
