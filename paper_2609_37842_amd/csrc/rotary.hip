@@ -62,6 +62,7 @@ struct RotateArgs {
   int shift;                      // 2^shift lanes hold a head
   int chunks[2];                  // workers that share a token's heads, of queries and keys
   int splits;                     // blocks that share a group's tokens, for each chunk
+  uint32_t block0;                // of the first block of the launch, among all of the call (fewer than 2^32)
   float* part;                    // backward: [groups][splits][chunks][part_ld] sums, or NULL
   int64_t part_ld;
 };
@@ -281,12 +282,13 @@ template <typename T, int NORM, int NW, int R, int LAYOUT>
 struct Share {
   static constexpr int E = kPiece<T>, NT = NW == 64 ? 256 : NW, kWorkers = NT / NW;
   int place, tensor, H, head0, step, group, first_token, token_step, worker;
+  uint32_t block;
   Slot<T, LAYOUT> slot;
 
   __device__ __forceinline__ Share(const RotateArgs<T>& a) {
-    const int chunks = a.chunks[0] + a.chunks[1], b = blockIdx.x;
-    const int chunk = b % chunks, split = b / chunks % a.splits;
-    group = b / chunks / a.splits;
+    const uint32_t chunks = (uint32_t)a.chunks[0] + (uint32_t)a.chunks[1], unit = (block = a.block0 + blockIdx.x) / chunks;
+    const int chunk = (int)(block - unit * chunks), split = (int)(unit % (uint32_t)a.splits);
+    group = (int)(unit / (uint32_t)a.splits);
     worker = NW == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     place = NW == 64 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     tensor = chunk >= a.chunks[0];
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate_back(const Rotat
         for (int wv = 1; wv < 4; ++wv) v += staged[((wv * kSets + r) * 2 * E + e) * 64 + share.place];
       }
   }
-  float* part = a.part + (int64_t)blockIdx.x * a.part_ld;
+  float* part = a.part + (int64_t)share.block * a.part_ld;
 #pragma unroll
   for (int r = 0; r < kSets; ++r) {
     if constexpr (!kRow) {                     // the wave's heads
@@ -640,7 +642,7 @@ RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_
   }
   const int64_t per_block = p.worker == 64 ? 4 : 1, want = p.worker == 1024 ? kRotateBlocks / 4 : kRotateBlocks;
   p.splits = std::min(std::max<int64_t>(1, ceil_div(tokens, per_block)),
-                      std::max<int64_t>(1, want / std::max<int64_t>(1, groups * (p.chunks[0] + p.chunks[1]))));
+                      std::max<int64_t>(1, want / std::max<int64_t>(1, groups * ((int64_t)p.chunks[0] + p.chunks[1]))));
   return p;
 }
 
@@ -675,6 +677,18 @@ RotateArgs<T> rotate_args(const eogp_heads* in, const eogp_heads* grad, const eo
   a.splits = (int)p.splits;
   a.part_ld = p.part_ld;
   return a;
+}
+
+// The blocks of a call, in as many launches as they take (one but for millions of examples or heads).
+template <typename K, typename T>
+eogp_status launch_all(const char* what, K* kfn, RotateArgs<T>& a, const RotatePlan& p, int64_t groups, hipStream_t s) {
+  const int64_t blocks = groups * p.splits * ((int64_t)p.chunks[0] + p.chunks[1]);
+  for (int64_t from = 0; from < blocks; from += kMostLaunched) {
+    a.block0 = (uint32_t)from;
+    hipLaunchKernelGGL(kfn, dim3((unsigned)std::min(blocks - from, kMostLaunched)), dim3(std::max(256, p.worker)), 0, s, a);
+    EOGP_LAUNCH_CHECK(what);
+  }
+  return EOGP_OK;
 }
 
 // f(threads of a worker, heads of a lane, layout). (fp32 rows of up to 8,192 elements in heads of 8 or more take up to
@@ -746,7 +760,6 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
                          int64_t D, hipStream_t s) {
   if (N * T_ == 0) return EOGP_OK;
   const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, 1, N * T_);
-  if (p.splits * (p.chunks[0] + p.chunks[1]) > kMostLaunched) return fail(EOGP_ERR_INVALID, "rotate_heads: too many heads for one call");
   timing::Scope ts(EOGP_KT_ROTARY, s);
   return with_type(t, [&](auto el) {
     using T = decltype(el);
@@ -756,10 +769,8 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
     return with_norm(norm, [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
       return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {
-        hipLaunchKernelGGL((k_rotate<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>),
-                           dim3((unsigned)(p.splits * (p.chunks[0] + p.chunks[1]))), dim3(std::max(256, p.worker)), 0, s, a);
-        EOGP_LAUNCH_CHECK("rotate_heads");
-        return EOGP_OK;
+        return launch_all("rotate_heads", k_rotate<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>, a,
+                          p, 1, s);
       });
     });
   });
@@ -768,7 +779,7 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
 size_t rotate_back_ws(eogp_dtype t, int norm, int64_t Hq, int64_t Hk, int64_t D, int64_t width, int64_t groups, int64_t tokens) {
   // the blocks of any call of up to `groups` groups of up to `tokens` tokens, with one head a lane
   const RotatePlan p = rotate_plan(t, norm, (int)Hq, (int)Hk, D, width, 0, 1, 1);
-  const int64_t chunks = p.chunks[0] + p.chunks[1];
+  const int64_t chunks = (int64_t)p.chunks[0] + p.chunks[1];
   const int64_t blocks = std::min(groups * std::max<int64_t>(1, tokens) * chunks, std::max(kRotateBlocks, groups * chunks));
   return align256((size_t)blocks * p.part_ld * sizeof(float));
 }
@@ -782,8 +793,6 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
   if (groups == 0) return EOGP_OK;
   const RotatePlan p = rotate_plan(t, norm, (int)out[0].heads, (int)out[1].heads, D, width, interleaved, groups, tokens);
   float* part = dqw || dkw ? static_cast<float*>(ws) : nullptr;
-  if (groups * p.splits * (p.chunks[0] + p.chunks[1]) > kMostLaunched)
-    return fail(EOGP_ERR_INVALID, "rotate_heads_backward: too many examples and heads for one call");
   timing::Scope ts(EOGP_KT_ROTARY, s);
   const eogp_status st = with_type(t, [&](auto el) {
     using T = decltype(el);
@@ -793,11 +802,8 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
     auto go = [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
       return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {
-        hipLaunchKernelGGL((k_rotate_back<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>),
-                           dim3((unsigned)(groups * p.splits * (p.chunks[0] + p.chunks[1]))), dim3(std::max(256, p.worker)), 0,
-                           s, a);
-        EOGP_LAUNCH_CHECK("rotate_heads_backward");
-        return EOGP_OK;
+        return launch_all("rotate_heads_backward",
+                          k_rotate_back<T, NORM, decltype(nw)::value, decltype(reps)::value, decltype(layout)::value>, a, p, groups, s);
       });
     };
     using std::integral_constant;

@@ -136,3 +136,21 @@ def test_elements_that_pass(dtype, D, width, interleaved):
             assert torch.equal(torch.nan_to_num(x[..., width:], nan=7.0), torch.nan_to_num(y[..., width:], nan=7.0))
             assert torch.equal(x[..., width:].isnan(), y[..., width:].isnan())
             assert bool(y[..., :width].isfinite().all())
+
+
+# ---- more blocks than a launch holds
+@pytest.mark.parametrize("norm", ["head", "row"])
+def test_gradients_of_a_million_examples(norm):
+    """2^20 + 5 examples of a token, weights' gradients of each: 2^21 + 10 blocks. Bounds as in test_gpu_block_middle."""
+    B.test_rotate_heads_backward(((1 << 20) + 5, 1, 1, 1, 8, 8, norm, False, "all", "split", 0), True, "f32")
+
+
+def test_millions_of_heads():
+    """2^28 + 300 heads of one element: 2^21 + 3 blocks. Without table and norm the heads are copied."""
+    say("[rotate_heads] 2^28 + 300 heads")
+    q = torch.randint(-(1 << 15), 1 << 15, ((1 << 28) + 300,), dtype=torch.int16, device=DEV).view(1, 1, -1, 1)
+    for call in (lambda x, y: E.eogp_rotate_heads(x, q_out=y), lambda x, y: E.eogp_rotate_heads_backward(x, dq_in=y)):
+        out = torch.zeros_like(q)
+        call(q.view(torch.bfloat16), out.view(torch.bfloat16))
+        # (every NaN is as good as another)
+        assert bool(((out == q) | (((out & 0x7FFF) > 0x7F80) & ((q & 0x7FFF) > 0x7F80))).all())
