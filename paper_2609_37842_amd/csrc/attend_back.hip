@@ -76,26 +76,40 @@ __global__ __launch_bounds__(256) void k_attend_zero(uint32_t* p, int64_t n) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
 }
 
-// fp16: the largest norms of rows of v. A row takes `lanes` lanes, 16 bytes each.
+// fp16: the largest norms of rows of v, of keys between the first and the last that queries of the example see (what others
+// hold is nobody's). A row takes `lanes` lanes, 16 bytes each; a block has kNormSteps steps of an example's rows.
+constexpr int kNormSteps = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int lanes, int64_t rows) {
+__global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int lanes, int chunks) {
   constexpr int E = kPiece<T>;
-  const int lane = threadIdx.x & 63, per = 64 / lanes, c = (lane % lanes) * E;
-  for (int64_t id0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * per; id0 < rows; id0 += (int64_t)gridDim.x * 4 * per) {
-    const int64_t id = id0 + lane / lanes, rc = id < rows ? id : rows - 1;
-    const int h = (int)(rc % a.Hkv);
-    const int64_t j = rc / a.Hkv % a.sight.Tk, n = rc / a.Hkv / a.sight.Tk;
-    const bool live = id < rows && (!a.sight.k_mask || a.sight.k_mask[n * a.sight.Tk + j]);
-    float square = 0.f;
-    if (live) {
-      float x[E];
-      load_piece<T, E>(a.v.row(n, j, h), c, a.D, 0.f, x);
-#pragma unroll
-      for (int e = 0; e < E; ++e) square += x[e] * x[e];
+  const int lane = threadIdx.x & 63, per = 64 / lanes, c = (lane % lanes) * E, rows = a.sight.Tk * a.Hkv;
+  for (int64_t part = blockIdx.x; part < (int64_t)a.N * chunks; part += gridDim.x) {
+    const int n = (int)(part / chunks), from = (int)(part - (int64_t)n * chunks) * kNormSteps * 4 * per;
+    int i0 = 0, i1 = a.sight.Tq;
+    if (a.sight.q_mask && i1 > 0) {
+      const MaskRange r = mask_range(a.sight.q_mask + (int64_t)n * i1, i1, 0, i1);
+      i0 = r.first;
+      i1 = r.last;
     }
-    square = sum_of(square, lanes);
-    // (the largest of a set does not depend on the order; a key that no query sees only makes the bound larger)
-    if (live && lane % lanes == 0) atomicMax(a.norms + 2 * (n * a.Hkv + h) + 1, __float_as_uint(square == square ? square : 0.f));
+    if (i0 >= i1) continue;
+    const int64_t start = a.sight.start(n);
+    const Span first = span_of(a.sight, start + i0), last = span_of(a.sight, start + i1 - 1);
+    for (int step = threadIdx.x >> 6; step < 4 * kNormSteps; step += 4) {
+      const int id = from + step * per + lane / lanes, rc = id < rows ? id : rows - 1;
+      const int j = rc / a.Hkv, h = rc - j * a.Hkv;
+      const bool live = id < rows && ((j >= first.lo && j < last.hi) || j < last.sk) &&
+                        (!a.sight.k_mask || a.sight.k_mask[(int64_t)n * a.sight.Tk + j]);
+      float square = 0.f;
+      if (live) {
+        float x[E];
+        load_piece<T, E>(a.v.row(n, j, h), c, a.D, 0.f, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) square += x[e] * x[e];
+      }
+      square = sum_of(square, lanes);
+      // (the largest of a set does not depend on the order)
+      if (live && lane % lanes == 0) atomicMax(a.norms + 2 * (n * a.Hkv + h) + 1, __float_as_uint(square == square ? square : 0.f));
+    }
   }
 }
 
@@ -650,8 +664,9 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
                          a.norms, 2 * units);
       EOGP_LAUNCH_CHECK("attention_backward (zero)");
       if (keys > 0) {
-        hipLaunchKernelGGL(k_attend_norms<T>, dim3((unsigned)std::min<int64_t>(ceil_div(keys * lanes, 256), 16 * kCus)), dim3(256),
-                           0, s, a, lanes, keys);
+        const int64_t chunks = ceil_div(Tk * Hkv, kNormSteps * 4 * (64 / lanes));
+        hipLaunchKernelGGL(k_attend_norms<T>, dim3((unsigned)std::min<int64_t>(N * chunks, 16 * kCus)), dim3(256), 0, s, a, lanes,
+                           (int)chunks);
         EOGP_LAUNCH_CHECK("attention_backward (norms)");
       }
     }

@@ -154,3 +154,32 @@ def test_millions_of_heads():
         call(q.view(torch.bfloat16), out.view(torch.bfloat16))
         # (every NaN is as good as another)
         assert bool(((out == q) | (((out & 0x7FFF) > 0x7F80) & ((q & 0x7FFF) > 0x7F80))).all())
+
+
+@pytest.mark.parametrize("hold", [float("inf"), 60000.0, float("nan")])
+@pytest.mark.parametrize("how", [dict(), dict(window=9, sinks=2), dict(q_mask=True), dict(causal=False, window=9)])
+def test_fp16_gradients_beside_unseen_values(hold, how):
+    """What keys hold that no query sees changes no bit of small gradients: fp16 score gradients are lifted by what the
+    seen values allow."""
+    say(f"[attention_backward] unseen values {hold} {how}")
+    torch.manual_seed(7)
+    N, Tq, Tk, H, D = 2, 40, 200, 2, 64
+    q, do = (torch.randn(N, Tq, H, D, device=DEV).half() for _ in range(2))
+    do *= 1e-4
+    k, v = (torch.randn(N, Tk, H, D, device=DEV).half() for _ in range(2))
+    start = torch.tensor([30, 60], device=DEV)
+    how = dict(how, q_start=start)
+    mask = None
+    if how.pop("q_mask", False):
+        mask = torch.ones(N, Tq, dtype=torch.uint8, device=DEV)
+        mask[:, 25:] = 0
+        mask[1, :4] = 0
+    seen = [M.sight(n, Tq, Tk, **dict(how, q_start=[30, 60], q_mask=None if mask is None else host(mask))).any(0) for n in range(N)]
+    unseen = ~torch.from_numpy(np.stack(seen)).to(DEV)
+    assert bool(unseen.any(1).all())
+    out, lse = E.eogp_attention(q, k, v, q_mask=mask, **how)
+    clean = E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask, **how)
+    for x in (k, v):
+        x[unseen] = hold
+    for a, b in zip(clean, E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask, **how)):
+        assert torch.equal(a, b)
