@@ -691,8 +691,9 @@ eogp_status launch_all(const char* what, K* kfn, RotateArgs<T>& a, const RotateP
   return EOGP_OK;
 }
 
-// f(threads of a worker, heads of a lane, layout). (fp32 rows of up to 8,192 elements in heads of 8 or more take up to
-// 4,096 lanes, 16-bit ones 2,048; layouts of whole pieces up to 1,024 and 2,048, and of 2,048 elements in all others.)
+// f(threads of a worker, heads of a lane, layout). (Rows of one norm have up to 8,192 elements in heads of 8 and more, and 2,048
+// in others. Whole pieces take D / 2 E lanes a head, less than twice as many as a power of two: fewer than 2,048 lanes in fp32,
+// 1,024 in 16 bits; other widths fewer than 4,096 and up to 2,048.)
 template <typename T, int NORM, typename F>
 eogp_status with_shape(const RotatePlan& p, F&& f) {
   using std::integral_constant;
@@ -713,10 +714,11 @@ eogp_status with_shape(const RotatePlan& p, F&& f) {
     }
     if constexpr (NORM == kNormRow) {
       if (p.worker == 256) return f(W256{}, Two{}, layout);
+      constexpr bool kAnyWidth = decltype(layout)::value == kAny;
       if (p.reps == 1) return f(W1024{}, One{}, layout);
-      if constexpr (sizeof(T) == 4)
+      if constexpr (sizeof(T) == 4 && kAnyWidth)
         if (p.reps > 2) return f(W1024{}, Four{}, layout);
-      return f(W1024{}, Two{}, layout);
+      if constexpr (sizeof(T) == 4 || kAnyWidth) return f(W1024{}, Two{}, layout);
     }
     return EOGP_ERR_UNSUPPORTED;
   };

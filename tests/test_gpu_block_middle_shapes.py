@@ -197,3 +197,31 @@ def test_many_tokens(case):
         turned = torch.stack([a, b], -1).flatten(-2) if inter else torch.cat([a, b], -1)
         terms = torch.cat([turned, d64[..., width:]], -1) * x64 * (x64.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
         near(got[2 + i], host(terms.sum((0, 1, 2))), (n * H / 8192 + 80 + 60) * U * host(terms.abs().sum((0, 1, 2))) * 2.5, "dw")
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_longest_rows(dtype):
+    """The most heads that one norm takes, of every width: none is refused. Ones come out as 1 / (1 + eps)^1/2, with gradients
+    of ones near 0: dx = rstd (1 - rstd^2)."""
+    dt = DT[dtype]
+    say(f"[rotate_heads] longest rows {dtype}")
+    for D in range(1, 257):
+        H = (2048 if D < 8 else 8192) // D
+        x = torch.ones(1, 1, H, D, device=DEV, dtype=dt)
+        for width in {0, D // 2 * 2, min(2, D // 2 * 2), D // 4 * 2}:
+            table = torch.zeros(1, width // 2, 2, device=DEV)
+            table[..., 0] = 1.0
+            table = table if width else None
+            y, _ = E.eogp_rotate_heads(x, None, table, norm="row", eps=1e-6)
+            dx, _, dw, _ = E.eogp_rotate_heads_backward(x, None, x, None, table, norm="row", eps=1e-6)
+            assert bool(((y.float() - (1 + 1e-6) ** -0.5).abs() <= B.ULP[dt] + 8 * U).all()), (D, width)
+            assert bool((dx.float().abs() <= 1e-6 + 64 * U).all()) and bool(((dw - (1 + 1e-6) ** -0.5).abs() <= 64 * U).all()), (D, width)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("case", [
+    (1, 3, 204, 3, 40, 40, "row", False, "some", "split", 0), (1, 3, 102, 2, 80, 80, "row", True, "some", "split", 0),
+    (1, 3, 2, 170, 48, 48, "row", False, "some", "split", 0), (1, 3, 682, 1, 12, 10, "row", True, "some", "split", 0)], ids=name)
+def test_rows_of_a_block(case, dtype):
+    B.test_rotate_heads(case, dtype)
+    B.test_rotate_heads_backward(case, False, dtype)
