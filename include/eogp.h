@@ -642,7 +642,9 @@ eogp_status eogp_rotate_heads_backward(const eogp_heads* dq, const eogp_heads* d
  *   q_start   [N] int64 or NULL: chunks of new tokens and single ones over a cache whose rows from q_start[n] + Tq on
  *             (causal) are not read, whatever they hold.
  *   q_mask, k_mask  [N, Tq], [N, Tk] uint8 or NULL. Masked queries and keys count for nothing, whatever they hold; a
- *             value that is not finite at a key that some query of the example sees may reach others of its queries.
+ *             value that is not finite at a key that some query of the example sees, or that lies between such keys, may
+ *             reach others of its queries. Finite ones are taken up to 2^90 (weights of up to 2^8 are summed before they
+ *             are divided).
  *   lse       [N, Tq, heads of q] fp32: ln sum_j exp(scale q . k), for the backward pass, or NULL.
  *   ws        eogp_attention_workspace_size bytes (0: none; NULL then), no fewer for more examples, queries, query heads
  *             or keys.
@@ -666,7 +668,8 @@ eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_
  * key heads summed over their query heads. Zeros at masked queries and keys and those that see, or are seen by, nothing.
  *   d_out, dq, dk, dv  of `dtype`, shaped as out, q, k, v; the gradients overlap nothing else.
  *   out, lse           of the forward pass (out of `dtype` or fp32), from the same arguments.
- *   ws                 eogp_attention_backward_workspace_size bytes, no fewer for more examples, queries, heads or keys.
+ *   ws                 eogp_attention_backward_workspace_size bytes, no fewer for more examples, queries, query heads
+ *                      or keys.
  * An output gradient that is not finite may reach every key and query of its example.
  * Weights are made from lse, to 2^-22 |lse| of their size while that is below 710; rows beyond have theirs summed anew, so
  * that they add up to 1 for scores of any size.

@@ -68,7 +68,7 @@ struct Divide {
     int s = 0;
     while (((int64_t)1 << s) < d) ++s;
     shift = 31 + s;
-    mul = (uint32_t)((((uint64_t)1 << shift) / (uint64_t)d) + 1);   // at most 2^31 + 1, as 2^s < 2 d
+    mul = (uint32_t)((((uint64_t)1 << shift) / (uint64_t)d) + 1);   // below 2^32, as 2^s < 2 d: a product with n fits 63 bits
   }
   __device__ __forceinline__ int quotient(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
   __device__ __forceinline__ int rest(int n, int q) const { return n - q * (int)by; }

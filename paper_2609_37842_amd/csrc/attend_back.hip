@@ -40,6 +40,11 @@ __device__ __forceinline__ float far_score(float s, float scale_log2, float lse2
   return fabsf(lse2) < kFar ? __builtin_fmaf(s, scale_log2, -lse2) : rounded(s * scale_log2) - lse2;
 }
 
+// 16-bit weights P and score gradients dS are rounded to the type before the products that take them, which run at the 16-bit
+// rate that way, and delta comes from the forward pass's output as it was rounded (in fp32 where the caller kept that):
+// gradients are off by 0.0026 of their size (root mean square, bf16; fp16 0.00042) where one rounding at the end would leave
+// 0.0017 (0.00021).
+//
 // fp16 score gradients P (dP - delta) are small where many keys share a row, and lie below fp16's normal range where
 // the output gradients are small as well. They are held times 2^e, e from |dP - delta| <= 2 max |dout row| max |v row|
 // of the key head's rows, so that none passes 2^14.
@@ -60,9 +65,10 @@ constexpr int back_share(int size, int dp) { return size == 4 && dp <= 128 ? 2 :
 
 // Whether one kernel makes the gradients of keys and values. Together they take seven products where two kernels take eight
 // (scores are made again), apart they leave two waves a SIMD: 16-bit heads of 128 are faster apart (2 x 2,048 tokens of
-// 40 / 8 x 128 bf16, whole backward pass: 386 us, together 418), fp32 heads of 64, bound by the products, together (32 x 512
-// tokens of 12 x 64: 359 us, apart 399); wider ones do not fit the registers together.
-constexpr bool kv_together(int size, int dp) { return dp <= 64; }
+// 40 / 8 x 128 bf16, whole backward pass: 386 us, together 418), heads of 64 together (fp32, bound by the products, 32 x 512
+// tokens of 12 x 64: 359 us, apart 399; bf16, 32 x 1,024: 320, apart 377; fp16, 32 x 512: 141, apart 165); wider ones do not
+// fit the registers together.
+constexpr bool kv_together(int dp) { return dp <= 64; }
 
 // Waves of a SIMD, by the bytes of a row: so that registers are taken from one file without copies.
 constexpr int back_waves(int row_bytes, int most) { return row_bytes <= most ? 2 : 1; }
@@ -689,7 +695,7 @@ eogp_status attention_back(const eogp_heads& dout, const eogp_heads& q, const eo
       if (rows > 0) st = launch(k_attend_back_q<T, DP, FAST>, units * a.row_tiles);
       if (st == EOGP_OK && keys > 0) {
         const int64_t blocks = units * a.key_tiles * a.splits;
-        if constexpr (!kv_together((int)sizeof(T), DP)) {
+        if constexpr (!kv_together(DP)) {
           st = launch(k_attend_back_kv<T, DP, 1, FAST>, blocks);
           if (st == EOGP_OK) st = launch(k_attend_back_kv<T, DP, 2, FAST>, blocks);
         } else {

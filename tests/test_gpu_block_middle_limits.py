@@ -183,3 +183,19 @@ def test_fp16_gradients_beside_unseen_values(hold, how):
         x[unseen] = hold
     for a, b in zip(clean, E.eogp_attention_backward(do, q, k, v, out, lse, q_mask=mask, **how)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Tq", [1, 40])
+@pytest.mark.parametrize("size", [2.0 ** 90, 2.0 ** -90])
+def test_large_and_small_values(dtype, Tq, size):
+    """Values of 2^90 and of 2^-90 over 4,500 keys, scores of either sign: outputs are those of values near 1, times that. (A
+    weight's product with 2^-90 is exact down to weights of 2^-36 of the largest; all smaller ones together are below 2^-23.)"""
+    dt = DT[dtype]
+    say(f"[attention] values of {size}, {dtype}, {Tq} queries")
+    g = gen(34, Tq)
+    q, k, v = (B.rounded(g.standard_normal((1, n, 2, 64)), dt) for n in (Tq, 4500, 4500))
+    ref, _ = M.attention(q, k, v, 0.3, causal=False)
+    tol, _ = B.attend_bounds(q, k, v, 0.3, dt, dict(causal=False))
+    out, _ = E.eogp_attention(dev(q, dt), dev(k, dt), dev(v * size, dt), 0.3, causal=False)
+    near(out, ref * size, (tol + 2.0 ** -23 * np.abs(v).max()) * size, "out")
