@@ -199,3 +199,28 @@ def test_large_and_small_values(dtype, Tq, size):
     tol, _ = B.attend_bounds(q, k, v, 0.3, dt, dict(causal=False))
     out, _ = E.eogp_attention(dev(q, dt), dev(k, dt), dev(v * size, dt), 0.3, causal=False)
     near(out, ref * size, (tol + 2.0 ** -23 * np.abs(v).max()) * size, "out")
+
+
+@pytest.mark.parametrize("dtype,score", [(d, SCORES[d][i]) for d in DT for i in (0, 1, -1)])
+@pytest.mark.parametrize("Tq,Tk", [(1, 900), (40, 100), (300, 300)])
+def test_large_scores_beside_small_ones(dtype, score, Tq, Tk, monkeypatch):
+    """Query heads of one key head, every second of them with scores of 1 and less: rows of both kinds share a wave, forward and
+    backward. (A small score rounded in powers of two is off by 2^-25.)"""
+    dt = DT[dtype]
+    say(f"[attention] scores {score} beside small ones, {dtype}, {Tq} queries, {Tk} keys")
+    g = gen(35, Tq, Tk)
+    q, k, v = large_scores(*score, dt, 2, Tq, Tk, 4, 64, g)
+    k, v = k[:, :, :1].copy(), v[:, :, :1].copy()
+    dout = B.rounded(0.01 * g.standard_normal(q.shape), dt)
+    how = dict(causal=Tq == Tk)
+    qd, kd, vd, dd = (dev(x, dt) for x in (q, k, v, dout))
+    out, lse = E.eogp_attention(qd, kd, vd, 0.5, **how)
+    ref, rlse = M.attention(q, k, v, 0.5, **how)
+    tol, rel = exact_bounds(q, k, v, 0.5, dt, how)
+    near(out, ref, tol, "out")
+    near(lse, rlse, rel + 4 * U * (np.abs(rlse) + 12), "lse")
+    monkeypatch.setattr(B, "attend_bounds", gradient_bounds)
+    got = E.eogp_attention_backward(dd, qd, kd, vd, out, lse, 0.5, **how)
+    ref = M.attention_backward(dout, q, k, v, 0.5, **how)
+    for x, y, t, name in zip(got, ref, B.back_bounds(dout, q, k, v, 0.5, dt, how), ("dq", "dk", "dv")):
+        near(x, y, t, name)
