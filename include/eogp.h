@@ -598,8 +598,8 @@ eogp_status eogp_rotary_table(int64_t positions, int64_t width, double base, dou
  *                 the table gets NaN in its turned elements.
  *   token_mask    [N * T] uint8 or NULL; masked tokens count for nothing and get zeros.
  * Errors: EOGP_ERR_INVALID for bad sizes, NULL pointers, an odd width or one above D, eps < 0;
- * EOGP_ERR_UNSUPPORTED for D > 256, other weight types, or a row norm of more than 8,192 elements (2,048 of heads of
- * fewer than 8). */
+ * EOGP_ERR_UNSUPPORTED for D > 256, other weight types, or a row norm over more than 128 heads that have more than 8,192
+ * elements (2,048 of heads of fewer than 8). */
 #define EOGP_NORM_NONE 0
 #define EOGP_NORM_HEAD 1
 #define EOGP_NORM_ROW 2

@@ -86,7 +86,7 @@ eogp_status sample_tokens(const void* logits, eogp_dtype t, int64_t ldl, int64_t
                           double top_p, double min_p, int64_t* out, hipStream_t s);
 eogp_status rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
                          double high, double magnitude, float* table, hipStream_t s);
-int64_t rotate_max_row(int64_t D);
+bool rotate_row_fits(int64_t heads, int64_t D);
 eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype t, int norm, const void* qw,
                          const void* kw, eogp_dtype wt, float eps, const float* table, int64_t positions, int64_t width,
                          int interleaved, bool back, const int64_t* at, const uint8_t* mask, int64_t N, int64_t T_,
@@ -854,8 +854,9 @@ eogp_status check_rotate(const char* op, eogp_dtype dtype, int64_t N, int64_t T,
     return fail(EOGP_ERR_INVALID, std::string(op) + ": weights without a norm");
   if (norm != EOGP_NORM_NONE && (!(eps >= 0.f) || std::isinf(eps)))
     return fail(EOGP_ERR_INVALID, std::string(op) + ": eps must be >= 0");
-  if (norm == EOGP_NORM_ROW && std::max(Hq, Hk) * D > rotate_max_row(D))
-    return fail(EOGP_ERR_UNSUPPORTED, std::string(op) + ": a norm over more than 8192 elements (2048 of heads below 8) is not supported");
+  if (norm == EOGP_NORM_ROW && !rotate_row_fits(std::max(Hq, Hk), D))
+    return fail(EOGP_ERR_UNSUPPORTED,
+                std::string(op) + ": a norm over more than 128 heads of more than 8192 elements (2048 of heads below 8) is not supported");
   if (table_positions < 0 || table_positions >= kMaxFlat)
     return fail(EOGP_ERR_INVALID, std::string(op) + ": table positions outside [0, 2^31)");
   if (width > 0 && table_positions > 0 && !table) return fail(EOGP_ERR_INVALID, std::string(op) + ": NULL table");

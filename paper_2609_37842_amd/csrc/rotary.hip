@@ -562,6 +562,149 @@ __global__ __launch_bounds__(NW == 64 ? 256 : NW) void k_rotate_back(const Rotat
   }
 }
 
+// Rows that the registers of a block do not hold: it goes over the row twice, for its sums and for its results, a head of a lane
+// at a time (of any width). bf16, 2,048 tokens of 128 + 16 heads of 256: 121 us (2.5 TB/s, the second reading from the L2s);
+// the gradient 783 us, bound by the weights' sums, which it adds to in memory.
+template <typename T>
+struct LongRow {
+  using Layout = Share<T, kNormRow, 1024, 1, kAny>;
+  static constexpr int E = kPiece<T>;
+  const RotateArgs<T>& a;
+  const Layout& share;
+  const int rounds;
+
+  __device__ __forceinline__ LongRow(const RotateArgs<T>& args, const Layout& s)
+      : a(args), share(s), rounds((s.H + s.step - 1) / s.step) {}
+  __device__ __forceinline__ Values<T, kAny> load(const T* row, int64_t ld, int r) const {
+    Raw<T, kAny> raw;
+    raw.request(share.slot, row + (share.has(r) ? share.head(r) : 0) * ld, a.D);
+    Values<T, kAny> v;
+    v.take(share.slot, raw, a.D);
+    return v;
+  }
+  __device__ __forceinline__ Values<T, kAny> weights(int r) const {
+    const void* w = a.weight[share.tensor];
+    if (w && (sizeof(T) == 4 || a.wt != EOGP_F32)) return load(static_cast<const T*>(w), a.D, r);
+    const int64_t from = (int64_t)(share.has(r) ? share.head(r) : 0) * a.D;
+    Values<T, kAny> v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int ia = share.slot.at_a(e), ib = share.slot.at_b(e);
+      v.a[e] = w && ia < share.slot.end_a ? load_any(w, a.wt, from + ia) : 1.f;
+      v.b[e] = w && ib < share.slot.end_b ? load_any(w, a.wt, from + ib) : 1.f;
+    }
+    return v;
+  }
+  __device__ __forceinline__ void clear(T* out) const {
+    Values<T, kAny> zero;
+    zero.clear();
+    for (int r = 0; r < rounds; ++r)
+      if (share.has(r)) zero.put(share.slot, out + share.head(r) * a.out[share.tensor].ld_h);
+  }
+};
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_rotate_long(const RotateArgs<T> a) {
+  constexpr int E = kPiece<T>;
+  __shared__ float2 sums[2][16];
+  const typename LongRow<T>::Layout share(a);
+  const LongRow<T> row(a, share);
+  TokenQueue queue(a.mask, a.at, share.first_token, share.token_step, a.tokens, 0, a.by_length);
+  for (int turn_no = 0; queue.next();) {
+    T* out = a.out[share.tensor].row(queue.example, queue.index, 0);
+    if (!queue.live) {
+      row.clear(out);
+      continue;
+    }
+    const T* in = a.in[share.tensor].row(queue.example, queue.index, 0);
+    const int64_t ld = a.in[share.tensor].ld_h;
+    Turn<T, kAny> turn;
+    turn.request(share.slot, a.table, a.positions, queue.position, a.width);
+    float square = 0.f;
+    for (int r = 0; r < row.rounds; ++r) {
+      const float of = row.load(in, ld, r).square();
+      square += share.has(r) ? of : 0.f;
+    }
+    square = row_sums<1024>(square, 0.f, sums[turn_no]).x;
+    turn_no ^= 1;
+    const float rstd = 1.f / sqrtf(square / (float)(share.H * a.D) + a.eps);
+    for (int r = 0; r < row.rounds; ++r) {
+      Values<T, kAny> v = row.load(in, ld, r), w = row.weights(r);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v.a[e] *= rstd * w.a[e];
+        v.b[e] *= rstd * w.b[e];
+      }
+      turn.apply(share.slot, a.sin_sign, v);
+      if (share.has(r)) v.put(share.slot, out + share.head(r) * a.out[share.tensor].ld_h);
+    }
+  }
+}
+
+// (The weights' sums lie in the block's part, each element with the thread that adds to it.)
+template <typename T>
+__global__ __launch_bounds__(1024) void k_rotate_back_long(const RotateArgs<T> a) {
+  constexpr int E = kPiece<T>;
+  __shared__ float2 sums[2][16];
+  const typename LongRow<T>::Layout share(a);
+  const LongRow<T> row(a, share);
+  TokenQueue queue(a.mask, a.at, share.first_token, share.token_step, a.tokens, share.group * a.tokens, a.by_length);
+  float* part = a.part ? a.part + (int64_t)share.block * a.part_ld : nullptr;
+  auto each = [&](int r, auto&& f) {            // f(place in the part, element, of b)
+    if (!part || !share.has(r)) return;
+    float* to = part + (int64_t)share.head(r) * a.D;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int ia = share.slot.at_a(e), ib = share.slot.at_b(e);
+      if (ia < share.slot.end_a) f(to[ia], e, false);
+      if (ib < share.slot.end_b) f(to[ib], e, true);
+    }
+  };
+  for (int r = 0; r < row.rounds; ++r) each(r, [](float& to, int, bool) { to = 0.f; });
+  for (int turn_no = 0; queue.next();) {
+    T* out = a.out[share.tensor].row(queue.example, queue.index, 0);
+    if (!queue.live) {
+      row.clear(out);
+      continue;
+    }
+    const T *in = a.in[share.tensor].row(queue.example, queue.index, 0), *grad = a.grad[share.tensor].row(queue.example, queue.index, 0);
+    const int64_t ld = a.in[share.tensor].ld_h, ld_g = a.grad[share.tensor].ld_h;
+    Turn<T, kAny> turn;
+    turn.request(share.slot, a.table, a.positions, queue.position, a.width);
+    float square = 0.f, dot = 0.f;
+    for (int r = 0; r < row.rounds; ++r) {
+      const Values<T, kAny> x = row.load(in, ld, r), w = row.weights(r);
+      Values<T, kAny> g = row.load(grad, ld_g, r);
+      turn.apply(share.slot, -a.sin_sign, g);
+      float of = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) of += g.a[e] * w.a[e] * x.a[e] + g.b[e] * w.b[e] * x.b[e];
+      square += share.has(r) ? x.square() : 0.f;
+      dot += share.has(r) ? of : 0.f;
+    }
+    const float2 both = row_sums<1024>(square, dot, sums[turn_no]);
+    turn_no ^= 1;
+    const float count = (float)(share.H * a.D), rstd = 1.f / sqrtf(both.x / count + a.eps), m = both.y * rstd / count;
+    for (int r = 0; r < row.rounds; ++r) {
+      Values<T, kAny> x = row.load(in, ld, r), g = row.load(grad, ld_g, r);
+      const Values<T, kAny> w = row.weights(r);
+      turn.apply(share.slot, -a.sin_sign, g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x.a[e] *= rstd;
+        x.b[e] *= rstd;
+      }
+      each(r, [&](float& to, int e, bool b) { to += b ? g.b[e] * x.b[e] : g.a[e] * x.a[e]; });
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x.a[e] = rstd * (g.a[e] * w.a[e] - x.a[e] * m);
+        x.b[e] = rstd * (g.b[e] * w.b[e] - x.b[e] * m);
+      }
+      if (share.has(r)) x.put(share.slot, out + share.head(r) * a.out[share.tensor].ld_h);
+    }
+  }
+}
+
 // Sums of the blocks' parts, in a fixed order: 32 columns x 32 slices of the parts per block, eight requests of a thread
 // at a time. Columns run over both tensors' weights.
 __global__ __launch_bounds__(1024) void k_rotate_fold(const float* __restrict__ part, int64_t part_ld, int64_t groups, int splits,
@@ -603,12 +746,14 @@ __global__ __launch_bounds__(1024) void k_rotate_fold(const float* __restrict__ 
 
 // How a token's heads and a group's tokens are shared out.
 struct RotatePlan {
-  int shift, worker, reps, chunks[2], layout;  // lanes of a head, threads of a worker, heads of a lane
+  int shift, worker, reps, chunks[2], layout;  // lanes of a head, threads of a worker, heads of a lane (0: a long row's)
   int64_t splits, part_ld;
 };
 
 constexpr int64_t kRotateBlocks = 8 * kCus;    // that are there at once, about (of 256 threads)
 constexpr int64_t kMostLaunched = 1 << 21;     // blocks of a launch (of up to 1,024 threads)
+
+inline int64_t want_blocks(const RotatePlan& p) { return p.worker == 1024 ? kRotateBlocks / 4 : kRotateBlocks; }
 
 RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_t width, int interleaved, int64_t groups,
                        int64_t tokens) {
@@ -626,6 +771,7 @@ RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_
     p.worker = lanes <= 256 ? 64 : lanes <= 512 ? 256 : 1024;
     p.reps = 1;
     while (p.reps * p.worker < lanes) p.reps *= 2;
+    if (lanes > (t == EOGP_F32 ? 2048 : 1024) * (whole ? 1 : 2)) p.reps = 0;
     for (int i = 0; i < 2; ++i) p.chunks[i] = heads[i] > 0;
     p.part_ld = std::max(Hq, Hk) * D;
   } else {
@@ -640,7 +786,7 @@ RotatePlan rotate_plan(eogp_dtype t, int norm, int Hq, int Hk, int64_t D, int64_
     for (int i = 0; i < 2; ++i) p.chunks[i] = (int)ceil_div(heads[i], at_once * p.reps);
     p.part_ld = D;
   }
-  const int64_t per_block = p.worker == 64 ? 4 : 1, want = p.worker == 1024 ? kRotateBlocks / 4 : kRotateBlocks;
+  const int64_t per_block = p.worker == 64 ? 4 : 1, want = want_blocks(p);
   p.splits = std::min(std::max<int64_t>(1, ceil_div(tokens, per_block)),
                       std::max<int64_t>(1, want / std::max<int64_t>(1, groups * ((int64_t)p.chunks[0] + p.chunks[1]))));
   return p;
@@ -691,9 +837,9 @@ eogp_status launch_all(const char* what, K* kfn, RotateArgs<T>& a, const RotateP
   return EOGP_OK;
 }
 
-// f(threads of a worker, heads of a lane, layout). (Rows of one norm have up to 8,192 elements in heads of 8 and more, and 2,048
-// in others. Whole pieces take D / 2 E lanes a head, less than twice as many as a power of two: fewer than 2,048 lanes in fp32,
-// 1,024 in 16 bits; other widths fewer than 4,096 and up to 2,048.)
+// f(threads of a worker, heads of a lane, layout), for rows that are not long. (Whole pieces take D / 2 E lanes a head, less than
+// twice as many as a power of two. So rows of 8,192 elements have fewer than 2,048 lanes in fp32, 1,024 in 16 bits; other widths
+// fewer than 4,096 and up to 2,048. Longer ones are held up to the same number of lanes.)
 template <typename T, int NORM, typename F>
 eogp_status with_shape(const RotatePlan& p, F&& f) {
   using std::integral_constant;
@@ -737,8 +883,8 @@ eogp_status with_norm(int norm, F&& f) {
 
 }  // namespace
 
-// Elements of a row that one norm takes.
-int64_t rotate_max_row(int64_t D) { return D < 8 ? 2048 : 8192; }
+// Whether one norm takes a row of that many heads.
+bool rotate_row_fits(int64_t heads, int64_t D) { return heads <= 128 || heads * D <= (D < 8 ? 2048 : 8192); }
 
 eogp_status rotary_table(int64_t positions, int64_t width, double base, double factor, double original, double low,
                          double high, double magnitude, float* table, hipStream_t s) {
@@ -768,6 +914,7 @@ eogp_status rotate_heads(const eogp_heads* in, const eogp_heads* out, eogp_dtype
     RotateArgs<T> a = rotate_args<T>(in, nullptr, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_,
                                      N * T_, p);
     a.sin_sign = back ? -1.f : 1.f;
+    if (p.reps == 0) return launch_all("rotate_heads", k_rotate_long<T>, a, p, 1, s);
     return with_norm(norm, [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
       return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {
@@ -782,7 +929,7 @@ size_t rotate_back_ws(eogp_dtype t, int norm, int64_t Hq, int64_t Hk, int64_t D,
   // the blocks of any call of up to `groups` groups of up to `tokens` tokens, with one head a lane
   const RotatePlan p = rotate_plan(t, norm, (int)Hq, (int)Hk, D, width, 0, 1, 1);
   const int64_t chunks = (int64_t)p.chunks[0] + p.chunks[1];
-  const int64_t blocks = std::min(groups * std::max<int64_t>(1, tokens) * chunks, std::max(kRotateBlocks, groups * chunks));
+  const int64_t blocks = std::min(groups * std::max<int64_t>(1, tokens) * chunks, std::max(want_blocks(p), groups * chunks));
   return align256((size_t)blocks * p.part_ld * sizeof(float));
 }
 
@@ -801,6 +948,7 @@ eogp_status rotate_heads_back(const eogp_heads* in, const eogp_heads* grad, cons
     RotateArgs<T> a = rotate_args<T>(in, grad, out, D, qw, kw, wt, eps, table, positions, width, interleaved, at, mask, T_,
                                      tokens, p);
     a.part = part;
+    if (p.reps == 0) return launch_all("rotate_heads_backward", k_rotate_back_long<T>, a, p, groups, s);
     auto go = [&](auto nm) {
       constexpr int NORM = decltype(nm)::value;
       return with_shape<T, NORM>(p, [&](auto nw, auto reps, auto layout) {

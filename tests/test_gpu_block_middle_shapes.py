@@ -225,3 +225,17 @@ def test_longest_rows(dtype):
 def test_rows_of_a_block(case, dtype):
     B.test_rotate_heads(case, dtype)
     B.test_rotate_heads_backward(case, False, dtype)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("case", [                                      # up to 128 heads of any width
+    (2, 5, 128, 16, 128, 128, "row", False, "some", "split", 0), (1, 4, 128, 3, 256, 256, "row", True, "all", "heads", 0),
+    (2, 3, 100, 128, 250, 250, "row", False, "some", "gaps", 1), (1, 3, 128, 128, 256, 250, "row", True, "some", "split", 0),
+    (2, 7, 65, 8, 128, 64, "row", False, "prefix", "split", 0), (2, 5, 120, 0, 199, 46, "row", False, "none", "gaps", 3),
+    (1, 600, 128, 1, 137, 80, "row", True, "some", "split", 0)], ids=name)
+def test_long_rows(case, dtype):
+    """Rows that a block goes over twice: a sum's chain is 16 roundings of a lane's head, 8 heads of a lane, 22 over lanes and
+    waves, within the 50 that the bounds count."""
+    B.test_rotate_heads(case, dtype)
+    for per_example in (False, True):
+        B.test_rotate_heads_backward(case, per_example, dtype)
