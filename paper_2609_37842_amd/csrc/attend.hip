@@ -93,10 +93,11 @@ __device__ __forceinline__ void put_rows(const AttendArgs<T>& a, const f32x16* a
 // product of the last one's weights with V, so that the vector units make exponentials while the matrix units multiply.
 // (A step's weights may move a row's reference: the output takes its factor at the step's end, when the last tile's
 // product, made with the old one, is in.)
-// Bound by the vector units' maxima, exponentials and roundings beside the matrix units: bf16 heads of 128, causal, 8 x 1,024
-// to 2,048 tokens of 16 heads 148 us (81 GFLOP, 548 TFLOP/s; vector units busy 0.37 of the SIMDs' time, matrix 0.28, and
-// few blocks: 1.7 waves a SIMD), 2 x 8,192 tokens and more 900 TFLOP/s; heads of 64 880, of 256 (one wave a SIMD) 417; fp32
-// 116 to 129 of the 154 that a large matrix product reaches. With the three steps of one tile after another the first took
+// Bound by its vector instructions and by LDS (each wave reads whole tiles for its 32 or 64 rows) between barriers every 32
+// keys, with neither unit full: bf16 heads of 128, causal, 8 x 1,024 to 2,048 tokens of 16 heads 150 us (81 GFLOP, 540 TFLOP/s;
+// vector units busy 0.39 of the SIMDs' time, matrix 0.29, and few blocks: 1.66 waves a SIMD), 2 x 8,192 tokens and more 860 to
+// 910 TFLOP/s; heads of 64 720, of 256 (one wave a SIMD) 660; fp32 109 to 123 of the 154 that a large matrix product reaches, 27
+// in heads of 256, whose rows do not fit the registers. With the three steps of one tile after another the first took
 // 381 us; with three tiles at once but masks and rows' bounds read one after another before the first tile, 226.
 template <typename T, int DP, int QG, bool FAST>
 __global__ __launch_bounds__(256, DP * QG * (int)sizeof(T) <= 256 ? 2 : 1) void k_attend(const AttendArgs<T> a) {

@@ -122,9 +122,9 @@ __global__ __launch_bounds__(256) void k_attend_norms(const BackArgs<T> a, int l
 // Gradients of keys and values: a wave has 32 keys, their rows of K and V and both gradients in registers; the
 // block's waves share tiles of 32 rows of queries and output gradients, over all query heads of the key head.
 // PARTS: 1 gradients of V, 2 of K, 3 both. Bound by the products at one or two waves a SIMD (registers) and the latency of a
-// tile's scores, which the next product waits for: fp32, 32 x 64 to 512 tokens of 12 x 64, both 235 us under a profiler (matrix
-// units busy 0.35 of the SIMDs' time); bf16, 2 x 1,024 to 2,048 of 40 / 8 x 128, V 97 us (0.24, vector units 0.33), K 122
-// (0.30, 0.34).
+// tile's scores, which the next product waits for: under a profiler, fp32, 32 x 64 to 512 tokens of 12 x 64, both 246 us (matrix
+// units busy 0.34 of the SIMDs' time); bf16, 2 x 1,024 to 2,048 of 40 / 8 x 128, V 102 us (0.23, vector units 0.32), K 133
+// (0.27, 0.33).
 template <typename T, int DP, int PARTS, bool FAST>
 __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), PARTS == 3 ? 128 : 256)) void k_attend_back_kv(
     const BackArgs<T> a) {
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(256) void k_attend_back_join(const BackArgs<T> a) {
 // Gradients of queries: a wave has 32 rows of queries, output gradients and the result in registers; the block's
 // waves share tiles of keys and values. Before that each row's delta = dout . out is formed, and its log-sum-exp in powers
 // of two, which the other kernels read (+inf: the row counts for nothing). Bound as k_attend_back_kv is: the fp32 batch
-// there 158 us (matrix units busy 0.39), the bf16 one 151 (0.29, vector units 0.31).
+// there 165 us (matrix units busy 0.38), the bf16 one 156 (0.28, vector units 0.31).
 template <typename T, int DP, bool FAST>
 __global__ __launch_bounds__(64 * back_share((int)sizeof(T), DP), back_waves(DP * (int)sizeof(T), 256)) void k_attend_back_q(const BackArgs<T> a) {
   constexpr int NW = back_share((int)sizeof(T), DP), NT = 64 * NW, KB = 32;
