@@ -674,7 +674,8 @@ eogp_status eogp_attention(const eogp_heads* q, const eogp_heads* k, const eogp_
  * Weights are made from lse, to 2^-22 |lse| of their size while that is below 710; rows beyond have theirs summed anew, so
  * that they add up to 1 for scores of any size.
  * Sums run in a fixed order. 16-bit weights and score gradients are rounded to `dtype` once, before the products that
- * take them. Errors as for eogp_attention. */
+ * take them; rowsum(d_out out) takes `out` as it is given, so that fp32 beside 16-bit inputs keeps the bits that its rounding
+ * would cost where queries see few keys. Errors as for eogp_attention. */
 size_t eogp_attention_backward_workspace_size(int64_t N, int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,
                                               int64_t D, eogp_dtype dtype);
 eogp_status eogp_attention_backward(const eogp_heads* d_out, const eogp_heads* q, const eogp_heads* k,
